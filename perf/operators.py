@@ -158,6 +158,9 @@ def prepare(case, seed):
             st["index"] = torch.empty((T, K), dtype=torch.int32, device="cuda")
             st["logprob"] = torch.empty((T, K), device="cuda")
             st["lse"] = torch.empty(T, device="cuda")
+            from paper_2602_14338_amd import aero_workspace_bytes, binding
+            size = aero_workspace_bytes(binding.OP_TOPK_LOGPROB, T=T, V=V, H=K)
+            st["workspace"] = torch.empty(size, dtype=torch.uint8, device="cuda")
         return st
     if kind == "distill":
         T, K = case["T"], case["K"]
@@ -220,7 +223,8 @@ def _run_own(st):
     case = st["case"]
     kind, V = case["kind"], case["V"]
     if kind == "topk":
-        aero.aero_topk_logprob(st["logits"], case["T"], V, case["ld"], None, case["K"], st["index"], st["logprob"], st["lse"])
+        aero.aero_topk_logprob(st["logits"], case["T"], V, case["ld"], None, case["K"], st["index"], st["logprob"], st["lse"],
+                               st["workspace"])
         return st["index"], st["logprob"], st["lse"]
     if kind == "distill":
         aero.aero_distill_loss_bwd(st["logits"], case["T"], V, case["ld"], st["index"], st["logprob"], case["K"], st["weight"],
