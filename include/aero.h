@@ -70,7 +70,11 @@ enum { AERO_DW_ACCUMULATE = 0x100 };
 enum { AERO_ROW_PADDING = -1, AERO_ROW_UNTOUCHED = -2 };
 
 /* bits of the device error word */
-enum { AERO_DERR_NONBINARY_REWARD = 1, AERO_DERR_BAD_TARGET = 2, AERO_DERR_BAD_ROLLOUT = 4 };
+enum { AERO_DERR_NONBINARY_REWARD = 1, AERO_DERR_BAD_TARGET = 2, AERO_DERR_BAD_ROLLOUT = 4,
+       AERO_DERR_BAD_TEACHER = 8, AERO_DERR_BAD_COUNT = 16 };
+
+/* What a teacher's list says about the ids that are not on it (aero_distill_loss_bwd). */
+enum { AERO_TAIL_RENORM = 0, AERO_TAIL_BUCKET = 1 };
 
 /* group_category[q]: low two bits = four-way category by success rate u = c/n with
  * threshold tau (App. C, "Problem Categorization"); bit 2 = rescue stratum u <= S/n
@@ -79,7 +83,8 @@ enum { AERO_CAT_ZERO = 0, AERO_CAT_PARTIAL = 1, AERO_CAT_GOOD = 2, AERO_CAT_PERF
        AERO_CAT_RESCUE_BIT = 4 };
 
 enum { AERO_OP_GROUP_ADVANTAGE = 0, AERO_OP_LOGPROB_FWD = 1, AERO_OP_GRPO_LOSS_BWD = 2,
-       AERO_OP_LMHEAD_FUSED = 3 };
+       AERO_OP_LMHEAD_FUSED = 3, AERO_OP_TOPK_LOGPROB = 4, AERO_OP_DISTILL_LOSS_BWD = 5,
+       AERO_OP_VERIFY_DRAFT = 6, AERO_OP_EMBEDDING_BWD = 7 };
 
 /* Hyper-parameters of the curation step (Table 8; Sec. 4.2). */
 typedef struct {
@@ -273,6 +278,117 @@ aero_status aero_lmhead_logprob_fused(
     float kl_coef, const float* ref_logprob /*nullable*/,
     float* loss, float* clip_frac /*nullable*/, void* dhidden, void* dweight, int32_t dweight_dtype,
     int32_t* err_flag /*nullable*/,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The four calls below keep a drafter close to the policy and draft with it: the rollouts that this update is made
+ * of are cheaper to generate when a small model proposes tokens and the policy's rows verify several of them at once.
+ * Their common conventions, besides those at the top of this file:
+ *   - Temperature 1, as for the policy (Table 8).
+ *   - Masked logits are allowed here: a logit of -inf or at or below -1e30 (such as the lowest value of fp32 or bf16, as
+ *     masks write it) has probability 0.  A row without any other logit is empty: its lse is -inf.  A NaN or +inf logit
+ *     makes the row's lse NaN.
+ *   - logits [T, ld] row-major in the four storage types, ld >= V, columns >= V never touched, any alignment; rows are
+ *     moved as 16-byte vectors between their ragged ends unless a base is not a multiple of the element size.
+ *     1 <= V <= 2^24, T < 2^22 rows.
+ */
+
+/*
+ * The K largest logits of each row: what a teacher's distribution is handed on as.
+ *   index[t, 0 .. K) ids in descending order of the logit, the lower id first where logits are equal (+0 and -0
+ *   are equal); logprob[t, k] = z[t, index[t, k]] - lse[t]; lse[t] as aero_logprob_fwd's.
+ * Rows with fewer than K unmasked logits: the entries behind them are id -1, log-prob -inf (a NaN logit is not listed
+ * and makes the row's log-probs NaN).  Rows with row_active == 0 are not read: ids -1, log-probs and lse 0.
+ * 1 <= K <= AERO_TOPK_MAX (AERO_ERR_LIMIT beyond); K > V is valid.  T = 0 is valid.
+ * row_active u8[T] or NULL; index i32[T, K], logprob f32[T, K], lse f32[T] or NULL.
+ * workspace: aero_workspace_bytes(AERO_OP_TOPK_LOGPROB, T, V, K, 0, 0) (K in the place of H).
+ */
+#define AERO_TOPK_MAX 256
+aero_status aero_topk_logprob(
+    const void* logits, int32_t dtype, int64_t T, int32_t V, int64_t ld,
+    const uint8_t* row_active /*nullable*/, int32_t K,
+    int32_t* index, float* logprob, float* lse /*nullable*/,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Distillation from a teacher's top logits: divergence of the student's rows from the lists, and its gradient.
+ * Row t with weight w = token_weight[t] != 0, listed ids i_k (distinct, an id < 0 is an absent entry), their log-probs
+ * l_k (at most 0; -inf: listed with probability 0), p_k = exp(l_k), q = softmax(z[t]):
+ *   AERO_TAIL_RENORM  the teacher is its list: p'_k = p_k / sum p,
+ *       L_t = sum_k p'_k (ln p'_k - ln q(i_k)),   dz_j = q_j - p'_j (p'_j = 0 for ids that are not listed)
+ *   AERO_TAIL_BUCKET  all other ids are one event: p_r = max(0, 1 - sum p), q_r = sum of q over them,
+ *       L_t = sum_k p_k (ln p_k - ln q(i_k)) + p_r (ln p_r - ln q_r),   P = sum p + p_r,
+ *       dz_j = P q_j - p_j for listed ids,  (P - p_r / q_r) q_j for the others;
+ *       a student without mass outside the list (q_r = 0) has no bucket: p_r counts as 0.
+ *   row_loss[t] = L_t,  loss = sum_t w L_t,  dlogits[t, j] = grad_scale w dz_j.
+ * Rows with w == 0 are not read; they, rows without a listed entry (in the first form: without teacher probability) and empty rows
+ * of the student have L_t = 0 and a dlogits row of +0.  A row with an id >= V or the same id twice is treated alike
+ * and raises AERO_DERR_BAD_TEACHER.  Teacher probability on a masked logit makes L_t +inf (the gradient stays finite).
+ *
+ * logits / dlogits [T, ld], same dtype and ld; dlogits may alias logits (in place), NULL: loss only.
+ * teacher_index i32[T, K], teacher_logprob f32[T, K], 1 <= K <= AERO_TOPK_MAX (AERO_ERR_LIMIT beyond); token_weight f32[T].
+ * loss f32[1] (fixed-order sum), row_loss f32[T] or NULL.
+ * Probabilities, their sums and the loss terms of the lists are formed in 64 bits, everything per logit in 32.
+ * workspace: aero_workspace_bytes(AERO_OP_DISTILL_LOSS_BWD, T, V, 0, 0, 0).
+ */
+aero_status aero_distill_loss_bwd(
+    const void* logits, int32_t dtype, int64_t T, int32_t V, int64_t ld,
+    const int32_t* teacher_index, const float* teacher_logprob, int32_t K,
+    const float* token_weight, int32_t tail, float grad_scale,
+    float* loss, float* row_loss /*nullable*/, void* dlogits /*nullable*/, int32_t* err_flag /*nullable*/,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens: B sequences, up to G drafted tokens each, from given random numbers; what comes out is
+ * distributed as if the policy had drawn every token itself.
+ *   p_i = softmax of target_logits[b, i] (i = 0 .. G), q_i = softmax of draft_logits[b, i] (i = 0 .. G-1); with
+ *   draft_logits == NULL the drafter has no probabilities (a copied token, say): q_i = 1 at the drafted token, else 0.
+ *   Drafted token x_i = draft_tokens[b, i] is accepted while uniform[b, i] q_i(x_i) < p_i(x_i), up to the first refusal
+ *   or draft_count[b] tokens: n of them.  The token behind them is the j with the largest r_j / noise[b, j] (the lowest
+ *   where equal), r = max(0, p_n - q_n) after a refusal, r = p_n after draft_count[b] accepted tokens; with noise drawn
+ *   from the exponential distribution that is a draw from r / sum r.  Where r vanishes, p_n takes its place.
+ * Outputs  accepted i32[B] = n; tokens i32[B, G+1]: x_0 .. x_{n-1}, the drawn token, -1 behind it; logprob f32[B, G+1] or
+ *          NULL: ln p_i(token) - the old_logprob that the update needs - and 0 behind the drawn token.
+ * A drafted id outside [0, V) ends the sequence's drafted tokens in front of it (an id >= V raises AERO_DERR_BAD_TARGET).
+ * draft_count[b] < 0: the sequence is idle (nothing read; accepted 0, tokens -1, logprob 0); > G: the same, and
+ * AERO_DERR_BAD_COUNT.  A position whose target row is empty or has a NaN or +inf logit accepts nothing and draws
+ * -1 (logprob 0); one whose draft row has is refused and drawn from p.
+ *
+ * target_logits [B, G+1, ld], draft_logits [B, G, ld] of the same dtype; draft_tokens i32[B, G], draft_count i32[B] or
+ * NULL (= G for all), uniform f32[B, G] in [0, 1), noise f32[B, V], > 0.  0 <= G <= AERO_DRAFT_MAX (AERO_ERR_LIMIT beyond);
+ * with G = 0 draft_tokens, uniform and draft_logits may be NULL.  B = 0 is valid.
+ * workspace: aero_workspace_bytes(AERO_OP_VERIFY_DRAFT, B * (G + 1), V, 0, 0, B).
+ */
+#define AERO_DRAFT_MAX 63
+aero_status aero_verify_draft(
+    const void* target_logits, const void* draft_logits /*nullable*/, int32_t dtype, int32_t B, int32_t G, int32_t V,
+    int64_t ld, const int32_t* draft_tokens, const int32_t* draft_count /*nullable*/,
+    const float* uniform, const float* noise,
+    int32_t* accepted, int32_t* tokens, float* logprob /*nullable*/, int32_t* err_flag /*nullable*/,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Embedding rows: out[t, :] = scale * table[ids[t], :], formed in fp32 and rounded once.
+ * table [V, H] contiguous, out [T, ld_out] (ld_out >= H, columns >= H untouched: rows of a wider buffer), both of dtype AERO_F32, AERO_BF16
+ * or AERO_F16; ids i32[T].  A negative id is padding: its row is +0; an id >= V likewise, and raises
+ * AERO_DERR_BAD_TARGET.  1 <= V <= 2^24, 1 <= H <= 2^20; any alignment (16-byte vectors where table, out, H and ld_out allow them).
+ */
+aero_status aero_embedding_fwd(
+    const void* table, int32_t dtype, int32_t V, int32_t H, const int32_t* ids, int64_t T, float scale,
+    void* out, int64_t ld_out, int32_t* err_flag /*nullable*/, void* stream);
+
+/*
+ * Its gradient: dtable[v, :] = scale * sum over the tokens t with ids[t] == v of dout[t, :], rows without a token +0; with
+ * AERO_DW_ACCUMULATE in dtable_dtype the sum is added to what dtable holds (for a table that is the LM head too: onto
+ * the dweight of aero_lmhead_logprob_fused) and rows without a token are not touched.  Tokens are sorted by id first; a row's
+ * sum is formed in fp32 in an order that the ids alone determine (the same bits every time) and rounded once.
+ * dout [T, ld_dout] of dtype AERO_F32, AERO_BF16 or AERO_F16; dtable [V, H] contiguous, AERO_F32 or AERO_BF16.  ids, V, H as above
+ * (ids outside [0, V) take no part).  T = 0 is valid.
+ * workspace: aero_workspace_bytes(AERO_OP_EMBEDDING_BWD, T, V, H, 0, 0).
+ */
+aero_status aero_embedding_bwd(
+    const void* dout, int32_t dtype, int64_t T, int32_t H, int64_t ld_dout, const int32_t* ids, int32_t V, float scale,
+    void* dtable, int32_t dtable_dtype, int32_t* err_flag /*nullable*/,
     void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -8,11 +8,16 @@ fallback: importing the binding without the built library raises.
 from .binding import (  # noqa: F401
     AdvParams,
     AeroError,
+    aero_distill_loss_bwd,
+    aero_embedding_bwd,
+    aero_embedding_fwd,
     aero_group_advantage,
     aero_grpo_loss_bwd,
     aero_grpo_loss_bwd_noalloc,
     aero_lmhead_logprob_fused,
     aero_logprob_fwd,
+    aero_topk_logprob,
+    aero_verify_draft,
     aero_workspace_bytes,
     library_path,
     AERO_F32,
@@ -21,4 +26,6 @@ from .binding import (  # noqa: F401
     AERO_F8E4M3,
     AERO_ROW_PADDING,
     AERO_ROW_UNTOUCHED,
+    AERO_TAIL_BUCKET,
+    AERO_TAIL_RENORM,
 )

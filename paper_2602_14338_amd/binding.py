@@ -16,6 +16,9 @@ AERO_F32, AERO_BF16, AERO_F16, AERO_F8E4M3 = 0, 1, 2, 3
 AERO_ROW_PADDING, AERO_ROW_UNTOUCHED = -1, -2
 AERO_DW_ACCUMULATE = 0x100
 OP_GROUP_ADVANTAGE, OP_LOGPROB_FWD, OP_GRPO_LOSS_BWD, OP_LMHEAD_FUSED = 0, 1, 2, 3
+OP_TOPK_LOGPROB, OP_DISTILL_LOSS_BWD, OP_VERIFY_DRAFT, OP_EMBEDDING_BWD = 4, 5, 6, 7
+AERO_TAIL_RENORM, AERO_TAIL_BUCKET = 0, 1
+AERO_TOPK_MAX, AERO_DRAFT_MAX = 256, 63
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libaero_hip.so")
 
@@ -73,6 +76,16 @@ def _load() -> C.CDLL:
     lib.aero_lmhead_logprob_fused.restype = i32
     lib.aero_lmhead_logprob_fused.argtypes = [p, p, i64, i32, i32, p, p, p, p, p, p, p, p, i32, f32, f32, f32, f32,
                                               f32, p, p, p, p, p, i32, p, p, sz, p]
+    lib.aero_topk_logprob.restype = i32
+    lib.aero_topk_logprob.argtypes = [p, i32, i64, i32, i64, p, i32, p, p, p, p, sz, p]
+    lib.aero_distill_loss_bwd.restype = i32
+    lib.aero_distill_loss_bwd.argtypes = [p, i32, i64, i32, i64, p, p, i32, p, i32, f32, p, p, p, p, p, sz, p]
+    lib.aero_verify_draft.restype = i32
+    lib.aero_verify_draft.argtypes = [p, p, i32, i32, i32, i32, i64, p, p, p, p, p, p, p, p, p, sz, p]
+    lib.aero_embedding_fwd.restype = i32
+    lib.aero_embedding_fwd.argtypes = [p, i32, i32, i32, p, i64, f32, p, i64, p, p]
+    lib.aero_embedding_bwd.restype = i32
+    lib.aero_embedding_bwd.argtypes = [p, i32, i64, i32, i64, p, i32, f32, p, i32, p, p, sz, p]
     return lib
 
 
@@ -255,3 +268,57 @@ def aero_lmhead_logprob_fused(hidden, weight, T: int, H: int, V: int, targets, l
         *p[:2], T, H, V, *p[2:10], R, eps_lo, eps_hi, grad_scale, entropy_coef, kl_coef, *p[10:15], dweight_dtype,
         *p[15:], workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream(hidden))
     _check(st, "aero_lmhead_logprob_fused")
+
+
+def _bytes(t: Optional[torch.Tensor]) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+def aero_topk_logprob(logits, T: int, V: int, ld: int, row_active, K: int, index, logprob, lse, workspace) -> None:
+    z, *p, ws = _m.pointers(logits, None, "logits", row_active, _U8, "row_active", index, _I32, "index", logprob, _F32, "logprob",
+                            lse, _F32, "lse", workspace, None, "workspace")
+    st = _lib.aero_topk_logprob(z, _dtype_code(logits), T, V, ld, p[0], K, *p[1:], ws, _bytes(workspace), _stream(logits))
+    _check(st, "aero_topk_logprob")
+
+
+def aero_distill_loss_bwd(logits, T: int, V: int, ld: int, teacher_index, teacher_logprob, K: int, token_weight, tail: int,
+                          grad_scale: float, loss, row_loss, dlogits, workspace, err_flag=None) -> None:
+    if dlogits is not None and dlogits.dtype != logits.dtype:
+        raise AeroError("dlogits must have the dtype of logits")
+    z, index, lp, w, *p = _m.pointers(
+        logits, None, "logits", teacher_index, _I32, "teacher_index", teacher_logprob, _F32, "teacher_logprob",
+        token_weight, _F32, "token_weight", loss, _F32, "loss", row_loss, _F32, "row_loss", dlogits, None, "dlogits",
+        err_flag, _I32, "err_flag", workspace, None, "workspace")
+    st = _lib.aero_distill_loss_bwd(z, _dtype_code(logits), T, V, ld, index, lp, K, w, tail, grad_scale, *p, _bytes(workspace),
+                                    _stream(logits))
+    _check(st, "aero_distill_loss_bwd")
+
+
+def aero_verify_draft(target_logits, draft_logits, B: int, G: int, V: int, ld: int, draft_tokens, draft_count, uniform, noise,
+                      accepted, tokens, logprob, workspace, err_flag=None) -> None:
+    if draft_logits is not None and draft_logits.dtype != target_logits.dtype:
+        raise AeroError("draft_logits must have the dtype of target_logits")
+    zt, zd, *p, err, ws = _m.pointers(
+        target_logits, None, "target_logits", draft_logits, None, "draft_logits", draft_tokens, _I32, "draft_tokens",
+        draft_count, _I32, "draft_count", uniform, _F32, "uniform", noise, _F32, "noise", accepted, _I32, "accepted",
+        tokens, _I32, "tokens", logprob, _F32, "logprob", err_flag, _I32, "err_flag", workspace, None, "workspace")
+    st = _lib.aero_verify_draft(zt, zd, _dtype_code(target_logits), B, G, V, ld, *p, err, ws, _bytes(workspace),
+                                _stream(target_logits))
+    _check(st, "aero_verify_draft")
+
+
+def aero_embedding_fwd(table, V: int, H: int, ids, T: int, scale: float, out, ld_out: int, err_flag=None) -> None:
+    if out.dtype != table.dtype:
+        raise AeroError("out must have the dtype of table")
+    e, i, o, err = _m.pointers(table, None, "table", ids, _I32, "ids", out, None, "out", err_flag, _I32, "err_flag")
+    st = _lib.aero_embedding_fwd(e, _dtype_code(table), V, H, i, T, scale, o, ld_out, err, _stream(table))
+    _check(st, "aero_embedding_fwd")
+
+
+def aero_embedding_bwd(dout, T: int, H: int, ld_dout: int, ids, V: int, scale: float, dtable, workspace,
+                       accumulate: bool = False, err_flag=None) -> None:
+    d, i, g, err, ws = _m.pointers(dout, None, "dout", ids, _I32, "ids", dtable, None, "dtable", err_flag, _I32, "err_flag",
+                                   workspace, None, "workspace")
+    code = _dtype_code(dtable) | (AERO_DW_ACCUMULATE if accumulate else 0)
+    st = _lib.aero_embedding_bwd(d, _dtype_code(dout), T, H, ld_dout, i, V, scale, g, code, err, ws, _bytes(workspace), _stream(dout))
+    _check(st, "aero_embedding_bwd")

@@ -4,6 +4,10 @@
 namespace aero {
 size_t loss_workspace_bytes(int64_t T);
 size_t fused_workspace_bytes(int64_t T, int32_t V, int32_t H);
+size_t topk_workspace_bytes(int64_t T, int32_t V, int32_t K);
+size_t distill_workspace_bytes(int64_t T, int32_t V);
+size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B);
+size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H);
 }  // namespace aero
 
 extern "C" const char* aero_status_string(aero_status s) {
@@ -22,11 +26,14 @@ extern "C" const char* aero_status_string(aero_status s) {
 
 extern "C" size_t aero_workspace_bytes(int32_t op, int64_t T, int32_t V, int32_t H, int32_t R, int32_t Q) {
   (void)R;
-  (void)Q;
   if (T < 0) return 0;
   switch (op) {
     case AERO_OP_GRPO_LOSS_BWD: return aero::loss_workspace_bytes(T);
     case AERO_OP_LMHEAD_FUSED: return aero::fused_workspace_bytes(T, V, H);
+    case AERO_OP_TOPK_LOGPROB: return aero::topk_workspace_bytes(T, V, H);
+    case AERO_OP_DISTILL_LOSS_BWD: return aero::distill_workspace_bytes(T, V);
+    case AERO_OP_VERIFY_DRAFT: return aero::verify_workspace_bytes(T, V, Q);
+    case AERO_OP_EMBEDDING_BWD: return aero::embedding_workspace_bytes(T, V, H);
     default: return 0;
   }
 }
