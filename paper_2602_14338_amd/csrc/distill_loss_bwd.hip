@@ -182,7 +182,10 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   const SoftSum rest = soft_block_reduce<NT>(st, s_sum);
   __syncthreads();
   SoftSum own = soft_identity();
-  if (there && !(own_z <= kMasked)) own = SoftSum{own_z, 1.f};
+  if (there && !(own_z <= kMasked)) {
+    float z[1] = {own_z};
+    soft_update<1>(own, z);
+  }
   own = soft_block_reduce<NT>(own, s_sum);
   const SoftSum all = soft_merge(rest, own);
   if (all.s == 0.f) {   // uniform: nothing but masked logits
@@ -190,10 +193,10 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     zero_fill();
     return;
   }
-  const double lse = all.m < INFINITY ? double(all.m) + log(double(all.s)) : __builtin_nan("");   // a +inf logit
+  const double lse = soft_lse(all);
   const bool has_rest = rest.s != 0.f;
-  const double rest_lse = has_rest ? double(rest.m) + log(double(rest.s)) : 0.0;
-  const double rest_lq = rest_lse - lse, rest_q = has_rest ? exp(rest_lq) : 0.0;
+  const double rest_lq = has_rest ? soft_lse(rest) - lse : 0.0;
+  const double rest_q = has_rest ? double(rest.s) / double(all.s) * exp2(double(rest.o) - double(all.o)) : 0.0;
   double scale_p = 1.0, rest_p = 0.0, total = 1.0, lnorm = 0.0;
   if (a.tail == AERO_TAIL_RENORM) {
     scale_p = 1.0 / mass;
@@ -216,21 +219,21 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   // The others' coefficient is taken relative to their own softmax, (P - p_r / q_r) q_j = (P q_r - p_r) q_j / q_r, so that it
   // stays bounded however little mass they have.
   const double g = double(w) * double(a.grad_scale);
-  const float at_listed = float(g * total), at_other = float(g * (total * rest_q - rest_p));
-  const float c = float(-lse * 1.4426950408889634), c_other = float(-rest_lse * 1.4426950408889634);
+  const float at_listed = float(g * total / double(all.s));
+  const float at_other = has_rest ? float(g * (total * rest_q - rest_p) / double(rest.s)) : 0.f;
   int listed = next_listed(list, -1);
   auto turn = [&](const u32x4_t& v, int i) {
     float z[E], d[E];
     View::unpack(v, z);
 #pragma unroll
-    for (int e = 0; e < E; ++e) d[e] = at_other * exp2_fast(fmaf(z[e], kLog2e, c_other));
+    for (int e = 0; e < E; ++e) d[e] = at_other * exp2_fast(fmaf(z[e], kLog2e, -rest.o));
     if (__builtin_amdgcn_ballot_w64(i == listed) != 0 && i == listed) {
       for (int k = list.head[tid]; k >= 0; k = list.next[k])
         if (list.vec[k] == i) {
           const int own = list.elt[k];
           const float p = list.p[k];
 #pragma unroll
-          for (int e = 0; e < E; ++e) d[e] = e == own ? fmaf(at_listed, exp2_fast(fmaf(z[e], kLog2e, c)), -p) : d[e];
+          for (int e = 0; e < E; ++e) d[e] = e == own ? fmaf(at_listed, exp2_fast(fmaf(z[e], kLog2e, -all.o)), -p) : d[e];
         }
       listed = next_listed(list, i);
     }
@@ -247,10 +250,10 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   }
   for (; i < nvec; i += NT) turn(row.load(i), i);
   if (jr >= 0) {
-    float d = at_other * exp2_fast(fmaf(zr, kLog2e, c_other));
+    float d = at_other * exp2_fast(fmaf(zr, kLog2e, -rest.o));
     if (listed == nvec)
       for (int k = list.head[tid]; k >= 0; k = list.next[k])
-        if (list.vec[k] == nvec) d = fmaf(at_listed, exp2_fast(fmaf(zr, kLog2e, c)), -list.p[k]);
+        if (list.vec[k] == nvec) d = fmaf(at_listed, exp2_fast(fmaf(zr, kLog2e, -all.o)), -list.p[k]);
     store_elt<DT>(drow, jr, d);
   }
 }

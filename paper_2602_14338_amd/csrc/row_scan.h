@@ -5,18 +5,24 @@
 
 namespace aero {
 
-// A logit at or below this is masked (-inf, or the lowest value of fp32 / bf16, as masks write it).  It is also where a running
-// offset starts: exp(z - offset) of a masked logit is then 0 by itself, and never inf - inf.
+// A logit at or below this is masked (-inf, or the lowest value of fp32 / bf16, as masks write it).
 constexpr float kMasked = -1e30f;
+// Where a running offset starts, in units of log 2 and a little above the masked logits: their exponentials are 0 by
+// themselves, and never exp(inf - inf).
+constexpr float kMaskedLog2 = -1.4426e30f;
 
-// Sum of exp(z - m) with an offset m that is near the largest z.  s == 0: nothing but masked logits.  A NaN or +inf logit makes
-// s NaN.
+// 2^o s = sum of 2^(z log2 e) over the logits, o a whole number near the largest z log2 e.  Being whole, it is subtracted inside the fused
+// multiply-add without a rounding of its own, and sums with different offsets meet without one either: the error of an exponential is
+// that of its argument near the offset, whatever the size of the logits.  (An offset in the logits' own units costs
+// 2^-24 |z| in every probability, 3 times the error of a gradient in fp32.)  s == 0: nothing but masked logits.  A NaN or +inf logit
+// makes s NaN.
 struct SoftSum {
-  float m, s;
+  float o, s;
 };
-__device__ __forceinline__ SoftSum soft_identity() { return SoftSum{kMasked, 0.f}; }
+__device__ __forceinline__ SoftSum soft_identity() { return SoftSum{kMaskedLog2, 0.f}; }
+__device__ __forceinline__ float soft_offset(float z) { return rintf(z * kLog2e); }
 
-// The offset moves only for a logit more than kLazy above it (see stat_update, whose sums these are without the third one).
+// The largest of a vector's logits (NaN are passed over).
 template <int N> __device__ __forceinline__ float vec_max(const float (&z)[N]) {
   float vm = z[0];
   if constexpr (N >= 3) {
@@ -28,32 +34,36 @@ template <int N> __device__ __forceinline__ float vec_max(const float (&z)[N]) {
   }
   return vm;
 }
+
+// The offset moves only for a logit more than 2^kAbove above it, so the rescaling is rare (the test in front and the side effect keep it a
+// branch, see stat_update).
+constexpr float kAbove = 17.f;
 template <int N> __device__ __forceinline__ void soft_update(SoftSum& st, const float (&z)[N], float vm) {
-  const bool grow = vm > st.m + kLazy;
+  const bool grow = fmaf(vm, kLog2e, -st.o) > kAbove;
   if (__builtin_amdgcn_ballot_w64(grow) != 0) {
-    asm volatile("" ::: "memory");   // a side effect: the block cannot be if-converted
+    asm volatile("" ::: "memory");
     if (grow) {
-      st.s *= exp2_fast((st.m - vm) * kLog2e);
-      st.m = vm;
+      const float o = soft_offset(vm);
+      st.s *= exp2_fast(st.o - o);
+      st.o = o;
     }
   }
-  const float c = -st.m * kLog2e;
 #pragma unroll
-  for (int k = 0; k < N; ++k) st.s += exp2_fast(fmaf(z[k], kLog2e, c));
+  for (int k = 0; k < N; ++k) st.s += exp2_fast(fmaf(z[k], kLog2e, -st.o));
 }
 template <int N> __device__ __forceinline__ void soft_update(SoftSum& st, const float (&z)[N]) { soft_update<N>(st, z, vec_max<N>(z)); }
 
-__device__ __forceinline__ SoftSum soft_rescaled(SoftSum a, float M) {
-  return SoftSum{M, a.m == M ? a.s : a.s * exp2_fast((a.m - M) * kLog2e)};
+__device__ __forceinline__ SoftSum soft_rescaled(SoftSum a, float o) {
+  return SoftSum{o, a.o == o ? a.s : a.s * exp2_fast(a.o - o)};
 }
 __device__ __forceinline__ SoftSum soft_merge(SoftSum a, SoftSum b) {
-  const float M = fmaxf(a.m, b.m);
-  return SoftSum{M, soft_rescaled(a, M).s + soft_rescaled(b, M).s};
+  const float o = fmaxf(a.o, b.o);
+  return SoftSum{o, soft_rescaled(a, o).s + soft_rescaled(b, o).s};
 }
 template <bool WAVE> __device__ __forceinline__ SoftSum soft_reduce(SoftSum a) {
   auto all = [](float x, auto op) { return WAVE ? wave_reduce(x, op) : row16_reduce(x, op); };
-  const float M = all(a.m, [](float x, float y) { return fmaxf(x, y); });
-  return SoftSum{M, all(soft_rescaled(a, M).s, [](float x, float y) { return x + y; })};
+  const float o = all(a.o, [](float x, float y) { return fmaxf(x, y); });
+  return SoftSum{o, all(soft_rescaled(a, o).s, [](float x, float y) { return x + y; })};
 }
 // Over the workgroup, every thread gets the result; one barrier.  lds is free again after the next barrier.
 template <int NT> __device__ __forceinline__ SoftSum soft_block_reduce(SoftSum a, SoftSum* lds /*[NT/64]*/) {
@@ -69,10 +79,18 @@ template <int NT> __device__ __forceinline__ SoftSum soft_block_reduce(SoftSum a
   return a;
 }
 
-// Log-partition, log-prob of a logit zy of the row and its rounding remainder.  An empty row: lse -inf, log-probs NaN.
-__device__ __forceinline__ RowLogProb soft_logprob(SoftSum st, float zy) {
-  if (st.s == 0.f) return RowLogProb{-INFINITY, __builtin_nanf(""), 0.f};
-  return row_logprob(RowStat{st.m, st.s, 0.f}, zy);
+// log sum exp in 64 bits: (o + k + log2 f) / log2 e with s = 2^k f, f in [1/sqrt 2, sqrt 2), whose logarithm rounds by 2^-26 at most; log2 e is
+// the rounded one that the sums were formed with.  -inf for an empty row, NaN for one with a NaN or +inf logit.
+__device__ __forceinline__ double soft_lse(SoftSum st) {
+  if (st.s == 0.f) return -INFINITY;
+  float f = __builtin_amdgcn_frexp_mantf(st.s);
+  int k = __builtin_amdgcn_frexp_expf(st.s);
+  if (f < 0.70710678f) {
+    f *= 2.f;
+    --k;
+  }
+  const double lse = (double(st.o) + double(k) + double(logf(f)) * 1.4426950408889634) * (1.0 / double(kLog2e));
+  return st.o < INFINITY && st.s == st.s ? lse : __builtin_nan("");
 }
 
 // One row as E-element vectors (VEC: 16 bytes between the ragged ends; otherwise single elements), of which this workgroup looks
@@ -95,6 +113,11 @@ template <int DT, bool VEC> struct RowView {
     } else {
       return u32x4_t{__float_as_uint(load_elt<DT>(row, vec)), 0u, 0u, 0u};
     }
+  }
+  // the same for a vector that was read before: out of the caches
+  __device__ __forceinline__ u32x4_t load_again(int vec) const {
+    if constexpr (VEC) return reinterpret_cast<const u32x4_t*>(row + head * Storage<DT>::kBytes)[vec];
+    else return load(vec);
   }
   __device__ __forceinline__ static void unpack(const u32x4_t& v, float (&z)[E]) {
     if constexpr (VEC) unpack_vec<DT>(v, z);

@@ -110,8 +110,26 @@ struct Drawn {
 __device__ __forceinline__ void race(Drawn& d, float score, int j) {
   if (score > d.score) d = Drawn{score, j};   // columns ascend within a thread
 }
-__device__ __forceinline__ unsigned long long drawn_key(Drawn d) {
+__device__ __forceinline__ uint64_t drawn_key(Drawn d) {
   return d.score > 0.f ? (uint64_t(__float_as_uint(d.score)) << 32) | uint32_t(~d.j) : 0;
+}
+// E elements from column j on, or floats, at any element's alignment.
+typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(1)));
+typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+template <int DT, bool VEC> __device__ __forceinline__ u32x4_t load_elts(const char* row, int j) {
+  if constexpr (VEC) return *reinterpret_cast<const u32x4_any_t*>(row + int64_t(j) * Storage<DT>::kBytes);
+  else return u32x4_t{__float_as_uint(load_elt<DT>(row, j)), 0u, 0u, 0u};
+}
+template <int E> __device__ __forceinline__ void load_floats(const float* x, float (&y)[E]) {
+  if constexpr (E == 1) {
+    y[0] = x[0];
+  } else {
+#pragma unroll
+    for (int k = 0; k < E; k += 4) {
+      const f32x4_any_t v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any_t*>(x + k));
+      y[k] = v.x; y[k + 1] = v.y; y[k + 2] = v.z; y[k + 3] = v.w;
+    }
+  }
 }
 template <int NT> __device__ __forceinline__ uint64_t block_max_u64(uint64_t x, uint64_t* lds) {
 #pragma unroll
@@ -129,6 +147,7 @@ template <int NT> __device__ __forceinline__ uint64_t block_max_u64(uint64_t x, 
 
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
+  constexpr int E = RowView<DT, VEC>::E;
   __shared__ uint64_t s_key[2][NT / kWave];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid % kWave, b = blockIdx.x, part = blockIdx.y, parts = gridDim.y;
@@ -151,50 +170,60 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   // ---- lane i: position i ----
   const int64_t n_target = int64_t(a.B) * (a.G + 1);
   bool ok = false;
-  float lp = 0.f;
+  double lp = 0.0;
   if (lane < count) {
     const int64_t rt = int64_t(b) * (a.G + 1) + lane, rd = int64_t(b) * a.G + lane;
-    const RowLogProb p = soft_logprob(row_sum(a, rt), load_elt<DT>(row_ptr<DT>(a.target, rt, a.ld), token));
+    lp = double(load_elt<DT>(row_ptr<DT>(a.target, rt, a.ld), token)) - soft_lse(row_sum(a, rt));
     double q = 1.0;
-    if (a.draft) {
-      const RowLogProb d = soft_logprob(row_sum(a, n_target + rd), load_elt<DT>(row_ptr<DT>(a.draft, rd, a.ld), token));
-      q = exp(double(d.lp) + double(d.low));
-    }
-    lp = p.lp;
-    ok = double(a.uniform[rd]) * q < exp(double(p.lp) + double(p.low));
+    if (a.draft) q = exp(double(load_elt<DT>(row_ptr<DT>(a.draft, rd, a.ld), token)) - soft_lse(row_sum(a, n_target + rd)));
+    ok = double(a.uniform[rd]) * q < exp(lp);
   }
   const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(ok));   // at most 63 positions
   const bool refused = n < count;
-  const int own = refused ? __builtin_amdgcn_readlane(token, n) : -1;   // drafted id that was refused
+  const int own = refused && !a.draft ? __builtin_amdgcn_readlane(token, n) : -1;   // the whole of q
 
   // ---- the draw: this workgroup's slice of row n ----
   const int64_t rt = int64_t(b) * (a.G + 1) + n, rd = int64_t(b) * a.G + n;
   const SoftSum pt = row_sum(a, rt);
-  const float lse = soft_logprob(pt, 0.f).lse;
-  const float cp = -lse * kLog2e;
-  const bool subtract = refused && a.draft;
-  float cq = 0.f;
-  bool usable_q = false;
-  if (subtract) {
-    const float lq = soft_logprob(row_sum(a, n_target + rd), 0.f).lse;
-    usable_q = fabsf(lq) < INFINITY;
-    cq = -lq * kLog2e;
-  }
+  const double lse = soft_lse(pt);
   Drawn left{0.f, 0}, whole{0.f, 0};
-  if (fabsf(lse) < INFINITY) {
-    const char* const trow = row_ptr<DT>(a.target, rt, a.ld);
-    const char* const qrow = usable_q ? row_ptr<DT>(a.draft, rd, a.ld) : nullptr;
+  if (lse - lse == 0.0) {   // finite
+    SoftSum qt = soft_identity();
+    if (refused && a.draft) qt = row_sum(a, n_target + rd);
+    const double lse_q = soft_lse(qt);
+    const bool minus = lse_q - lse_q == 0.0;
+    const float op = -pt.o, sp = 1.f / pt.s, oq = minus ? -qt.o : 0.f, sq = minus ? 1.f / qt.s : 0.f;
+    const RowView<DT, VEC> prow(a.target, rt, a.ld, a.V);
+    const char* const qrow = minus ? row_ptr<DT>(a.draft, rd, a.ld) : nullptr;
     const float* const noise = a.noise + int64_t(b) * a.V;
-    const int per = ((a.V + parts - 1) / parts + 63) / 64 * 64;
-    const int first = min(part * per, a.V), last = min(first + per, a.V);
-    for (int j = first + tid; j < last; j += NT) {
-      const float e = noise[j];
-      const float p = exp2_fast(fmaf(load_elt<DT>(trow, j), kLog2e, cp));
-      float r = p;
-      if (qrow) r = p - exp2_fast(fmaf(load_elt<DT>(qrow, j), kLog2e, cq));
-      else if (j == own && !a.draft) r = 0.f;
-      race(left, r / e, j);
-      if (refused) race(whole, p / e, j);
+    auto consider = [&](float z, float y, float e, int j) {
+#pragma clang fp contract(off)   // equal probabilities leave nothing
+      const float p = sp * exp2_fast(fmaf(z, kLog2e, op)), chance = __builtin_amdgcn_rcpf(e);
+      const float q = sq * exp2_fast(fmaf(y, kLog2e, oq)), r = j == own ? 0.f : p - q;
+      race(left, r * chance, j);
+      race(whole, p * chance, j);
+    };
+    const int per = (prow.nvec + parts - 1) / parts;
+    const int first = min(part * per, prow.nvec), last = min(first + per, prow.nvec);
+    for (int i = first + tid; i < last; i += NT) {
+      const int j = prow.column(i);
+      float z[E], y[E], e[E];
+      const u32x4_t zv = prow.load_again(i);
+      u32x4_t yv = {0u, 0u, 0u, 0u};
+      if (minus) yv = load_elts<DT, VEC>(qrow, j);
+      load_floats<E>(noise + j, e);
+      prow.unpack(zv, z);
+      prow.unpack(yv, y);
+#pragma unroll
+      for (int k = 0; k < E; ++k) consider(z[k], y[k], e[k], j + k);
+    }
+    const int jr = part == 0 ? prow.ragged() : -1;
+    if (jr >= 0) {   // a tie goes to the lower id, which is not the later one here
+      Drawn l = left, w = whole;
+      left = whole = Drawn{0.f, 0};
+      consider(prow.at(jr), minus ? load_elt<DT>(qrow, jr) : 0.f, noise[jr], jr);
+      left = drawn_key(l) > drawn_key(left) ? l : left;
+      whole = drawn_key(w) > drawn_key(whole) ? w : whole;
     }
   }
   const uint64_t k_left = block_max_u64<NT>(drawn_key(left), s_key[0]);
@@ -211,11 +240,11 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   uint64_t key = atomicMax(&a.best[2 * b], 0ull);
   if (!key && refused) key = atomicMax(&a.best[2 * b + 1], 0ull);
   const int drawn = key ? int(~uint32_t(key)) : -1;
-  const float drawn_lp = drawn >= 0 ? soft_logprob(pt, load_elt<DT>(row_ptr<DT>(a.target, rt, a.ld), drawn)).lp : 0.f;
+  const float drawn_lp = drawn >= 0 ? float(double(load_elt<DT>(row_ptr<DT>(a.target, rt, a.ld), drawn)) - lse) : 0.f;
   if (lane == 0) a.accepted[b] = n;
   if (lane <= a.G) {
     out[lane] = lane < n ? token : lane == n ? drawn : -1;
-    if (lp_out) lp_out[lane] = lane < n ? lp : lane == n ? drawn_lp : 0.f;
+    if (lp_out) lp_out[lane] = lane < n ? float(lp) : lane == n ? drawn_lp : 0.f;
   }
 }
 
@@ -228,9 +257,10 @@ size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B) {
 template <int DT, bool VEC> static void verify_launch(VerifyArgs a, hipStream_t s) {
   constexpr int NT = 512;
   const int64_t rows = int64_t(a.B) * (a.G + 1) + (a.draft ? int64_t(a.B) * a.G : 0);
-  a.parts = 1;
+  const int nvec = a.V / RowView<DT, VEC>::E;
+  a.parts = int(std::max<int64_t>(1, std::min<int64_t>({kVerifyParts, 2 * compute_units() / rows, nvec / (4 * NT)})));
   hipLaunchKernelGGL((k_verify_rows<NT, DT, VEC>), dim3(unsigned(rows), unsigned(a.parts)), dim3(NT), 0, s, a);
-  const int parts = int(std::min<int64_t>(std::max<int64_t>(1, 1024 / a.B), (a.V + 4095) / 4096));
+  const int parts = int(std::max<int64_t>(1, std::min<int64_t>(4 * compute_units() / a.B, nvec / NT)));
   hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC>), dim3(unsigned(a.B), unsigned(parts)), dim3(NT), 0, s, a);
 }
 
