@@ -10,46 +10,16 @@
 // listed places out (they count as masked while it runs) and their K exponentials are added to it.  Each thread knows from a
 // chain of the entries that fall into its vectors which of them hold listed places, so that all other vectors pay one
 // comparison.
+#include <algorithm>
+#include <mutex>
+
 #include "row_scan.h"
 
 namespace aero {
 
 constexpr int kListMax = AERO_TOPK_MAX;
-constexpr int kNowhere = 0x7fffffff;
-
-// The entries of a row's list by the thread that looks after their place.
-template <int NT> struct ListPlaces {
-  int32_t head[NT];          // first entry of a thread's chain, -1: none
-  int32_t next[kListMax];
-  int32_t vec[kListMax];     // vector of the place; nvec: the ragged element of its thread
-  uint8_t elt[kListMax];
-  float p[kListMax];         // w grad_scale p_k once the row's terms are known
-  int bad;
-};
-
-// Next vector of this thread from `after` on (exclusive) that holds a listed place.
-template <int NT> __device__ __forceinline__ int next_listed(const ListPlaces<NT>& l, int after) {
-  int v = kNowhere;
-  for (int k = l.head[threadIdx.x]; k >= 0; k = l.next[k]) {
-    const int at = l.vec[k];
-    if (at > after && at < v) v = at;
-  }
-  return v;
-}
-
-template <int NT> __device__ __forceinline__ double block_sum_d(double x, double* lds /*[NT/64]*/) {
-  x = wave_sum_d(x);
-  constexpr int kWaves = NT / kWave;
-  if constexpr (kWaves > 1) {
-    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = x;
-    __syncthreads();
-    x = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) x += lds[w];
-    __syncthreads();
-  }
-  return x;
-}
+constexpr int kListWaves = kListMax / kWave;
+constexpr int kRagged = 31;   // in the place of a vector's number within its thread: the element outside the vectors
 
 struct DistillArgs {
   const void* logits;
@@ -67,14 +37,164 @@ struct DistillArgs {
   int32_t* err_flag;
 };
 
-// One workgroup per row, which is read twice.  VEC: 16-byte vectors (logits and dlogits at the same offset from 16 bytes).
+// The entries of a row's list by the thread that looks after their place (thread = vector % NT).
+template <int NT> struct ListPlaces {
+  int32_t head[NT];         // first entry of a thread's chain, -1: none
+  int16_t next[kListMax];
+  uint16_t turn[kListMax];  // vector / NT; kRagged with elt kRagged: the thread's ragged element
+  uint8_t elt[kListMax];
+  float p[kListMax];        // teacher probability
+};
+
+// One entry as its thread holds it, and what a wave of them adds up to.
+struct ListEntry {
+  int j;      // id, -1: absent
+  double p, lp;
+  float z;
+};
+struct ListSums {
+  double mass, p_lp_z;   // sum p, sum p (ln p - z)
+  SoftSum own;           // of the listed logits
+  int32_t any, bad;
+};
+
+// The list's ids find their threads.  entry.j >= V has been told apart before.
+template <int NT, int DT, bool VEC>
+__device__ __forceinline__ void list_place(ListPlaces<NT>& list, const RowView<DT, VEC>& row, int k, int j) {
+  constexpr int E = RowView<DT, VEC>::E;
+  const int at = j - row.head;
+  int owner, turn, elt;
+  if (at >= 0 && at < row.nvec * E) {
+    const int vec = at / E;
+    owner = vec % NT;
+    turn = vec / NT;
+    elt = at % E;
+  } else {
+    owner = at < 0 ? j : E + at - row.nvec * E;
+    turn = kRagged;
+    elt = kRagged;
+  }
+  list.turn[k] = uint16_t(turn);
+  list.elt[k] = uint8_t(elt);
+  list.next[k] = int16_t(atomicExch(&list.head[owner], k));
+}
+// After the barrier behind list_place: is the entry's place taken by another entry further down the chain?
+template <int NT> __device__ __forceinline__ bool list_twice(const ListPlaces<NT>& list, int k) {
+  bool twice = false;
+  for (int e = list.next[k]; e >= 0; e = list.next[e]) twice |= list.turn[e] == list.turn[k] && list.elt[e] == list.elt[k];
+  return twice;
+}
+// Calls f(entry, element) for this thread's listed places of one turn.
+template <int NT, class F> __device__ __forceinline__ void each_listed(const ListPlaces<NT>& list, int turn, bool ragged, F f) {
+  for (int k = list.head[threadIdx.x]; k >= 0; k = list.next[k])
+    if (list.turn[k] == turn && (list.elt[k] == kRagged) == ragged) f(k, int(list.elt[k]));
+}
+
+// Sums over the entries of a wave, left in s[wave] by its first lane.
+__device__ __forceinline__ void list_sum(const ListEntry& e, bool bad, ListSums* s) {
+  ListSums sum;
+  const bool there = e.j >= 0;
+  sum.own = soft_identity();
+  if (there && !(e.z <= kMasked)) {
+    float z[1] = {e.z};
+    soft_update<1>(sum.own, z);
+  }
+  sum.own = soft_reduce<true>(sum.own);
+  sum.mass = wave_sum_d(there ? e.p : 0.0);
+  sum.p_lp_z = wave_sum_d(there && e.p != 0.0 ? e.p * (e.lp - (e.z <= kMasked ? -INFINITY : double(e.z))) : 0.0);
+  sum.any = __builtin_amdgcn_ballot_w64(there) != 0;
+  sum.bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+  if (threadIdx.x % kWave == 0) s[threadIdx.x / kWave] = sum;
+}
+
+__device__ __forceinline__ void put_loss(const DistillArgs& a, int64_t t, float w, float loss) {
+  a.term[t] = loss == 0.f ? 0.f : w * loss;   // a quiet row's weight may be anything
+  if (a.row_loss) a.row_loss[t] = loss;
+}
+// The same value in every lane, said to the compiler: it lives in a scalar register.
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+
+// A gradient vector: at_other 2^(z log2 e - o_rest), and at the listed places at_listed 2^(z log2 e - o_all) - scale_p p.  The others'
+// coefficient is taken relative to their own softmax, (P - p_r / q_r) q_j = (P q_r - p_r) q_j / q_r, so that it stays bounded however
+// little mass they have.
+struct RowGrad {
+  float at_other, o_rest, at_listed, o_all, scale_p;
+  bool quiet;   // no loss, no gradient
+};
+// What the sum over the other places and the list come to; the first thread writes the loss (a quiet row's too).  By all threads.
+__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftSum rest, const ListSums* s, int waves) {
+  double mass = 0.0, p_lp_z = 0.0;
+  SoftSum all = rest;
+  bool any = false, bad = false;
+  for (int k = 0; k < waves; ++k) {   // uniform
+    mass += s[k].mass;
+    p_lp_z += s[k].p_lp_z;
+    all = soft_merge(all, s[k].own);
+    any |= s[k].any != 0;
+    bad |= s[k].bad != 0;
+  }
+  const bool has_rest = rest.s != 0.f, renorm = a.tail == AERO_TAIL_RENORM;
+  const float rest_q = has_rest ? rest.s / all.s * exp2_fast(rest.o - all.o) : 0.f;
+  const double g = double(w) * double(a.grad_scale);
+  const double rest_p = renorm || !has_rest || mass >= 1.0 ? 0.0 : 1.0 - mass;
+  const double total = renorm ? 1.0 : mass + rest_p;
+  RowGrad r;
+  r.quiet = bad || !any || all.s == 0.f || (renorm && mass == 0.0);
+  r.scale_p = uniform(float(renorm ? g / mass : g));
+  r.at_listed = uniform(float(g * total) / all.s);
+  r.o_all = uniform(all.o);
+  r.at_other = uniform(has_rest ? float(g * (total * double(rest_q) - rest_p)) / rest.s : 0.f);
+  r.o_rest = uniform(rest.o);
+  if (threadIdx.x == 0) {
+    if (bad && a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_TEACHER);
+    double loss = 0.0;
+    if (!r.quiet) {   // logarithms of 32-bit numbers: 2^-24 of the logarithm
+      const double lse = soft_lse(all);
+      if (renorm) {
+        loss = p_lp_z / mass - double(logf(float(mass))) + lse;
+      } else {
+        loss = p_lp_z + (mass != 0.0 ? mass * lse : 0.0);
+        if (rest_p != 0.0) loss += rest_p * (double(logf(float(rest_p))) - (soft_lse(rest) - lse));
+      }
+    }
+    put_loss(a, t, w, float(loss));
+  }
+  return r;
+}
+
+// One vector of the gradient row.  listed: some of its places are.
+template <int NT, int E>
+__device__ __forceinline__ void grad_elts(const float (&z)[E], float (&d)[E], const RowGrad& r, const ListPlaces<NT>& list, bool listed, int turn) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) d[e] = r.at_other * exp2_fast(fmaf(z[e], kLog2e, -r.o_rest));
+  if (listed)
+    each_listed(list, turn, false, [&](int k, int own) {
+      const float less = r.scale_p * list.p[k];
+#pragma unroll
+      for (int e = 0; e < E; ++e) d[e] = e == own ? r.at_listed * exp2_fast(fmaf(z[e], kLog2e, -r.o_all)) - less : d[e];
+    });
+}
+template <int NT> __device__ __forceinline__ float grad_ragged(float z, const RowGrad& r, const ListPlaces<NT>& list) {
+  float d = r.at_other * exp2_fast(fmaf(z, kLog2e, -r.o_rest));
+  each_listed(list, kRagged, true, [&](int k, int) { d = r.at_listed * exp2_fast(fmaf(z, kLog2e, -r.o_all)) - r.scale_p * list.p[k]; });
+  return d;
+}
+template <int NT, int E> __device__ __forceinline__ void mask_listed(float (&z)[E], const ListPlaces<NT>& list, int turn) {
+  each_listed(list, turn, false, [&](int, int own) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = e == own ? -INFINITY : z[e];
+  });
+}
+
+// One workgroup per row, which is read twice: any row.
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   using View = RowView<DT, VEC>;
   constexpr int E = View::E, kAhead = 4, kWaves = NT / kWave;
+  static_assert(NT >= kListMax, "an entry per thread");
   __shared__ ListPlaces<NT> list;
   __shared__ SoftSum s_sum[kWaves];
-  __shared__ double s_dbl[kWaves];
+  __shared__ ListSums s_list[kListWaves];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, K = a.K;
   const float w = a.weight[t];
@@ -87,12 +207,6 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     else
       store_elt<DT>(drow, vec, d[0]);
   };
-  auto finish = [&](float loss) {
-    if (tid == 0) {
-      a.term[t] = loss == 0.f ? 0.f : w * loss;   // an ignored row's weight may be anything
-      if (a.row_loss) a.row_loss[t] = loss;
-    }
-  };
   auto zero_fill = [&]() {
     if (!drow) return;
     float zero[E];
@@ -102,159 +216,377 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
   };
   if (w == 0.f) {   // uniform
-    finish(0.f);
+    if (tid == 0) put_loss(a, t, w, 0.f);
     zero_fill();
     return;
   }
-
-  // ---- the list: probabilities, and whose vectors the places are in ----
   list.head[tid] = -1;
-  if (tid == 0) list.bad = 0;
   __syncthreads();
-  double mass = 0.0, own_p = 0.0, own_lp = 0.0;
-  float own_z = -INFINITY;
-  bool there = false;
-  if (tid < K) {   // K <= NT
-    const int j = a.index[t * K + tid];
-    if (j >= a.V) list.bad = 1;
-    there = j >= 0 && j < a.V;
-    if (there) {
-      own_lp = double(a.logprob[t * K + tid]);
-      own_p = exp(own_lp);
-      own_z = row.at(j);
-      int vec = (j - row.head) / E, elt = (j - row.head) % E, owner = vec % NT;
-      if constexpr (VEC) {
-        if (j < row.head || vec >= nvec) {
-          owner = j < row.head ? j : E + j - row.head - nvec * E;
-          vec = nvec;
-          elt = 0;
-        }
-      }
-      list.vec[tid] = vec;
-      list.elt[tid] = uint8_t(elt);
-      list.next[tid] = atomicExch(&list.head[owner], tid);
+  ListEntry entry{-1, 0.0, 0.0, 0.f};
+  bool bad = false;
+  if (tid < K) {
+    entry.j = a.index[t * K + tid];
+    bad = entry.j >= a.V;
+    if (bad) entry.j = -1;
+    if (entry.j >= 0) {
+      entry.lp = double(a.logprob[t * K + tid]);
+      entry.z = row.at(entry.j);
+      list_place(list, row, tid, entry.j);
+      entry.p = exp(entry.lp);
+      list.p[tid] = float(entry.p);
     }
   }
-  mass = block_sum_d<NT>(there ? own_p : 0.0, s_dbl);
-  if (there)
-    for (int k = list.next[tid]; k >= 0; k = list.next[k])
-      if (list.vec[k] == list.vec[tid] && list.elt[k] == list.elt[tid]) list.bad = 1;
-  const bool any = __syncthreads_or(there);
-  if (list.bad && tid == 0 && a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_TEACHER);
-  if (list.bad || !any || (a.tail == AERO_TAIL_RENORM && mass == 0.0)) {   // uniform
-    finish(0.f);
-    zero_fill();
-    return;
+  __syncthreads();
+  if (tid < kListMax) {   // whole waves
+    if (entry.j >= 0) bad |= list_twice(list, tid);
+    list_sum(entry, bad, s_list);
   }
+  const bool chained = list.head[tid] >= 0;
 
-  // ---- sum over the other places, then the list's part ----
   SoftSum st = soft_identity();
-  {
-    int listed = next_listed(list, -1);
-    auto fold = [&](const u32x4_t& v, int i) {
-      float z[E];
-      View::unpack(v, z);
-      if (__builtin_amdgcn_ballot_w64(i == listed) != 0 && i == listed) {
-        for (int k = list.head[tid]; k >= 0; k = list.next[k])
-          if (list.vec[k] == i) {
-            const int own = list.elt[k];
+  auto fold = [&](const u32x4_t& v, int turn) {
+    float z[E];
+    View::unpack(v, z);
+    if (chained) mask_listed(z, list, turn);
+    soft_update<E>(st, z);
+  };
+  int i = tid, turn = 0;
+  for (; i + (kAhead - 1) * NT < nvec; i += kAhead * NT, turn += kAhead) {
+    u32x4_t v[kAhead];
 #pragma unroll
-            for (int e = 0; e < E; ++e) z[e] = e == own ? -INFINITY : z[e];
-          }
-        listed = next_listed(list, i);
-      }
-      soft_update<E>(st, z);
-    };
-    int i = tid;
-    for (; i + (kAhead - 1) * NT < nvec; i += kAhead * NT) {
-      u32x4_t v[kAhead];
+    for (int u = 0; u < kAhead; ++u) v[u] = row.load_again(i + u * NT);
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) v[u] = row.load(i + u * NT);
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) fold(v[u], i + u * NT);
-    }
-    for (; i < nvec; i += NT) fold(row.load(i), i);
-    if (jr >= 0 && listed != nvec) {
-      float z[1] = {row.at(jr)};
-      soft_update<1>(st, z);
-    }
+    for (int u = 0; u < kAhead; ++u) fold(v[u], turn + u);
   }
-  const SoftSum rest = soft_block_reduce<NT>(st, s_sum);
-  __syncthreads();
-  SoftSum own = soft_identity();
-  if (there && !(own_z <= kMasked)) {
-    float z[1] = {own_z};
-    soft_update<1>(own, z);
+  for (; i < nvec; i += NT) fold(row.load_again(i), turn++);
+  const float zr = jr >= 0 ? row.at(jr) : 0.f;
+  if (jr >= 0) {
+    float z[1] = {zr};
+    each_listed(list, kRagged, true, [&](int, int) { z[0] = -INFINITY; });
+    soft_update<1>(st, z);
   }
-  own = soft_block_reduce<NT>(own, s_sum);
-  const SoftSum all = soft_merge(rest, own);
-  if (all.s == 0.f) {   // uniform: nothing but masked logits
-    finish(0.f);
+  st = soft_block_reduce<NT>(st, s_sum);   // its barrier: s_list
+  const RowGrad r = row_terms(a, t, w, st, s_list, kListWaves);
+  if (!drow) return;
+  if (r.quiet) {   // uniform
     zero_fill();
     return;
   }
-  const double lse = soft_lse(all);
-  const bool has_rest = rest.s != 0.f;
-  const double rest_lq = has_rest ? soft_lse(rest) - lse : 0.0;
-  const double rest_q = has_rest ? double(rest.s) / double(all.s) * exp2(double(rest.o) - double(all.o)) : 0.0;
-  double scale_p = 1.0, rest_p = 0.0, total = 1.0, lnorm = 0.0;
-  if (a.tail == AERO_TAIL_RENORM) {
-    scale_p = 1.0 / mass;
-    lnorm = log(mass);
-  } else {
-    if (has_rest) rest_p = fmax(0.0, 1.0 - mass);
-    total = mass + rest_p;
-  }
-  double part = 0.0;
-  if (there) {
-    if (own_p != 0.0) part = own_p * scale_p * (own_lp - lnorm - ((own_z <= kMasked ? -INFINITY : double(own_z)) - lse));
-    list.p[tid] = float(double(w) * double(a.grad_scale) * own_p * scale_p);
-  }
-  part = block_sum_d<NT>(part, s_dbl);   // its barriers: list.p is written
-  if (rest_p > 0.0) part += rest_p * (log(rest_p) - rest_lq);
-  finish(float(part));
-  if (!drow) return;
 
-  // ---- gradient row ----
-  // The others' coefficient is taken relative to their own softmax, (P - p_r / q_r) q_j = (P q_r - p_r) q_j / q_r, so that it
-  // stays bounded however little mass they have.
-  const double g = double(w) * double(a.grad_scale);
-  const float at_listed = float(g * total / double(all.s));
-  const float at_other = has_rest ? float(g * (total * rest_q - rest_p) / double(rest.s)) : 0.f;
-  int listed = next_listed(list, -1);
-  auto turn = [&](const u32x4_t& v, int i) {
+  auto turned = [&](const u32x4_t& v, int vec, int turn) {
     float z[E], d[E];
     View::unpack(v, z);
-#pragma unroll
-    for (int e = 0; e < E; ++e) d[e] = at_other * exp2_fast(fmaf(z[e], kLog2e, -rest.o));
-    if (__builtin_amdgcn_ballot_w64(i == listed) != 0 && i == listed) {
-      for (int k = list.head[tid]; k >= 0; k = list.next[k])
-        if (list.vec[k] == i) {
-          const int own = list.elt[k];
-          const float p = list.p[k];
-#pragma unroll
-          for (int e = 0; e < E; ++e) d[e] = e == own ? fmaf(at_listed, exp2_fast(fmaf(z[e], kLog2e, -all.o)), -p) : d[e];
-        }
-      listed = next_listed(list, i);
-    }
-    put(i, d);
+    grad_elts<NT, E>(z, d, r, list, chained, turn);
+    put(vec, d);
   };
-  const float zr = jr >= 0 ? row.at(jr) : 0.f;
-  int i = tid;
-  for (; i + (kAhead - 1) * NT < nvec; i += kAhead * NT) {
+  for (i = tid, turn = 0; i + (kAhead - 1) * NT < nvec; i += kAhead * NT, turn += kAhead) {
     u32x4_t v[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) v[u] = row.load(i + u * NT);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) turn(v[u], i + u * NT);
+    for (int u = 0; u < kAhead; ++u) turned(v[u], i + u * NT, turn + u);
   }
-  for (; i < nvec; i += NT) turn(row.load(i), i);
+  for (; i < nvec; i += NT) turned(row.load(i), i, turn++);
+  if (jr >= 0) store_elt<DT>(drow, jr, grad_ragged(zr, r, list));
+}
+
+// One workgroup per row, which its threads hold: kHeldVecs vectors each in registers.
+constexpr int kHeldVecs = 8;
+template <int NT, int DT>
+__global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
+  using View = RowView<DT, true>;
+  constexpr int E = View::E, kWaves = NT / kWave;
+  __shared__ ListPlaces<NT> list;
+  __shared__ SoftSum s_sum[kWaves];
+  __shared__ ListSums s_list[kListWaves];
+  const int64_t t = blockIdx.x;
+  const int tid = threadIdx.x, K = a.K;
+  const float w = a.weight[t];
+  int j = -1;
+  float lp = 0.f;
+  if (tid < K) {   // asked for ahead of what depends on the weight
+    j = a.index[t * K + tid];
+    lp = a.logprob[t * K + tid];
+  }
+  const View row(a.logits, t, a.ld, a.V);
+  const int nvec = row.nvec, jr = row.ragged();
+  char* const drow = a.dlogits ? row_ptr<DT>(a.dlogits, t, a.ld) : nullptr;
+  const __amdgpu_buffer_rsrc_t src = row.buffer(row.row), dst = row.buffer(drow ? drow : row.row);
+  const uint32_t voff = uint32_t(tid) * 16u;
+  auto zero_fill = [&]() {
+    if (!drow) return;
+    const u32x4_t zero = {0u, 0u, 0u, 0u};
+    for (int i = tid; i < nvec; i += NT) __builtin_amdgcn_raw_buffer_store_b128(zero, dst, uint32_t(i) * 16u, 0, 2);
+    if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
+  };
+  if (w == 0.f) {   // uniform
+    if (tid == 0) put_loss(a, t, w, 0.f);
+    zero_fill();
+    return;
+  }
+  ListEntry entry{j, 0.0, 0.0, 0.f};
+  bool bad = j >= a.V;
+  if (bad) entry.j = -1;
+  if (entry.j >= 0) entry.z = row.at(entry.j);
+  u32x4_t v[kHeldVecs];
+#pragma unroll
+  for (int u = 0; u < kHeldVecs; ++u) v[u] = __builtin_amdgcn_raw_buffer_load_b128(src, voff + uint32_t(u) * (NT * 16u), 0, 2);
+  const float zr = jr >= 0 ? row.at(jr) : 0.f;
+  list.head[tid] = -1;
+  __syncthreads();
+  if (entry.j >= 0) {
+    entry.lp = double(lp);
+    list_place(list, row, tid, entry.j);
+    entry.p = exp(entry.lp);
+    list.p[tid] = float(entry.p);
+  }
+  __syncthreads();
+  const int list_waves = (K + kWave - 1) / kWave;
+  if (tid < list_waves * kWave) {
+    if (entry.j >= 0) bad |= list_twice(list, tid);
+    list_sum(entry, bad, s_list);
+  }
+  uint32_t listed = 0;   // bit u: vector u has listed places
+  for (int k = list.head[tid]; k >= 0; k = list.next[k]) listed |= 1u << list.turn[k];
+
+  SoftSum st = soft_identity();
+#pragma unroll
+  for (int u = 0; u < kHeldVecs; ++u) {
+    if (tid < nvec - u * NT) {
+      float z[E];
+      View::unpack(v[u], z);
+      if (listed & (1u << u)) mask_listed(z, list, u);
+      soft_update<E>(st, z);
+    }
+    __builtin_amdgcn_sched_barrier(0);   // one vector at a time: keeps temporaries from piling up
+  }
   if (jr >= 0) {
-    float d = at_other * exp2_fast(fmaf(zr, kLog2e, -rest.o));
-    if (listed == nvec)
-      for (int k = list.head[tid]; k >= 0; k = list.next[k])
-        if (list.vec[k] == nvec) d = fmaf(at_listed, exp2_fast(fmaf(zr, kLog2e, -all.o)), -list.p[k]);
-    store_elt<DT>(drow, jr, d);
+    float z[1] = {listed >> kRagged ? -INFINITY : zr};
+    soft_update<1>(st, z);
+  }
+  // orders the loads of the row before the stores over it, for a gradient in place: by its barrier, and with one wave because
+  // every lane's result needs every lane's loads
+  st = soft_block_reduce<NT>(st, s_sum);
+  if constexpr (kWaves == 1) __syncthreads();
+  const RowGrad r = row_terms(a, t, w, st, s_list, list_waves);
+  if (!drow) return;
+  if (r.quiet) {   // uniform
+    zero_fill();
+    return;
+  }
+  uint32_t voff_st = voff;
+  asm volatile("" : "+v"(voff_st));   // the store offsets are formed again; the load offsets need not stay
+#pragma unroll
+  for (int u = 0; u < kHeldVecs; ++u) {
+    if (tid < nvec - u * NT) {
+      float z[E], d[E];
+      View::unpack(v[u], z);
+      grad_elts<NT, E>(z, d, r, list, listed & (1u << u), u);
+      __builtin_amdgcn_raw_buffer_store_b128(pack_vec<DT>(d), dst, voff_st + uint32_t(u) * (NT * 16u), 0, 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (jr >= 0) store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+}
+
+// Rows by a counter, those with a weight first: a persistent workgroup per CU draws its next row while it works on one.
+// ctr[0]: next position to hand out, ctr[1], ctr[2]: rows placed from the front and from the back.
+constexpr int kOrderNT = 1024;
+__global__ void k_distill_start(int32_t* ctr, int32_t grid) {
+  ctr[0] = grid;
+  ctr[1] = 0;
+  ctr[2] = 0;
+}
+// ONE: a single workgroup, which counts in LDS and needs no launch in front of it.
+template <bool ONE>
+__global__ __launch_bounds__(kOrderNT) void k_distill_order(int64_t T, const float* __restrict__ weight, int32_t grid,
+                                                            int32_t* __restrict__ ctr, int32_t* __restrict__ order) {
+  __shared__ int32_t own[2];
+  const int lane = threadIdx.x % kWave;
+  if constexpr (ONE) {
+    if (threadIdx.x < 2) own[threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x == 0) ctr[0] = grid;
+  }
+  int32_t* const count = ONE ? own : ctr + 1;
+  for (int64_t t0 = int64_t(blockIdx.x) * kOrderNT; t0 < T; t0 += int64_t(gridDim.x) * kOrderNT) {   // uniform
+    const int64_t t = t0 + threadIdx.x;
+    const bool in = t < T, need = in && weight[t] != 0.f;
+    const uint64_t m_need = __builtin_amdgcn_ballot_w64(need), m_rest = __builtin_amdgcn_ballot_w64(in && !need);
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    int front = 0, back = 0;
+    if (lane == 0) {
+      if (m_need) front = atomicAdd(count, __popcll(m_need));
+      if (m_rest) back = atomicAdd(count + 1, __popcll(m_rest));
+    }
+    front = __builtin_amdgcn_readfirstlane(front);
+    back = __builtin_amdgcn_readfirstlane(back);
+    if (need) order[front + __popcll(m_need & below)] = int32_t(t);
+    else if (in) order[T - 1 - (back + __popcll(m_rest & below))] = int32_t(t);
+  }
+}
+
+// Long rows that a CU holds: kStreamVecs vectors per thread of 1024, the first kStreamLds of them in LDS, in slots of the wave's own that
+// are filled by direct loads: as soon as a slot has been turned into gradient it is asked to be filled with the next row's vector, so
+// that a CU reads while it writes.  Two barriers a row: behind the placing of the list, and in the reduction; everything that
+// passes between waves is held twice, by the row's parity.
+constexpr int kStreamNT = 1024, kStreamVecs = 20, kStreamLds = 9;
+constexpr int kStreamLdsBytes = kStreamLds * kStreamNT * 16;
+template <int DT>
+__global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, int32_t* ctr, const int32_t* __restrict__ order) {
+  using View = RowView<DT, true>;
+  constexpr int E = View::E, NT = kStreamNT, NL = kStreamLds, NR = kStreamVecs - kStreamLds;
+  __shared__ ListPlaces<NT> lists[2];
+  __shared__ SoftSum s_sum[2][NT / kWave];
+  __shared__ ListSums s_list[2][kListWaves];
+  __shared__ int s_next[2];
+  extern __shared__ __align__(16) u32x4_t slots_raw[];   // NL x NT vectors
+  u32x4_t(*slots)[NT] = reinterpret_cast<u32x4_t(*)[NT]>(slots_raw);
+  const int tid = threadIdx.x, K = a.K, list_waves = (K + kWave - 1) / kWave;
+  const uint32_t voff = uint32_t(tid) * 16u;
+  const u32x4_t zero = {0u, 0u, 0u, 0u};
+  auto fill_slot = [&](__amdgpu_buffer_rsrc_t src, int u) {   // lane l of wave w lands at slots[u][64 w + l]
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, &slots[u][(tid >> 6) << 6], 16, voff + uint32_t(u) * (NT * 16u), 0, 0, 2);
+  };
+  auto row_at = [&](int64_t p) -> int64_t { return p < a.T ? int64_t(order[p]) : a.T; };
+  auto weight_of = [&](int64_t t) { return t < a.T ? a.weight[t] : 0.f; };
+  auto entry_of = [&](int64_t t, bool need, int& j, float& lp) {
+    j = -1;
+    lp = 0.f;
+    if (need && tid < K) {
+      j = a.index[t * K + tid];
+      lp = a.logprob[t * K + tid];
+    }
+  };
+
+  // position gridDim.x onwards are handed out by the counter; p: position of the next row
+  int64_t t = row_at(blockIdx.x);
+  if (tid == 0) s_next[1] = atomicAdd(ctr, 1);
+  lists[0].head[tid] = -1;
+  __syncthreads();
+  int64_t p = __builtin_amdgcn_readfirstlane(s_next[1]);
+  float w = weight_of(t);
+  int j;
+  float lp;
+  entry_of(t, w != 0.f, j, lp);
+  if (w != 0.f) {
+    const View row(a.logits, t, a.ld, a.V);
+    const __amdgpu_buffer_rsrc_t src = row.buffer(row.row);
+#pragma unroll
+    for (int u = 0; u < NL; ++u) fill_slot(src, u);
+  }
+  for (int par = 0; t < a.T; par ^= 1) {
+    ListPlaces<NT>& list = lists[par];
+    const bool need = w != 0.f;   // uniform
+    const int64_t tn = row_at(p);
+    int drawn = 0;
+    if (tid == 0) drawn = p < a.T ? atomicAdd(ctr, 1) : int(a.T);
+    const View row(a.logits, t, a.ld, a.V);
+    const int nvec = row.nvec, jr = row.ragged();
+    char* const drow = row_ptr<DT>(a.dlogits, t, a.ld);
+    const float wn = weight_of(tn);
+    const View nrow(a.logits, wn != 0.f ? tn : t, a.ld, a.V);
+    const __amdgpu_buffer_rsrc_t nsrc = nrow.buffer(nrow.row), dst = row.buffer(drow);
+    int jn;
+    float lpn;
+    entry_of(tn, wn != 0.f, jn, lpn);
+    RowGrad r;
+    r.quiet = true;
+    u32x4_t v[NR];
+    float zr = 0.f;
+    uint32_t listed = 0;
+    if (need) {
+      ListEntry entry{j, 0.0, 0.0, 0.f};
+      bool bad = j >= a.V;
+      if (bad) entry.j = -1;
+      if (entry.j >= 0) entry.z = row.at(entry.j);
+      if (jr >= 0) zr = row.at(jr);
+      const __amdgpu_buffer_rsrc_t src = row.buffer(row.row);
+      uint32_t voff_ld = voff;
+      asm volatile("" : "+v"(voff_ld));   // offsets are formed per row: hoisted out of the loop they are twenty registers
+#pragma unroll
+      for (int u = 0; u < NR; ++u) v[u] = __builtin_amdgcn_raw_buffer_load_b128(src, voff_ld + uint32_t(NL + u) * (NT * 16u), 0, 2);
+      if (entry.j >= 0) {
+        list_place(list, row, tid, entry.j);
+      }
+      lists[par ^ 1].head[tid] = -1;
+      if (tid == 0) s_next[par] = drawn;
+      __syncthreads();
+      if (tid < list_waves * kWave) {
+        if (entry.j >= 0) {
+          bad |= list_twice(list, tid);
+          entry.lp = double(lp);
+          entry.p = exp(entry.lp);
+          list.p[tid] = float(entry.p);
+        }
+        list_sum(entry, bad, s_list[par]);
+      }
+      for (int k = list.head[tid]; k >= 0; k = list.next[k]) listed |= 1u << list.turn[k];
+      // Loads return in order and the NR of the registers were issued behind those into this wave's slots: with no more than NR
+      // outstanding the slots have landed (the compiler does not track them; other accesses only make the wait longer).
+      static_assert(NR <= 15, "immediate below holds vmcnt in 4 bits");
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0F70 | NR);
+      asm volatile("" ::: "memory");
+      SoftSum st = soft_identity();
+#pragma unroll
+      for (int u = 0; u < kStreamVecs; ++u) {
+        if (tid < nvec - u * NT) {
+          const u32x4_t x = u < NL ? slots[u < NL ? u : 0][tid] : v[u < NL ? 0 : u - NL];
+          float z[E];
+          View::unpack(x, z);
+          if (listed & (1u << u)) mask_listed(z, list, u);
+          soft_update<E>(st, z);
+        }
+        __builtin_amdgcn_sched_barrier(0);   // one vector at a time: keeps temporaries from piling up
+      }
+      if (jr >= 0) {
+        float z[1] = {listed >> kRagged ? -INFINITY : zr};
+        soft_update<1>(st, z);
+      }
+      st = soft_block_reduce<NT>(st, s_sum[par]);   // its barrier also orders loads before stores over them
+      r = row_terms(a, t, w, st, s_list[par], list_waves);
+    } else {
+      lists[par ^ 1].head[tid] = -1;
+      if (tid == 0) {
+        s_next[par] = drawn;
+        put_loss(a, t, w, 0.f);
+      }
+      __syncthreads();
+    }
+    if (!r.quiet) {
+      uint32_t voff_st = voff;
+      asm volatile("" : "+v"(voff_st));
+#pragma unroll
+      for (int u = 0; u < kStreamVecs; ++u) {
+        const u32x4_t x = u < NL ? slots[u < NL ? u : 0][tid] : v[u < NL ? 0 : u - NL];
+        if (tid < nvec - u * NT) {
+          float z[E], d[E];
+          View::unpack(x, z);
+          grad_elts<NT, E>(z, d, r, list, listed & (1u << u), u);
+          __builtin_amdgcn_raw_buffer_store_b128(pack_vec<DT>(d), dst, voff_st + uint32_t(u) * (NT * 16u), 0, 2);
+        }
+        asm volatile("" ::: "memory");
+        if (u < NL && wn != 0.f) fill_slot(nsrc, u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (jr >= 0)
+        store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+    } else {
+      __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): every read of this row's slots has returned
+      asm volatile("" ::: "memory");
+      if (wn != 0.f) {
+#pragma unroll
+        for (int u = 0; u < NL; ++u) fill_slot(nsrc, u);
+      }
+      for (int i = tid; i < nvec; i += NT) __builtin_amdgcn_raw_buffer_store_b128(zero, dst, uint32_t(i) * 16u, 0, 2);
+      if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
+    }
+    t = tn;
+    w = wn;
+    j = jn;
+    lp = lpn;
+    p = __builtin_amdgcn_readfirstlane(s_next[par]);
   }
 }
 
@@ -271,19 +603,69 @@ __global__ __launch_bounds__(kSumNT) void k_distill_sum(const float* __restrict_
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) acc += double(x[u]);
   }
-  acc = block_sum_d<kSumNT>(acc, lds);
+  acc = wave_sum_d(acc);
+  if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = acc;
+  __syncthreads();
+  if (threadIdx.x >= kWave) return;
+  acc = wave_sum_d(threadIdx.x < kSumNT / kWave ? lds[threadIdx.x] : 0.0);
   if (threadIdx.x == 0) loss[0] = float(acc);
 }
 
+struct DistillWorkspace {
+  float* term;      // [T]
+  int32_t* order;   // [T]
+  int32_t* ctr;     // [4]
+  size_t bytes;
+};
+static DistillWorkspace distill_workspace(void* base, int64_t T) {
+  const size_t each = (size_t(T) * 4 + 255) / 256 * 256;
+  char* const p = reinterpret_cast<char*>(base);
+  return DistillWorkspace{reinterpret_cast<float*>(p), reinterpret_cast<int32_t*>(p + each), reinterpret_cast<int32_t*>(p + 2 * each),
+                          2 * each + 256};
+}
 size_t distill_workspace_bytes(int64_t T, int32_t V) {
   (void)V;
-  return (size_t(T) * 4 + 255) / 256 * 256 + 256;
+  return distill_workspace(nullptr, T).bytes;
 }
 
-template <int DT, bool VEC> static void distill_launch(const DistillArgs& a, hipStream_t s) {
-  const int nvec = a.V / RowView<DT, VEC>::E;
-  if (nvec <= 4 * 256) hipLaunchKernelGGL((k_distill_row<256, DT, VEC>), dim3(unsigned(a.T)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_distill_row<512, DT, VEC>), dim3(unsigned(a.T)), dim3(512), 0, s, a);
+template <int NT, int DT> static void held_launch(const DistillArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_distill_held<NT, DT>), dim3(unsigned(a.T)), dim3(NT), 0, s, a);
+}
+
+template <int DT> static aero_status distill_launch(const DistillArgs& a, bool vec, const DistillWorkspace& ws, hipStream_t s) {
+  const int nvec = vec ? a.V / Storage<DT>::kPerVec : a.V;
+  if (!vec) {
+    hipLaunchKernelGGL((k_distill_row<512, DT, false>), dim3(unsigned(a.T)), dim3(512), 0, s, a);
+  } else if (nvec > kStreamVecs * kStreamNT || (!a.dlogits && nvec > kHeldVecs * 1024)) {
+    hipLaunchKernelGGL((k_distill_row<512, DT, true>), dim3(unsigned(a.T)), dim3(512), 0, s, a);
+  } else if (nvec <= kHeldVecs * 64 && a.K <= 64) {
+    held_launch<64, DT>(a, s);
+  } else if (nvec <= kHeldVecs * 256) {
+    held_launch<256, DT>(a, s);
+  } else if (nvec <= kHeldVecs * 512) {
+    held_launch<512, DT>(a, s);
+  } else if (nvec <= kHeldVecs * 1024) {
+    held_launch<1024, DT>(a, s);
+  } else {
+    // raising the limit of dynamic LDS is per function; done once per process, safely from any thread
+    static std::once_flag once;
+    static hipError_t rc = hipSuccess;
+    std::call_once(once, [] {
+      rc = hipFuncSetAttribute(reinterpret_cast<const void*>(k_distill_stream<DT>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               kStreamLdsBytes);
+    });
+    if (rc != hipSuccess) return AERO_ERR_HIP;
+    const unsigned grid = unsigned(std::min<int64_t>(a.T, compute_units()));
+    if (a.T <= 4 * kOrderNT) {
+      hipLaunchKernelGGL(k_distill_order<true>, dim3(1), dim3(kOrderNT), 0, s, a.T, a.weight, int32_t(grid), ws.ctr, ws.order);
+    } else {
+      hipLaunchKernelGGL(k_distill_start, dim3(1), dim3(1), 0, s, ws.ctr, int32_t(grid));
+      hipLaunchKernelGGL(k_distill_order<false>, dim3(unsigned((a.T + kOrderNT - 1) / kOrderNT)), dim3(kOrderNT), 0, s, a.T, a.weight,
+                         int32_t(grid), ws.ctr, ws.order);
+    }
+    hipLaunchKernelGGL(k_distill_stream<DT>, dim3(grid), dim3(kStreamNT), kStreamLdsBytes, s, a, ws.ctr, ws.order);
+  }
+  return AERO_OK;
 }
 
 }  // namespace aero
@@ -304,16 +686,13 @@ extern "C" aero_status aero_distill_loss_bwd(const void* logits, int32_t dtype, 
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < distill_workspace_bytes(T, V))
     return AERO_ERR_WORKSPACE;
   const hipStream_t s = as_stream(stream);
-  const DistillArgs a{logits, T, V, ld, teacher_index, teacher_logprob, K, token_weight, tail, grad_scale,
-                      reinterpret_cast<float*>(workspace), row_loss, dlogits, err_flag};
+  const DistillWorkspace ws = distill_workspace(workspace, T);
+  const DistillArgs a{logits, T, V, ld, teacher_index, teacher_logprob, K, token_weight, tail, grad_scale, ws.term, row_loss, dlogits, err_flag};
   if (T > 0) {
     const bool vec = rows_alike(logits, dlogits, storage_bytes(dtype));
-    switch (dtype) {
-      case AERO_BF16: vec ? distill_launch<kBF16, true>(a, s) : distill_launch<kBF16, false>(a, s); break;
-      case AERO_F16: vec ? distill_launch<kF16, true>(a, s) : distill_launch<kF16, false>(a, s); break;
-      case AERO_F8E4M3: vec ? distill_launch<kF8, true>(a, s) : distill_launch<kF8, false>(a, s); break;
-      default: vec ? distill_launch<kF32, true>(a, s) : distill_launch<kF32, false>(a, s);
-    }
+    const aero_status st = dtype == AERO_BF16 ? distill_launch<kBF16>(a, vec, ws, s) : dtype == AERO_F16 ? distill_launch<kF16>(a, vec, ws, s)
+                           : dtype == AERO_F8E4M3 ? distill_launch<kF8>(a, vec, ws, s) : distill_launch<kF32>(a, vec, ws, s);
+    if (st != AERO_OK) return st;
   }
   hipLaunchKernelGGL(k_distill_sum, dim3(1), dim3(kSumNT), 0, s, a.term, T, loss);
   return launch_status();

@@ -123,6 +123,11 @@ template <int DT, bool VEC> struct RowView {
     if constexpr (VEC) unpack_vec<DT>(v, z);
     else z[0] = __uint_as_float(v.x);
   }
+  // the vectors as a buffer, whose bounds check returns zeros (and drops stores) behind the last one
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* base) const {
+    static_assert(VEC, "of 16-byte vectors");
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base) + head * Storage<DT>::kBytes, 0, nvec * 16, 0x00020000);
+  }
   __device__ __forceinline__ float at(int j) const { return load_elt<DT>(row, j); }
   // the element outside the vectors that this thread looks after, -1: none
   __device__ __forceinline__ int ragged() const {
