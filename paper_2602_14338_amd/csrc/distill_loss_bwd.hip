@@ -55,7 +55,7 @@ struct ListEntry {
 struct ListSums {
   double mass, p_lp_z;   // sum p, sum p (ln p - z)
   SoftSum own;           // of the listed logits
-  int32_t any, bad;
+  int32_t any, bad;      // entries; ids outside the vocabulary, or the same place twice
 };
 
 // The list's ids find their threads.  entry.j >= V has been told apart before.
@@ -90,6 +90,9 @@ template <int NT, class F> __device__ __forceinline__ void each_listed(const Lis
     if (list.turn[k] == turn && (list.elt[k] == kRagged) == ragged) f(k, int(list.elt[k]));
 }
 
+// Probability of a listed log-prob: where it is near 1, what it lacks of 1 keeps its own precision (p_r is formed from it).
+__device__ __forceinline__ double list_prob(float lp) { return lp > -0.5f ? 1.0 + double(expm1f(lp)) : double(expf(lp)); }
+
 // Sums over the entries of a wave, left in s[wave] by its first lane.
 __device__ __forceinline__ void list_sum(const ListEntry& e, bool bad, ListSums* s) {
   ListSums sum;
@@ -121,11 +124,11 @@ struct RowGrad {
   float at_other, o_rest, at_listed, o_all, scale_p;
   bool quiet;   // no loss, no gradient
 };
-// What the sum over the other places and the list come to; the first thread writes the loss (a quiet row's too).  By all threads.
-__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftSum rest, const ListSums* s, int waves) {
+// What the sum over the other places and the list come to; one thread writes the loss (a quiet row's too).  By all threads.
+__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftSum rest, const ListSums* s, int waves, bool bad = false) {
   double mass = 0.0, p_lp_z = 0.0;
   SoftSum all = rest;
-  bool any = false, bad = false;
+  bool any = false;
   for (int k = 0; k < waves; ++k) {   // uniform
     mass += s[k].mass;
     p_lp_z += s[k].p_lp_z;
@@ -145,7 +148,7 @@ __device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, fl
   r.o_all = uniform(all.o);
   r.at_other = uniform(has_rest ? float(g * (total * double(rest_q) - rest_p)) / rest.s : 0.f);
   r.o_rest = uniform(rest.o);
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == blockDim.x - 1) {   // the first wave has the list to look after
     if (bad && a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_TEACHER);
     double loss = 0.0;
     if (!r.quiet) {   // logarithms of 32-bit numbers: 2^-24 of the logarithm
@@ -229,10 +232,11 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     bad = entry.j >= a.V;
     if (bad) entry.j = -1;
     if (entry.j >= 0) {
-      entry.lp = double(a.logprob[t * K + tid]);
+      const float lp = a.logprob[t * K + tid];
+      entry.lp = double(lp);
       entry.z = row.at(entry.j);
       list_place(list, row, tid, entry.j);
-      entry.p = exp(entry.lp);
+      entry.p = list_prob(lp);
       list.p[tid] = float(entry.p);
     }
   }
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
   if (entry.j >= 0) {
     entry.lp = double(lp);
     list_place(list, row, tid, entry.j);
-    entry.p = exp(entry.lp);
+    entry.p = list_prob(lp);
     list.p[tid] = float(entry.p);
   }
   __syncthreads();
@@ -389,26 +393,20 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
   if (jr >= 0) store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
 }
 
-// Rows by a counter, those with a weight first: a persistent workgroup per CU draws its next row while it works on one.
-// ctr[0]: next position to hand out, ctr[1], ctr[2]: rows placed from the front and from the back.
+// The rows with a weight in front, then the others, each in no particular order.  ctr[0], ctr[1]: rows placed from the front and from
+// the back.  ONE: a single workgroup, which counts in LDS and needs no launch in front of it.
 constexpr int kOrderNT = 1024;
-__global__ void k_distill_start(int32_t* ctr, int32_t grid) {
-  ctr[0] = grid;
-  ctr[1] = 0;
-  ctr[2] = 0;
-}
-// ONE: a single workgroup, which counts in LDS and needs no launch in front of it.
+__global__ void k_distill_start(int32_t* ctr) { ctr[threadIdx.x] = 0; }
 template <bool ONE>
-__global__ __launch_bounds__(kOrderNT) void k_distill_order(int64_t T, const float* __restrict__ weight, int32_t grid,
-                                                            int32_t* __restrict__ ctr, int32_t* __restrict__ order) {
+__global__ __launch_bounds__(kOrderNT) void k_distill_order(int64_t T, const float* __restrict__ weight, int32_t* __restrict__ ctr,
+                                                            int32_t* __restrict__ order) {
   __shared__ int32_t own[2];
   const int lane = threadIdx.x % kWave;
   if constexpr (ONE) {
     if (threadIdx.x < 2) own[threadIdx.x] = 0;
     __syncthreads();
-    if (threadIdx.x == 0) ctr[0] = grid;
   }
-  int32_t* const count = ONE ? own : ctr + 1;
+  int32_t* const count = ONE ? own : ctr;
   for (int64_t t0 = int64_t(blockIdx.x) * kOrderNT; t0 < T; t0 += int64_t(gridDim.x) * kOrderNT) {   // uniform
     const int64_t t = t0 + threadIdx.x;
     const bool in = t < T, need = in && weight[t] != 0.f;
@@ -428,99 +426,100 @@ __global__ __launch_bounds__(kOrderNT) void k_distill_order(int64_t T, const flo
 
 // Long rows that a CU holds: kStreamVecs vectors per thread of 1024, the first kStreamLds of them in LDS, in slots of the wave's own that
 // are filled by direct loads: as soon as a slot has been turned into gradient it is asked to be filled with the next row's vector, so
-// that a CU reads while it writes.  Two barriers a row: behind the placing of the list, and in the reduction; everything that
-// passes between waves is held twice, by the row's parity.
+// that a CU reads while it writes.  Nothing in the row's course may wait for the stores under way, which a wait for any load behind them
+// does: the next row's list, its places and sums are looked after while this row's registers fill, between the sums over the
+// slots and over the registers, and no loaded register is carried from one row to the next.  (With the list at the top of its own
+// row: 885 us for 8192 x 151936 bf16.)
 constexpr int kStreamNT = 1024, kStreamVecs = 20, kStreamLds = 9;
 constexpr int kStreamLdsBytes = kStreamLds * kStreamNT * 16;
 template <int DT>
-__global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, int32_t* ctr, const int32_t* __restrict__ order) {
+__global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, const float* __restrict__ weight,
+                                                               const int32_t* __restrict__ order) {
   using View = RowView<DT, true>;
   constexpr int E = View::E, NT = kStreamNT, NL = kStreamLds, NR = kStreamVecs - kStreamLds;
-  __shared__ ListPlaces<NT> lists[2];
+  __shared__ ListPlaces<NT> lists[2];          // by the row's parity, like everything below
   __shared__ SoftSum s_sum[2][NT / kWave];
   __shared__ ListSums s_list[2][kListWaves];
-  __shared__ int s_next[2];
+  __shared__ int s_twice[2][kListWaves];
   extern __shared__ __align__(16) u32x4_t slots_raw[];   // NL x NT vectors
   u32x4_t(*slots)[NT] = reinterpret_cast<u32x4_t(*)[NT]>(slots_raw);
-  const int tid = threadIdx.x, K = a.K, list_waves = (K + kWave - 1) / kWave;
+  const int tid = threadIdx.x, wave = tid / kWave, K = a.K, list_waves = (K + kWave - 1) / kWave;
+  const bool lister = wave < list_waves;   // uniform in a wave
   const uint32_t voff = uint32_t(tid) * 16u;
   const u32x4_t zero = {0u, 0u, 0u, 0u};
   auto fill_slot = [&](__amdgpu_buffer_rsrc_t src, int u) {   // lane l of wave w lands at slots[u][64 w + l]
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src, &slots[u][(tid >> 6) << 6], 16, voff + uint32_t(u) * (NT * 16u), 0, 0, 2);
   };
   auto row_at = [&](int64_t p) -> int64_t { return p < a.T ? int64_t(order[p]) : a.T; };
-  auto weight_of = [&](int64_t t) { return t < a.T ? a.weight[t] : 0.f; };
-  auto entry_of = [&](int64_t t, bool need, int& j, float& lp) {
-    j = -1;
-    lp = 0.f;
-    if (need && tid < K) {
-      j = a.index[t * K + tid];
-      lp = a.logprob[t * K + tid];
+  auto weight_of = [&](int64_t t) { return t < a.T ? weight[t] : 0.f; };
+  // a lister's entry of a row: place, probability; its logit is on its way
+  auto take = [&](ListPlaces<NT>& list, const View& row, int j, float lp, ListEntry& entry, bool& bad, uint32_t& raw) {
+    if (tid >= K) j = -1;
+    bad = j >= a.V;
+    if (bad) j = -1;
+    entry = ListEntry{j, 0.0, double(lp), 0.f};
+    raw = load_raw<DT>(row.row, max(j, 0));
+    if (j >= 0) {
+      list_place(list, row, tid, j);
+      entry.p = list_prob(lp);
+      list.p[tid] = float(entry.p);
     }
   };
 
-  // position gridDim.x onwards are handed out by the counter; p: position of the next row
-  int64_t t = row_at(blockIdx.x);
-  if (tid == 0) s_next[1] = atomicAdd(ctr, 1);
+  // rows with a weight, which are alike in their cost, come first, then those that are only zeroed: every gridDim.x-th is this
+  // workgroup's; p: position of the next row
+  int64_t p = blockIdx.x;
+  int64_t t = row_at(p);
+  p += gridDim.x;
   lists[0].head[tid] = -1;
+  lists[1].head[tid] = -1;
   __syncthreads();
-  int64_t p = __builtin_amdgcn_readfirstlane(s_next[1]);
   float w = weight_of(t);
-  int j;
-  float lp;
-  entry_of(t, w != 0.f, j, lp);
+  bool have = false;   // this thread has an entry of the row's list
   if (w != 0.f) {
     const View row(a.logits, t, a.ld, a.V);
+    if (lister) {
+      ListEntry entry;
+      bool bad;
+      uint32_t raw;
+      const int k = min(tid, K - 1);
+      take(lists[0], row, a.index[t * K + k], a.logprob[t * K + k], entry, bad, raw);
+      entry.z = widen<DT>(raw);
+      list_sum(entry, bad, s_list[0]);
+      have = entry.j >= 0;
+    }
     const __amdgpu_buffer_rsrc_t src = row.buffer(row.row);
 #pragma unroll
     for (int u = 0; u < NL; ++u) fill_slot(src, u);
   }
+  __syncthreads();
   for (int par = 0; t < a.T; par ^= 1) {
     ListPlaces<NT>& list = lists[par];
-    const bool need = w != 0.f;   // uniform
     const int64_t tn = row_at(p);
-    int drawn = 0;
-    if (tid == 0) drawn = p < a.T ? atomicAdd(ctr, 1) : int(a.T);
     const View row(a.logits, t, a.ld, a.V);
     const int nvec = row.nvec, jr = row.ragged();
     char* const drow = row_ptr<DT>(a.dlogits, t, a.ld);
     const float wn = weight_of(tn);
     const View nrow(a.logits, wn != 0.f ? tn : t, a.ld, a.V);
     const __amdgpu_buffer_rsrc_t nsrc = nrow.buffer(nrow.row), dst = row.buffer(drow);
-    int jn;
-    float lpn;
-    entry_of(tn, wn != 0.f, jn, lpn);
-    RowGrad r;
-    r.quiet = true;
-    u32x4_t v[NR];
-    float zr = 0.f;
-    uint32_t listed = 0;
-    if (need) {
-      ListEntry entry{j, 0.0, 0.0, 0.f};
-      bool bad = j >= a.V;
-      if (bad) entry.j = -1;
-      if (entry.j >= 0) entry.z = row.at(entry.j);
-      if (jr >= 0) zr = row.at(jr);
+    bool zeros = true;
+    if (w != 0.f) {   // uniform
+      const int64_t at = (wn != 0.f ? tn : t) * K + min(tid, K - 1);
+      const int jn = a.index[at];
+      const float lpn = a.logprob[at];
+      const uint32_t zraw = load_raw<DT>(row.row, max(jr, 0));
       const __amdgpu_buffer_rsrc_t src = row.buffer(row.row);
       uint32_t voff_ld = voff;
       asm volatile("" : "+v"(voff_ld));   // offsets are formed per row: hoisted out of the loop they are twenty registers
+      u32x4_t v[NR];
 #pragma unroll
       for (int u = 0; u < NR; ++u) v[u] = __builtin_amdgcn_raw_buffer_load_b128(src, voff_ld + uint32_t(NL + u) * (NT * 16u), 0, 2);
-      if (entry.j >= 0) {
-        list_place(list, row, tid, entry.j);
+      if (lister) {
+        const bool twice = have && list_twice(list, tid);
+        const uint64_t any = __builtin_amdgcn_ballot_w64(twice);
+        if (tid % kWave == 0) s_twice[par][wave] = any != 0;
       }
-      lists[par ^ 1].head[tid] = -1;
-      if (tid == 0) s_next[par] = drawn;
-      __syncthreads();
-      if (tid < list_waves * kWave) {
-        if (entry.j >= 0) {
-          bad |= list_twice(list, tid);
-          entry.lp = double(lp);
-          entry.p = exp(entry.lp);
-          list.p[tid] = float(entry.p);
-        }
-        list_sum(entry, bad, s_list[par]);
-      }
+      uint32_t listed = 0;   // bit u: vector u has listed places
       for (int k = list.head[tid]; k >= 0; k = list.next[k]) listed |= 1u << list.turn[k];
       // Loads return in order and the NR of the registers were issued behind those into this wave's slots: with no more than NR
       // outstanding the slots have landed (the compiler does not track them; other accesses only make the wait longer).
@@ -529,50 +528,71 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, int
       __builtin_amdgcn_s_waitcnt(0x0F70 | NR);
       asm volatile("" ::: "memory");
       SoftSum st = soft_identity();
+      auto fold = [&](const u32x4_t& x, int u) {
+        float z[E];
+        View::unpack(x, z);
+        if (listed & (1u << u)) mask_listed(z, list, u);
+        soft_update<E>(st, z);
+      };
 #pragma unroll
-      for (int u = 0; u < kStreamVecs; ++u) {
-        if (tid < nvec - u * NT) {
-          const u32x4_t x = u < NL ? slots[u < NL ? u : 0][tid] : v[u < NL ? 0 : u - NL];
-          float z[E];
-          View::unpack(x, z);
-          if (listed & (1u << u)) mask_listed(z, list, u);
-          soft_update<E>(st, z);
-        }
+      for (int u = 0; u < NL; ++u) {
+        if (tid < nvec - u * NT) fold(slots[u][tid], u);
         __builtin_amdgcn_sched_barrier(0);   // one vector at a time: keeps temporaries from piling up
       }
+      ListEntry entry{-1, 0.0, 0.0, 0.f};
+      bool bad = false;
+      uint32_t raw = 0;
+      if (lister && wn != 0.f) take(lists[par ^ 1], nrow, jn, lpn, entry, bad, raw);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < NR; ++u) {
+        if (tid < nvec - (NL + u) * NT) fold(v[u], NL + u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const float zr = widen<DT>(zraw);
       if (jr >= 0) {
         float z[1] = {listed >> kRagged ? -INFINITY : zr};
         soft_update<1>(st, z);
       }
-      st = soft_block_reduce<NT>(st, s_sum[par]);   // its barrier also orders loads before stores over them
-      r = row_terms(a, t, w, st, s_list[par], list_waves);
-    } else {
-      lists[par ^ 1].head[tid] = -1;
-      if (tid == 0) {
-        s_next[par] = drawn;
-        put_loss(a, t, w, 0.f);
+      if (lister && wn != 0.f) {
+        entry.z = widen<DT>(raw);
+        list_sum(entry, bad, s_list[par ^ 1]);
       }
-      __syncthreads();
-    }
-    if (!r.quiet) {
-      uint32_t voff_st = voff;
-      asm volatile("" : "+v"(voff_st));
-#pragma unroll
-      for (int u = 0; u < kStreamVecs; ++u) {
-        const u32x4_t x = u < NL ? slots[u < NL ? u : 0][tid] : v[u < NL ? 0 : u - NL];
-        if (tid < nvec - u * NT) {
+      have = entry.j >= 0;
+      st = soft_block_reduce<NT>(st, s_sum[par]);   // its barrier also orders loads before stores over them
+      bool twice = false;
+      for (int k = 0; k < list_waves; ++k) twice |= s_twice[par][k] != 0;
+      const RowGrad r = row_terms(a, t, w, st, s_list[par], list_waves, twice);
+      if (!r.quiet) {
+        zeros = false;
+        uint32_t voff_st = voff;
+        asm volatile("" : "+v"(voff_st));
+        auto turned = [&](const u32x4_t& x, int u) {
           float z[E], d[E];
           View::unpack(x, z);
           grad_elts<NT, E>(z, d, r, list, listed & (1u << u), u);
           __builtin_amdgcn_raw_buffer_store_b128(pack_vec<DT>(d), dst, voff_st + uint32_t(u) * (NT * 16u), 0, 2);
+        };
+#pragma unroll
+        for (int u = 0; u < NL; ++u) {   // LDS part first: each slot is filled again right after its last use
+          const u32x4_t x = slots[u][tid];
+          if (tid < nvec - u * NT) turned(x, u);
+          asm volatile("" ::: "memory");
+          if (wn != 0.f) fill_slot(nsrc, u);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        asm volatile("" ::: "memory");
-        if (u < NL && wn != 0.f) fill_slot(nsrc, u);
-        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < NR; ++u) {
+          if (tid < nvec - (NL + u) * NT) turned(v[u], NL + u);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (jr >= 0)
+          store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
       }
-      if (jr >= 0)
-        store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
-    } else {
+    } else if (tid == 0) {
+      put_loss(a, t, w, 0.f);
+    }
+    if (zeros) {
       __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): every read of this row's slots has returned
       asm volatile("" ::: "memory");
       if (wn != 0.f) {
@@ -582,11 +602,14 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, int
       for (int i = tid; i < nvec; i += NT) __builtin_amdgcn_raw_buffer_store_b128(zero, dst, uint32_t(i) * 16u, 0, 2);
       if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
     }
+    list.head[tid] = -1;   // for the row after the next
+    // what is placed and written before the next row's reduction may still be read here; stores need not have landed
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     t = tn;
     w = wn;
-    j = jn;
-    lp = lpn;
-    p = __builtin_amdgcn_readfirstlane(s_next[par]);
+    p += gridDim.x;
   }
 }
 
@@ -656,14 +679,14 @@ template <int DT> static aero_status distill_launch(const DistillArgs& a, bool v
     });
     if (rc != hipSuccess) return AERO_ERR_HIP;
     const unsigned grid = unsigned(std::min<int64_t>(a.T, compute_units()));
-    if (a.T <= 4 * kOrderNT) {
-      hipLaunchKernelGGL(k_distill_order<true>, dim3(1), dim3(kOrderNT), 0, s, a.T, a.weight, int32_t(grid), ws.ctr, ws.order);
+    if (a.T <= 8 * kOrderNT) {
+      hipLaunchKernelGGL(k_distill_order<true>, dim3(1), dim3(kOrderNT), 0, s, a.T, a.weight, ws.ctr, ws.order);
     } else {
-      hipLaunchKernelGGL(k_distill_start, dim3(1), dim3(1), 0, s, ws.ctr, int32_t(grid));
-      hipLaunchKernelGGL(k_distill_order<false>, dim3(unsigned((a.T + kOrderNT - 1) / kOrderNT)), dim3(kOrderNT), 0, s, a.T, a.weight,
-                         int32_t(grid), ws.ctr, ws.order);
+      hipLaunchKernelGGL(k_distill_start, dim3(1), dim3(2), 0, s, ws.ctr);
+      hipLaunchKernelGGL(k_distill_order<false>, dim3(unsigned((a.T + kOrderNT - 1) / kOrderNT)), dim3(kOrderNT), 0, s, a.T, a.weight, ws.ctr,
+                         ws.order);
     }
-    hipLaunchKernelGGL(k_distill_stream<DT>, dim3(grid), dim3(kStreamNT), kStreamLdsBytes, s, a, ws.ctr, ws.order);
+    hipLaunchKernelGGL(k_distill_stream<DT>, dim3(grid), dim3(kStreamNT), kStreamLdsBytes, s, a, a.weight, ws.order);
   }
   return AERO_OK;
 }

@@ -93,6 +93,19 @@ __device__ __forceinline__ double soft_lse(SoftSum st) {
   return st.o < INFINITY && st.s == st.s ? lse : __builtin_nan("");
 }
 
+// An element as it is stored, to be widened where it is needed: a conversion next to the load waits for it there.
+template <int DT> __device__ __forceinline__ uint32_t load_raw(const char* row, int j) {
+  if constexpr (Storage<DT>::kBytes == 2) return reinterpret_cast<const uint16_t*>(row)[j];
+  else if constexpr (Storage<DT>::kBytes == 1) return reinterpret_cast<const uint8_t*>(row)[j];
+  else return reinterpret_cast<const uint32_t*>(row)[j];
+}
+template <int DT> __device__ __forceinline__ float widen(uint32_t raw) {
+  if constexpr (DT == kBF16) return bf16_to_f32(uint16_t(raw));
+  else if constexpr (DT == kF16) return f16_to_f32(uint16_t(raw));
+  else if constexpr (DT == kF8) return f8_to_f32(uint8_t(raw));
+  else return __uint_as_float(raw);
+}
+
 // One row as E-element vectors (VEC: 16 bytes between the ragged ends; otherwise single elements), of which this workgroup looks
 // after [first, last); the ragged ends belong to the part that starts at 0.
 template <int DT, bool VEC> struct RowView {

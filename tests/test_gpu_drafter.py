@@ -683,3 +683,49 @@ def test_refusals(gh):
     refused("dtype", bwd, z, 4, 16, 16, i(4), 9, 1.0, f(9, 16).half(), ws)
     refused("NULL", bwd, z, 4, 16, 16, None, 9, 1.0, f(9, 16), ws)
     refused("workspace", bwd, z, 4, 16, 16, i(4), 9, 1.0, f(9, 16), ws[:100])
+
+
+@pytest.mark.parametrize("dtype,V,ld,K,tail", [("bf16", 66001, 66001, 40, 1), ("f32", 33003, 33004, 70, 0), ("f8", 140001, 140003, 20, 1)])
+def test_distill_of_more_long_rows_than_compute_units(gh, dtype, V, ld, K, tail):
+    """Several rows per workgroup of the streaming kernel, each at another offset from 16 bytes, with rows of weight 0, bad lists and
+    empty rows among them; checked on some of them."""
+    import paper_2602_14338_amd as aero
+    T = 600
+    rng = np.random.default_rng(V)
+    base = normal([V, 3], 40, V)
+    pick = rng.integers(0, 40, size=T)
+    shift = rng.integers(1, V, size=T)
+    z = np.stack([np.roll(base[p], s) for p, s in zip(pick, shift)])
+    if dtype != "f8":   # which has no infinities
+        z[7] = -np.inf
+    dev, host = stored(z, dtype, ld, 3)
+    index = np.zeros((T, K), np.int32)
+    lp = np.zeros((T, K), np.float32)
+    lists = [make_lists(k, host[np.flatnonzero(pick == k)[:1]], K) if (pick == k).any() else None for k in range(40)]
+    for t in range(T):
+        first = np.flatnonzero(pick == pick[t])[0]
+        index[t] = (lists[pick[t]][0][0] - shift[first] + shift[t]) % V
+        lp[t] = lists[pick[t]][1][0]
+    index[7] = np.arange(K)
+    index[11, 3] = index[11, 5]
+    index[300, 0] = V
+    index[400, : K // 2] = -1
+    w = rng.uniform(0.2, 1.0, size=T).astype(np.float32)
+    w[rng.random(T) < 0.2] = 0.0
+    w[[7, 11, 300, 400]] = 0.5
+    some = np.unique(np.concatenate([[0, 7, 11, 299, 300, 301, 400, 599], rng.integers(0, T, size=24)]))
+    ref = orc.distill(host[some], V, index[some], lp[some], w[some], tail, SCALE[dtype])
+    dz = sevens(T, ld, dtype, 3)
+    loss, rows, err = run_distill(dev, T, V, ld, index, lp, w, tail, SCALE[dtype], dz)
+    assert err == 8 and abs(loss - (rows * w).sum()) <= 2.0 ** -20 * (np.abs(rows * w)).sum()
+    got = wide(dz.view(T, ld)[torch.from_numpy(some).to("cuda")] if dtype != "f8" else
+               dz.view(torch.uint8).view(T, ld)[torch.from_numpy(some).to("cuda")].view(torch.float8_e4m3fn))
+    assert (got[:, V:] == 7.0).all()
+    row_bound, grad_bound = distill_bounds(ref, host[some], w[some], dtype, SCALE[dtype])
+    assert (np.abs(rows[some] - ref["row_loss"]) <= row_bound).all()
+    assert (np.abs(got[:, :V] - ref["dlogits"]) <= grad_bound).all()
+    assert not rows[w == 0].any()
+    again = sevens(T, ld, dtype, 3)
+    run_distill(dev, T, V, ld, index, lp, w, tail, SCALE[dtype], again)
+    raw = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[again.element_size()]
+    assert torch.equal(dz.view(raw), again.view(raw))
