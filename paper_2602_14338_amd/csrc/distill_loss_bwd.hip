@@ -9,7 +9,7 @@
 // q_r is what a converging drafter makes small, and 1 - sum q(i_k) would leave nothing of it: the sum over the row leaves the
 // listed places out (they count as masked while it runs) and their K exponentials are added to it.  Each thread knows from a
 // chain of the entries that fall into its vectors which of them hold listed places, so that all other vectors pay one
-// comparison.
+// comparison; in the gradient row the listed places are stored over what the others' multiple left there.
 #include <algorithm>
 #include <mutex>
 
@@ -19,7 +19,6 @@ namespace aero {
 
 constexpr int kListMax = AERO_TOPK_MAX;
 constexpr int kListWaves = kListMax / kWave;
-constexpr int kRagged = 31;   // in the place of a vector's number within its thread: the element outside the vectors
 
 struct DistillArgs {
   const void* logits;
@@ -37,13 +36,14 @@ struct DistillArgs {
   int32_t* err_flag;
 };
 
-// The entries of a row's list by the thread that looks after their place (thread = vector % NT).
+// The entries of a row's list by the thread that looks after their place (thread = vector % NT).  A place within a thread is the number
+// of its vector there times E plus the element; kRagged: the thread's element outside the vectors.
+constexpr int kRagged = 0xffff;
 template <int NT> struct ListPlaces {
   int32_t head[NT];         // first entry of a thread's chain, -1: none
   int16_t next[kListMax];
-  uint16_t turn[kListMax];  // vector / NT; kRagged with elt kRagged: the thread's ragged element
-  uint8_t elt[kListMax];
-  float p[kListMax];        // teacher probability
+  uint16_t place[kListMax];
+  float p[kListMax], z[kListMax];   // teacher probability, logit
 };
 
 // One entry as its thread holds it, and what a wave of them adds up to.
@@ -63,32 +63,57 @@ template <int NT, int DT, bool VEC>
 __device__ __forceinline__ void list_place(ListPlaces<NT>& list, const RowView<DT, VEC>& row, int k, int j) {
   constexpr int E = RowView<DT, VEC>::E;
   const int at = j - row.head;
-  int owner, turn, elt;
+  int owner, place;
   if (at >= 0 && at < row.nvec * E) {
-    const int vec = at / E;
-    owner = vec % NT;
-    turn = vec / NT;
-    elt = at % E;
+    owner = at / E % NT;
+    place = at / E / NT * E + at % E;
   } else {
     owner = at < 0 ? j : E + at - row.nvec * E;
-    turn = kRagged;
-    elt = kRagged;
+    place = kRagged;
   }
-  list.turn[k] = uint16_t(turn);
-  list.elt[k] = uint8_t(elt);
+  list.place[k] = uint16_t(place);
   list.next[k] = int16_t(atomicExch(&list.head[owner], k));
 }
 // After the barrier behind list_place: is the entry's place taken by another entry further down the chain?
 template <int NT> __device__ __forceinline__ bool list_twice(const ListPlaces<NT>& list, int k) {
   bool twice = false;
-  for (int e = list.next[k]; e >= 0; e = list.next[e]) twice |= list.turn[e] == list.turn[k] && list.elt[e] == list.elt[k];
+  for (int e = list.next[k]; e >= 0; e = list.next[e]) twice |= list.place[e] == list.place[k];
   return twice;
 }
-// Calls f(entry, element) for this thread's listed places of one turn.
-template <int NT, class F> __device__ __forceinline__ void each_listed(const ListPlaces<NT>& list, int turn, bool ragged, F f) {
-  for (int k = list.head[threadIdx.x]; k >= 0; k = list.next[k])
-    if (list.turn[k] == turn && (list.elt[k] == kRagged) == ragged) f(k, int(list.elt[k]));
+// Calls f(entry, place) for this thread's entries.
+template <int NT, class F> __device__ __forceinline__ void each_listed(const ListPlaces<NT>& list, F f) {
+  for (int k = list.head[threadIdx.x]; k >= 0; k = list.next[k]) f(k, int(list.place[k]));
 }
+// This thread's listed places as bits, for N vectors of E elements, and whether its ragged element is one.
+template <int N, int E> struct PlaceBits {
+  static constexpr int kWords = (N * E + 31) / 32;
+  uint32_t bits[kWords];
+  bool ragged;
+  template <int NT> __device__ __forceinline__ explicit PlaceBits(const ListPlaces<NT>& list) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) bits[i] = 0;
+    ragged = false;
+    each_listed(list, [&](int, int place) {
+      ragged |= place == kRagged;
+      const uint32_t bit = 1u << (place % 32);
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) bits[i] |= place / 32 == i ? bit : 0;
+    });
+  }
+  // the listed logits of vector u count as masked
+  __device__ __forceinline__ void mask(float (&z)[E], int u) const {
+    static_assert(32 % E == 0, "a vector's bits are in one word");
+    const uint32_t word = bits[u * E / 32];
+    const int shift = u * E % 32;
+    if (word >> shift & ((1u << E) - 1)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t m = uint32_t(__builtin_amdgcn_sbfe(int(word), shift + e, 1));   // all ones or zeros
+        z[e] = __uint_as_float((m & 0xff800000u) | (~m & __float_as_uint(z[e])));      // -inf or the logit
+      }
+    }
+  }
+};
 
 // Probability of a listed log-prob: where it is near 1, what it lacks of 1 keeps its own precision (p_r is formed from it).
 __device__ __forceinline__ double list_prob(float lp) { return lp > -0.5f ? 1.0 + double(expm1f(lp)) : double(expf(lp)); }
@@ -165,27 +190,18 @@ __device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, fl
   return r;
 }
 
-// One vector of the gradient row.  listed: some of its places are.
-template <int NT, int E>
-__device__ __forceinline__ void grad_elts(const float (&z)[E], float (&d)[E], const RowGrad& r, const ListPlaces<NT>& list, bool listed, int turn) {
+// A vector of the gradient row as if none of its places were listed, and the listed ones over it: the thread that stored a vector
+// stores them behind it, so that they land in that order.
+template <int E> __device__ __forceinline__ void grad_elts(const float (&z)[E], float (&d)[E], const RowGrad& r) {
 #pragma unroll
   for (int e = 0; e < E; ++e) d[e] = r.at_other * exp2_fast(fmaf(z[e], kLog2e, -r.o_rest));
-  if (listed)
-    each_listed(list, turn, false, [&](int k, int own) {
-      const float less = r.scale_p * list.p[k];
-#pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = e == own ? r.at_listed * exp2_fast(fmaf(z[e], kLog2e, -r.o_all)) - less : d[e];
-    });
 }
-template <int NT> __device__ __forceinline__ float grad_ragged(float z, const RowGrad& r, const ListPlaces<NT>& list) {
-  float d = r.at_other * exp2_fast(fmaf(z, kLog2e, -r.o_rest));
-  each_listed(list, kRagged, true, [&](int k, int) { d = r.at_listed * exp2_fast(fmaf(z, kLog2e, -r.o_all)) - r.scale_p * list.p[k]; });
-  return d;
-}
-template <int NT, int E> __device__ __forceinline__ void mask_listed(float (&z)[E], const ListPlaces<NT>& list, int turn) {
-  each_listed(list, turn, false, [&](int, int own) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) z[e] = e == own ? -INFINITY : z[e];
+template <int NT, int DT, bool VEC>
+__device__ __forceinline__ void put_listed(const ListPlaces<NT>& list, const RowView<DT, VEC>& row, const RowGrad& r, char* drow, int jr) {
+  constexpr int E = RowView<DT, VEC>::E;
+  each_listed(list, [&](int k, int place) {
+    const int j = place == kRagged ? jr : row.head + (place / E * NT + int(threadIdx.x)) * E + place % E;
+    store_elt<DT>(drow, j, r.at_listed * exp2_fast(fmaf(list.z[k], kLog2e, -r.o_all)) - r.scale_p * list.p[k]);
   });
 }
 
@@ -238,6 +254,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
       list_place(list, row, tid, entry.j);
       entry.p = list_prob(lp);
       list.p[tid] = float(entry.p);
+      list.z[tid] = entry.z;
     }
   }
   __syncthreads();
@@ -251,7 +268,11 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   auto fold = [&](const u32x4_t& v, int turn) {
     float z[E];
     View::unpack(v, z);
-    if (chained) mask_listed(z, list, turn);
+    if (chained)
+      each_listed(list, [&](int, int place) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = place == turn * E + e ? -INFINITY : z[e];
+      });
     soft_update<E>(st, z);
   };
   int i = tid, turn = 0;
@@ -266,7 +287,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   const float zr = jr >= 0 ? row.at(jr) : 0.f;
   if (jr >= 0) {
     float z[1] = {zr};
-    each_listed(list, kRagged, true, [&](int, int) { z[0] = -INFINITY; });
+    each_listed(list, [&](int, int place) { z[0] = place == kRagged ? -INFINITY : z[0]; });
     soft_update<1>(st, z);
   }
   st = soft_block_reduce<NT>(st, s_sum);   // its barrier: s_list
@@ -277,21 +298,22 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     return;
   }
 
-  auto turned = [&](const u32x4_t& v, int vec, int turn) {
+  auto turned = [&](const u32x4_t& v, int vec) {
     float z[E], d[E];
     View::unpack(v, z);
-    grad_elts<NT, E>(z, d, r, list, chained, turn);
+    grad_elts<E>(z, d, r);
     put(vec, d);
   };
-  for (i = tid, turn = 0; i + (kAhead - 1) * NT < nvec; i += kAhead * NT, turn += kAhead) {
+  for (i = tid; i + (kAhead - 1) * NT < nvec; i += kAhead * NT) {
     u32x4_t v[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) v[u] = row.load(i + u * NT);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) turned(v[u], i + u * NT, turn + u);
+    for (int u = 0; u < kAhead; ++u) turned(v[u], i + u * NT);
   }
-  for (; i < nvec; i += NT) turned(row.load(i), i, turn++);
-  if (jr >= 0) store_elt<DT>(drow, jr, grad_ragged(zr, r, list));
+  for (; i < nvec; i += NT) turned(row.load(i), i);
+  if (jr >= 0) store_elt<DT>(drow, jr, r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+  put_listed(list, row, r, drow, jr);
 }
 
 // One workgroup per row, which its threads hold: kHeldVecs vectors each in registers.
@@ -343,6 +365,7 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
     list_place(list, row, tid, entry.j);
     entry.p = list_prob(lp);
     list.p[tid] = float(entry.p);
+    list.z[tid] = entry.z;
   }
   __syncthreads();
   const int list_waves = (K + kWave - 1) / kWave;
@@ -350,22 +373,20 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
     if (entry.j >= 0) bad |= list_twice(list, tid);
     list_sum(entry, bad, s_list);
   }
-  uint32_t listed = 0;   // bit u: vector u has listed places
-  for (int k = list.head[tid]; k >= 0; k = list.next[k]) listed |= 1u << list.turn[k];
-
+  const PlaceBits<kHeldVecs, E> listed(list);
   SoftSum st = soft_identity();
 #pragma unroll
   for (int u = 0; u < kHeldVecs; ++u) {
     if (tid < nvec - u * NT) {
       float z[E];
       View::unpack(v[u], z);
-      if (listed & (1u << u)) mask_listed(z, list, u);
+      listed.mask(z, u);
       soft_update<E>(st, z);
     }
     __builtin_amdgcn_sched_barrier(0);   // one vector at a time: keeps temporaries from piling up
   }
   if (jr >= 0) {
-    float z[1] = {listed >> kRagged ? -INFINITY : zr};
+    float z[1] = {listed.ragged ? -INFINITY : zr};
     soft_update<1>(st, z);
   }
   // orders the loads of the row before the stores over it, for a gradient in place: by its barrier, and with one wave because
@@ -385,12 +406,13 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
     if (tid < nvec - u * NT) {
       float z[E], d[E];
       View::unpack(v[u], z);
-      grad_elts<NT, E>(z, d, r, list, listed & (1u << u), u);
+      grad_elts<E>(z, d, r);
       __builtin_amdgcn_raw_buffer_store_b128(pack_vec<DT>(d), dst, voff_st + uint32_t(u) * (NT * 16u), 0, 2);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (jr >= 0) store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+  if (jr >= 0) store_elt<DT>(drow, jr, r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+  put_listed(list, row, r, drow, jr);
 }
 
 // The rows with a weight in front, then the others, each in no particular order.  ctr[0], ctr[1]: rows placed from the front and from
@@ -485,6 +507,7 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
       const int k = min(tid, K - 1);
       take(lists[0], row, a.index[t * K + k], a.logprob[t * K + k], entry, bad, raw);
       entry.z = widen<DT>(raw);
+      if (entry.j >= 0) lists[0].z[tid] = entry.z;
       list_sum(entry, bad, s_list[0]);
       have = entry.j >= 0;
     }
@@ -519,8 +542,7 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
         const uint64_t any = __builtin_amdgcn_ballot_w64(twice);
         if (tid % kWave == 0) s_twice[par][wave] = any != 0;
       }
-      uint32_t listed = 0;   // bit u: vector u has listed places
-      for (int k = list.head[tid]; k >= 0; k = list.next[k]) listed |= 1u << list.turn[k];
+      const PlaceBits<kStreamVecs, E> listed(list);
       // Loads return in order and the NR of the registers were issued behind those into this wave's slots: with no more than NR
       // outstanding the slots have landed (the compiler does not track them; other accesses only make the wait longer).
       static_assert(NR <= 15, "immediate below holds vmcnt in 4 bits");
@@ -531,7 +553,7 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
       auto fold = [&](const u32x4_t& x, int u) {
         float z[E];
         View::unpack(x, z);
-        if (listed & (1u << u)) mask_listed(z, list, u);
+        listed.mask(z, u);
         soft_update<E>(st, z);
       };
 #pragma unroll
@@ -551,11 +573,12 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
       }
       const float zr = widen<DT>(zraw);
       if (jr >= 0) {
-        float z[1] = {listed >> kRagged ? -INFINITY : zr};
+        float z[1] = {listed.ragged ? -INFINITY : zr};
         soft_update<1>(st, z);
       }
       if (lister && wn != 0.f) {
         entry.z = widen<DT>(raw);
+        if (entry.j >= 0) lists[par ^ 1].z[tid] = entry.z;
         list_sum(entry, bad, s_list[par ^ 1]);
       }
       have = entry.j >= 0;
@@ -570,7 +593,7 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
         auto turned = [&](const u32x4_t& x, int u) {
           float z[E], d[E];
           View::unpack(x, z);
-          grad_elts<NT, E>(z, d, r, list, listed & (1u << u), u);
+          grad_elts<E>(z, d, r);
           __builtin_amdgcn_raw_buffer_store_b128(pack_vec<DT>(d), dst, voff_st + uint32_t(u) * (NT * 16u), 0, 2);
         };
 #pragma unroll
@@ -586,8 +609,8 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
           if (tid < nvec - (NL + u) * NT) turned(v[u], NL + u);
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (jr >= 0)
-          store_elt<DT>(drow, jr, listed >> kRagged ? grad_ragged(zr, r, list) : r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+        if (jr >= 0) store_elt<DT>(drow, jr, r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
+        put_listed(list, row, r, drow, jr);
       }
     } else if (tid == 0) {
       put_loss(a, t, w, 0.f);
