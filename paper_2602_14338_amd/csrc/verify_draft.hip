@@ -1,10 +1,10 @@
 // Verification of drafted tokens against the policy's rows, from given random numbers.
 //
-// Two launches.  The first forms the running sums of every row that can matter, (target rows up to the count of drafted
-// tokens, the draft rows in front), a row split over several workgroups when there are few.  The second finds, in every
-// workgroup of a sequence alike, the first position whose uniform number is not below p / q, and its slice of the vocabulary for the
-// largest max(0, p - q) / noise there; the slices meet in one 64-bit maximum of (score, lowest id), which does not
-// depend on their order, and the workgroup that comes last writes the sequence's outputs.
+// Three launches.  The first forms the running sums of every row that can matter (target rows up to the count of drafted tokens,
+// the draft rows in front of it), a row split over several workgroups.  The second finds, in every workgroup of a sequence
+// alike, the first position whose uniform number is not below p / q, and its slice of the vocabulary for the largest
+// max(0, p - q) / noise there.  The third joins a sequence's slices: the larger score, the lower id where equal, which does not depend on
+// their order.  (Joining in the second launch by atomics takes a device-wide fence per workgroup, 50 of 129 us for 128 sequences.)
 #include <algorithm>
 
 #include "row_scan.h"
@@ -23,23 +23,22 @@ struct VerifyArgs {
   int32_t* out;
   float* logprob;
   int32_t* err_flag;
-  SoftSum* sums;                    // [B * (2 G + 1)][parts]: target rows, then draft rows
-  unsigned long long* best;         // [B][2]: of the residual, of p itself
-  int32_t* arrived;                 // [B]
-  int parts;
+  SoftSum* sums;      // [B * (2 G + 1)][parts]: target rows, then draft rows
+  uint64_t* best;     // [B][slices]: largest score and its id
+  double* lse;        // [B]: of the row that is drawn from
+  int parts, slices;
 };
 
 // Drafted tokens of a sequence that count: up to its count, and to the first id outside the vocabulary.  -1: idle.  Every lane of the
-// wave gets it; token = this lane's drafted id (lanes in front of the result).
+// wave gets it; token = this lane's drafted id.
 __device__ __forceinline__ int drafted(const VerifyArgs& a, int b, int lane, int& token, int32_t& flags) {
   const int n = a.count ? a.count[b] : a.G;
+  token = lane < a.G ? a.tokens[int64_t(b) * a.G + lane] : -1;
   flags = 0;
-  token = -1;
   if (n < 0 || n > a.G) {
     if (n > a.G) flags = AERO_DERR_BAD_COUNT;
     return -1;
   }
-  if (lane < n) token = a.tokens[int64_t(b) * a.G + lane];
   const uint64_t bad = __builtin_amdgcn_ballot_w64(lane < n && (token < 0 || token >= a.V));
   if (!bad) return n;
   const int first = __builtin_ctzll(bad);
@@ -57,11 +56,6 @@ __global__ __launch_bounds__(NT) void k_verify_rows(VerifyArgs a) {
   const int width = is_target ? a.G + 1 : a.G;
   const int64_t rr = is_target ? r : r - n_target;
   const int b = int(rr / width), i = int(rr % width);
-  if (is_target && i == 0 && part == 0 && tid == 0) {
-    a.best[2 * b] = 0;
-    a.best[2 * b + 1] = 0;
-    a.arrived[b] = 0;
-  }
   int token;
   int32_t flags;
   const int n = drafted(a, b, tid % kWave, token, flags);
@@ -96,10 +90,23 @@ __global__ __launch_bounds__(NT) void k_verify_rows(VerifyArgs a) {
   if (tid == 0) a.sums[r * parts + part] = st;
 }
 
-__device__ __forceinline__ SoftSum row_sum(const VerifyArgs& a, int64_t r) {
-  SoftSum st = soft_identity();
-  for (int p = 0; p < a.parts; ++p) st = soft_merge(st, a.sums[r * a.parts + p]);
-  return st;
+// The parts of a row's sum, all asked for at once, and the row's sum from them.
+struct RowParts {
+  SoftSum part[kVerifyParts];
+  __device__ __forceinline__ void load(const VerifyArgs& a, int64_t r) {
+#pragma unroll
+    for (int p = 0; p < kVerifyParts; ++p) part[p] = p < a.parts ? a.sums[r * a.parts + p] : soft_identity();
+  }
+  __device__ __forceinline__ SoftSum sum() const {
+    SoftSum st = part[0];
+#pragma unroll
+    for (int p = 1; p < kVerifyParts; ++p) st = soft_merge(st, part[p]);
+    return st;
+  }
+};
+__device__ __forceinline__ SoftSum from_lane(SoftSum s, int lane) {
+  return SoftSum{__int_as_float(__builtin_amdgcn_readlane(__float_as_int(s.o), lane)),
+                 __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s.s), lane))};
 }
 
 // Largest score so far and its column.
@@ -110,9 +117,26 @@ struct Drawn {
 __device__ __forceinline__ void race(Drawn& d, float score, int j) {
   if (score > d.score) d = Drawn{score, j};   // columns ascend within a thread
 }
+// (score, lowest id) as a number that grows with the score; 0: none.
 __device__ __forceinline__ uint64_t drawn_key(Drawn d) {
   return d.score > 0.f ? (uint64_t(__float_as_uint(d.score)) << 32) | uint32_t(~d.j) : 0;
 }
+// The largest over the workgroup, in its first thread; one barrier.
+template <int NT> __device__ __forceinline__ uint64_t block_drawn(Drawn d, uint64_t* lds /*[NT/64]*/) {
+  const int lane = threadIdx.x % kWave;
+  const float most = wave_reduce(d.score, [](float x, float y) { return fmaxf(x, y); });
+  d.j = -wave_max_i(d.score == most ? -d.j : INT32_MIN + 1);
+  d.score = most;
+  if (lane == 0) lds[threadIdx.x / kWave] = drawn_key(d);
+  __syncthreads();
+  uint64_t key = 0;
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 0; w < NT / kWave; ++w) key = lds[w] > key ? lds[w] : key;
+  }
+  return key;
+}
+
 // E elements from column j on, or floats, at any element's alignment.
 typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(1)));
 typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
@@ -131,137 +155,187 @@ template <int E> __device__ __forceinline__ void load_floats(const float* x, flo
     }
   }
 }
-template <int NT> __device__ __forceinline__ uint64_t block_max_u64(uint64_t x, uint64_t* lds) {
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
-    const uint64_t y = __shfl_xor(x, m, kWave);
-    x = y > x ? y : x;
-  }
-  if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = x;
-  __syncthreads();
-  x = lds[0];
-#pragma unroll
-  for (int w = 1; w < NT / kWave; ++w) x = lds[w] > x ? lds[w] : x;
-  return x;
-}
-
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   constexpr int E = RowView<DT, VEC>::E;
-  __shared__ uint64_t s_key[2][NT / kWave];
-  __shared__ int s_last;
-  const int tid = threadIdx.x, lane = tid % kWave, b = blockIdx.x, part = blockIdx.y, parts = gridDim.y;
+  __shared__ uint64_t s_key[NT / kWave];
+  const int tid = threadIdx.x, lane = tid % kWave, b = blockIdx.x, slice = blockIdx.y, slices = gridDim.y;
+  // ---- lane i: position i.  Everything that the count does not decide is asked for together with it; what belongs to positions
+  // behind it may never have been written and is not used. ----
+  const int64_t n_target = int64_t(a.B) * (a.G + 1);
+  const int64_t my_t = int64_t(b) * (a.G + 1) + min(lane, a.G), my_d = int64_t(b) * a.G + min(lane, a.G - 1);
+  const bool minus = a.draft != nullptr;   // and so G > 0
+  RowParts pp, qp;
+  pp.load(a, my_t);
+  if (minus) qp.load(a, n_target + my_d);
+  const float u = lane < a.G ? a.uniform[my_d] : 0.f;
   int token;
   int32_t flags;
   const int count = drafted(a, b, lane, token, flags);
-  if (part == 0 && tid == 0 && flags && a.err_flag) atomicOr(a.err_flag, flags);
+  if (slice == 0 && tid == 0 && flags && a.err_flag) atomicOr(a.err_flag, flags);
   int32_t* const out = a.out + int64_t(b) * (a.G + 1);
   float* const lp_out = a.logprob ? a.logprob + int64_t(b) * (a.G + 1) : nullptr;
-  if (count < 0) {
-    if (part == 0) {
+  if (count < 0) {   // uniform
+    if (slice == 0 && tid <= a.G) {
       if (tid == 0) a.accepted[b] = 0;
-      for (int i = tid; i <= a.G; i += NT) {
-        out[i] = -1;
-        if (lp_out) lp_out[i] = 0.f;
-      }
+      out[tid] = -1;
+      if (lp_out) lp_out[tid] = 0.f;
     }
     return;
   }
-  // ---- lane i: position i ----
-  const int64_t n_target = int64_t(a.B) * (a.G + 1);
-  bool ok = false;
-  double lp = 0.0;
-  if (lane < count) {
-    const int64_t rt = int64_t(b) * (a.G + 1) + lane, rd = int64_t(b) * a.G + lane;
-    lp = double(load_elt<DT>(row_ptr<DT>(a.target, rt, a.ld), token)) - soft_lse(row_sum(a, rt));
-    double q = 1.0;
-    if (a.draft) q = exp(double(load_elt<DT>(row_ptr<DT>(a.draft, rd, a.ld), token)) - soft_lse(row_sum(a, n_target + rd)));
-    ok = double(a.uniform[rd]) * q < exp(lp);
-  }
+  const bool on = lane < count;
+  const int column = on ? token : 0;
+  const float zp = load_elt<DT>(row_ptr<DT>(a.target, my_t, a.ld), column);
+  const float zq = minus ? load_elt<DT>(row_ptr<DT>(a.draft, my_d, a.ld), column) : 0.f;
+  const SoftSum sp = pp.sum(), sq = minus ? qp.sum() : soft_identity();
+  const double my_lse = soft_lse(sp), lp = double(zp) - my_lse;
+  const double ratio = minus ? lp - (double(zq) - soft_lse(sq)) : lp;   // ln(p / q)
+  const float coarse = float(ratio);
+  const double fine = fabsf(coarse) < INFINITY ? 1.0 + (ratio - double(coarse)) : 1.0;
+  const bool ok = on && double(u) < double(expf(coarse)) * fine;
   const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(ok));   // at most 63 positions
   const bool refused = n < count;
-  const int own = refused && !a.draft ? __builtin_amdgcn_readlane(token, n) : -1;   // the whole of q
+  const int own = refused && !minus ? __builtin_amdgcn_readlane(token, n) : -1;   // the whole of q
 
   // ---- the draw: this workgroup's slice of row n ----
   const int64_t rt = int64_t(b) * (a.G + 1) + n, rd = int64_t(b) * a.G + n;
-  const SoftSum pt = row_sum(a, rt);
+  const SoftSum pt = from_lane(sp, n);
   const double lse = soft_lse(pt);
-  Drawn left{0.f, 0}, whole{0.f, 0};
+  if (slice == 0 && tid <= a.G) {   // all but the drawn token, which the last launch puts in its place
+    if (tid == 0) {
+      a.accepted[b] = n;
+      a.lse[b] = lse;
+    }
+    out[tid] = tid < n ? token : -1;
+    if (lp_out) lp_out[tid] = tid < n ? float(lp) : 0.f;
+  }
+  Drawn left{0.f, 0};
   if (lse - lse == 0.0) {   // finite
-    SoftSum qt = soft_identity();
-    if (refused && a.draft) qt = row_sum(a, n_target + rd);
+    const SoftSum qt = refused && minus ? from_lane(sq, n) : soft_identity();
     const double lse_q = soft_lse(qt);
-    const bool minus = lse_q - lse_q == 0.0;
-    const float op = -pt.o, sp = 1.f / pt.s, oq = minus ? -qt.o : 0.f, sq = minus ? 1.f / qt.s : 0.f;
+    const bool less = lse_q - lse_q == 0.0;
+    const float op = -pt.o, ip = 1.f / pt.s, oq = less ? -qt.o : 0.f, iq = less ? 1.f / qt.s : 0.f;
     const RowView<DT, VEC> prow(a.target, rt, a.ld, a.V);
-    const char* const qrow = minus ? row_ptr<DT>(a.draft, rd, a.ld) : nullptr;
+    const char* const qrow = less ? row_ptr<DT>(a.draft, rd, a.ld) : nullptr;
     const float* const noise = a.noise + int64_t(b) * a.V;
     auto consider = [&](float z, float y, float e, int j) {
 #pragma clang fp contract(off)   // equal probabilities leave nothing
-      const float p = sp * exp2_fast(fmaf(z, kLog2e, op)), chance = __builtin_amdgcn_rcpf(e);
-      const float q = sq * exp2_fast(fmaf(y, kLog2e, oq)), r = j == own ? 0.f : p - q;
-      race(left, r * chance, j);
-      race(whole, p * chance, j);
+      const float p = ip * exp2_fast(fmaf(z, kLog2e, op)), q = iq * exp2_fast(fmaf(y, kLog2e, oq));
+      race(left, (j == own ? 0.f : p - q) * __builtin_amdgcn_rcpf(e), j);
     };
-    const int per = (prow.nvec + parts - 1) / parts;
-    const int first = min(part * per, prow.nvec), last = min(first + per, prow.nvec);
-    for (int i = first + tid; i < last; i += NT) {
-      const int j = prow.column(i);
-      float z[E], y[E], e[E];
-      const u32x4_t zv = prow.load_again(i);
-      u32x4_t yv = {0u, 0u, 0u, 0u};
-      if (minus) yv = load_elts<DT, VEC>(qrow, j);
-      load_floats<E>(noise + j, e);
-      prow.unpack(zv, z);
-      prow.unpack(yv, y);
+    const int per = (prow.nvec + slices - 1) / slices;
+    const int first = min(slice * per, prow.nvec), last = min(first + per, prow.nvec);
+    constexpr int kAhead = VEC ? 2 : 4;
+    for (int i0 = first + tid; i0 < last; i0 += kAhead * NT) {
+      u32x4_t zv[kAhead], yv[kAhead];
+      float e[kAhead][E];
 #pragma unroll
-      for (int k = 0; k < E; ++k) consider(z[k], y[k], e[k], j + k);
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = min(i0 + k * NT, last - 1), j = prow.column(i);
+        load_floats<E>(noise + j, e[k]);
+        zv[k] = prow.load_again(i);
+        yv[k] = u32x4_t{0u, 0u, 0u, 0u};
+        if (less) yv[k] = load_elts<DT, VEC>(qrow, j);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (i0 + k * NT >= last) break;
+        float z[E], y[E];
+        prow.unpack(zv[k], z);
+        prow.unpack(yv[k], y);
+        const int j = prow.column(i0 + k * NT);
+#pragma unroll
+        for (int c = 0; c < E; ++c) consider(z[c], y[c], e[k][c], j + c);
+      }
     }
-    const int jr = part == 0 ? prow.ragged() : -1;
+    const int jr = slice == 0 ? prow.ragged() : -1;
     if (jr >= 0) {   // a tie goes to the lower id, which is not the later one here
-      Drawn l = left, w = whole;
-      left = whole = Drawn{0.f, 0};
-      consider(prow.at(jr), minus ? load_elt<DT>(qrow, jr) : 0.f, noise[jr], jr);
-      left = drawn_key(l) > drawn_key(left) ? l : left;
-      whole = drawn_key(w) > drawn_key(whole) ? w : whole;
+      const Drawn before = left;
+      left = Drawn{0.f, 0};
+      consider(prow.at(jr), less ? load_elt<DT>(qrow, jr) : 0.f, noise[jr], jr);
+      left = drawn_key(before) > drawn_key(left) ? before : left;
     }
   }
-  const uint64_t k_left = block_max_u64<NT>(drawn_key(left), s_key[0]);
-  const uint64_t k_whole = block_max_u64<NT>(drawn_key(whole), s_key[1]);
-  if (tid == 0) {
-    if (k_left) atomicMax(&a.best[2 * b], (unsigned long long)k_left);
-    if (k_whole) atomicMax(&a.best[2 * b + 1], (unsigned long long)k_whole);
-    __threadfence();
-    s_last = atomicAdd(&a.arrived[b], 1) == parts - 1;
+  const uint64_t key = block_drawn<NT>(left, s_key);
+  if (tid == 0) a.best[int64_t(b) * slices + slice] = key;
+}
+
+// The sequence's drawn token.  Where the residual vanishes (rows that are the same but for roundings) it is drawn from p, by this
+// workgroup alone.
+constexpr int kEndNT = 256;
+template <int DT> __global__ __launch_bounds__(kEndNT) void k_verify_end(VerifyArgs a) {
+  __shared__ uint64_t s_key[kEndNT / kWave];
+  __shared__ uint64_t s_best;
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const int count = a.count ? a.count[b] : a.G;
+  if (count < 0 || count > a.G) return;   // uniform
+  const int n = a.accepted[b];
+  const double lse = a.lse[b];
+  uint64_t key = 0;
+  for (int k = tid; k < a.slices; k += kEndNT) {
+    const uint64_t x = a.best[int64_t(b) * a.slices + k];
+    key = x > key ? x : key;
   }
+  Drawn d{__uint_as_float(uint32_t(key >> 32)), int(~uint32_t(key))};
+  if (key == 0) d = Drawn{0.f, 0};
+  key = block_drawn<kEndNT>(d, s_key);
+  if (tid == 0) s_best = key;
   __syncthreads();
-  if (!s_last || tid >= kWave) return;
-  __threadfence();
-  uint64_t key = atomicMax(&a.best[2 * b], 0ull);
-  if (!key && refused) key = atomicMax(&a.best[2 * b + 1], 0ull);
-  const int drawn = key ? int(~uint32_t(key)) : -1;
-  const float drawn_lp = drawn >= 0 ? float(double(load_elt<DT>(row_ptr<DT>(a.target, rt, a.ld), drawn)) - lse) : 0.f;
-  if (lane == 0) a.accepted[b] = n;
-  if (lane <= a.G) {
-    out[lane] = lane < n ? token : lane == n ? drawn : -1;
-    if (lp_out) lp_out[lane] = lane < n ? float(lp) : lane == n ? drawn_lp : 0.f;
+  key = s_best;
+  const int64_t rt = int64_t(b) * (a.G + 1) + n;
+  const char* const row = row_ptr<DT>(a.target, rt, a.ld);
+  if (key == 0 && lse - lse == 0.0) {   // uniform
+    d = Drawn{0.f, 0};
+    for (int j = tid; j < a.V; j += kEndNT)
+      race(d, expf(float(double(load_elt<DT>(row, j)) - lse)) * __builtin_amdgcn_rcpf(a.noise[int64_t(b) * a.V + j]), j);
+    key = block_drawn<kEndNT>(d, s_key);   // between the two uses of s_key lie the barriers around s_best
+  }
+  if (tid == 0 && key != 0) {
+    const int drawn = int(~uint32_t(key));
+    a.out[rt] = drawn;
+    if (a.logprob) a.logprob[rt] = float(double(load_elt<DT>(row, drawn)) - lse);
   }
 }
 
-static size_t verify_sum_bytes(int64_t rows) { return (size_t(2 * rows) * kVerifyParts * sizeof(SoftSum) + 255) / 256 * 256; }
+// Workgroups that a row's sum is split over: 8 to a CU in all.  (151936 bf16, 72 rows: 2 / 4 / 8 parts 9.9 / 8.3 / 7.6 us; 1408 rows, of which
+// 768 are read: 1 / 2 / 4 parts 43.7 / 41.0 / 41.5.)
+static int verify_parts(int64_t rows, int nvec, int NT) {
+  return int(std::max<int64_t>(1, std::min<int64_t>({kVerifyParts, (8 * compute_units() + rows - 1) / rows, nvec / (2 * NT)})));
+}
+// Workgroups that the draw of a sequence is split over: one to a CU in all, since each goes through the decision first.  (8 sequences: 4 / 16 /
+// 32 / 37 slices 14.2 / 7.8 / 7.4 / 9.4 us; 128: 2 / 8 / 32 slices 27.9 / 29.6 / 41.2.)
+constexpr int kMaxSlices = 64;
+static int verify_slices(int64_t B, int nvec, int NT) {
+  return int(std::max<int64_t>(1, std::min<int64_t>({kMaxSlices, compute_units() / B, nvec / NT})));
+}
+
+struct VerifyWorkspace {
+  SoftSum* sums;
+  uint64_t* best;
+  double* lse;
+  size_t bytes;
+};
+static VerifyWorkspace verify_workspace(void* base, int64_t rows, int64_t B) {
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  char* const p = reinterpret_cast<char*>(base);
+  const size_t sums = up(size_t(2 * rows) * kVerifyParts * sizeof(SoftSum)), best = up(size_t(B) * kMaxSlices * 8);
+  return VerifyWorkspace{reinterpret_cast<SoftSum*>(p), reinterpret_cast<uint64_t*>(p + sums), reinterpret_cast<double*>(p + sums + best),
+                         sums + best + up(size_t(B) * 8) + 256};
+}
 size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B) {
   (void)V;
-  return verify_sum_bytes(rows) + (size_t(B > 0 ? B : 0) * 20 + 255) / 256 * 256 + 256;
+  return verify_workspace(nullptr, rows, B > 0 ? B : 0).bytes;
 }
 
 template <int DT, bool VEC> static void verify_launch(VerifyArgs a, hipStream_t s) {
   constexpr int NT = 512;
   const int64_t rows = int64_t(a.B) * (a.G + 1) + (a.draft ? int64_t(a.B) * a.G : 0);
   const int nvec = a.V / RowView<DT, VEC>::E;
-  a.parts = int(std::max<int64_t>(1, std::min<int64_t>({kVerifyParts, 2 * compute_units() / rows, nvec / (4 * NT)})));
+  a.parts = verify_parts(rows, nvec, NT);
+  a.slices = verify_slices(a.B, nvec, NT);
   hipLaunchKernelGGL((k_verify_rows<NT, DT, VEC>), dim3(unsigned(rows), unsigned(a.parts)), dim3(NT), 0, s, a);
-  const int parts = int(std::max<int64_t>(1, std::min<int64_t>(4 * compute_units() / a.B, nvec / NT)));
-  hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC>), dim3(unsigned(a.B), unsigned(parts)), dim3(NT), 0, s, a);
+  hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC>), dim3(unsigned(a.B), unsigned(a.slices)), dim3(NT), 0, s, a);
+  hipLaunchKernelGGL((k_verify_end<DT>), dim3(unsigned(a.B)), dim3(kEndNT), 0, s, a);
 }
 
 }  // namespace aero
@@ -280,10 +354,9 @@ extern "C" aero_status aero_verify_draft(const void* target_logits, const void* 
   const int64_t rows = int64_t(B) * (G + 1);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < verify_workspace_bytes(rows, V, B))
     return AERO_ERR_WORKSPACE;
-  char* const ws = reinterpret_cast<char*>(workspace);
-  unsigned long long* const best = reinterpret_cast<unsigned long long*>(ws + verify_sum_bytes(rows));
+  const VerifyWorkspace ws = verify_workspace(workspace, rows, B);
   const VerifyArgs a{target_logits, G > 0 ? draft_logits : nullptr, B, G, V, ld, draft_tokens, draft_count, uniform, noise, accepted, tokens,
-                     logprob, err_flag, reinterpret_cast<SoftSum*>(ws), best, reinterpret_cast<int32_t*>(best + 2 * size_t(B)), 1};
+                     logprob, err_flag, ws.sums, ws.best, ws.lse, 1, 1};
   const bool vec = rows_alike(target_logits, nullptr, storage_bytes(dtype)) && rows_alike(a.draft, nullptr, storage_bytes(dtype));
   const hipStream_t s = as_stream(stream);
   switch (dtype) {
