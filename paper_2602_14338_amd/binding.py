@@ -126,7 +126,8 @@ class _Marshal:
     ``group_advantage`` and the others: a whole call whose arguments are all plain, NotImplemented for any other."""
 
     def __getattr__(self, name):
-        if name not in ("pointers", "group_advantage", "logprob_fwd", "loss_bwd", "fused"):
+        if name not in ("pointers", "group_advantage", "logprob_fwd", "loss_bwd", "fused", "topk", "distill", "verify", "embed_fwd",
+                        "embed_bwd"):
             raise AttributeError(name)
         try:
             from . import _marshal
@@ -137,7 +138,8 @@ class _Marshal:
             _marshal.setup(AeroError, _ptr)
         else:
             entries = (_lib.aero_group_advantage, _lib.aero_logprob_fwd, _lib.aero_grpo_loss_bwd,
-                       _lib.aero_grpo_loss_bwd_noalloc, _lib.aero_lmhead_logprob_fused)
+                       _lib.aero_grpo_loss_bwd_noalloc, _lib.aero_lmhead_logprob_fused, _lib.aero_topk_logprob,
+                       _lib.aero_distill_loss_bwd, _lib.aero_verify_draft, _lib.aero_embedding_fwd, _lib.aero_embedding_bwd)
             _marshal.bind(torch._C._cuda_getCurrentRawStream, AdvParams, *(C.cast(f, C.c_void_p).value for f in entries))
         fn = getattr(_marshal, name)
         setattr(self, name, fn)
@@ -275,6 +277,9 @@ def _bytes(t: Optional[torch.Tensor]) -> int:
 
 
 def aero_topk_logprob(logits, T: int, V: int, ld: int, row_active, K: int, index, logprob, lse, workspace) -> None:
+    st = _m.topk(logits, T, V, ld, row_active, K, index, logprob, lse, workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_topk_logprob")
     z, *p, ws = _m.pointers(logits, None, "logits", row_active, _U8, "row_active", index, _I32, "index", logprob, _F32, "logprob",
                             lse, _F32, "lse", workspace, None, "workspace")
     st = _lib.aero_topk_logprob(z, _dtype_code(logits), T, V, ld, p[0], K, *p[1:], ws, _bytes(workspace), _stream(logits))
@@ -283,6 +288,10 @@ def aero_topk_logprob(logits, T: int, V: int, ld: int, row_active, K: int, index
 
 def aero_distill_loss_bwd(logits, T: int, V: int, ld: int, teacher_index, teacher_logprob, K: int, token_weight, tail: int,
                           grad_scale: float, loss, row_loss, dlogits, workspace, err_flag=None) -> None:
+    st = _m.distill(logits, T, V, ld, teacher_index, teacher_logprob, K, token_weight, tail, grad_scale, loss, row_loss, dlogits, err_flag,
+                    workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_distill_loss_bwd")
     if dlogits is not None and dlogits.dtype != logits.dtype:
         raise AeroError("dlogits must have the dtype of logits")
     z, index, lp, w, *p = _m.pointers(
@@ -296,6 +305,10 @@ def aero_distill_loss_bwd(logits, T: int, V: int, ld: int, teacher_index, teache
 
 def aero_verify_draft(target_logits, draft_logits, B: int, G: int, V: int, ld: int, draft_tokens, draft_count, uniform, noise,
                       accepted, tokens, logprob, workspace, err_flag=None) -> None:
+    st = _m.verify(target_logits, draft_logits, B, G, V, ld, draft_tokens, draft_count, uniform, noise, accepted, tokens, logprob, err_flag,
+                   workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_verify_draft")
     if draft_logits is not None and draft_logits.dtype != target_logits.dtype:
         raise AeroError("draft_logits must have the dtype of target_logits")
     zt, zd, *p, err, ws = _m.pointers(
@@ -308,6 +321,9 @@ def aero_verify_draft(target_logits, draft_logits, B: int, G: int, V: int, ld: i
 
 
 def aero_embedding_fwd(table, V: int, H: int, ids, T: int, scale: float, out, ld_out: int, err_flag=None) -> None:
+    st = _m.embed_fwd(table, V, H, ids, T, scale, out, ld_out, err_flag)
+    if st is not NotImplemented:
+        return _check(st, "aero_embedding_fwd")
     if out.dtype != table.dtype:
         raise AeroError("out must have the dtype of table")
     e, i, o, err = _m.pointers(table, None, "table", ids, _I32, "ids", out, None, "out", err_flag, _I32, "err_flag")
@@ -317,6 +333,9 @@ def aero_embedding_fwd(table, V: int, H: int, ids, T: int, scale: float, out, ld
 
 def aero_embedding_bwd(dout, T: int, H: int, ld_dout: int, ids, V: int, scale: float, dtable, workspace,
                        accumulate: bool = False, err_flag=None) -> None:
+    st = _m.embed_bwd(dout, T, H, ld_dout, ids, V, scale, dtable, accumulate, err_flag, workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_embedding_bwd")
     d, i, g, err, ws = _m.pointers(dout, None, "dout", ids, _I32, "ids", dtable, None, "dtable", err_flag, _I32, "err_flag",
                                    workspace, None, "workspace")
     code = _dtype_code(dtable) | (AERO_DW_ACCUMULATE if accumulate else 0)

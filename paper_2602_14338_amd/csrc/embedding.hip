@@ -1,14 +1,15 @@
 // Embedding rows looked up and scaled, and the gradient of the table from tokens sorted by id.
 //
-// The sort is a launch of independent workgroups, each of which owns the ids that are alike modulo their number and goes
-// over all tokens twice: once to count (its own ids one by one, what lies in front of them as a whole), once to place its
-// tokens, in ascending order within an id.  Every token is read by every workgroup, out of the caches; nothing passes
-// between workgroups and there are no counters whose order could show.  What a frequent id has to add up is cut into
-// pieces of kPiece tokens, summed in a second launch and, where there is more than one, joined in order in a third.  Rows
-// that no token has are zeroed in the second launch, beside the sums, so that the sort has nothing to wait for.
+// The sort is a launch of independent workgroups, each of which owns the ids that are alike modulo their number: it counts
+// its own ids one by one and the tokens of those in front of it as a whole, and places its tokens in ascending order within an id.
+// Every token is read by every workgroup, out of the caches; nothing passes between workgroups and there are no counters whose order
+// could show.  The sums are a second launch of workgroups that go over three kinds of work, found by halving in the owners' counts:
+// pieces of kPiece tokens of frequent ids by column blocks, whole rows of the others, and zeros for the ids that no token has.  The zeros are
+// small workgroups in the order of their addresses where rows are whole vectors: that writes 6.8 TB/s, workgroups that walk over rows 5.2.  Ids
+// with several pieces are joined in order in a third.
 #include <algorithm>
 
-#include "aero_device.h"
+#include "row_scan.h"
 
 namespace aero {
 
@@ -42,20 +43,28 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const void* __restrict__ tabl
 }
 
 // ---- gradient ----
-constexpr int kSortNT = 1024, kSortAhead = 4, kSortChunk = kSortNT * kSortAhead;
-constexpr int kLogBins = 10, kBins = 1 << kLogBins;   // ids of a sorting workgroup
-constexpr int kMinOwners = 256;  // sorting workgroups, a power of two
-constexpr int kPiece = 32;       // tokens that one wave adds up
-constexpr int kFillParts = 4;    // workgroups that zero the rows of an owner
+constexpr int kSortNT = 1024, kSortWaves = kSortNT / kWave;
+constexpr int kSortRuns = 8, kSortEach = 4, kSortRun = kSortNT * kSortEach, kSortChunk = kSortRun * kSortRuns;   // tokens that a sorting workgroup holds
+constexpr int kListed = 4096;                            // of its own among them
+constexpr int kLogBins = 10, kBins = 1 << kLogBins;      // ids of a sorting workgroup
+constexpr int kMinOwners = 256;                          // sorting workgroups, a power of two
+constexpr int kPiece = 32;                               // tokens of a frequent id that one wave adds up
+constexpr int kFew = 4;                                  // up to so many tokens: a wave takes the whole row
+constexpr int kZeroRows = 16;                            // rows that a wave zeroes at a time
 
-// A run of sorted tokens: pieces of an id.  Slot s describes the piece whose first piece's tokens start at sorted position
-// s - piece; slots that no piece has are empty (count 0).
+// Sorted tokens [start, start + count) of an id.  row: where the sum goes when the id has several pieces, -1: to the table.
 struct Piece {
-  int32_t id, start, count;
-  int32_t part;   // 0: the id has one piece; else 1 + the piece's number
-  int32_t whole;  // tokens of the id
-  int32_t row;    // where the piece's sum goes when there are several
-  int32_t pad[2];
+  int32_t id, start, count, row;
+};
+// An id with several pieces, whose sums are rows [row, row + pieces).
+struct Whole {
+  int32_t id, row, pieces, pad;
+};
+// How many of each a sorting workgroup has.  Its pieces lie from its first sorted position on: those of frequent ids in front, the
+// others behind, from the last position backwards; its wholes from the same position on.
+struct OwnerCounts {
+  int32_t *heavy, *few, *whole, *none;   // [owners]
+  int32_t *base, *end;                   // [owners] first sorted position, and the one behind the last
 };
 
 static int embed_owners(int32_t V) {
@@ -66,26 +75,31 @@ static int embed_owners(int32_t V) {
 struct EmbedWorkspace {
   int32_t* order;   // [T] tokens sorted by id
   Piece* piece;     // [T]
-  int32_t* n_empty; // [owners]
-  int32_t* empty;   // [owners][kBins] ids that no token has
+  Whole* whole;     // [T]
+  int32_t* none;    // [owners][kBins] ids that no token has
+  uint8_t* there;   // [V] a token has the id
+  OwnerCounts n;
   float* partial;   // [2 (T / kPiece + 1)][H]
   size_t bytes;
 };
 static EmbedWorkspace embed_workspace(void* base, int64_t T, int32_t V, int64_t H) {
-  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  char* p = reinterpret_cast<char*>(base);
-  EmbedWorkspace w;
-  w.order = reinterpret_cast<int32_t*>(p);
-  size_t at = up(size_t(T) * 4);
-  w.piece = reinterpret_cast<Piece*>(p + at);
-  at += up(size_t(T) * sizeof(Piece));
+  char* const p = reinterpret_cast<char*>(base);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    char* const q = p + at;
+    at += (n + 255) / 256 * 256;
+    return q;
+  };
   const size_t owners = embed_owners(V);
-  w.n_empty = reinterpret_cast<int32_t*>(p + at);
-  at += up(owners * 4);
-  w.empty = reinterpret_cast<int32_t*>(p + at);
-  at += up(owners * kBins * 4);
-  w.partial = reinterpret_cast<float*>(p + at);
-  at += up(size_t(2 * (T / kPiece + 1)) * size_t(H) * 4);
+  EmbedWorkspace w;
+  w.order = reinterpret_cast<int32_t*>(take(size_t(T) * 4));
+  w.piece = reinterpret_cast<Piece*>(take(size_t(T) * sizeof(Piece)));
+  w.whole = reinterpret_cast<Whole*>(take(size_t(T) * sizeof(Whole)));
+  w.none = reinterpret_cast<int32_t*>(take(owners * kBins * 4));
+  w.there = reinterpret_cast<uint8_t*>(take(size_t(V)));
+  int32_t** const counts[] = {&w.n.heavy, &w.n.few, &w.n.whole, &w.n.none, &w.n.base, &w.n.end};
+  for (int32_t** c : counts) *c = reinterpret_cast<int32_t*>(take(owners * 4));
+  w.partial = reinterpret_cast<float*>(take(size_t(2 * (T / kPiece + 1)) * size_t(H) * 4));
   w.bytes = at + 256;
   return w;
 }
@@ -93,48 +107,62 @@ size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H) {
   return embed_workspace(nullptr, T, V > 0 ? V : 1, H > 0 ? H : 0).bytes;
 }
 
-// Workgroup g owns the ids with id % owners == g.  Its ids without a token go to empty[g * kBins ...], their number to n_empty[g].
+// Workgroup g owns the ids with id % owners == g.  A chunk of tokens is kSortRuns runs, of which a thread holds kSortEach tokens that follow
+// each other: (run, thread, number) is their order.
 __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restrict__ ids, int64_t T, int V, int log_owners,
-                                                        int32_t* __restrict__ order, Piece* __restrict__ pieces,
-                                                        int32_t* __restrict__ empty, int32_t* __restrict__ n_empty,
+                                                        int32_t* __restrict__ order, Piece* __restrict__ pieces, Whole* __restrict__ wholes,
+                                                        int32_t* __restrict__ none, uint8_t* __restrict__ there, OwnerCounts counts,
                                                         int32_t* __restrict__ err_flag) {
   __shared__ int s_count[kBins], s_at[kBins];
-  __shared__ int s_wave[kSortNT / kWave];
-  __shared__ int s_none;
-  __shared__ int32_t s_tok[kSortChunk];
-  __shared__ __align__(16) uint16_t s_bin[kSortChunk];
+  __shared__ int s_wave[2][kSortWaves], s_run[kSortRuns * kSortWaves], s_all;
+  __shared__ int s_n[4];
+  __shared__ int32_t s_tok[kListed];
+  __shared__ uint16_t s_bin[kListed];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int g = blockIdx.x, mask = (1 << log_owners) - 1;
   const int bins = (V - g + mask) >> log_owners;   // ids g, g + owners, ... below V
+  const uint64_t below = (uint64_t(1) << lane) - 1;
   s_count[tid] = 0;
-  if (tid == 0) s_none = 0;
+  if (tid < 4) s_n[tid] = 0;
   __syncthreads();
   // ---- count ----
+  int id[kSortRuns][kSortEach];
+  uint32_t own = 0;   // bit kSortEach r + u: id[r][u] is this workgroup's
   int before = 0;
   bool bad = false;
-  for (int64_t t0 = 0; t0 < T; t0 += 2 * kSortChunk) {
-    int id[2 * kSortAhead];
+  auto load = [&](int64_t t0, bool count) {
+    const bool whole = t0 + kSortChunk <= T && reinterpret_cast<uintptr_t>(ids) % 16 == 0;   // uniform
 #pragma unroll
-    for (int u = 0; u < 2 * kSortAhead; ++u) {
-      const int64_t t = t0 + u * kSortNT + tid;
-      id[u] = t < T ? ids[t] : -1;
-    }
+    for (int r = 0; r < kSortRuns; ++r) {
+      const int64_t t = t0 + r * kSortRun + tid * kSortEach;
+      if (whole) {
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(ids + t);
+        id[r][0] = int(v.x); id[r][1] = int(v.y); id[r][2] = int(v.z); id[r][3] = int(v.w);
+      } else {
 #pragma unroll
-    for (int u = 0; u < 2 * kSortAhead; ++u) {
-      bad |= id[u] >= V;
-      const bool in = id[u] >= 0 && id[u] < V;
-      const int owner = id[u] & mask;
-      before += in && owner < g;
-      if (in && owner == g) atomicAdd(&s_count[id[u] >> log_owners], 1);
+        for (int u = 0; u < kSortEach; ++u) id[r][u] = t + u < T ? ids[t + u] : -1;
+      }
     }
-  }
+    own = 0;
+#pragma unroll
+    for (int r = 0; r < kSortRuns; ++r) {
+      if (t0 + r * kSortRun >= T) break;   // uniform
+#pragma unroll
+      for (int u = 0; u < kSortEach; ++u) {
+        const int i = id[r][u], owner = uint32_t(i) < uint32_t(V) ? i & mask : kSortNT * kBins;
+        own |= owner == g ? 1u << (kSortEach * r + u) : 0u;
+        if (count) {
+          before += owner < g;
+          bad |= i >= V;
+          if (owner == g) atomicAdd(&s_count[i >> log_owners], 1);
+        }
+      }
+    }
+  };
+  for (int64_t t0 = 0; t0 < T; t0 += kSortChunk) load(t0, true);
   if (g == 0 && bad && err_flag) atomicOr(err_flag, AERO_DERR_BAD_TARGET);
   before = wave_sum_i(before);
-  if (lane == 0) s_wave[wave] = before;
-  __syncthreads();
-  int base = 0;
-#pragma unroll
-  for (int w = 0; w < kSortNT / kWave; ++w) base += s_wave[w];
+  if (lane == 0) s_wave[0][wave] = before;
   __syncthreads();
   // ---- where each id starts ----
   static_assert(kBins == kSortNT, "a thread per id");
@@ -145,200 +173,353 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
     const int y = __shfl_up(incl, m, kWave);
     if (lane >= m) incl += y;
   }
-  if (lane == kWave - 1) s_wave[wave] = incl;
+  if (lane == kWave - 1) s_wave[1][wave] = incl;
   __syncthreads();
-  int start = base + incl - mine, total = 0;
+  int base = 0, start = incl - mine, total = 0;
 #pragma unroll
-  for (int w = 0; w < kSortNT / kWave; ++w) {
-    if (w < wave) start += s_wave[w];
-    total += s_wave[w];
+  for (int w = 0; w < kSortWaves; ++w) {
+    base += s_wave[0][w];
+    if (w < wave) start += s_wave[1][w];
+    total += s_wave[1][w];
   }
+  start += base;
   s_at[tid] = start;
-  // ---- pieces ----
-  // (behind the last owner's tokens lie the slots of tokens that no id counts)
-  const int64_t slots = g == int(gridDim.x) - 1 ? T - base : total;
-  for (int64_t k = tid; k < slots; k += kSortNT) pieces[base + k].count = 0;
-  __syncthreads();
+  // ---- pieces, in whatever order ----
   const int id_mine = (tid << log_owners) + g;
-  if (mine > 0) {
-    const int np = (mine + kPiece - 1) / kPiece;
-    for (int k = 0; k < np; ++k)
-      pieces[start + k] = Piece{id_mine, start + k * kPiece, min(kPiece, mine - k * kPiece), np == 1 ? 0 : 1 + k, mine,
-                                2 * (start / kPiece) + k, {0, 0}};
+  if (tid < bins) there[id_mine] = mine > 0;
+  if (mine > kFew) {
+    const int np = (mine + kPiece - 1) / kPiece, row = 2 * (start / kPiece);   // np <= 2 (mine / kPiece): the next id's rows lie behind
+    const int at = base + atomicAdd(&s_n[0], np);
+    for (int k = 0; k < np; ++k) pieces[at + k] = Piece{id_mine, start + k * kPiece, min(kPiece, mine - k * kPiece), np == 1 ? -1 : row + k};
+    if (np > 1) wholes[base + atomicAdd(&s_n[2], 1)] = Whole{id_mine, row, np, 0};
+  } else if (mine > 0) {
+    pieces[base + total - 1 - atomicAdd(&s_n[1], 1)] = Piece{id_mine, start, mine, -1};
   } else if (tid < bins) {
-    empty[g * kBins + atomicAdd(&s_none, 1)] = id_mine;   // rows of zeros: their order is nothing's
+    none[g * kBins + atomicAdd(&s_n[3], 1)] = id_mine;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    counts.heavy[g] = s_n[0];
+    counts.few[g] = s_n[1];
+    counts.whole[g] = s_n[2];
+    counts.none[g] = s_n[3];
+    counts.base[g] = base;
+    counts.end[g] = base + total;
   }
   // ---- place, in order ----
-  for (int64_t t0 = 0; total > 0 && t0 < T; t0 += kSortChunk) {
-    // a thread's tokens follow each other, so that (thread, u) is their order
-    int id[kSortAhead];
-    bool own[kSortAhead];
-    int ahead = 0, in_wave = 0;
+  if (total == 0) return;
+  for (int64_t t0 = 0; t0 < T; t0 += kSortChunk) {
+    if (T > kSortChunk) load(t0, false);   // a single chunk is still there
+    int ahead[kSortRuns];   // of the wave's own tokens of the run, those of the lanes in front
 #pragma unroll
-    for (int u = 0; u < kSortAhead; ++u) {
-      const int64_t t = t0 + tid * kSortAhead + u;
-      id[u] = t < T ? ids[t] : -1;
-      own[u] = id[u] >= 0 && id[u] < V && (id[u] & mask) == g;
-      const uint64_t m = __builtin_amdgcn_ballot_w64(own[u]);
-      ahead += __popcll(m & ((uint64_t(1) << lane) - 1));
-      in_wave += __popcll(m);
-    }
-    if (lane == 0) s_wave[wave] = in_wave;
-    __syncthreads();
-    int n = 0;
+    for (int r = 0; r < kSortRuns; ++r) {
+      int in_wave = 0;
+      ahead[r] = 0;
 #pragma unroll
-    for (int w = 0; w < kSortNT / kWave; ++w) {
-      if (w < wave) ahead += s_wave[w];
-      n += s_wave[w];
-    }
-#pragma unroll
-    for (int u = 0; u < kSortAhead; ++u) {
-      if (own[u]) {
-        s_tok[ahead] = int32_t(t0 + tid * kSortAhead + u);
-        s_bin[ahead] = uint16_t(id[u] >> log_owners);
-        ++ahead;
+      for (int u = 0; u < kSortEach; ++u) {
+        const uint64_t m = __builtin_amdgcn_ballot_w64((own >> (kSortEach * r + u) & 1) != 0);
+        ahead[r] += __popcll(m & below);
+        in_wave += __popcll(m);
       }
+      if (lane == 0) s_run[r * kSortWaves + wave] = in_wave;
     }
     __syncthreads();
-    // 64 at a time by the first wave: a token's place is its id's next one plus the lanes in front with the same id
+    static_assert(kSortRuns * kSortWaves == 2 * kWave, "two counts per lane");
     if (wave == 0) {
-      for (int k0 = 0; k0 < n; k0 += kWave) {
-        const int k = k0 + lane;
-        const bool in = k < n;
-        const int bin = in ? s_bin[k] : 0;
-        uint64_t same = __builtin_amdgcn_ballot_w64(in);
+      const int x = s_run[2 * lane], y = s_run[2 * lane + 1];
+      int sum = x + y;
 #pragma unroll
-        for (int bit = 0; bit < kLogBins; ++bit) {
-          const uint64_t m = __builtin_amdgcn_ballot_w64((bin >> bit & 1) != 0);
-          same &= (bin >> bit & 1) != 0 ? m : ~m;
-        }
-        if (in) {
-          const int rank = __popcll(same & ((uint64_t(1) << lane) - 1));
-          const int at = s_at[bin];
-          order[at + rank] = s_tok[k];
-          if (rank == 0) s_at[bin] = at + __popcll(same);   // read above by every lane of the id: one wave, in step
+      for (int m = 1; m < kWave; m <<= 1) {
+        const int z = __shfl_up(sum, m, kWave);
+        if (lane >= m) sum += z;
+      }
+      s_run[2 * lane] = sum - x - y;
+      s_run[2 * lane + 1] = sum - y;
+      if (lane == kWave - 1) s_all = sum;
+    }
+    __syncthreads();
+    const int n = s_all;
+    for (int from = 0; from < n; from += kListed) {   // kListed of the workgroup's own tokens at a time
+      if (own != 0) {
+#pragma unroll
+        for (int r = 0; r < kSortRuns; ++r) {
+          int at = s_run[r * kSortWaves + wave] + ahead[r] - from;
+#pragma unroll
+          for (int u = 0; u < kSortEach; ++u) {
+            if (own >> (kSortEach * r + u) & 1) {
+              if (at >= 0 && at < kListed) {
+                s_tok[at] = int32_t(t0 + r * kSortRun + tid * kSortEach + u);
+                s_bin[at] = uint16_t(id[r][u] >> log_owners);
+              }
+              ++at;
+            }
+          }
         }
       }
+      __syncthreads();
+      // 64 at a time by the first wave: a token's place is its id's next one plus the lanes in front with the same id
+      const int listed = min(n - from, kListed);
+      if (wave == 0) {
+        for (int k0 = 0; k0 < listed; k0 += kWave) {
+          const int k = k0 + lane;
+          const bool in = k < listed;
+          const int bin = in ? s_bin[k] : 0;
+          uint64_t same = __builtin_amdgcn_ballot_w64(in);
+#pragma unroll
+          for (int bit = 0; bit < kLogBins; ++bit) {
+            const uint64_t m = __builtin_amdgcn_ballot_w64((bin >> bit & 1) != 0);
+            same &= (bin >> bit & 1) != 0 ? m : ~m;
+          }
+          if (in) {
+            const int rank = __popcll(same & below);
+            const int first = s_at[bin];
+            order[first + rank] = s_tok[k];
+            if (rank == 0) s_at[bin] = first + __popcll(same);   // behind the read by every lane of the id: one wave, in step
+          }
+        }
+      }
+      __syncthreads();
     }
     __syncthreads();
   }
-  if (tid == 0) n_empty[g] = s_none;
+}
+
+// Inclusive sums of the owners' counts in LDS, and the owner that the u-th of all lies with (and which of its own it is).
+constexpr int kSumNT = 256, kSumWaves = kSumNT / kWave;
+__device__ __forceinline__ int scan_owners(const int32_t* __restrict__ n, int owners, int* s_end /*[owners]*/, int* s_wave /*[kSumWaves]*/,
+                                           int unit) {
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  int total = 0;
+  __syncthreads();   // s_end may still be in use
+  for (int g0 = 0; g0 < owners; g0 += kSumNT) {   // owners is a multiple of kSumNT
+    int incl = (n[g0 + tid] + unit - 1) / unit;
+#pragma unroll
+    for (int m = 1; m < kWave; m <<= 1) {
+      const int y = __shfl_up(incl, m, kWave);
+      if (lane >= m) incl += y;
+    }
+    if (lane == kWave - 1) s_wave[wave] = incl;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kSumWaves; ++w) {
+      if (w < wave) incl += s_wave[w];
+      all += s_wave[w];
+    }
+    s_end[g0 + tid] = total + incl;
+    total += all;
+    __syncthreads();
+  }
+  return total;
+}
+__device__ __forceinline__ int find_owner(const int* s_end, int owners, int u, int& own) {
+  int lo = 0, hi = owners - 1;   // the first owner whose end is behind u
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (s_end[mid] > u) hi = mid;
+    else lo = mid + 1;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  own = u - (lo > 0 ? __builtin_amdgcn_readfirstlane(s_end[lo - 1]) : 0);
+  return lo;
 }
 
 // N sums, scaled, to consecutive columns of the table: added to what is there, or in its place.
 template <int OUT, int N> __device__ __forceinline__ void put_sums(char* at, const float (&sum)[N], float scale, bool accumulate) {
-  constexpr int kBytes = N * Storage<OUT>::kBytes;
   float x[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = scale * sum[e];
-  if constexpr (kBytes % 16 == 0) {
-    constexpr int E = Storage<OUT>::kPerVec;
+  if constexpr (N == Storage<OUT>::kPerVec) {
+    u32x4_t* const p = reinterpret_cast<u32x4_t*>(at);
+    if (accumulate) {
+      float y[N];
+      unpack_vec<OUT>(*p, y);
 #pragma unroll
-    for (int v = 0; v < kBytes / 16; ++v) {
-      u32x4_t* const p = reinterpret_cast<u32x4_t*>(at) + v;
-      float y[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = 0.f;
-      if (accumulate) unpack_vec<OUT>(*p, y);
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = accumulate ? y[e] + x[v * E + e] : x[v * E + e];
-      __builtin_nontemporal_store(pack_vec<OUT>(y), p);
+      for (int e = 0; e < N; ++e) x[e] += y[e];
     }
+    __builtin_nontemporal_store(pack_vec<OUT>(x), p);
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e) store_elt<OUT>(at, e, accumulate ? load_elt<OUT>(at, e) + x[e] : x[e]);
   }
 }
 
-constexpr int kSumNT = 256, kSumWaves = kSumNT / kWave, kRowsAhead = 4;
-// The first n_sum workgroups: wave (slot, column block), the sum of a piece's rows, to the table or, of an id with several pieces, to
-// `partial`.  The others (not with accumulate): rows of zeros for the ids that no token has.  VEC: dout in 16-byte vectors, and the table
-// where a lane's sums are whole vectors of it.
-template <int DT, int OUT, bool VEC>
-__global__ __launch_bounds__(kSumNT) void k_embed_sum(const void* __restrict__ dout, int64_t ld, int H, int64_t T, int n_sum, int n_owners,
-                                                      const int32_t* __restrict__ order, const Piece* __restrict__ pieces,
-                                                      const int32_t* __restrict__ empty, const int32_t* __restrict__ n_empty, float scale,
-                                                      int accumulate, float* __restrict__ partial, void* __restrict__ table) {
-  constexpr int E = VEC ? Storage<DT>::kPerVec : 1;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  if (int(blockIdx.x) >= n_sum) {
-    const int part = (int(blockIdx.x) - n_sum) * gridDim.y + blockIdx.y, g = part / kFillParts;
-    if (g >= n_owners) return;
-    const int n = n_empty[g];
-    for (int k = part % kFillParts * kSumWaves + wave; k < n; k += kFillParts * kSumWaves) {
-      const int64_t id = empty[g * kBins + k];
-      char* const row = row_ptr<OUT>(table, id, H);
-      const RowGeom geom = row_geom<OUT>(table, id, H, H);
+struct EmbedSums {
+  const void* dout;
+  int64_t ld;
+  int H, owners;
+  const int32_t* order;
+  const Piece* piece;
+  const int32_t* none;
+  const uint8_t* there;
+  OwnerCounts n;
+  float scale;
+  int accumulate;
+  int workers, segments;   // workgroups that go over the work; those that zero a row each, 0: the workers do
+  float* partial;
+  void* table;
+};
+// Sums of a lane: a 16-byte vector of the table (VEC), so that a wave's stores follow each other (two vectors of fp32 from one of 16
+// bits, stored 32 bytes apart: 2 TB/s).
+template <int DT, int OUT, bool VEC> struct ColumnSums {
+  static constexpr int E = VEC ? Storage<OUT>::kPerVec : 1, kBlock = kWave * E;
+  struct Raw {
+    uint32_t w[(E * Storage<DT>::kBytes + 3) / 4];
+  };
+  __device__ __forceinline__ static Raw load(const EmbedSums& a, int token, int c) {
+    const char* const at = row_ptr<DT>(a.dout, token, a.ld, c);
+    Raw r;
+    if constexpr (!VEC) r.w[0] = load_raw<DT>(at, 0);
+    else if constexpr (sizeof(Raw) == 8) {
+      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+      const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(at));
+      r.w[0] = v.x; r.w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int k = 0; k < int(sizeof(Raw)) / 16; ++k) {
+        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(at) + k);
+        r.w[4 * k] = v.x; r.w[4 * k + 1] = v.y; r.w[4 * k + 2] = v.z; r.w[4 * k + 3] = v.w;
+      }
+    }
+    return r;
+  }
+  __device__ __forceinline__ static float elt(const Raw& r, int e) {
+    if constexpr (Storage<DT>::kBytes == 4) return __uint_as_float(r.w[e]);
+    else return widen<DT>(e % 2 ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xffffu);
+  }
+  // R rows, of which `count` are there, C column blocks, all asked for before any is used
+  template <int R, int C>
+  __device__ __forceinline__ static void add(const EmbedSums& a, const int (&token)[R], int count, int c0, float (&sum)[C][E]) {
+    Raw v[C][R];
+#pragma unroll
+    for (int b = 0; b < C; ++b)
+#pragma unroll
+      for (int k = 0; k < R; ++k) v[b][k] = load(a, token[k], min(c0 + b * kBlock, a.H - E));   // H is a multiple of E
+#pragma unroll
+    for (int b = 0; b < C; ++b)
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (k < count) {   // uniform
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[b][e] += elt(v[b][k], e);
+        }
+  }
+  // the whole row of an id with R tokens
+  template <int R, int C> __device__ __forceinline__ static void row(const EmbedSums& a, const Piece& p, int own) {
+    int token[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) token[k] = __builtin_amdgcn_readlane(own, k);
+    for (int c0 = threadIdx.x % kWave * E; c0 < a.H; c0 += C * kBlock) {
+      float sum[C][E] = {};
+      add<R, C>(a, token, R, c0, sum);
+#pragma unroll
+      for (int b = 0; b < C; ++b)
+        if (c0 + b * kBlock < a.H) put_sums<OUT, E>(row_ptr<OUT>(a.table, p.id, a.H, c0 + b * kBlock), sum[b], a.scale, a.accumulate != 0);
+    }
+  }
+};
+
+template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT) void k_embed_sum(EmbedSums a) {
+  using Sums = ColumnSums<DT, OUT, VEC>;
+  constexpr int E = Sums::E;
+  extern __shared__ int s_end[];   // [owners]
+  __shared__ int s_wave[kSumWaves];
+  const int lane = threadIdx.x % kWave;
+  if (int(blockIdx.x) >= a.workers) {   // a row, or a segment of one
+    const uint32_t b = blockIdx.x - uint32_t(a.workers), id = b / uint32_t(a.segments), i = b % uint32_t(a.segments) * kSumNT + threadIdx.x;
+    const u32x4_t zero = {0u, 0u, 0u, 0u};
+    if (!a.there[id] && i < uint32_t(a.H) / Storage<OUT>::kPerVec)
+      __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_t*>(row_ptr<OUT>(a.table, id, a.H)) + i);
+    return;
+  }
+  const int first = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kSumWaves + int(threadIdx.x) / kWave), waves = a.workers * kSumWaves;
+  // ---- pieces of frequent ids, by column blocks ----
+  const int blocks = (a.H + Sums::kBlock - 1) / Sums::kBlock;
+  int64_t units = int64_t(scan_owners(a.n.heavy, a.owners, s_end, s_wave, 1)) * blocks;
+  for (int64_t u = first; u < units; u += waves) {
+    int k;
+    const int g = find_owner(s_end, a.owners, int(u / blocks), k);
+    const Piece p = a.piece[a.n.base[g] + k];
+    const int own = lane < p.count ? a.order[p.start + lane] : 0;   // lane k: the piece's k-th token
+    const int c = int(u % blocks) * Sums::kBlock + lane * E;
+    float sum[1][E] = {};
+    constexpr int R = 8;
+    for (int k0 = 0; k0 < p.count; k0 += R) {
+      int token[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) token[r] = __builtin_amdgcn_readlane(own, min(k0 + r, p.count - 1));
+      Sums::template add<R, 1>(a, token, p.count - k0, c, sum);
+    }
+    if (c < a.H) {
+      if (p.row < 0) {
+        put_sums<OUT, E>(row_ptr<OUT>(a.table, p.id, a.H, c), sum[0], a.scale, a.accumulate != 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) a.partial[size_t(p.row) * a.H + c + e] = sum[0][e];
+      }
+    }
+  }
+  // ---- whole rows of the others ----
+  units = scan_owners(a.n.few, a.owners, s_end, s_wave, 1);
+  for (int64_t u = first; u < units; u += waves) {
+    int k;
+    const int g = find_owner(s_end, a.owners, int(u), k);
+    const Piece p = a.piece[a.n.end[g] - 1 - k];
+    const int own = lane < p.count ? a.order[p.start + lane] : 0;
+    static_assert(kFew == 4, "cases below");
+    switch (p.count) {   // uniform
+      case 1: Sums::template row<1, 8>(a, p, own); break;
+      case 2: Sums::template row<2, 4>(a, p, own); break;
+      case 3: Sums::template row<3, 4>(a, p, own); break;
+      default: Sums::template row<4, 4>(a, p, own);
+    }
+  }
+  if (a.accumulate || a.segments) return;   // uniform
+  // ---- zeros ----
+  units = scan_owners(a.n.none, a.owners, s_end, s_wave, kZeroRows);
+  for (int64_t u = first; u < units; u += waves) {
+    int k;
+    const int g = find_owner(s_end, a.owners, int(u), k);
+    const int n = min(a.n.none[g] - k * kZeroRows, kZeroRows);
+    const int id = lane < n ? a.none[int64_t(g) * kBins + k * kZeroRows + lane] : 0;
+    for (int r = 0; r < n; ++r) {
+      const int64_t at = __builtin_amdgcn_readlane(id, r);
+      char* const row = row_ptr<OUT>(a.table, at, a.H);
+      const RowGeom geom = row_geom<OUT>(a.table, at, a.H, a.H);
       const u32x4_t zero = {0u, 0u, 0u, 0u};
       for (int i = lane; i < geom.nvec; i += kWave)
         __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_t*>(row + geom.head * Storage<OUT>::kBytes) + i);
-      const int j = ragged_elt<OUT>(geom, H, lane);
+      const int j = ragged_elt<OUT>(geom, a.H, lane);
       if (j >= 0) store_elt<OUT>(row, j, 0.f);
-    }
-    return;
-  }
-  const int64_t slot = int64_t(blockIdx.x) * kSumWaves + wave;
-  if (slot >= T) return;
-  const int count = pieces[slot].count;
-  if (count == 0) return;
-  const Piece p = pieces[slot];
-  const int own = lane < kPiece && lane < count ? order[p.start + lane] : 0;   // lane k: the piece's k-th token
-  for (int c = (blockIdx.y * kWave + lane) * E; c < H; c += gridDim.y * kWave * E) {
-    float sum[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0.f;
-    for (int k0 = 0; k0 < count; k0 += kRowsAhead) {
-      float x[kRowsAhead][E];
-      u32x4_t v[kRowsAhead];
-#pragma unroll
-      for (int k = 0; k < kRowsAhead; ++k) {
-        const char* const row = row_ptr<DT>(dout, __builtin_amdgcn_readlane(own, min(k0 + k, count - 1)), ld, c);
-        if constexpr (VEC) v[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row));
-        else x[k][0] = load_elt<DT>(row, 0);
-      }
-#pragma unroll
-      for (int k = 0; k < kRowsAhead; ++k) {
-        if constexpr (VEC) unpack_vec<DT>(v[k], x[k]);
-        if (k0 + k < count) {   // uniform
-#pragma unroll
-          for (int e = 0; e < E; ++e) sum[e] += x[k][e];
-        }
-      }
-    }
-    if (p.part == 0) {
-      put_sums<OUT, E>(row_ptr<OUT>(table, p.id, H, c), sum, scale, accumulate != 0);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) partial[size_t(p.row) * H + c + e] = sum[e];
     }
   }
 }
 
-// Workgroup (unit, column block): the id with several pieces whose tokens start in the unit's kPiece sorted positions (at most one
-// does: it has more tokens than the unit has positions).
+// Ids with several pieces: workgroup by (id, kSumNT columns).
 template <int OUT>
-__global__ __launch_bounds__(kSumNT) void k_embed_join(int64_t T, int H, const Piece* __restrict__ pieces, float scale, int accumulate,
-                                                       const float* __restrict__ partial, void* __restrict__ table) {
-  static_assert(kPiece <= kWave, "a lane per position");
-  const int lane = threadIdx.x % kWave;
-  const int64_t slot = int64_t(blockIdx.x) * kPiece + lane;
-  const bool head = lane < kPiece && slot < T && pieces[slot].count > 0 && pieces[slot].part == 1;
-  const uint64_t first = __builtin_amdgcn_ballot_w64(head);
-  if (!first) return;
-  const Piece p = pieces[int64_t(blockIdx.x) * kPiece + __builtin_ctzll(first)];
-  const int np = (p.whole + kPiece - 1) / kPiece;
-  for (int c = blockIdx.y * kSumNT + threadIdx.x; c < H; c += gridDim.y * kSumNT) {
+__global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a, const Whole* __restrict__ wholes) {
+  extern __shared__ int s_end[];   // [owners]
+  __shared__ int s_wave[kSumWaves];
+  const int blocks = (a.H + kSumNT - 1) / kSumNT;
+  const int64_t units = int64_t(scan_owners(a.n.whole, a.owners, s_end, s_wave, 1)) * blocks;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    int k;
+    const int g = find_owner(s_end, a.owners, int(u / blocks), k);
+    const Whole w = wholes[a.n.base[g] + k];
+    const int c = int(u % blocks) * kSumNT + threadIdx.x;
+    if (c >= a.H) continue;
+    const float* const x = a.partial + size_t(w.row) * a.H + c;
     float sum[1] = {0.f};
-    int k = 0;
-    for (; k + 8 <= np; k += 8) {
-      float x[8];
+    int r = 0;
+    for (; r + 8 <= w.pieces; r += 8) {
+      float y[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = partial[size_t(p.row + k + u) * H + c];
+      for (int e = 0; e < 8; ++e) y[e] = x[size_t(r + e) * a.H];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum[0] += x[u];
+      for (int e = 0; e < 8; ++e) sum[0] += y[e];
     }
-    for (; k < np; ++k) sum[0] += partial[size_t(p.row + k) * H + c];
-    put_sums<OUT, 1>(row_ptr<OUT>(table, p.id, H, c), sum, scale, accumulate != 0);
+    for (; r < w.pieces; ++r) sum[0] += x[size_t(r) * a.H];
+    put_sums<OUT, 1>(row_ptr<OUT>(a.table, w.id, a.H, c), sum, a.scale, a.accumulate != 0);
   }
 }
 
@@ -358,21 +539,23 @@ struct EmbedArgs {
 template <int DT, int OUT> static void embed_bwd_launch(const EmbedArgs& a, void* workspace, hipStream_t s) {
   const EmbedWorkspace w = embed_workspace(workspace, a.T, a.V, a.H);
   const int owners = embed_owners(a.V), log_owners = __builtin_ctz(unsigned(owners));
-  hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.order, w.piece, w.empty,
-                     w.n_empty, a.err_flag);
-  constexpr int E = Storage<DT>::kPerVec;
-  const bool vec = a.H % E == 0 && a.ld % E == 0 && reinterpret_cast<uintptr_t>(a.dout) % 16 == 0 &&
-                   a.H % Storage<OUT>::kPerVec == 0 && reinterpret_cast<uintptr_t>(a.table) % 16 == 0;
-  const int per_wave = kWave * (vec ? E : 1);
-  const int columns = std::min(8, (a.H + per_wave - 1) / per_wave), n_sum = int((a.T + kSumWaves - 1) / kSumWaves);
-  const int fill = a.accumulate ? 0 : (owners * kFillParts + columns - 1) / columns;
+  hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.order, w.piece, w.whole,
+                     w.none, w.there, w.n, a.err_flag);
+  // a vector of the table and the same columns of dout, as 8, 16 or 32 bytes
+  constexpr int E = Storage<OUT>::kPerVec, kLoad = E * Storage<DT>::kBytes < 16 ? E * Storage<DT>::kBytes : 16;
+  const bool vec = a.H % E == 0 && reinterpret_cast<uintptr_t>(a.table) % 16 == 0 && a.ld * Storage<DT>::kBytes % kLoad == 0 &&
+                   reinterpret_cast<uintptr_t>(a.dout) % kLoad == 0;
+  const int64_t segments = (int64_t(a.H) / E + kSumNT - 1) / kSumNT;
+  const bool by_address = !a.accumulate && a.H % E == 0 && reinterpret_cast<uintptr_t>(a.table) % 16 == 0 &&
+                          grid_fits(a.V * segments + 8 * compute_units(), kSumNT);
+  const int workers = (by_address ? 4 : 8) * compute_units();   // 32768 tokens of width 3584, 2 / 4 / 6 / 8 to a CU: 142 / 127 / 130 / 133 us
+  const EmbedSums sums{a.dout, a.ld, a.H, owners, w.order, w.piece, w.none, w.there, w.n, a.scale, a.accumulate, workers,
+                       by_address ? int(segments) : 0, w.partial, a.table};
   const auto sum = vec ? k_embed_sum<DT, OUT, true> : k_embed_sum<DT, OUT, false>;
-  if (n_sum + fill > 0)
-    hipLaunchKernelGGL(sum, dim3(unsigned(n_sum + fill), unsigned(columns)), dim3(kSumNT), 0, s, a.dout, a.ld, a.H, a.T, n_sum, owners, w.order,
-                       w.piece, w.empty, w.n_empty, a.scale, a.accumulate, w.partial, a.table);
+  const size_t lds = size_t(owners) * 4;   // at most 64 KB
+  hipLaunchKernelGGL(sum, dim3(unsigned(workers + (by_address ? a.V * segments : 0))), dim3(kSumNT), lds, s, sums);
   if (a.T > kPiece)
-    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned((a.T + kPiece - 1) / kPiece), unsigned(std::min(8, (a.H + kSumNT - 1) / kSumNT))),
-                       dim3(kSumNT), 0, s, a.T, a.H, w.piece, a.scale, a.accumulate, w.partial, a.table);
+    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(4 * compute_units())), dim3(kSumNT), lds, s, sums, w.whole);
 }
 
 template <int DT>
@@ -385,6 +568,7 @@ static void embed_fwd_launch(const void* table, int V, int H, const int32_t* ids
 }
 
 constexpr int kMaxWidth = 1 << 20;
+
 
 }  // namespace aero
 

@@ -82,11 +82,17 @@ decltype(&aero_logprob_fwd) g_logprob_fwd = nullptr;
 decltype(&aero_grpo_loss_bwd) g_loss_bwd = nullptr;
 decltype(&aero_grpo_loss_bwd_noalloc) g_loss_bwd_noalloc = nullptr;
 decltype(&aero_lmhead_logprob_fused) g_fused = nullptr;
+decltype(&aero_topk_logprob) g_topk = nullptr;
+decltype(&aero_distill_loss_bwd) g_distill = nullptr;
+decltype(&aero_verify_draft) g_verify = nullptr;
+decltype(&aero_embedding_fwd) g_embed_fwd = nullptr;
+decltype(&aero_embedding_bwd) g_embed_bwd = nullptr;
 
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *stream, *params;
-  unsigned long long f[5];
-  if (!PyArg_ParseTuple(args, "OOKKKKK", &stream, &params, &f[0], &f[1], &f[2], &f[3], &f[4])) return nullptr;
+  unsigned long long f[10];
+  if (!PyArg_ParseTuple(args, "OOKKKKKKKKKK", &stream, &params, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9]))
+    return nullptr;
   Py_INCREF(stream);
   Py_INCREF(params);
   Py_XSETREF(g_stream, stream);
@@ -96,6 +102,11 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_loss_bwd = reinterpret_cast<decltype(g_loss_bwd)>(f[2]);
   g_loss_bwd_noalloc = reinterpret_cast<decltype(g_loss_bwd_noalloc)>(f[3]);
   g_fused = reinterpret_cast<decltype(g_fused)>(f[4]);
+  g_topk = reinterpret_cast<decltype(g_topk)>(f[5]);
+  g_distill = reinterpret_cast<decltype(g_distill)>(f[6]);
+  g_verify = reinterpret_cast<decltype(g_verify)>(f[7]);
+  g_embed_fwd = reinterpret_cast<decltype(g_embed_fwd)>(f[8]);
+  g_embed_bwd = reinterpret_cast<decltype(g_embed_bwd)>(f[9]);
   Py_RETURN_NONE;
 }
 
@@ -318,18 +329,160 @@ PyObject* fused(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// topk(logits, T, V, ld, row_active, K, index, logprob, lse, workspace)
+PyObject* topk(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 10 || !g_topk) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const at::Tensor* on = peek(*p.next);
+  const void* logits = p.any();
+  const int32_t dtype = on ? dtype_code(*on) : -1;
+  if (dtype < 0) p.ok = false;
+  const int64_t T = p.int64();
+  const int32_t V = p.int32();
+  const int64_t ld = p.int64();
+  const uint8_t* active = p.u8();
+  const int32_t K = p.int32();
+  int32_t* index = p.i32();
+  float *logprob = p.f32(), *lse = p.f32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) { return g_topk(logits, dtype, T, V, ld, active, K, index, logprob, lse, ws, bytes, s); });
+  END_HANDLE_TH_ERRORS
+}
+
+// distill(logits, T, V, ld, teacher_index, teacher_logprob, K, token_weight, tail, grad_scale, loss, row_loss, dlogits, err_flag, workspace)
+PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 15 || !g_distill) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const at::Tensor* on = peek(*p.next);
+  const void* logits = p.any();
+  const int32_t dtype = on ? dtype_code(*on) : -1;
+  if (dtype < 0) p.ok = false;
+  const int64_t T = p.int64();
+  const int32_t V = p.int32();
+  const int64_t ld = p.int64();
+  const int32_t* index = p.i32();
+  const float* logprob = p.f32();
+  const int32_t K = p.int32();
+  const float* weight = p.f32();
+  const int32_t tail = p.int32();
+  const float scale = p.real();
+  float *loss = p.f32(), *row_loss = p.f32();
+  const at::Tensor* d = peek(*p.next);
+  void* dlogits = p.any();
+  if (d && on && d->scalar_type() != on->scalar_type()) p.ok = false;
+  int32_t* err = p.i32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) {
+    return g_distill(logits, dtype, T, V, ld, index, logprob, K, weight, tail, scale, loss, row_loss, dlogits, err, ws, bytes, s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// verify(target_logits, draft_logits, B, G, V, ld, draft_tokens, draft_count, uniform, noise, accepted, tokens, logprob, err_flag, workspace)
+PyObject* verify(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 15 || !g_verify) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const at::Tensor* on = peek(*p.next);
+  const void* target = p.any();
+  const int32_t dtype = on ? dtype_code(*on) : -1;
+  if (dtype < 0) p.ok = false;
+  const at::Tensor* d = peek(*p.next);
+  const void* draft = p.any();
+  if (d && on && d->scalar_type() != on->scalar_type()) p.ok = false;
+  const int32_t B = p.int32(), G = p.int32(), V = p.int32();
+  const int64_t ld = p.int64();
+  const int32_t *drafted = p.i32(), *count = p.i32();
+  const float *uniform = p.f32(), *noise = p.f32();
+  int32_t *accepted = p.i32(), *tokens = p.i32();
+  float* logprob = p.f32();
+  int32_t* err = p.i32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) {
+    return g_verify(target, draft, dtype, B, G, V, ld, drafted, count, uniform, noise, accepted, tokens, logprob, err, ws, bytes, s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// embed_fwd(table, V, H, ids, T, scale, out, ld_out, err_flag)
+PyObject* embed_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 9 || !g_embed_fwd) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const at::Tensor* on = peek(*p.next);
+  const void* table = p.any();
+  const int32_t dtype = on ? dtype_code(*on) : -1;
+  if (dtype < 0) p.ok = false;
+  const int32_t V = p.int32(), H = p.int32();
+  const int32_t* ids = p.i32();
+  const int64_t T = p.int64();
+  const float scale = p.real();
+  const at::Tensor* o = peek(*p.next);
+  void* out = p.any();
+  if (o && on && o->scalar_type() != on->scalar_type()) p.ok = false;
+  const int64_t ld = p.int64();
+  int32_t* err = p.i32();
+  return finish(p, on, [&](void* s) { return g_embed_fwd(table, dtype, V, H, ids, T, scale, out, ld, err, s); });
+  END_HANDLE_TH_ERRORS
+}
+
+// embed_bwd(dout, T, H, ld_dout, ids, V, scale, dtable, accumulate, err_flag, workspace)
+PyObject* embed_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 11 || !g_embed_bwd) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const at::Tensor* on = peek(*p.next);
+  const void* dout = p.any();
+  const int32_t dtype = on ? dtype_code(*on) : -1;
+  if (dtype < 0) p.ok = false;
+  const int64_t T = p.int64();
+  const int32_t H = p.int32();
+  const int64_t ld = p.int64();
+  const int32_t* ids = p.i32();
+  const int32_t V = p.int32();
+  const float scale = p.real();
+  const at::Tensor* t = peek(*p.next);
+  void* table = p.any();
+  int32_t out_dtype = t ? dtype_code(*t) : -1;
+  if (out_dtype < 0) p.ok = false;
+  PyObject* accumulate = *p.next++;
+  if (accumulate == Py_True) out_dtype |= AERO_DW_ACCUMULATE;
+  else if (accumulate != Py_False) p.ok = false;
+  int32_t* err = p.i32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) {
+    return g_embed_bwd(dout, dtype, T, H, ld, ids, V, scale, table, out_dtype, err, ws, bytes, s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> constexpr PyCFunction fast() {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F));
 }
 
 PyMethodDef methods[] = {
     {"setup", setup, METH_VARARGS, "setup(error class, pointer function for other kinds of tensors)"},
-    {"bind", bind, METH_VARARGS, "bind(raw stream function, parameter class, five entry points' addresses)"},
+    {"bind", bind, METH_VARARGS, "bind(raw stream function, parameter class, ten entry points' addresses)"},
     {"pointers", fast<pointers>(), METH_FASTCALL, "pointers(t0, dtype0, name0, ...) -> tuple of addresses"},
     {"group_advantage", fast<group_advantage>(), METH_FASTCALL, "status, or NotImplemented"},
     {"logprob_fwd", fast<logprob_fwd>(), METH_FASTCALL, "status, or NotImplemented"},
     {"loss_bwd", fast<loss_bwd>(), METH_FASTCALL, "status, or NotImplemented"},
     {"fused", fast<fused>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"topk", fast<topk>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"distill", fast<distill>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"verify", fast<verify>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"embed_fwd", fast<embed_fwd>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"embed_bwd", fast<embed_bwd>(), METH_FASTCALL, "status, or NotImplemented"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
