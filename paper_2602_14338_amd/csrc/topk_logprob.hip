@@ -1,11 +1,11 @@
 // The K largest logits of each row with their log-probs, and the row's log-partition, in one pass over the row.
 //
 // While the row streams by, each thread notes the largest logit of every group of kGroup of its vectors in LDS (the maximum of a
-// vector is formed for the running offset anyway): 152K logits of 16 bits leave 4.7K numbers.  A threshold that at least K
-// logits reach follows from the threads' own maxima: each wave removes its lanes' largest ceil(K / waves) times over, and the least of what
-// the waves removed last is it.  Groups that reach it, about twice K, are read again, all at once and out of the caches, and
-// what reaches it among their logits are the candidates.  A candidate's rank is the count of larger ones; pairs of value and id are
-// distinct, so the order is total and ties go to the lower id.
+// vector is formed for the running offset anyway), 16 bits of its order: 152K logits of 16 bits leave 9.5K numbers.  A threshold that at least
+// K logits reach follows from the threads' own maxima: it is the least of the waves' ceil(K / waves)-th largest ones.  Groups that
+// reach it, about twice K, are read again, all at once and out of the caches, and what reaches it among their logits are the
+// candidates.  A candidate's rank is the count of larger ones; pairs of value and id are distinct, so the order is total and ties
+// go to the lower id.
 // (Comparing every vector with a threshold from the row's first vectors instead: 900 candidates, a branch in nearly every step of a
 // wave, 3.4 times the time of the whole call at 4096 x 151936 bf16.)
 // Rows with more candidates than fit (thousands of equal logits at the threshold) are selected digit by digit over their keys, nine more passes.
@@ -15,49 +15,46 @@
 
 namespace aero {
 
-constexpr int kGroup = 4;            // vectors in flight per thread, and of a group
-constexpr int kGroupMax = 5120;      // maxima that are noted; longer rows note one for several groups
-constexpr int kCandidates = 1792, kHits = 2048;
+constexpr int kGroup = 2, kAhead = 4;   // vectors of a group, groups in flight per thread
+constexpr int kGroupMax = 10240;      // maxima that are noted; longer rows note one for several groups
+constexpr int kCandidates = 1792, kHits = 1024;
+
+// The order of floats as that of whole numbers; -0 and 0 are the same.
+__device__ __forceinline__ uint32_t float_order(float z) {
+  const uint32_t u = __float_as_uint(z + 0.f);
+  return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float order_float(uint32_t ord) { return __uint_as_float(ord & 0x80000000u ? ord ^ 0x80000000u : ~ord); }
 
 // (value, id) as a number that grows with the value and falls with the id; 0: masked or NaN.
 __device__ __forceinline__ uint64_t top_key(float z, int j) {
   if (!(z > kMasked)) return 0;
-  const uint32_t u = __float_as_uint(z + 0.f);   // -0 and 0 are the same logit
-  const uint32_t ord = u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
-  return (uint64_t(ord) << 32) | uint32_t(~j);
+  return (uint64_t(float_order(z)) << 32) | uint32_t(~j);
 }
-__device__ __forceinline__ float key_logit(uint64_t key) {
-  const uint32_t ord = uint32_t(key >> 32);
-  return __uint_as_float(ord & 0x80000000u ? ord ^ 0x80000000u : ~ord);
-}
+__device__ __forceinline__ float key_logit(uint64_t key) { return order_float(uint32_t(key >> 32)); }
 __device__ __forceinline__ int key_id(uint64_t key) { return int(~uint32_t(key)); }
 
-// A lower bound on the K-th largest logit of the workgroup, from the threads' largest ones (-inf: none); -inf where the
-// threads cannot give one.
-template <int NT> __device__ float top_threshold(float z, int K, float* lds /*[NT/64]*/) {
-  constexpr int kWaves = NT / kWave;
-  const int lane = threadIdx.x % kWave;
-  const int r = (K + kWaves - 1) / kWaves;
-  float least = -INFINITY;
-  if (r <= kWave) {
-    for (int k = 0; k < r; ++k) {   // uniform
-      least = wave_reduce(z, [](float a, float b) { return fmaxf(a, b); });
-      const uint64_t with = __builtin_amdgcn_ballot_w64(z == least);
-      if (with && lane == __builtin_ctzll(with)) z = -INFINITY;
-    }
-  }
-  if (lane == 0) lds[threadIdx.x / kWave] = least;
-  __syncthreads();
-  least = lds[0];
+// A lower bound on the wave's r-th largest of z (-inf: none), -inf where it has none.  Digits of three bits, from the count of lanes that
+// reach a number, the seven of a digit at a time; 18 bits tell all 16- and 8-bit logits apart and leave a bound for the others.
+__device__ __forceinline__ float wave_threshold(float z, int r) {
+  if (r > kWave) return -INFINITY;   // uniform
+  const uint32_t ord = float_order(z);
+  uint32_t reached = 0;
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) least = fminf(least, lds[w]);
-  return least;
+  for (int shift = 29; shift >= 14; shift -= 3) {
+    uint32_t digit = 0;
+#pragma unroll
+    for (uint32_t d = 1; d < 8; ++d) digit += __popcll(__builtin_amdgcn_ballot_w64(ord >= (reached | d << shift))) >= r;
+    reached |= digit << shift;
+  }
+  const float least = order_float(reached);   // without a logit: at or below -inf's bits
+  return least > kMasked ? least : -INFINITY;
 }
 
 struct TopBuffer {
   uint64_t key[kCandidates];
   union {
-    float group[kGroupMax];
+    __align__(16) uint16_t group[kGroupMax];
     uint32_t hist[256];
   };
   uint16_t hit[kHits];
@@ -112,14 +109,22 @@ __device__ __attribute__((noinline)) void top_by_digits(const RowView<DT, VEC>& 
   __syncthreads();
 }
 
-// Ranks of the buffer's keys; put(rank, key) for the K first.
+// Ranks of the buffer's keys; put(rank, key) for the K first.  As many threads share a key as there are for each.
 template <int NT, class Put> __device__ __forceinline__ void top_rank(const TopBuffer& b, int n, int K, Put put) {
-  for (int i = threadIdx.x; i < n; i += NT) {
-    const uint64_t key = b.key[i];
+  int share = 1;
+  while (share < 16 && 2 * share * n <= NT) share *= 2;   // uniform; threads that share a key are in one row of 16 lanes
+  const int sub = threadIdx.x % share;
+  for (int i0 = 0; i0 < n; i0 += NT / share) {
+    const int i = i0 + threadIdx.x / share;
+    const uint64_t key = i < n ? b.key[i] : ~uint64_t(0);
     int above = 0;
-#pragma unroll 8
-    for (int k = 0; k < n; ++k) above += b.key[k] > key;
-    if (above < K) put(above, key);
+#pragma unroll 4
+    for (int k = sub; k < n; k += share) above += b.key[k] > key;
+    if (share > 1) above += dpp_move_i<0xB1>(above);
+    if (share > 2) above += dpp_move_i<0x4E>(above);
+    if (share > 4) above += dpp_move_i<0x141>(above);   // the mirrors stand for exchanges at distance 4 and 8
+    if (share > 8) above += dpp_move_i<0x140>(above);
+    if (sub == 0 && i < n && above < K) put(above, key);
   }
 }
 
@@ -132,6 +137,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   constexpr int E = RowView<DT, VEC>::E, kWaves = NT / kWave;
   __shared__ TopBuffer buf;
   __shared__ float s_least[kWaves];
+  __shared__ int s_above[kWaves];
   __shared__ SoftSum s_sum[kWaves];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, parts = gridDim.y, part = blockIdx.y;
@@ -152,6 +158,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
     buf.count = 0;
     buf.hits = 0;
   }
+  if (tid < kWaves) s_above[tid] = 0;
   const int steps = (last - first + kGroup * NT - 1) / (kGroup * NT);          // of the workgroup
   const int fold = (steps * NT + kGroupMax - 1) / kGroupMax;                   // steps that share a maximum
   const int jr = part == 0 ? row.ragged() : -1;
@@ -159,63 +166,108 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   SoftSum st = soft_identity();
   float best = -INFINITY, noted = -INFINITY;
   int i = first + tid;
-  for (int step = 0, kept = 0; step < steps; ++step, i += kGroup * NT) {
-    u32x4_t v[kGroup];
-    if (i + (kGroup - 1) * NT < last) {
-#pragma unroll
-      for (int u = 0; u < kGroup; ++u) v[u] = row.load(i + u * NT);
-#pragma unroll
-      for (int u = 0; u < kGroup; ++u) {
-        float z[E];
-        row.unpack(v[u], z);
-        const float vm = vec_max<E>(z);
-        soft_update<E>(st, z, vm);
-        noted = fmaxf(noted, vm);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < kGroup; ++u)
-        if (i + u * NT < last) {
-          float z[E];
-          row.unpack(row.load(i + u * NT), z);
-          const float vm = vec_max<E>(z);
-          soft_update<E>(st, z, vm);
-          noted = fmaxf(noted, vm);
-        }
-    }
+  int step = 0, kept = 0;
+  auto note = [&]() {   // the end of a step
     if (++kept == fold || step == steps - 1) {
-      buf.group[(step / fold) * NT + tid] = noted;
+      buf.group[(step / fold) * NT + tid] = uint16_t(float_order(noted) >> 16);
       best = fmaxf(best, noted);
       noted = -INFINITY;
       kept = 0;
     }
+    ++step;
+  };
+  auto take = [&](const u32x4_t& x) {
+    float z[E];
+    row.unpack(x, z);
+    const float vm = vec_max<E>(z);
+    soft_update<E>(st, z, vm);
+    noted = fmaxf(noted, vm);
+  };
+  for (; i + (kAhead * kGroup - 1) * NT < last; i += kAhead * kGroup * NT) {
+    u32x4_t v[kAhead * kGroup];
+#pragma unroll
+    for (int u = 0; u < kAhead * kGroup; ++u) v[u] = row.load(i + u * NT);
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) {
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) take(v[g * kGroup + u]);
+      note();
+    }
+  }
+  while (step < steps) {   // note() counts
+    u32x4_t v[kGroup];
+#pragma unroll
+    for (int u = 0; u < kGroup; ++u)
+      if (i + u * NT < last) v[u] = row.load(i + u * NT);
+#pragma unroll
+    for (int u = 0; u < kGroup; ++u)
+      if (i + u * NT < last) take(v[u]);
+    note();
+    i += kGroup * NT;
   }
   if (jr >= 0) {
     float z[1] = {zr};
     soft_update<1>(st, z);
     best = fmaxf(best, zr);
   }
-  const float least = top_threshold<NT>(best > kMasked ? best : -INFINITY, K, s_least);   // its barrier: buf.count, buf.hits
+  st = soft_reduce<true>(st);
+  const float own = wave_threshold(best > kMasked ? best : -INFINITY, (K + kWaves - 1) / kWaves);
+  if (tid % kWave == 0) {
+    s_sum[tid / kWave] = st;
+    s_least[tid / kWave] = own;
+  }
+  __syncthreads();
+  // the largest of the waves' bounds that K of the threads' maxima reach: the least one is, a larger one may be too
+  int above[kWaves];
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) above[w] = __popcll(__builtin_amdgcn_ballot_w64(best >= s_least[w]));
+  if (tid % kWave == 0) {
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) atomicAdd(&s_above[w], above[w]);
+  }
+  __syncthreads();
+  st = soft_reduce<false>(tid % 16 < kWaves ? s_sum[tid % 16] : soft_identity());
+  float least = s_least[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) least = fminf(least, s_least[w]);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) least = s_above[w] >= K ? fmaxf(least, s_least[w]) : least;
   auto reaches = [&](float z) { return z >= least && z > kMasked; };
   if (reaches(zr)) top_push(buf, top_key(zr, jr));
-  if (reaches(best))
-    for (int g = 0; g * fold < steps; ++g)
-      if (reaches(buf.group[g * NT + tid])) {
+  // ---- groups that reach the threshold, eight at a time ----
+  const uint32_t bound = float_order(fmaxf(least, kMasked)) >> 16;
+  const int groups = (steps + fold - 1) / max(fold, 1) * NT;
+  for (int k = 8 * tid; k < groups; k += 8 * NT) {
+    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(buf.group + k);
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if ((e % 2 ? word[e / 2] >> 16 : word[e / 2] & 0xffffu) >= bound) {
         const int at = atomicAdd(&buf.hits, 1);
-        if (at < kHits) buf.hit[at] = uint16_t(g * NT + tid);
+        if (at < kHits) buf.hit[at] = uint16_t(k + e);
       }
-  st = soft_block_reduce<NT>(st, s_sum);   // its barrier: the hits are complete
+  }
+  __syncthreads();
+  // ---- their logits ----
   const int hits = buf.hits, span = kGroup * fold;
   if (hits <= kHits)
-    for (int k = tid; k < hits * span; k += NT) {
-      const int slot = buf.hit[k / span];
-      const int vec = first + slot % NT + ((slot / NT) * span + k % span) * NT;
-      if (vec < last) {
+    for (int k0 = 0; k0 < hits * span; k0 += 4 * NT) {
+      u32x4_t v[4];
+      int vec[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = min(k0 + u * NT + tid, hits * span - 1), slot = buf.hit[k / span];
+        vec[u] = first + slot % NT + ((slot / NT) * span + k % span) * NT;
+        if (k0 + u * NT + tid >= hits * span || vec[u] >= last) vec[u] = -1;
+        v[u] = row.load_again(max(vec[u], 0));
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
         float z[E];
-        row.unpack(row.load_again(vec), z);
+        row.unpack(v[u], z);
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          if (reaches(z[e])) top_push(buf, top_key(z[e], row.column(vec) + e));
+          if (vec[u] >= 0 && reaches(z[e])) top_push(buf, top_key(z[e], row.column(vec[u]) + e));
       }
     }
   __syncthreads();
@@ -248,38 +300,39 @@ __global__ __launch_bounds__(kJoinNT) void k_topk_join(const uint8_t* __restrict
                                                        int32_t* __restrict__ index, float* __restrict__ logprob,
                                                        float* __restrict__ lse) {
   __shared__ uint64_t s_key[kMaxParts * AERO_TOPK_MAX];
+  __shared__ int s_n;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
   if (row_active && row_active[t] == 0) return;   // uniform; its outputs were written by its first part
   SoftSum st = soft_identity();
-  for (int p = 0; p < parts; ++p) st = soft_merge(st, part_sums[t * parts + p]);
+  if (tid % 16 < parts) st = part_sums[t * parts + tid % 16];
+  if (tid == 0) s_n = 0;
   for (int k = tid; k < parts * K; k += kJoinNT) s_key[k] = part_keys[t * parts * K + k];
+  st = soft_reduce<false>(st);   // over 16 lanes, the same in each row of them
   __syncthreads();
   const double z0 = soft_lse(st);
-  int mine = 0;
+  int mine = 0, top_step = 1;
+  while (2 * top_step <= K) top_step *= 2;
   for (int k = tid; k < parts * K; k += kJoinNT) {
     const uint64_t key = s_key[k];
     if (key == 0) continue;
     ++mine;
-    int rank = k % K;
-    for (int p = 0; p < parts && rank < K; ++p) {
-      if (p == k / K) continue;
-      int lo = 0, hi = K;   // entries [0, lo) are above the key, [hi, K) are not
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (s_key[p * K + mid] > key) lo = mid + 1;
-        else hi = mid;
-      }
-      rank += lo;
+    int before[kMaxParts] = {};   // entries of each list that are above the key
+    for (int step = top_step; step > 0; step /= 2) {   // all lists at a time: what is read is in LDS, and its latency counts
+      uint64_t x[kMaxParts];
+#pragma unroll
+      for (int p = 0; p < kMaxParts; ++p) x[p] = s_key[min(p, parts - 1) * K + min(before[p] + step, K) - 1];
+#pragma unroll
+      for (int p = 0; p < kMaxParts; ++p) before[p] += before[p] + step <= K && x[p] > key ? step : 0;
     }
+    int rank = 0;
+#pragma unroll
+    for (int p = 0; p < kMaxParts; ++p) rank += p < parts ? before[p] : 0;
     if (rank < K) {
       index[t * K + rank] = key_id(key);
       logprob[t * K + rank] = float(double(key_logit(key)) - z0);
     }
   }
-  __shared__ int s_n;
-  if (tid == 0) s_n = 0;
-  __syncthreads();
   if (mine) atomicAdd(&s_n, mine);
   __syncthreads();
   for (int k = s_n + tid; k < K; k += kJoinNT) {
@@ -289,15 +342,16 @@ __global__ __launch_bounds__(kJoinNT) void k_topk_join(const uint8_t* __restrict
   if (tid == 0 && lse) lse[t] = float(z0);
 }
 
-// Parts of a row.
+// Parts of a row: a workgroup per CU in all.  (151936 bf16, K = 64, one / two / four workgroups per CU: 64 rows 17.8 / 20.8 / 20.9 us,
+// 200 26.6 / 30.0 / 36.8, 300 28.8 / 37.4 / 38.8.)
 static int topk_parts(int64_t T, int nvec, int cus) {
-  if (T >= 2 * cus || nvec < 2 * kGroup * 256) return 1;
-  return int(std::min<int64_t>({kMaxParts, (2 * cus + T - 1) / T, nvec / (kGroup * 256)}));
+  if (T > cus / 2 || nvec < 2 * 4 * 256) return 1;
+  return int(std::min<int64_t>({kMaxParts, cus / T, nvec / (4 * 256)}));
 }
 
 size_t topk_workspace_bytes(int64_t T, int32_t V, int32_t K) {
   (void)V;
-  const int64_t rows = std::min<int64_t>(T, 2 * compute_units());   // more are not split
+  const int64_t rows = std::min<int64_t>(T, compute_units());   // more are not split
   return size_t(rows) * kMaxParts * (size_t(K > 0 ? K : 0) * 8 + sizeof(SoftSum)) + 256;
 }
 
@@ -310,10 +364,14 @@ static void topk_launch(const void* logits, int64_t T, int V, int64_t ld, const 
   uint64_t* keys = reinterpret_cast<uint64_t*>(sums + (parts > 1 ? T * parts : 0));
   const dim3 grid{unsigned(T), unsigned(parts)};
   const int per = (nvec + parts - 1) / parts;
-  if (per <= kGroup * 256)
-    hipLaunchKernelGGL((k_topk<256, DT, VEC>), grid, dim3(256), 0, s, logits, V, ld, row_active, K, index, logprob, lse, keys, sums);
-  else
-    hipLaunchKernelGGL((k_topk<512, DT, VEC>), grid, dim3(512), 0, s, logits, V, ld, row_active, K, index, logprob, lse, keys, sums);
+  // 512 / 1024 threads (151936 bf16): 200 rows, K = 16, 64, 256: 21.0 / 19.1, 22.1 / 19.7, 33.5 / 25.8 us; 64 rows split in four 16.2 / 18.3, 17.6 /
+  // 19.3, 32.5 / 28.9; 300 rows 27.8 / 37.3, 4096 242 / 316 at K = 64
+  auto launch = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, grid, dim3(unsigned(threads)), 0, s, logits, V, ld, row_active, K, index, logprob, lse, keys, sums);
+  };
+  if (per <= 4 * 256) launch(k_topk<256, DT, VEC>, 256);
+  else if (T * parts <= compute_units() && (parts == 1 || K > 128)) launch(k_topk<1024, DT, VEC>, 1024);
+  else launch(k_topk<512, DT, VEC>, 512);
   if (parts > 1)
     hipLaunchKernelGGL(k_topk_join, dim3(unsigned(T)), dim3(kJoinNT), 0, s, row_active, K, parts, keys, sums, index, logprob, lse);
 }
