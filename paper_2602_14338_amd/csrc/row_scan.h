@@ -38,7 +38,7 @@ template <int N> __device__ __forceinline__ float vec_max(const float (&z)[N]) {
 // The offset moves only for a logit more than 2^kAbove above it, so the rescaling is rare (the test in front and the side effect keep it a
 // branch, see stat_update).
 constexpr float kAbove = 17.f;
-template <int N> __device__ __forceinline__ void soft_update(SoftSum& st, const float (&z)[N], float vm) {
+__device__ __forceinline__ void soft_grow(SoftSum& st, float vm) {
   const bool grow = fmaf(vm, kLog2e, -st.o) > kAbove;
   if (__builtin_amdgcn_ballot_w64(grow) != 0) {
     asm volatile("" ::: "memory");
@@ -48,8 +48,14 @@ template <int N> __device__ __forceinline__ void soft_update(SoftSum& st, const 
       st.o = o;
     }
   }
+}
+template <int N> __device__ __forceinline__ void soft_add(SoftSum& st, const float (&z)[N]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) st.s += exp2_fast(fmaf(z[k], kLog2e, -st.o));
+}
+template <int N> __device__ __forceinline__ void soft_update(SoftSum& st, const float (&z)[N], float vm) {
+  soft_grow(st, vm);
+  soft_add<N>(st, z);
 }
 template <int N> __device__ __forceinline__ void soft_update(SoftSum& st, const float (&z)[N]) { soft_update<N>(st, z, vec_max<N>(z)); }
 

@@ -1,9 +1,9 @@
 // The K largest logits of each row with their log-probs, and the row's log-partition, in one pass over the row.
 //
-// While the row streams by, each thread notes the largest logit of every group of kGroup of its vectors in LDS (the maximum of a
-// vector is formed for the running offset anyway), 16 bits of its order: 152K logits of 16 bits leave 9.5K numbers.  A threshold that at least
-// K logits reach follows from the threads' own maxima: it is the least of the waves' ceil(K / waves)-th largest ones.  Groups that
-// reach it, about twice K, are read again, all at once and out of the caches, and what reaches it among their logits are the
+// While the row streams by, each thread notes the largest logit of every kGroup of its vectors in LDS, 16 bits of it (the maximum of a
+// vector is formed for the running offset anyway): 152K logits of 16 bits leave 9.5K numbers.  A threshold that at least
+// K logits reach follows from the threads' own maxima, joined into about 2 K of them: the K-th largest of these, found digit by digit by one wave.
+// Groups that reach it, little more than K, are read again, all at once and out of the caches, and what reaches it among their logits are the
 // candidates.  A candidate's rank is the count of larger ones; pairs of value and id are distinct, so the order is total and ties
 // go to the lower id.
 // (Comparing every vector with a threshold from the row's first vectors instead: 900 candidates, a branch in nearly every step of a
@@ -15,7 +15,7 @@
 
 namespace aero {
 
-constexpr int kGroup = 2, kAhead = 4;   // vectors of a group, groups in flight per thread
+constexpr int kGroup = 2, kAhead = 2;   // vectors of a group, groups of a batch
 constexpr int kGroupMax = 10240;      // maxima that are noted; longer rows note one for several groups
 constexpr int kCandidates = 1792, kHits = 1024;
 
@@ -34,27 +34,48 @@ __device__ __forceinline__ uint64_t top_key(float z, int j) {
 __device__ __forceinline__ float key_logit(uint64_t key) { return order_float(uint32_t(key >> 32)); }
 __device__ __forceinline__ int key_id(uint64_t key) { return int(~uint32_t(key)); }
 
-// A lower bound on the wave's r-th largest of z (-inf: none), -inf where it has none.  Digits of three bits, from the count of lanes that
-// reach a number, the seven of a digit at a time; 18 bits tell all 16- and 8-bit logits apart and leave a bound for the others.
-__device__ __forceinline__ float wave_threshold(float z, int r) {
-  if (r > kWave) return -INFINITY;   // uniform
-  const uint32_t ord = float_order(z);
+// A lower bound on the K-th largest of the NT numbers in `best` (-inf: none), -inf where there are no K of them; by one wave.  They are joined
+// into N x 64 maxima, K <= 32 N, of which at least as many reach it: for K = 64 joining 512 into 128 makes 89 of 68 candidates, and only
+// one wave counts (16 waves that each count their own lanes share the CU's one scalar unit: 6 times as long).  Digits of two bits, from the
+// counts of lanes that reach a number; 18 bits tell all 16- and 8-bit logits apart and leave a bound for the others.
+template <int NT, int N> __device__ __forceinline__ float top_threshold(const float* best, int K) {
+  constexpr int kJoined = NT / (kWave * N);
+  uint32_t ord[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float most = best[n * kWave + threadIdx.x];
+#pragma unroll
+    for (int j = 1; j < kJoined; ++j) most = fmaxf(most, best[(j * N + n) * kWave + threadIdx.x]);
+    ord[n] = float_order(most);
+  }
   uint32_t reached = 0;
 #pragma unroll
-  for (int shift = 29; shift >= 14; shift -= 3) {
+  for (int shift = 30; shift >= 14; shift -= 2) {
     uint32_t digit = 0;
 #pragma unroll
-    for (uint32_t d = 1; d < 8; ++d) digit += __popcll(__builtin_amdgcn_ballot_w64(ord >= (reached | d << shift))) >= r;
+    for (uint32_t d = 1; d < 4; ++d) {
+      int lanes = 0;
+#pragma unroll
+      for (int n = 0; n < N; ++n) lanes += __popcll(__builtin_amdgcn_ballot_w64(ord[n] >= (reached | d << shift)));
+      digit += lanes >= K;
+    }
     reached |= digit << shift;
   }
   const float least = order_float(reached);   // without a logit: at or below -inf's bits
   return least > kMasked ? least : -INFINITY;
 }
+template <int NT> __device__ __forceinline__ float top_threshold_of(const float* best, int K) {
+  constexpr int kMost = NT / kWave;
+  if (K <= 32) return top_threshold<NT, 1>(best, K);   // uniform
+  if (K <= 64) return top_threshold<NT, 2>(best, K);
+  if (K <= 128) return top_threshold<NT, 4>(best, K);
+  return top_threshold<NT, kMost < 8 ? kMost : 8>(best, K);
+}
 
 struct TopBuffer {
   uint64_t key[kCandidates];
   union {
-    __align__(16) uint16_t group[kGroupMax];
+    uint16_t group[kGroupMax];   // upper halves of the maxima
     uint32_t hist[256];
   };
   uint16_t hit[kHits];
@@ -66,9 +87,10 @@ __device__ __forceinline__ void top_push(TopBuffer& b, uint64_t key) {
   if (at < kCandidates) b.key[at] = key;
 }
 
-// Exactly the K largest keys of [first, last) of the row (fewer where fewer are unmasked), digit by digit.
+// Exactly the K largest keys of [first, last) of the row (fewer where fewer are unmasked), digit by digit.  In place: a call, rare as it
+// is, gives the kernel a stack, and a launch whose waves need one starts them so slowly that 4096 rows take 240 us for 200.
 template <int NT, int DT, bool VEC>
-__device__ __attribute__((noinline)) void top_by_digits(const RowView<DT, VEC>& row, int first, int last, int K, TopBuffer& b) {
+__device__ __forceinline__ void top_by_digits(const RowView<DT, VEC>& row, int first, int last, int K, TopBuffer& b) {
   constexpr int E = RowView<DT, VEC>::E;
   const int tid = threadIdx.x;
   const int jr = first == 0 ? row.ragged() : -1;
@@ -136,8 +158,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
                                              float* __restrict__ lse, uint64_t* __restrict__ part_keys, SoftSum* __restrict__ part_sums) {
   constexpr int E = RowView<DT, VEC>::E, kWaves = NT / kWave;
   __shared__ TopBuffer buf;
-  __shared__ float s_least[kWaves];
-  __shared__ int s_above[kWaves];
+  __shared__ float s_best[NT], s_least;
   __shared__ SoftSum s_sum[kWaves];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, parts = gridDim.y, part = blockIdx.y;
@@ -158,23 +179,23 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
     buf.count = 0;
     buf.hits = 0;
   }
-  if (tid < kWaves) s_above[tid] = 0;
   const int steps = (last - first + kGroup * NT - 1) / (kGroup * NT);          // of the workgroup
-  const int fold = (steps * NT + kGroupMax - 1) / kGroupMax;                   // steps that share a maximum
+  const int fold = max((steps * NT + kGroupMax - 1) / kGroupMax, 1);           // steps that share a maximum
   const int jr = part == 0 ? row.ragged() : -1;
   const float zr = jr >= 0 ? row.at(jr) : -INFINITY;
   SoftSum st = soft_identity();
   float best = -INFINITY, noted = -INFINITY;
   int i = first + tid;
-  int step = 0, kept = 0;
+  int step = 0, kept = 0, slot = tid;
   auto note = [&]() {   // the end of a step
-    if (++kept == fold || step == steps - 1) {
-      buf.group[(step / fold) * NT + tid] = uint16_t(float_order(noted) >> 16);
+    ++step;
+    if (++kept == fold || step == steps) {
+      buf.group[slot] = uint16_t(__float_as_uint(noted) >> 16);
+      slot += NT;
       best = fmaxf(best, noted);
       noted = -INFINITY;
       kept = 0;
     }
-    ++step;
   };
   auto take = [&](const u32x4_t& x) {
     float z[E];
@@ -183,14 +204,35 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
     soft_update<E>(st, z, vm);
     noted = fmaxf(noted, vm);
   };
-  for (; i + (kAhead * kGroup - 1) * NT < last; i += kAhead * kGroup * NT) {
-    u32x4_t v[kAhead * kGroup];
+  // batches of kAhead groups, the next one asked for before this one is used
+  constexpr int kBatch = kAhead * kGroup;
+  u32x4_t ahead[kBatch];
+  auto ask = [&](u32x4_t (&v)[kBatch]) {
 #pragma unroll
-    for (int u = 0; u < kAhead * kGroup; ++u) v[u] = row.load(i + u * NT);
+    for (int u = 0; u < kBatch; ++u) v[u] = row.load(i + u * NT);
+  };
+  bool more = i + (kBatch - 1) * NT < last;
+  if (more) ask(ahead);
+  while (more) {
+    u32x4_t v[kBatch];
 #pragma unroll
-    for (int g = 0; g < kAhead; ++g) {
+    for (int u = 0; u < kBatch; ++u) v[u] = ahead[u];
+    i += kBatch * NT;
+    more = i + (kBatch - 1) * NT < last;
+    if (more) ask(ahead);
 #pragma unroll
-      for (int u = 0; u < kGroup; ++u) take(v[g * kGroup + u]);
+    for (int g = 0; g < kAhead; ++g) {   // one test of the offset for a group
+      float z[kGroup * E];
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) {
+        float x[E];
+        row.unpack(v[g * kGroup + u], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[u * E + e] = x[e];
+      }
+      const float vm = vec_max<kGroup * E>(z);
+      soft_update<kGroup * E>(st, z, vm);
+      noted = fmaxf(noted, vm);
       note();
     }
   }
@@ -210,42 +252,34 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
     soft_update<1>(st, z);
     best = fmaxf(best, zr);
   }
-  st = soft_reduce<true>(st);
-  const float own = wave_threshold(best > kMasked ? best : -INFINITY, (K + kWaves - 1) / kWaves);
-  if (tid % kWave == 0) {
-    s_sum[tid / kWave] = st;
-    s_least[tid / kWave] = own;
+  s_best[tid] = best > kMasked ? best : -INFINITY;
+  st = soft_block_reduce<NT>(st, s_sum);   // its barrier: s_best
+  if (tid < kWave) {
+    const float reached = top_threshold_of<NT>(s_best, K);
+    if (tid == 0) s_least = reached;
   }
+  const double z0 = soft_lse(st);
   __syncthreads();
-  // the largest of the waves' bounds that K of the threads' maxima reach: the least one is, a larger one may be too
-  int above[kWaves];
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) above[w] = __popcll(__builtin_amdgcn_ballot_w64(best >= s_least[w]));
-  if (tid % kWave == 0) {
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) atomicAdd(&s_above[w], above[w]);
-  }
-  __syncthreads();
-  st = soft_reduce<false>(tid % 16 < kWaves ? s_sum[tid % 16] : soft_identity());
-  float least = s_least[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) least = fminf(least, s_least[w]);
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) least = s_above[w] >= K ? fmaxf(least, s_least[w]) : least;
+  const float least = s_least;
   auto reaches = [&](float z) { return z >= least && z > kMasked; };
   if (reaches(zr)) top_push(buf, top_key(zr, jr));
-  // ---- groups that reach the threshold, eight at a time ----
-  const uint32_t bound = float_order(fmaxf(least, kMasked)) >> 16;
-  const int groups = (steps + fold - 1) / max(fold, 1) * NT;
-  for (int k = 8 * tid; k < groups; k += 8 * NT) {
-    const u32x4_t w = *reinterpret_cast<const u32x4_t*>(buf.group + k);
-    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+  // ---- groups that reach the threshold: cutting off lower halves keeps the order ----
+  if (reaches(best)) {
+    const float bound = __uint_as_float(__float_as_uint(least) & 0xffff0000u);
+    const int groups = (steps + fold - 1) / fold;
+    for (int g0 = 0; g0 < groups; g0 += 4) {
+      uint32_t code[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if ((e % 2 ? word[e / 2] >> 16 : word[e / 2] & 0xffffu) >= bound) {
-        const int at = atomicAdd(&buf.hits, 1);
-        if (at < kHits) buf.hit[at] = uint16_t(k + e);
+      for (int u = 0; u < 4; ++u) code[u] = buf.group[min(g0 + u, groups - 1) * NT + tid];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float most = __uint_as_float(code[u] << 16);
+        if (g0 + u < groups && most >= bound && most > kMasked) {
+          const int at = atomicAdd(&buf.hits, 1);
+          if (at < kHits) buf.hit[at] = uint16_t((g0 + u) * NT + tid);
+        }
       }
+    }
   }
   __syncthreads();
   // ---- their logits ----
@@ -280,7 +314,6 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
     if (tid == 0) part_sums[t * parts + part] = st;
     return;
   }
-  const double z0 = soft_lse(st);
   top_rank<NT>(buf, n, K, [&](int r, uint64_t key) {
     index[t * K + r] = key_id(key);
     logprob[t * K + r] = float(double(key_logit(key)) - z0);
