@@ -1,17 +1,18 @@
 // Verification of drafted tokens against the policy's rows, from given random numbers.
 //
-// Three launches.  The first forms the running sums of every row that can matter (target rows up to the count of drafted tokens,
-// the draft rows in front of it), a row split over several workgroups.  The second finds, in every workgroup of a sequence
-// alike, the first position whose uniform number is not below p / q, and its slice of the vocabulary for the largest
-// max(0, p - q) / noise there.  The third joins a sequence's slices: the larger score, the lower id where equal, which does not depend on
-// their order.  (Joining in the second launch by atomics takes a device-wide fence per workgroup, 50 of 129 us for 128 sequences.)
+// The first launch forms the running sums of every row that can matter (target rows up to the count of drafted tokens,
+// the draft rows in front of it), a row split over several workgroups; with many sequences it also decides position by position, so that
+// rows behind a refusal are mostly left out.  The second finds the first position whose uniform number is not below p / q, and in every
+// slice of the vocabulary the largest max(0, p - q) / noise there.  The third joins a sequence's slices: the larger score, the lower id
+// where equal, which does not depend on their order.  (Joining in the second launch by atomics takes a device-wide fence per workgroup, 50 of 129
+// us for 128 sequences.)  Bound by the rows' and the noise's bytes.
 #include <algorithm>
 
 #include "row_scan.h"
 
 namespace aero {
 
-constexpr int kVerifyParts = 8;   // most parts of a row in the first launch
+constexpr int kVerifyParts = 8, kMaxSlices = 64;   // most parts of a row in the first launch, slices of a draw in the second
 
 struct VerifyArgs {
   const void *target, *draft;
@@ -26,6 +27,8 @@ struct VerifyArgs {
   SoftSum* sums;      // [B * (2 G + 1)][parts]: target rows, then draft rows
   uint64_t* best;     // [B][slices]: largest score and its id
   double* lse;        // [B]: of the row that is drawn from
+  int32_t* refused;   // [B]: first position known to be refused
+  double* lp;         // [B * (G + 1)]: ln p of a drafted token that was accepted, NaN of one that was refused
   int parts, slices;
 };
 
@@ -109,6 +112,86 @@ __device__ __forceinline__ SoftSum from_lane(SoftSum s, int lane) {
                  __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s.s), lane))};
 }
 
+// Is the drafted token accepted: u q < p, from ln p and ln(p / q).
+__device__ __forceinline__ bool accept(float u, double ratio) {
+  const float coarse = float(ratio);
+  const double fine = fabsf(coarse) < INFINITY ? 1.0 + (ratio - double(coarse)) : 1.0;
+  return double(u) < double(expf(coarse)) * fine;
+}
+
+// Many sequences: a workgroup per position, which goes over its target row and its draft row together and decides.  Positions
+// are the slow index of the grid, so that those behind a refused one, whose rows nobody needs, mostly find it refused when their turn comes; where they do
+// not, they are worked on for nothing.
+__global__ void k_verify_start(int32_t* refused, int B) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b < B) refused[b] = INT32_MAX;
+}
+template <int NT, int DT, bool VEC>
+__global__ __launch_bounds__(NT) void k_verify_positions(VerifyArgs a) {
+  using View = RowView<DT, VEC>;
+  constexpr int E = View::E, kAhead = 2;
+  __shared__ SoftSum s_sum[2][NT / kWave];
+  const int tid = threadIdx.x, i = blockIdx.x / a.B, b = blockIdx.x % a.B;
+  if (__hip_atomic_load(a.refused + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < i) return;   // uniform; an old value only costs time
+  int token;
+  int32_t flags;
+  const int n = drafted(a, b, tid % kWave, token, flags);
+  if (i > n) return;   // uniform
+  const int x = i < n ? __builtin_amdgcn_readlane(token, i) : 0;
+  const bool minus = a.draft && i < n;
+  const int64_t rt = int64_t(b) * (a.G + 1) + i, rd = int64_t(b) * a.G + min(i, a.G - 1), n_target = int64_t(a.B) * (a.G + 1);
+  const View prow(a.target, rt, a.ld, a.V), qrow(minus ? a.draft : a.target, minus ? rd : rt, a.ld, a.V);
+  const float zp = prow.at(x), zq = qrow.at(x), u = i < n ? a.uniform[rd] : 0.f;
+  SoftSum p = soft_identity(), q = soft_identity();
+  auto ragged = [&](const View& row, SoftSum& st) {
+    const int jr = row.ragged();
+    if (jr >= 0) {
+      float z[1] = {row.at(jr)};
+      soft_update<1>(st, z);
+    }
+  };
+  auto fold = [&](const u32x4_t& v, SoftSum& st) {
+    float z[E];
+    View::unpack(v, z);
+    soft_update<E>(st, z);
+  };
+  ragged(prow, p);
+  if (minus) ragged(qrow, q);
+  const int nvec = minus ? min(prow.nvec, qrow.nvec) : prow.nvec;   // the rows' vectors differ by one at most
+  int k = tid;
+  for (; k + (kAhead - 1) * NT < nvec; k += kAhead * NT) {
+    u32x4_t v[kAhead], w[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) v[j] = prow.load(k + j * NT);
+    if (minus) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) w[j] = qrow.load(k + j * NT);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) fold(v[j], p);
+    if (minus) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) fold(w[j], q);
+    }
+  }
+  for (; k < prow.nvec || (minus && k < qrow.nvec); k += NT) {
+    if (k < prow.nvec) fold(prow.load(k), p);
+    if (minus && k < qrow.nvec) fold(qrow.load(k), q);
+  }
+  p = soft_block_reduce<NT>(p, s_sum[0]);
+  if (minus) q = soft_block_reduce<NT>(q, s_sum[1]);
+  if (tid == 0) {
+    a.sums[rt] = p;
+    if (minus) a.sums[n_target + rd] = q;
+    if (i < n) {
+      const double lp = double(zp) - soft_lse(p);
+      const bool ok = accept(u, minus ? lp - (double(zq) - soft_lse(q)) : lp);
+      a.lp[rt] = ok ? lp : __builtin_nan("");
+      if (!ok) atomicMin(a.refused + b, i);
+    }
+  }
+}
+
 // Largest score so far and its column.
 struct Drawn {
   float score;
@@ -155,7 +238,31 @@ template <int E> __device__ __forceinline__ void load_floats(const float* x, flo
     }
   }
 }
-template <int NT, int DT, bool VEC>
+// The sequence's drawn token from its best key, which the first thread has.  Where the residual vanishes (rows that are the same but for
+// roundings) it is drawn from p, by this workgroup alone.
+template <int NT, int DT>
+__device__ __forceinline__ void put_drawn(const VerifyArgs& a, int b, int n, double lse, uint64_t key, uint64_t* lds /*[NT/64]*/) {
+  __shared__ uint64_t s_best;
+  if (threadIdx.x == 0) s_best = key;
+  __syncthreads();
+  key = s_best;
+  const int64_t rt = int64_t(b) * (a.G + 1) + n;
+  const char* const row = row_ptr<DT>(a.target, rt, a.ld);
+  if (key == 0 && lse - lse == 0.0) {   // uniform
+    Drawn d{0.f, 0};
+    for (int j = threadIdx.x; j < a.V; j += NT)
+      race(d, expf(float(double(load_elt<DT>(row, j)) - lse)) * __builtin_amdgcn_rcpf(a.noise[int64_t(b) * a.V + j]), j);
+    key = block_drawn<NT>(d, lds);   // the barrier above lies between two uses of lds
+  }
+  if (threadIdx.x == 0) {
+    const int drawn = key ? int(~uint32_t(key)) : -1;
+    a.out[rt] = drawn;
+    if (a.logprob) a.logprob[rt] = drawn >= 0 ? float(double(load_elt<DT>(row, drawn)) - lse) : 0.f;
+  }
+}
+
+// DECIDED: k_verify_positions has been there.  With one slice the drawn token too, else what k_verify_end needs.
+template <int NT, int DT, bool VEC, bool DECIDED>
 __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   constexpr int E = RowView<DT, VEC>::E;
   __shared__ uint64_t s_key[NT / kWave];
@@ -168,7 +275,10 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   RowParts pp, qp;
   pp.load(a, my_t);
   if (minus) qp.load(a, n_target + my_d);
-  const float u = lane < a.G ? a.uniform[my_d] : 0.f;
+  double lp = 0.0;
+  float u = 0.f;
+  if constexpr (DECIDED) lp = a.lp[my_t];
+  else u = lane < a.G ? a.uniform[my_d] : 0.f;
   int token;
   int32_t flags;
   const int count = drafted(a, b, lane, token, flags);
@@ -184,15 +294,17 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
     return;
   }
   const bool on = lane < count;
-  const int column = on ? token : 0;
-  const float zp = load_elt<DT>(row_ptr<DT>(a.target, my_t, a.ld), column);
-  const float zq = minus ? load_elt<DT>(row_ptr<DT>(a.draft, my_d, a.ld), column) : 0.f;
   const SoftSum sp = pp.sum(), sq = minus ? qp.sum() : soft_identity();
-  const double my_lse = soft_lse(sp), lp = double(zp) - my_lse;
-  const double ratio = minus ? lp - (double(zq) - soft_lse(sq)) : lp;   // ln(p / q)
-  const float coarse = float(ratio);
-  const double fine = fabsf(coarse) < INFINITY ? 1.0 + (ratio - double(coarse)) : 1.0;
-  const bool ok = on && double(u) < double(expf(coarse)) * fine;
+  bool ok;
+  if constexpr (DECIDED) {
+    ok = on && lp == lp;
+  } else {
+    const int column = on ? token : 0;
+    const float zp = load_elt<DT>(row_ptr<DT>(a.target, my_t, a.ld), column);
+    const float zq = minus ? load_elt<DT>(row_ptr<DT>(a.draft, my_d, a.ld), column) : 0.f;
+    lp = double(zp) - soft_lse(sp);
+    ok = on && accept(u, minus ? lp - (double(zq) - soft_lse(sq)) : lp);
+  }
   const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(ok));   // at most 63 positions
   const bool refused = n < count;
   const int own = refused && !minus ? __builtin_amdgcn_readlane(token, n) : -1;   // the whole of q
@@ -201,13 +313,15 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   const int64_t rt = int64_t(b) * (a.G + 1) + n, rd = int64_t(b) * a.G + n;
   const SoftSum pt = from_lane(sp, n);
   const double lse = soft_lse(pt);
-  if (slice == 0 && tid <= a.G) {   // all but the drawn token, which the last launch puts in its place
+  if (slice == 0 && tid <= a.G) {
     if (tid == 0) {
       a.accepted[b] = n;
       a.lse[b] = lse;
     }
-    out[tid] = tid < n ? token : -1;
-    if (lp_out) lp_out[tid] = tid < n ? float(lp) : 0.f;
+    if (tid != n) {   // the drawn token follows
+      out[tid] = tid < n ? token : -1;
+      if (lp_out) lp_out[tid] = tid < n ? float(lp) : 0.f;
+    }
   }
   Drawn left{0.f, 0};
   if (lse - lse == 0.0) {   // finite
@@ -257,44 +371,21 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
     }
   }
   const uint64_t key = block_drawn<NT>(left, s_key);
-  if (tid == 0) a.best[int64_t(b) * slices + slice] = key;
+  if (slices == 1) put_drawn<NT, DT>(a, b, n, lse, key, s_key);   // uniform
+  else if (tid == 0) a.best[int64_t(b) * slices + slice] = key;
 }
 
-// The sequence's drawn token.  Where the residual vanishes (rows that are the same but for roundings) it is drawn from p, by this
-// workgroup alone.
+// The slices of a sequence into its drawn token.
 constexpr int kEndNT = 256;
 template <int DT> __global__ __launch_bounds__(kEndNT) void k_verify_end(VerifyArgs a) {
   __shared__ uint64_t s_key[kEndNT / kWave];
-  __shared__ uint64_t s_best;
   const int tid = threadIdx.x, b = blockIdx.x;
   const int count = a.count ? a.count[b] : a.G;
   if (count < 0 || count > a.G) return;   // uniform
-  const int n = a.accepted[b];
-  const double lse = a.lse[b];
-  uint64_t key = 0;
-  for (int k = tid; k < a.slices; k += kEndNT) {
-    const uint64_t x = a.best[int64_t(b) * a.slices + k];
-    key = x > key ? x : key;
-  }
-  Drawn d{__uint_as_float(uint32_t(key >> 32)), int(~uint32_t(key))};
-  if (key == 0) d = Drawn{0.f, 0};
-  key = block_drawn<kEndNT>(d, s_key);
-  if (tid == 0) s_best = key;
-  __syncthreads();
-  key = s_best;
-  const int64_t rt = int64_t(b) * (a.G + 1) + n;
-  const char* const row = row_ptr<DT>(a.target, rt, a.ld);
-  if (key == 0 && lse - lse == 0.0) {   // uniform
-    d = Drawn{0.f, 0};
-    for (int j = tid; j < a.V; j += kEndNT)
-      race(d, expf(float(double(load_elt<DT>(row, j)) - lse)) * __builtin_amdgcn_rcpf(a.noise[int64_t(b) * a.V + j]), j);
-    key = block_drawn<kEndNT>(d, s_key);   // between the two uses of s_key lie the barriers around s_best
-  }
-  if (tid == 0 && key != 0) {
-    const int drawn = int(~uint32_t(key));
-    a.out[rt] = drawn;
-    if (a.logprob) a.logprob[rt] = float(double(load_elt<DT>(row, drawn)) - lse);
-  }
+  static_assert(kMaxSlices <= kEndNT, "a slice per thread");
+  const uint64_t x = tid < a.slices ? a.best[int64_t(b) * a.slices + tid] : 0;
+  const uint64_t key = block_drawn<kEndNT>(x ? Drawn{__uint_as_float(uint32_t(x >> 32)), int(~uint32_t(x))} : Drawn{0.f, 0}, s_key);
+  put_drawn<kEndNT, DT>(a, b, a.accepted[b], a.lse[b], key, s_key);
 }
 
 // Workgroups that a row's sum is split over: 8 to a CU in all.  (151936 bf16, 72 rows: 2 / 4 / 8 parts 9.9 / 8.3 / 7.6 us; 1408 rows, of which
@@ -304,7 +395,6 @@ static int verify_parts(int64_t rows, int nvec, int NT) {
 }
 // Workgroups that the draw of a sequence is split over: one to a CU in all, since each goes through the decision first.  (8 sequences: 4 / 16 /
 // 32 / 37 slices 14.2 / 7.8 / 7.4 / 9.4 us; 128: 2 / 8 / 32 slices 27.9 / 29.6 / 41.2.)
-constexpr int kMaxSlices = 64;
 static int verify_slices(int64_t B, int nvec, int NT) {
   return int(std::max<int64_t>(1, std::min<int64_t>({kMaxSlices, compute_units() / B, nvec / NT})));
 }
@@ -313,14 +403,27 @@ struct VerifyWorkspace {
   SoftSum* sums;
   uint64_t* best;
   double* lse;
+  double* lp;
+  int32_t* refused;
   size_t bytes;
 };
 static VerifyWorkspace verify_workspace(void* base, int64_t rows, int64_t B) {
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   char* const p = reinterpret_cast<char*>(base);
-  const size_t sums = up(size_t(2 * rows) * kVerifyParts * sizeof(SoftSum)), best = up(size_t(B) * kMaxSlices * 8);
-  return VerifyWorkspace{reinterpret_cast<SoftSum*>(p), reinterpret_cast<uint64_t*>(p + sums), reinterpret_cast<double*>(p + sums + best),
-                         sums + best + up(size_t(B) * 8) + 256};
+  VerifyWorkspace w;
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    char* const q = p + at;
+    at += up(n);
+    return q;
+  };
+  w.sums = reinterpret_cast<SoftSum*>(take(size_t(2 * rows) * kVerifyParts * sizeof(SoftSum)));
+  w.best = reinterpret_cast<uint64_t*>(take(size_t(B) * kMaxSlices * 8));
+  w.lse = reinterpret_cast<double*>(take(size_t(B) * 8));
+  w.lp = reinterpret_cast<double*>(take(size_t(rows) * 8));
+  w.refused = reinterpret_cast<int32_t*>(take(size_t(B) * 4));
+  w.bytes = at + 256;
+  return w;
 }
 size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B) {
   (void)V;
@@ -329,13 +432,24 @@ size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B) {
 
 template <int DT, bool VEC> static void verify_launch(VerifyArgs a, hipStream_t s) {
   constexpr int NT = 512;
-  const int64_t rows = int64_t(a.B) * (a.G + 1) + (a.draft ? int64_t(a.B) * a.G : 0);
+  const int64_t positions = int64_t(a.B) * (a.G + 1), rows = positions + (a.draft ? int64_t(a.B) * a.G : 0);
   const int nvec = a.V / RowView<DT, VEC>::E;
-  a.parts = verify_parts(rows, nvec, NT);
   a.slices = verify_slices(a.B, nvec, NT);
-  hipLaunchKernelGGL((k_verify_rows<NT, DT, VEC>), dim3(unsigned(rows), unsigned(a.parts)), dim3(NT), 0, s, a);
-  hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC>), dim3(unsigned(a.B), unsigned(a.slices)), dim3(NT), 0, s, a);
-  hipLaunchKernelGGL((k_verify_end<DT>), dim3(unsigned(a.B)), dim3(kEndNT), 0, s, a);
+  const dim3 draw{unsigned(a.B), unsigned(a.slices)};
+  // four positions to a CU and more: rows one by one / by position, 256 sequences x 8 drafted tokens 260 / 192 us, x 3 142 / 134, x 3 copied
+  // ones 94.0 / 91.8; fewer: 128 x 5 102 / 100, with drawn counts 75 / 85, 64 x 4 49.9 / 53.4
+  if (a.G > 0 && positions >= 4 * compute_units()) {
+    a.parts = 1;
+    hipLaunchKernelGGL(k_verify_start, dim3(unsigned((a.B + 255) / 256)), dim3(256), 0, s, a.refused, a.B);
+    // 1024 threads, so that two positions are under way on a CU (512, four: 223 / 141 / 97.2 us)
+    hipLaunchKernelGGL((k_verify_positions<1024, DT, VEC>), dim3(unsigned(positions)), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC, true>), draw, dim3(NT), 0, s, a);
+  } else {
+    a.parts = verify_parts(rows, nvec, NT);
+    hipLaunchKernelGGL((k_verify_rows<NT, DT, VEC>), dim3(unsigned(rows), unsigned(a.parts)), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC, false>), draw, dim3(NT), 0, s, a);
+  }
+  if (a.slices > 1) hipLaunchKernelGGL((k_verify_end<DT>), dim3(unsigned(a.B)), dim3(kEndNT), 0, s, a);
 }
 
 }  // namespace aero
@@ -356,7 +470,7 @@ extern "C" aero_status aero_verify_draft(const void* target_logits, const void* 
     return AERO_ERR_WORKSPACE;
   const VerifyWorkspace ws = verify_workspace(workspace, rows, B);
   const VerifyArgs a{target_logits, G > 0 ? draft_logits : nullptr, B, G, V, ld, draft_tokens, draft_count, uniform, noise, accepted, tokens,
-                     logprob, err_flag, ws.sums, ws.best, ws.lse, 1, 1};
+                     logprob, err_flag, ws.sums, ws.best, ws.lse, ws.refused, ws.lp, 1, 1};
   const bool vec = rows_alike(target_logits, nullptr, storage_bytes(dtype)) && rows_alike(a.draft, nullptr, storage_bytes(dtype));
   const hipStream_t s = as_stream(stream);
   switch (dtype) {

@@ -729,3 +729,38 @@ def test_distill_of_more_long_rows_than_compute_units(gh, dtype, V, ld, K, tail)
     run_distill(dev, T, V, ld, index, lp, w, tail, SCALE[dtype], again)
     raw = {1: torch.uint8, 2: torch.int16, 4: torch.int32}[again.element_size()]
     assert torch.equal(dz.view(raw), again.view(raw))
+
+
+@pytest.mark.parametrize("probs", [True, False])
+@pytest.mark.parametrize("dtype,V,ld", [("bf16", 300, 301), ("f32", 997, 997)])
+def test_verify_of_many_sequences(gh, dtype, V, ld, probs):
+    """Enough positions for the way that decides them one by one, with ragged counts, idle and bad sequences."""
+    B, G = 420, 3
+    case = draft_case(11, B, G, V, dtype, probs, ld)
+    count = np.random.default_rng(3).integers(0, G + 1, size=B).astype(np.int32)
+    count[:200] = G
+    count[201], count[202] = -1, G + 5
+    case["tokens"][7, 1], case["tokens"][8, 0] = -1, V + 3
+    zt = case["th"].copy()
+    zt[20, 0] = -np.inf
+    zt[21, 1] = np.nan
+    if dtype == "f32":
+        case["t"], case["th"] = stored(zt.reshape(-1, V), dtype, ld)[0], zt
+    ref = check_verify(case, B, G, V, ld, count, err=2 | 16)
+    assert len(set(ref["accepted"].tolist())) == G + 1
+    check_verify(draft_case(12, 1100, 0, 40, dtype, probs), 1100, 0, 40, 40, None)      # nothing drafted, one slice
+
+
+def test_verify_of_equal_rows_that_are_refused(gh):
+    """Where the residual vanishes the token is drawn from p: the drafter's rows are the policy's and the drafted token is masked in both,
+    so that it is refused; with one slice per sequence and with several."""
+    for B, V in ((3, 20000), (300, 600)):
+        case = draft_case(13, B, 1, V, "f32", True, miss=0.0)
+        z = case["th"].copy()
+        z[:, 0, 5] = -np.inf
+        case["t"], case["th"] = stored(z.reshape(-1, V), "f32")[0], z
+        zd = z[:, :1].copy()
+        case["d"], case["dh"] = stored(zd.reshape(-1, V), "f32")[0], zd
+        case["tokens"][:] = 5
+        ref = check_verify(case, B, 1, V, V, None)
+        assert not ref["accepted"].any() and (ref["tokens"][:, 0] >= 0).all() and (ref["tokens"][:, 0] != 5).all()
