@@ -150,7 +150,8 @@ struct RowGrad {
   bool quiet;   // no loss, no gradient
 };
 // What the sum over the other places and the list come to; one thread writes the loss (a quiet row's too).  By all threads.
-__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftSum rest, const ListSums* s, int waves, bool bad = false) {
+__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftSum rest, const ListSums* s, int waves, bool bad = false,
+                                              bool report = true) {
   double mass = 0.0, p_lp_z = 0.0;
   SoftSum all = rest;
   bool any = false;
@@ -173,7 +174,7 @@ __device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, fl
   r.o_all = uniform(all.o);
   r.at_other = uniform(has_rest ? float(g * (total * double(rest_q) - rest_p)) / rest.s : 0.f);
   r.o_rest = uniform(rest.o);
-  if (threadIdx.x == blockDim.x - 1) {   // the first wave has the list to look after
+  if (report && threadIdx.x == blockDim.x - 1) {   // the first wave has the list to look after
     if (bad && a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_TEACHER);
     double loss = 0.0;
     if (!r.quiet) {   // logarithms of 32-bit numbers: 2^-24 of the logarithm
@@ -197,17 +198,26 @@ template <int E> __device__ __forceinline__ void grad_elts(const float (&z)[E], 
   for (int e = 0; e < E; ++e) d[e] = r.at_other * exp2_fast(fmaf(z[e], kLog2e, -r.o_rest));
 }
 template <int NT, int DT, bool VEC>
-__device__ __forceinline__ void put_listed(const ListPlaces<NT>& list, const RowView<DT, VEC>& row, const RowGrad& r, char* drow, int jr) {
+__device__ __forceinline__ void put_listed(const ListPlaces<NT>& list, const RowView<DT, VEC>& row, const RowGrad& r, char* drow, int jr,
+                                           int from = 0, int to = kRagged) {   // places, of which the ragged one is its thread's with jr >= 0
   constexpr int E = RowView<DT, VEC>::E;
   each_listed(list, [&](int k, int place) {
+    if (place == kRagged ? jr < 0 : place < from || place >= to) return;
     const int j = place == kRagged ? jr : row.head + (place / E * NT + int(threadIdx.x)) * E + place % E;
     store_elt<DT>(drow, j, r.at_listed * exp2_fast(fmaf(list.z[k], kLog2e, -r.o_all)) - r.scale_p * list.p[k]);
   });
 }
 
-// One workgroup per row, which is read twice: any row.
-template <int NT, int DT, bool VEC>
-__global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
+// Any row, read twice: by one workgroup (kWhole), or split over gridDim.y workgroups that find the sums in one launch (kSums) and write
+// the gradient in a second (kGradient).  A part is whole turns of the workgroup's threads.
+enum { kWhole, kSums, kGradient };
+constexpr int kMaxParts = 16;
+struct RowSplit {
+  SoftSum part[kMaxParts];
+  ListSums list;
+};
+template <int STEP, int NT, int DT, bool VEC>
+__global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a, int summed, RowSplit* __restrict__ splits) {   // summed: parts of the sums
   using View = RowView<DT, VEC>;
   constexpr int E = View::E, kAhead = 4, kWaves = NT / kWave;
   static_assert(NT >= kListMax, "an entry per thread");
@@ -215,11 +225,14 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   __shared__ SoftSum s_sum[kWaves];
   __shared__ ListSums s_list[kListWaves];
   const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x, K = a.K;
+  const int tid = threadIdx.x, K = a.K, part = blockIdx.y, parts = gridDim.y;
   const float w = a.weight[t];
   const View row(a.logits, t, a.ld, a.V);
-  const int nvec = row.nvec, jr = row.ragged();
+  const int turns = (row.nvec + NT - 1) / NT, per = (turns + parts - 1) / parts;
+  const int first = min(part * per, turns), nvec = min(min(first + per, turns) * NT, row.nvec);   // of this part
+  const int jr = part == 0 ? row.ragged() : -1;
   char* const drow = a.dlogits ? row_ptr<DT>(a.dlogits, t, a.ld) : nullptr;
+  RowSplit* const split = STEP == kWhole ? nullptr : splits + t;
   auto put = [&](int vec, const float (&d)[E]) {
     if constexpr (VEC)
       __builtin_nontemporal_store(pack_vec<DT>(d), reinterpret_cast<u32x4_t*>(drow + row.head * Storage<DT>::kBytes) + vec);
@@ -227,15 +240,15 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
       store_elt<DT>(drow, vec, d[0]);
   };
   auto zero_fill = [&]() {
-    if (!drow) return;
+    if (STEP == kSums || !drow) return;
     float zero[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) zero[e] = 0.f;
-    for (int i = tid; i < nvec; i += NT) put(i, zero);
+    for (int i = first * NT + tid; i < nvec; i += NT) put(i, zero);
     if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
   };
   if (w == 0.f) {   // uniform
-    if (tid == 0) put_loss(a, t, w, 0.f);
+    if (STEP != kSums && part == 0 && tid == 0) put_loss(a, t, w, 0.f);
     zero_fill();
     return;
   }
@@ -258,40 +271,63 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     }
   }
   __syncthreads();
-  if (tid < kListMax) {   // whole waves
-    if (entry.j >= 0) bad |= list_twice(list, tid);
-    list_sum(entry, bad, s_list);
-  }
-  const bool chained = list.head[tid] >= 0;
-
-  SoftSum st = soft_identity();
-  auto fold = [&](const u32x4_t& v, int turn) {
-    float z[E];
-    View::unpack(v, z);
-    if (chained)
-      each_listed(list, [&](int, int place) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) z[e] = place == turn * E + e ? -INFINITY : z[e];
-      });
-    soft_update<E>(st, z);
-  };
-  int i = tid, turn = 0;
-  for (; i + (kAhead - 1) * NT < nvec; i += kAhead * NT, turn += kAhead) {
-    u32x4_t v[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = row.load_again(i + u * NT);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) fold(v[u], turn + u);
-  }
-  for (; i < nvec; i += NT) fold(row.load_again(i), turn++);
   const float zr = jr >= 0 ? row.at(jr) : 0.f;
-  if (jr >= 0) {
-    float z[1] = {zr};
-    each_listed(list, [&](int, int place) { z[0] = place == kRagged ? -INFINITY : z[0]; });
-    soft_update<1>(st, z);
+  SoftSum st = soft_identity();
+  if constexpr (STEP != kGradient) {
+    if (tid < kListMax) {   // whole waves
+      if (entry.j >= 0) bad |= list_twice(list, tid);
+      list_sum(entry, bad, s_list);
+    }
+    const bool chained = list.head[tid] >= 0;
+    auto fold = [&](const u32x4_t& v, int turn) {
+      float z[E];
+      View::unpack(v, z);
+      if (chained)
+        each_listed(list, [&](int, int place) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) z[e] = place == turn * E + e ? -INFINITY : z[e];
+        });
+      soft_update<E>(st, z);
+    };
+    int turn = first, i = first * NT + tid;
+    for (; i + (kAhead - 1) * NT < nvec; i += kAhead * NT, turn += kAhead) {
+      u32x4_t v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) v[u] = row.load_again(i + u * NT);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) fold(v[u], turn + u);
+    }
+    for (; i < nvec; i += NT) fold(row.load_again(i), turn++);
+    if (jr >= 0) {
+      float z[1] = {zr};
+      each_listed(list, [&](int, int place) { z[0] = place == kRagged ? -INFINITY : z[0]; });
+      soft_update<1>(st, z);
+    }
+    st = soft_block_reduce<NT>(st, s_sum);   // its barrier: s_list
   }
-  st = soft_block_reduce<NT>(st, s_sum);   // its barrier: s_list
-  const RowGrad r = row_terms(a, t, w, st, s_list, kListWaves);
+  if constexpr (STEP == kSums) {
+    if (tid == 0) {
+      split->part[part] = st;
+      if (part == 0) {
+        ListSums all = s_list[0];
+#pragma unroll
+        for (int k = 1; k < kListWaves; ++k) {
+          all.mass += s_list[k].mass;
+          all.p_lp_z += s_list[k].p_lp_z;
+          all.own = soft_merge(all.own, s_list[k].own);
+          all.any |= s_list[k].any;
+          all.bad |= s_list[k].bad;
+        }
+        split->list = all;
+      }
+    }
+    return;
+  }
+  if constexpr (STEP == kGradient) {
+    if (tid % 16 < summed) st = split->part[tid % 16];
+    st = soft_reduce<false>(st);
+  }
+  const RowGrad r = row_terms(a, t, w, st, STEP == kGradient ? &split->list : s_list, STEP == kGradient ? 1 : kListWaves, false, part == 0);
   if (!drow) return;
   if (r.quiet) {   // uniform
     zero_fill();
@@ -304,7 +340,8 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
     grad_elts<E>(z, d, r);
     put(vec, d);
   };
-  for (i = tid; i + (kAhead - 1) * NT < nvec; i += kAhead * NT) {
+  int i = first * NT + tid;
+  for (; i + (kAhead - 1) * NT < nvec; i += kAhead * NT) {
     u32x4_t v[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) v[u] = row.load(i + u * NT);
@@ -313,7 +350,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a) {
   }
   for (; i < nvec; i += NT) turned(row.load(i), i);
   if (jr >= 0) store_elt<DT>(drow, jr, r.at_other * exp2_fast(fmaf(zr, kLog2e, -r.o_rest)));
-  put_listed(list, row, r, drow, jr);
+  put_listed(list, row, r, drow, jr, first * E, (first + per) * E);
 }
 
 // One workgroup per row, which its threads hold: kHeldVecs vectors each in registers.
@@ -660,18 +697,30 @@ __global__ __launch_bounds__(kSumNT) void k_distill_sum(const float* __restrict_
 struct DistillWorkspace {
   float* term;      // [T]
   int32_t* order;   // [T]
-  int32_t* ctr;     // [4]
+  int32_t* ctr;     // [2]
+  RowSplit* split;  // [rows that are split]
   size_t bytes;
 };
 static DistillWorkspace distill_workspace(void* base, int64_t T) {
-  const size_t each = (size_t(T) * 4 + 255) / 256 * 256;
+  const size_t each = (size_t(T) * 4 + 255) / 256 * 256, split = std::min<int64_t>(T, compute_units()) * sizeof(RowSplit);
   char* const p = reinterpret_cast<char*>(base);
   return DistillWorkspace{reinterpret_cast<float*>(p), reinterpret_cast<int32_t*>(p + each), reinterpret_cast<int32_t*>(p + 2 * each),
-                          2 * each + 256};
+                          reinterpret_cast<RowSplit*>(p + 2 * each + 256), 2 * each + 256 + (split + 255) / 256 * 256};
 }
 size_t distill_workspace_bytes(int64_t T, int32_t V) {
   (void)V;
   return distill_workspace(nullptr, T).bytes;
+}
+
+// Workgroups that a row is split over, two to a CU in all: few rows that threads of one workgroup cannot hold in registers, and those that a CU cannot
+// hold up to one per CU.  (151936 bf16, whole / 4 / 8 / 16 parts: 16 rows 25.2 / 18.0 / 13.6 / 12.2 us, 64 26.3 / 18.7 / 16.1 / 17.0, 128 28.8 / 26.4 / 25.7 /
+// 29.2, 200 31.6 / 36.7 / 34.3 / 39.0; 151936 fp32 64 rows 50.7 / 25.2 / 22.4 / 22.4, 200 66.6 / 60.7 / 57.3 / 58.2; 50257 bf16, held in
+// registers, 16 rows 12.0 / 11.5 / 11.4 / 11.5.)
+static int distill_parts(const DistillArgs& a, bool vec, int nvec, int NT) {
+  const int cus = compute_units();
+  const bool held = vec && nvec <= kHeldVecs * 1024, streams = vec && a.dlogits && nvec <= kStreamVecs * kStreamNT;
+  if (held || a.T > (streams ? cus / 2 : cus)) return 1;
+  return int(std::max<int64_t>(1, std::min<int64_t>({kMaxParts, 2 * cus / a.T, nvec / (2 * NT)})));
 }
 
 template <int NT, int DT> static void held_launch(const DistillArgs& a, hipStream_t s) {
@@ -680,10 +729,18 @@ template <int NT, int DT> static void held_launch(const DistillArgs& a, hipStrea
 
 template <int DT> static aero_status distill_launch(const DistillArgs& a, bool vec, const DistillWorkspace& ws, hipStream_t s) {
   const int nvec = vec ? a.V / Storage<DT>::kPerVec : a.V;
-  if (!vec) {
-    hipLaunchKernelGGL((k_distill_row<512, DT, false>), dim3(unsigned(a.T)), dim3(512), 0, s, a);
+  constexpr int NT = 512;
+  const int parts = distill_parts(a, vec, nvec, NT);
+  if (parts > 1) {
+    const dim3 grid{unsigned(a.T), unsigned(parts)};
+    const auto sums = vec ? k_distill_row<kSums, NT, DT, true> : k_distill_row<kSums, NT, DT, false>;
+    const auto grad = vec ? k_distill_row<kGradient, NT, DT, true> : k_distill_row<kGradient, NT, DT, false>;
+    hipLaunchKernelGGL(sums, grid, dim3(NT), 0, s, a, parts, ws.split);
+    hipLaunchKernelGGL(grad, a.dlogits ? grid : dim3(unsigned(a.T)), dim3(NT), 0, s, a, parts, ws.split);
+  } else if (!vec) {
+    hipLaunchKernelGGL((k_distill_row<kWhole, NT, DT, false>), dim3(unsigned(a.T)), dim3(NT), 0, s, a, parts, ws.split);
   } else if (nvec > kStreamVecs * kStreamNT || (!a.dlogits && nvec > kHeldVecs * 1024)) {
-    hipLaunchKernelGGL((k_distill_row<512, DT, true>), dim3(unsigned(a.T)), dim3(512), 0, s, a);
+    hipLaunchKernelGGL((k_distill_row<kWhole, NT, DT, true>), dim3(unsigned(a.T)), dim3(NT), 0, s, a, parts, ws.split);
   } else if (nvec <= kHeldVecs * 64 && a.K <= 64) {
     held_launch<64, DT>(a, s);
   } else if (nvec <= kHeldVecs * 256) {

@@ -764,3 +764,24 @@ def test_verify_of_equal_rows_that_are_refused(gh):
         case["tokens"][:] = 5
         ref = check_verify(case, B, 1, V, V, None)
         assert not ref["accepted"].any() and (ref["tokens"][:, 0] >= 0).all() and (ref["tokens"][:, 0] != 5).all()
+
+
+@pytest.mark.parametrize("dtype,V,off_d", [("bf16", 90001, None), ("f32", 41003, None), ("f32", 100003, None), ("bf16", 9001, 1)])
+def test_distill_of_few_long_rows(gh, dtype, V, off_d):
+    """Rows that are split over workgroups: with and without a gradient, in place, with quiet rows among them."""
+    T, K = 7, 60
+    z = normal([V, 8], T, V)
+    host = torch.from_numpy(z).to(TORCH[dtype]).float().double().numpy()
+    index, lp = make_lists(V, host, K)
+    index[4, 7] = index[4, 50]
+    index[5] = -1
+    for tail in (0, 1):
+        a = check_distill(z, dtype, K, tail, off=3, off_d=off_d if off_d is None else off_d, lists=(index, lp))
+        if off_d is None:
+            b = check_distill(z, dtype, K, tail, off=3, lists=(index, lp), inplace=True)
+            assert np.array_equal(a[1], b[1]) and np.array_equal(a[2], b[2])
+        d, _ = stored(z, dtype, V, 3)
+        w = np.random.default_rng([0, 6]).uniform(0.2, 1.0, size=T).astype(np.float32)
+        w[::5] = 0.0
+        alone = run_distill(d, T, V, V, index, lp, w, tail, 1.0, None)
+        assert np.allclose(alone[1], a[1], rtol=0, atol=4 * rel(V, 16.0))
