@@ -371,7 +371,7 @@ aero_status aero_verify_draft(
  * Embedding rows: out[t, :] = scale * table[ids[t], :], formed in fp32 and rounded once.
  * table [V, H] contiguous, out [T, ld_out] (ld_out >= H, columns >= H untouched: rows of a wider buffer), both of dtype AERO_F32, AERO_BF16
  * or AERO_F16; ids i32[T].  A negative id is padding: its row is +0; an id >= V likewise, and raises
- * AERO_DERR_BAD_TARGET.  1 <= V <= 2^24, 1 <= H <= 2^20; any alignment (16-byte vectors where table, out, H and ld_out allow them).
+ * AERO_DERR_BAD_TARGET.  1 <= V <= 2^24, 1 <= H <= 2^20; any element's alignment.
  */
 aero_status aero_embedding_fwd(
     const void* table, int32_t dtype, int32_t V, int32_t H, const int32_t* ids, int64_t T, float scale,

@@ -3,17 +3,18 @@
 // The sort is a launch of independent workgroups, each of which owns the ids that are alike modulo their number: it counts
 // its own ids one by one and the tokens of those in front of it as a whole, and places its tokens in ascending order within an id.
 // Every token is read by every workgroup, out of the caches; nothing passes between workgroups and there are no counters whose order
-// could show.  The sums are a second launch of workgroups that go over three kinds of work, found by halving in the owners' counts:
-// pieces of kPiece tokens of frequent ids by column blocks, whole rows of the others, and zeros for the ids that no token has.  The zeros are
-// small workgroups in the order of their addresses where rows are whole vectors: that writes 6.8 TB/s, workgroups that walk over rows 5.2.  Ids
-// with several pieces are joined in order in a third.
+// could show.  The sums are a second launch of workgroups that go over two kinds of work, found by halving in the owners' counts:
+// pieces of kPiece tokens of frequent ids by column blocks, and whole rows of the others; and of small workgroups that zero the rows of the ids
+// that no token has, 16 bytes a thread in the order of their addresses: that writes 6.5 TB/s, workgroups that walk over rows 5.2.
+// Ids with several pieces are joined in order in a third.
 #include <algorithm>
 
 #include "row_scan.h"
 
 namespace aero {
 
-// One workgroup per token row.
+// One workgroup per token row.  VEC: rows of a vector and more, at any alignment; the last vector ends where the row ends and overlaps the one in
+// front.
 template <int DT, bool VEC>
 __global__ __launch_bounds__(256) void k_embed_fwd(const void* __restrict__ table, int V, int H, const int32_t* __restrict__ ids,
                                                    float scale, void* __restrict__ out, int64_t ld_out,
@@ -23,21 +24,23 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const void* __restrict__ tabl
   const int id = ids[t];
   if (id >= V && threadIdx.x == 0 && err_flag) atomicOr(err_flag, AERO_DERR_BAD_TARGET);
   const bool there = id >= 0 && id < V;
-  const char* const src = row_ptr<DT>(table, there ? id : 0, H);
-  char* const dst = row_ptr<DT>(out, t, ld_out);
-  for (int i = threadIdx.x; i < H / E; i += 256) {
+  for (int c0 = threadIdx.x * E; c0 < H; c0 += 256 * E) {
+    const int c = min(c0, H - E);
+    const char* const src = row_ptr<DT>(table, there ? id : 0, H, c);
+    char* const dst = row_ptr<DT>(out, t, ld_out, c);
     if constexpr (VEC) {
       u32x4_t v = {0u, 0u, 0u, 0u};
       if (there) {
         float x[E];
-        unpack_vec<DT>(reinterpret_cast<const u32x4_t*>(src)[i], x);
+        const u32x4_t in = *reinterpret_cast<const u32x4_any_t*>(src);
+        unpack_vec<DT>(in, x);
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] *= scale;
         v = pack_vec<DT>(x);
       }
-      reinterpret_cast<u32x4_t*>(dst)[i] = v;
+      *reinterpret_cast<u32x4_any_t*>(dst) = v;
     } else {
-      store_elt<DT>(dst, i, there ? scale * load_elt<DT>(src, i) : 0.f);
+      store_elt<DT>(dst, 0, there ? scale * load_elt<DT>(src, 0) : 0.f);
     }
   }
 }
@@ -50,7 +53,6 @@ constexpr int kLogBins = 10, kBins = 1 << kLogBins;      // ids of a sorting wor
 constexpr int kMinOwners = 256;                          // sorting workgroups, a power of two
 constexpr int kPiece = 32;                               // tokens of a frequent id that one wave adds up
 constexpr int kFew = 4;                                  // up to so many tokens: a wave takes the whole row
-constexpr int kZeroRows = 16;                            // rows that a wave zeroes at a time
 
 // Sorted tokens [start, start + count) of an id.  row: where the sum goes when the id has several pieces, -1: to the table.
 struct Piece {
@@ -63,8 +65,8 @@ struct Whole {
 // How many of each a sorting workgroup has.  Its pieces lie from its first sorted position on: those of frequent ids in front, the
 // others behind, from the last position backwards; its wholes from the same position on.
 struct OwnerCounts {
-  int32_t *heavy, *few, *whole, *none;   // [owners]
-  int32_t *base, *end;                   // [owners] first sorted position, and the one behind the last
+  int32_t *heavy, *few, *whole;   // [owners]
+  int32_t *base, *end;            // [owners] first sorted position, and the one behind the last
 };
 
 static int embed_owners(int32_t V) {
@@ -76,7 +78,6 @@ struct EmbedWorkspace {
   int32_t* order;   // [T] tokens sorted by id
   Piece* piece;     // [T]
   Whole* whole;     // [T]
-  int32_t* none;    // [owners][kBins] ids that no token has
   uint8_t* there;   // [V] a token has the id
   OwnerCounts n;
   float* partial;   // [2 (T / kPiece + 1)][H]
@@ -95,9 +96,8 @@ static EmbedWorkspace embed_workspace(void* base, int64_t T, int32_t V, int64_t 
   w.order = reinterpret_cast<int32_t*>(take(size_t(T) * 4));
   w.piece = reinterpret_cast<Piece*>(take(size_t(T) * sizeof(Piece)));
   w.whole = reinterpret_cast<Whole*>(take(size_t(T) * sizeof(Whole)));
-  w.none = reinterpret_cast<int32_t*>(take(owners * kBins * 4));
   w.there = reinterpret_cast<uint8_t*>(take(size_t(V)));
-  int32_t** const counts[] = {&w.n.heavy, &w.n.few, &w.n.whole, &w.n.none, &w.n.base, &w.n.end};
+  int32_t** const counts[] = {&w.n.heavy, &w.n.few, &w.n.whole, &w.n.base, &w.n.end};
   for (int32_t** c : counts) *c = reinterpret_cast<int32_t*>(take(owners * 4));
   w.partial = reinterpret_cast<float*>(take(size_t(2 * (T / kPiece + 1)) * size_t(H) * 4));
   w.bytes = at + 256;
@@ -111,11 +111,10 @@ size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H) {
 // each other: (run, thread, number) is their order.
 __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restrict__ ids, int64_t T, int V, int log_owners,
                                                         int32_t* __restrict__ order, Piece* __restrict__ pieces, Whole* __restrict__ wholes,
-                                                        int32_t* __restrict__ none, uint8_t* __restrict__ there, OwnerCounts counts,
-                                                        int32_t* __restrict__ err_flag) {
+                                                        uint8_t* __restrict__ there, OwnerCounts counts, int32_t* __restrict__ err_flag) {
   __shared__ int s_count[kBins], s_at[kBins];
   __shared__ int s_wave[2][kSortWaves], s_run[kSortRuns * kSortWaves], s_all;
-  __shared__ int s_n[4];
+  __shared__ int s_n[3];
   __shared__ int32_t s_tok[kListed];
   __shared__ uint16_t s_bin[kListed];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
@@ -123,7 +122,7 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   const int bins = (V - g + mask) >> log_owners;   // ids g, g + owners, ... below V
   const uint64_t below = (uint64_t(1) << lane) - 1;
   s_count[tid] = 0;
-  if (tid < 4) s_n[tid] = 0;
+  if (tid < 3) s_n[tid] = 0;
   __syncthreads();
   // ---- count ----
   int id[kSortRuns][kSortEach];
@@ -194,15 +193,12 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
     if (np > 1) wholes[base + atomicAdd(&s_n[2], 1)] = Whole{id_mine, row, np, 0};
   } else if (mine > 0) {
     pieces[base + total - 1 - atomicAdd(&s_n[1], 1)] = Piece{id_mine, start, mine, -1};
-  } else if (tid < bins) {
-    none[g * kBins + atomicAdd(&s_n[3], 1)] = id_mine;
   }
   __syncthreads();
   if (tid == 0) {
     counts.heavy[g] = s_n[0];
     counts.few[g] = s_n[1];
     counts.whole[g] = s_n[2];
-    counts.none[g] = s_n[3];
     counts.base[g] = base;
     counts.end[g] = base + total;
   }
@@ -286,13 +282,12 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
 
 // Inclusive sums of the owners' counts in LDS, and the owner that the u-th of all lies with (and which of its own it is).
 constexpr int kSumNT = 256, kSumWaves = kSumNT / kWave;
-__device__ __forceinline__ int scan_owners(const int32_t* __restrict__ n, int owners, int* s_end /*[owners]*/, int* s_wave /*[kSumWaves]*/,
-                                           int unit) {
+__device__ __forceinline__ int scan_owners(const int32_t* __restrict__ n, int owners, int* s_end /*[owners]*/, int* s_wave /*[kSumWaves]*/) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   int total = 0;
   __syncthreads();   // s_end may still be in use
   for (int g0 = 0; g0 < owners; g0 += kSumNT) {   // owners is a multiple of kSumNT
-    int incl = (n[g0 + tid] + unit - 1) / unit;
+    int incl = n[g0 + tid];
 #pragma unroll
     for (int m = 1; m < kWave; m <<= 1) {
       const int y = __shfl_up(incl, m, kWave);
@@ -324,24 +319,29 @@ __device__ __forceinline__ int find_owner(const int* s_end, int owners, int u, i
   return lo;
 }
 
-// N sums, scaled, to consecutive columns of the table: added to what is there, or in its place.
-template <int OUT, int N> __device__ __forceinline__ void put_sums(char* at, const float (&sum)[N], float scale, bool accumulate) {
+// N sums, scaled, to consecutive columns of the table from the skip-th on: added to what is there, or in its place.
+template <int OUT, int N> __device__ __forceinline__ void put_sums(char* at, const float (&sum)[N], int skip, float scale, bool accumulate) {
   float x[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) x[e] = scale * sum[e];
   if constexpr (N == Storage<OUT>::kPerVec) {
-    u32x4_t* const p = reinterpret_cast<u32x4_t*>(at);
-    if (accumulate) {
-      float y[N];
-      unpack_vec<OUT>(*p, y);
+    if (skip == 0) {
+      u32x4_any_t* const p = reinterpret_cast<u32x4_any_t*>(at);
+      if (accumulate) {
+        float y[N];
+        const u32x4_t old = *p;
+        unpack_vec<OUT>(old, y);
 #pragma unroll
-      for (int e = 0; e < N; ++e) x[e] += y[e];
+        for (int e = 0; e < N; ++e) x[e] += y[e];
+      }
+      const u32x4_any_t v = pack_vec<OUT>(x);
+      __builtin_nontemporal_store(v, p);
+      return;
     }
-    __builtin_nontemporal_store(pack_vec<OUT>(x), p);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) store_elt<OUT>(at, e, accumulate ? load_elt<OUT>(at, e) + x[e] : x[e]);
   }
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e >= skip) store_elt<OUT>(at, e, accumulate ? load_elt<OUT>(at, e) + x[e] : x[e]);
 }
 
 struct EmbedSums {
@@ -350,34 +350,42 @@ struct EmbedSums {
   int H, owners;
   const int32_t* order;
   const Piece* piece;
-  const int32_t* none;
   const uint8_t* there;
   OwnerCounts n;
   float scale;
   int accumulate;
-  int workers, segments;   // workgroups that go over the work; those that zero a row each, 0: the workers do
+  double per_width;      // 1 / H
+  int V, workers;        // workgroups that go over the sums; others zero the table in the order of its addresses
+  uint64_t zeros_from;   // the first of those
   float* partial;
   void* table;
 };
-// Sums of a lane: a 16-byte vector of the table (VEC), so that a wave's stores follow each other (two vectors of fp32 from one of 16
-// bits, stored 32 bytes apart: 2 TB/s).
+// Sums of a lane: a 16-byte vector of the table (VEC: rows of one and more, at any alignment), so that a wave's stores follow each other (two
+// vectors of fp32 from one of 16 bits, stored 32 bytes apart: 2 TB/s).  The last vector ends where the row ends and overlaps the one in front; its
+// first elements are that one's to store.
 template <int DT, int OUT, bool VEC> struct ColumnSums {
   static constexpr int E = VEC ? Storage<OUT>::kPerVec : 1, kBlock = kWave * E;
   struct Raw {
     uint32_t w[(E * Storage<DT>::kBytes + 3) / 4];
   };
+  // Column blocks of `rows` rows that are asked for at a time: at most 32 registers of them.
+  static constexpr int blocks(int rows) {
+    const int n = 32 / (rows * int(sizeof(Raw) / 4));
+    return n < 1 ? 1 : n > 8 ? 8 : n;
+  }
+  __device__ __forceinline__ static int column(const EmbedSums& a, int c) { return min(c, a.H - E); }
   __device__ __forceinline__ static Raw load(const EmbedSums& a, int token, int c) {
     const char* const at = row_ptr<DT>(a.dout, token, a.ld, c);
     Raw r;
-    if constexpr (!VEC) r.w[0] = load_raw<DT>(at, 0);
-    else if constexpr (sizeof(Raw) == 8) {
-      typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-      const u32x2_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(at));
+    if constexpr (!VEC) {
+      r.w[0] = load_raw<DT>(at, 0);
+    } else if constexpr (sizeof(Raw) == 8) {
+      const u32x2_any_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_any_t*>(at));
       r.w[0] = v.x; r.w[1] = v.y;
     } else {
 #pragma unroll
       for (int k = 0; k < int(sizeof(Raw)) / 16; ++k) {
-        const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(at) + k);
+        const u32x4_any_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any_t*>(at) + k);
         r.w[4 * k] = v.x; r.w[4 * k + 1] = v.y; r.w[4 * k + 2] = v.z; r.w[4 * k + 3] = v.w;
       }
     }
@@ -394,7 +402,7 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
 #pragma unroll
     for (int b = 0; b < C; ++b)
 #pragma unroll
-      for (int k = 0; k < R; ++k) v[b][k] = load(a, token[k], min(c0 + b * kBlock, a.H - E));   // H is a multiple of E
+      for (int k = 0; k < R; ++k) v[b][k] = load(a, token[k], column(a, c0 + b * kBlock));
 #pragma unroll
     for (int b = 0; b < C; ++b)
 #pragma unroll
@@ -403,6 +411,11 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
 #pragma unroll
           for (int e = 0; e < E; ++e) sum[b][e] += elt(v[b][k], e);
         }
+  }
+  __device__ __forceinline__ static void put(const EmbedSums& a, int64_t id, int c, const float (&sum)[E]) {
+    if (c >= a.H) return;
+    const int at = column(a, c);
+    put_sums<OUT, E>(row_ptr<OUT>(a.table, id, a.H, at), sum, c - at, a.scale, a.accumulate != 0);
   }
   // the whole row of an id with R tokens
   template <int R, int C> __device__ __forceinline__ static void row(const EmbedSums& a, const Piece& p, int own) {
@@ -413,29 +426,57 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
       float sum[C][E] = {};
       add<R, C>(a, token, R, c0, sum);
 #pragma unroll
-      for (int b = 0; b < C; ++b)
-        if (c0 + b * kBlock < a.H) put_sums<OUT, E>(row_ptr<OUT>(a.table, p.id, a.H, c0 + b * kBlock), sum[b], a.scale, a.accumulate != 0);
+      for (int b = 0; b < C; ++b) put(a, p.id, c0 + b * kBlock, sum[b]);
     }
   }
 };
 
-template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT) void k_embed_sum(EmbedSums a) {
+// A vector of the table by each thread of the workgroup, from element `before` on: zeros where no token has the row's id.  A vector that spans
+// two rows is stored whole where both are empty, and otherwise element by element.
+template <int OUT> __device__ __forceinline__ void put_zeros(const EmbedSums& a, uint64_t before) {
+  constexpr int Z = Storage<OUT>::kPerVec;
+  const uint32_t H = uint32_t(a.H);
+  const uint64_t all = uint64_t(a.V) * H, from = before + threadIdx.x * Z;
+  if (from >= all) return;
+  char* const at = reinterpret_cast<char*>(a.table) + from * Storage<OUT>::kBytes;
+  // row and column of the vector, by reciprocals and a correction (whole-number division: a third of the time of a narrow table)
+  uint32_t base = uint32_t(double(before) * a.per_width);
+  int64_t rest = int64_t(before) - int64_t(uint64_t(base) * H);
+  if (rest < 0) rest += H, --base;
+  if (rest >= int64_t(H)) rest -= H, ++base;
+  const uint32_t in = uint32_t(rest) + threadIdx.x * Z;
+  uint32_t more = uint32_t(float(in) * float(a.per_width));
+  int32_t column = int32_t(in - more * H);
+  if (column < 0) column += H, --more;
+  if (column >= int32_t(H)) column -= H, ++more;
+  const uint32_t row = base + more, left = H - uint32_t(column);   // columns of the row from here on
+  const bool spans = left < Z;
+  const bool none = !a.there[row], next_none = !a.there[min(row + 1, uint32_t(a.V) - 1)];   // asked for together
+  if (none && (!spans || (next_none && H >= Z && from + Z <= all))) {
+    const u32x4_any_t zero = {0u, 0u, 0u, 0u};
+    __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_any_t*>(at));
+  } else if (spans) {
+#pragma unroll
+    for (int e = 0; e < Z; ++e)
+      if (from + e < all && (e < int(left) ? none : H >= Z ? next_none : !a.there[row + 1 + (e - left) / H])) store_elt<OUT>(at, e, 0.f);
+  }
+}
+
+// 80 registers, six workgroups to a CU: 16384 tokens of width 1536 in bf16, 69 us; eight workgroups, with registers spilled, 74; five, 71.
+template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT, 6) void k_embed_sum(EmbedSums a) {
   using Sums = ColumnSums<DT, OUT, VEC>;
-  constexpr int E = Sums::E;
+  constexpr int E = Sums::E, Z = Storage<OUT>::kPerVec;
   extern __shared__ int s_end[];   // [owners]
   __shared__ int s_wave[kSumWaves];
   const int lane = threadIdx.x % kWave;
-  if (int(blockIdx.x) >= a.workers) {   // a row, or a segment of one
-    const uint32_t b = blockIdx.x - uint32_t(a.workers), id = b / uint32_t(a.segments), i = b % uint32_t(a.segments) * kSumNT + threadIdx.x;
-    const u32x4_t zero = {0u, 0u, 0u, 0u};
-    if (!a.there[id] && i < uint32_t(a.H) / Storage<OUT>::kPerVec)
-      __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_t*>(row_ptr<OUT>(a.table, id, a.H)) + i);
+  if (int(blockIdx.x) >= a.workers) {
+    put_zeros<OUT>(a, (a.zeros_from + (blockIdx.x - uint32_t(a.workers))) * (kSumNT * Z));
     return;
   }
   const int first = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kSumWaves + int(threadIdx.x) / kWave), waves = a.workers * kSumWaves;
   // ---- pieces of frequent ids, by column blocks ----
   const int blocks = (a.H + Sums::kBlock - 1) / Sums::kBlock;
-  int64_t units = int64_t(scan_owners(a.n.heavy, a.owners, s_end, s_wave, 1)) * blocks;
+  int64_t units = int64_t(scan_owners(a.n.heavy, a.owners, s_end, s_wave)) * blocks;
   for (int64_t u = first; u < units; u += waves) {
     int k;
     const int g = find_owner(s_end, a.owners, int(u / blocks), k);
@@ -443,24 +484,22 @@ template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT) void k
     const int own = lane < p.count ? a.order[p.start + lane] : 0;   // lane k: the piece's k-th token
     const int c = int(u % blocks) * Sums::kBlock + lane * E;
     float sum[1][E] = {};
-    constexpr int R = 8;
+    constexpr int R = sizeof(typename Sums::Raw) > 16 ? 4 : 8;
     for (int k0 = 0; k0 < p.count; k0 += R) {
       int token[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) token[r] = __builtin_amdgcn_readlane(own, min(k0 + r, p.count - 1));
       Sums::template add<R, 1>(a, token, p.count - k0, c, sum);
     }
-    if (c < a.H) {
-      if (p.row < 0) {
-        put_sums<OUT, E>(row_ptr<OUT>(a.table, p.id, a.H, c), sum[0], a.scale, a.accumulate != 0);
-      } else {
+    if (p.row < 0) {
+      Sums::put(a, p.id, c, sum[0]);
+    } else if (c < a.H) {   // columns that overlap have the same sums
 #pragma unroll
-        for (int e = 0; e < E; ++e) a.partial[size_t(p.row) * a.H + c + e] = sum[0][e];
-      }
+      for (int e = 0; e < E; ++e) a.partial[size_t(p.row) * a.H + Sums::column(a, c) + e] = sum[0][e];
     }
   }
   // ---- whole rows of the others ----
-  units = scan_owners(a.n.few, a.owners, s_end, s_wave, 1);
+  units = scan_owners(a.n.few, a.owners, s_end, s_wave);
   for (int64_t u = first; u < units; u += waves) {
     int k;
     const int g = find_owner(s_end, a.owners, int(u), k);
@@ -468,29 +507,10 @@ template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT) void k
     const int own = lane < p.count ? a.order[p.start + lane] : 0;
     static_assert(kFew == 4, "cases below");
     switch (p.count) {   // uniform
-      case 1: Sums::template row<1, 8>(a, p, own); break;
-      case 2: Sums::template row<2, 4>(a, p, own); break;
-      case 3: Sums::template row<3, 4>(a, p, own); break;
-      default: Sums::template row<4, 4>(a, p, own);
-    }
-  }
-  if (a.accumulate || a.segments) return;   // uniform
-  // ---- zeros ----
-  units = scan_owners(a.n.none, a.owners, s_end, s_wave, kZeroRows);
-  for (int64_t u = first; u < units; u += waves) {
-    int k;
-    const int g = find_owner(s_end, a.owners, int(u), k);
-    const int n = min(a.n.none[g] - k * kZeroRows, kZeroRows);
-    const int id = lane < n ? a.none[int64_t(g) * kBins + k * kZeroRows + lane] : 0;
-    for (int r = 0; r < n; ++r) {
-      const int64_t at = __builtin_amdgcn_readlane(id, r);
-      char* const row = row_ptr<OUT>(a.table, at, a.H);
-      const RowGeom geom = row_geom<OUT>(a.table, at, a.H, a.H);
-      const u32x4_t zero = {0u, 0u, 0u, 0u};
-      for (int i = lane; i < geom.nvec; i += kWave)
-        __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_t*>(row + geom.head * Storage<OUT>::kBytes) + i);
-      const int j = ragged_elt<OUT>(geom, a.H, lane);
-      if (j >= 0) store_elt<OUT>(row, j, 0.f);
+      case 1: Sums::template row<1, Sums::blocks(1)>(a, p, own); break;
+      case 2: Sums::template row<2, Sums::blocks(2)>(a, p, own); break;
+      case 3: Sums::template row<3, Sums::blocks(3)>(a, p, own); break;
+      default: Sums::template row<4, Sums::blocks(4)>(a, p, own);
     }
   }
 }
@@ -501,7 +521,7 @@ __global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a, const Whole*
   extern __shared__ int s_end[];   // [owners]
   __shared__ int s_wave[kSumWaves];
   const int blocks = (a.H + kSumNT - 1) / kSumNT;
-  const int64_t units = int64_t(scan_owners(a.n.whole, a.owners, s_end, s_wave, 1)) * blocks;
+  const int64_t units = int64_t(scan_owners(a.n.whole, a.owners, s_end, s_wave)) * blocks;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     int k;
     const int g = find_owner(s_end, a.owners, int(u / blocks), k);
@@ -519,7 +539,7 @@ __global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a, const Whole*
       for (int e = 0; e < 8; ++e) sum[0] += y[e];
     }
     for (; r < w.pieces; ++r) sum[0] += x[size_t(r) * a.H];
-    put_sums<OUT, 1>(row_ptr<OUT>(a.table, w.id, a.H, c), sum, a.scale, a.accumulate != 0);
+    put_sums<OUT, 1>(row_ptr<OUT>(a.table, w.id, a.H, c), sum, 0, a.scale, a.accumulate != 0);
   }
 }
 
@@ -536,24 +556,26 @@ struct EmbedArgs {
   int32_t* err_flag;
 };
 
+constexpr int kWorkers = 6;                       // to a CU: 16384 tokens of 1000 ids, width 3584, 4 / 6 / 8: 67.7 / 63.3 / 63.1 us
+constexpr int64_t kMaxZeros = int64_t(1) << 23;   // workgroups of a launch: half of the threads that a grid may have
 template <int DT, int OUT> static void embed_bwd_launch(const EmbedArgs& a, void* workspace, hipStream_t s) {
   const EmbedWorkspace w = embed_workspace(workspace, a.T, a.V, a.H);
   const int owners = embed_owners(a.V), log_owners = __builtin_ctz(unsigned(owners));
   hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.order, w.piece, w.whole,
-                     w.none, w.there, w.n, a.err_flag);
-  // a vector of the table and the same columns of dout, as 8, 16 or 32 bytes
-  constexpr int E = Storage<OUT>::kPerVec, kLoad = E * Storage<DT>::kBytes < 16 ? E * Storage<DT>::kBytes : 16;
-  const bool vec = a.H % E == 0 && reinterpret_cast<uintptr_t>(a.table) % 16 == 0 && a.ld * Storage<DT>::kBytes % kLoad == 0 &&
-                   reinterpret_cast<uintptr_t>(a.dout) % kLoad == 0;
-  const int64_t segments = (int64_t(a.H) / E + kSumNT - 1) / kSumNT;
-  const bool by_address = !a.accumulate && a.H % E == 0 && reinterpret_cast<uintptr_t>(a.table) % 16 == 0 &&
-                          grid_fits(a.V * segments + 8 * compute_units(), kSumNT);
-  const int workers = (by_address ? 4 : 8) * compute_units();   // 32768 tokens of width 3584, 2 / 4 / 6 / 8 to a CU: 142 / 127 / 130 / 133 us
-  const EmbedSums sums{a.dout, a.ld, a.H, owners, w.order, w.piece, w.none, w.there, w.n, a.scale, a.accumulate, workers,
-                       by_address ? int(segments) : 0, w.partial, a.table};
+                     w.there, w.n, a.err_flag);
+  constexpr int E = Storage<OUT>::kPerVec;
+  const bool vec = a.H >= E;
+  const int workers = kWorkers * compute_units();
+  const int64_t zeros = a.accumulate ? 0 : (int64_t(a.V) * a.H + int64_t(kSumNT) * E - 1) / (int64_t(kSumNT) * E);
+  EmbedSums sums{a.dout, a.ld, a.H, owners, w.order, w.piece, w.there, w.n, a.scale, a.accumulate, 1.0 / a.H, a.V, workers, 0, w.partial, a.table};
   const auto sum = vec ? k_embed_sum<DT, OUT, true> : k_embed_sum<DT, OUT, false>;
   const size_t lds = size_t(owners) * 4;   // at most 64 KB
-  hipLaunchKernelGGL(sum, dim3(unsigned(workers + (by_address ? a.V * segments : 0))), dim3(kSumNT), lds, s, sums);
+  hipLaunchKernelGGL(sum, dim3(unsigned(workers + std::min(zeros, kMaxZeros))), dim3(kSumNT), lds, s, sums);
+  sums.workers = 0;
+  for (int64_t from = kMaxZeros; from < zeros; from += kMaxZeros) {
+    sums.zeros_from = uint64_t(from);
+    hipLaunchKernelGGL(sum, dim3(unsigned(std::min(zeros - from, kMaxZeros))), dim3(kSumNT), lds, s, sums);
+  }
   if (a.T > kPiece)
     hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(4 * compute_units())), dim3(kSumNT), lds, s, sums, w.whole);
 }
@@ -561,14 +583,12 @@ template <int DT, int OUT> static void embed_bwd_launch(const EmbedArgs& a, void
 template <int DT>
 static void embed_fwd_launch(const void* table, int V, int H, const int32_t* ids, int64_t T, float scale, void* out, int64_t ld_out,
                              int32_t* err_flag, hipStream_t s) {
-  constexpr int E = Storage<DT>::kPerVec;
-  const bool vec = H % E == 0 && ld_out % E == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
+  const bool vec = H >= Storage<DT>::kPerVec;
   const auto fwd = vec ? k_embed_fwd<DT, true> : k_embed_fwd<DT, false>;
   hipLaunchKernelGGL(fwd, dim3(unsigned(T)), dim3(256), 0, s, table, V, H, ids, scale, out, ld_out, err_flag);
 }
 
 constexpr int kMaxWidth = 1 << 20;
-
 
 }  // namespace aero
 

@@ -112,6 +112,11 @@ template <int DT> __device__ __forceinline__ float widen(uint32_t raw) {
   else return __uint_as_float(raw);
 }
 
+// 16 bytes, or four floats, at any element's alignment: the same instructions, which the machine takes at any address.
+typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32x2_any_t __attribute__((ext_vector_type(2), aligned(1)));
+typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+
 // One row as E-element vectors (VEC: 16 bytes between the ragged ends; otherwise single elements), of which this workgroup looks
 // after [first, last); the ragged ends belong to the part that starts at 0.
 template <int DT, bool VEC> struct RowView {

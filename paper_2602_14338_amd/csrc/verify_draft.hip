@@ -221,8 +221,6 @@ template <int NT> __device__ __forceinline__ uint64_t block_drawn(Drawn d, uint6
 }
 
 // E elements from column j on, or floats, at any element's alignment.
-typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(1)));
-typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
 template <int DT, bool VEC> __device__ __forceinline__ u32x4_t load_elts(const char* row, int j) {
   if constexpr (VEC) return *reinterpret_cast<const u32x4_any_t*>(row + int64_t(j) * Storage<DT>::kBytes);
   else return u32x4_t{__float_as_uint(load_elt<DT>(row, j)), 0u, 0u, 0u};

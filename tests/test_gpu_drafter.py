@@ -555,10 +555,45 @@ def test_embedding_gradient_of_uneven_tokens(gh, ids_of):
         check_embed_bwd(T, V, H, H, "bf16", "f32", accumulate, ids, err=2 if ids_of == "bad" else 0)
 
 
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,H,off", [(1, 1, 1, 1), (9, 700, 3, 3), (30, 400, 24, 1), (64, 300, 257, 5), (5, 1000, 8, 0), (300, 40, 1001, 2)])
+def test_embedding_gradient_within_its_table(gh, T, V, H, off, grad):
+    """A table at any element of a buffer: the same bits as elsewhere, and nothing outside it is written."""
+    import paper_2602_14338_amd as aero
+    dout, _ = stored(normal([T, V, H], T, H, 1.0), "bf16")
+    ids = token_ids(4, T, V)
+    want, _ = run_embed_bwd(dout, T, H, H, ids, V, 0.75, grad, False)
+    buf = sevens(1, off + V * H + 64, grad).reshape(-1)
+    table = buf[off:off + V * H].reshape(V, H)
+    aero.aero_embedding_bwd(dout, T, H, H, torch.from_numpy(ids).to("cuda"), V, 0.75, table, workspace("OP_EMBEDDING_BWD", T=T, V=V, H=H))
+    torch.cuda.synchronize()
+    raw = {2: torch.int16, 4: torch.int32}[table.element_size()]
+    assert torch.equal(table.view(raw), want.reshape(V, H).view(raw))
+    assert bool((buf[:off] == 7.0).all()) and bool((buf[off + V * H:] == 7.0).all())
+
+
 def test_embedding_gradient_of_large_tables(gh):
     """More ids than 256 workgroups count, and lengths around a workgroup's step."""
     for T, V in ((4096, 300000), (4097, 262145), (8191, 151936)):
         check_embed_bwd(T, V, 8, 8, "bf16", "f32", False, token_ids(3, T, V))
+
+
+def test_embedding_gradient_of_a_table_past_32_bits(gh):
+    """Elements and bytes past 2^32, and more zeros than one launch writes; rows looked up from it at the same places."""
+    import paper_2602_14338_amd as aero
+    T, V, H = 40, 1 << 24, 513
+    ids = np.random.default_rng(5).integers(0, V, T).astype(np.int32)
+    ids[:4] = (0, V - 1, V - 2, V // 2)
+    dout, host = stored(normal([T, H], T, H, 1.0), "f32")
+    table = torch.full((V, H), 7.0, device="cuda")
+    dev = torch.from_numpy(ids).to("cuda")
+    aero.aero_embedding_bwd(dout, T, H, H, dev, V, 0.5, table, workspace("OP_EMBEDDING_BWD", T=T, V=V, H=H))
+    out = torch.empty((T, H), device="cuda")
+    aero.aero_embedding_fwd(table, V, H, dev, T, 2.0, out, H)
+    torch.cuda.synchronize()
+    assert len(set(ids.tolist())) == T and np.array_equal(wide(out).reshape(T, H), host.reshape(T, H))
+    total = sum(int(table[v:v + (1 << 20)].count_nonzero()) for v in range(0, V, 1 << 20))
+    assert total == np.count_nonzero(host)
 
 
 def test_embedding_gradient_without_tokens(gh):
