@@ -8,6 +8,7 @@
 // that no token has, 16 bytes a thread in the order of their addresses: that writes 6.5 TB/s, workgroups that walk over rows 5.2.
 // Ids with several pieces are joined in order in a third.
 #include <algorithm>
+#include <type_traits>
 
 #include "row_scan.h"
 
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const void* __restrict__ tabl
 // ---- gradient ----
 constexpr int kSortNT = 1024, kSortWaves = kSortNT / kWave;
 constexpr int kSortRuns = 8, kSortEach = 4, kSortRun = kSortNT * kSortEach, kSortChunk = kSortRun * kSortRuns;   // tokens that a sorting workgroup holds
-constexpr int kListed = 4096;                            // of its own among them
+constexpr int kListed = 16384;                           // of its own among them that it places at a time
 constexpr int kLogBins = 10, kBins = 1 << kLogBins;      // ids of a sorting workgroup
 constexpr int kMinOwners = 256;                          // sorting workgroups, a power of two
 constexpr int kPiece = 32;                               // tokens of a frequent id that one wave adds up
@@ -107,6 +108,18 @@ size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H) {
   return embed_workspace(nullptr, T, V > 0 ? V : 1, H > 0 ? H : 0).bytes;
 }
 
+// Inclusive sums over the lanes of a wave, lane by lane in the registers (LDS is not taken).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  const auto plus = [&](auto ctrl, auto rows) { x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), ctrl.value, rows.value, 0xf, true)); };
+  plus(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // 1, 2, 4, 8 lanes along a row of 16
+  plus(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  plus(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  plus(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  plus(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // a row's last lane to the row behind it
+  plus(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // the first half's last lane to the second half
+  return x;
+}
+
 // Workgroup g owns the ids with id % owners == g.  A chunk of tokens is kSortRuns runs, of which a thread holds kSortEach tokens that follow
 // each other: (run, thread, number) is their order.
 __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restrict__ ids, int64_t T, int V, int log_owners,
@@ -115,8 +128,9 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   __shared__ int s_count[kBins], s_at[kBins];
   __shared__ int s_wave[2][kSortWaves], s_run[kSortRuns * kSortWaves], s_all;
   __shared__ int s_n[3];
-  __shared__ int32_t s_tok[kListed];
-  __shared__ uint16_t s_bin[kListed];
+  __shared__ uint32_t s_list[kListed];                // own tokens in order: place in the chunk << kLogBins | id
+  static_assert(uint64_t(kSortChunk) << kLogBins <= uint64_t(1) << 32 && kListed < 1 << 16, "a word each; counts of half a word");
+  __shared__ uint32_t s_seg[kSortWaves][kBins / 2];   // listed tokens of an id in a wave's segment; ids 2 k and 2 k + 1 share a word
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int g = blockIdx.x, mask = (1 << log_owners) - 1;
   const int bins = (V - g + mask) >> log_owners;   // ids g, g + owners, ... below V
@@ -186,13 +200,21 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   // ---- pieces, in whatever order ----
   const int id_mine = (tid << log_owners) + g;
   if (tid < bins) there[id_mine] = mine > 0;
+  const int np = mine > kFew ? (mine + kPiece - 1) / kPiece : 0;
+  const int row = 2 * (start / kPiece);   // np <= 2 (mine / kPiece): the next id's rows lie behind
+  int at = 0;
   if (mine > kFew) {
-    const int np = (mine + kPiece - 1) / kPiece, row = 2 * (start / kPiece);   // np <= 2 (mine / kPiece): the next id's rows lie behind
-    const int at = base + atomicAdd(&s_n[0], np);
-    for (int k = 0; k < np; ++k) pieces[at + k] = Piece{id_mine, start + k * kPiece, min(kPiece, mine - k * kPiece), np == 1 ? -1 : row + k};
+    at = base + atomicAdd(&s_n[0], np);
     if (np > 1) wholes[base + atomicAdd(&s_n[2], 1)] = Whole{id_mine, row, np, 0};
+    else pieces[at] = Piece{id_mine, start, mine, -1};
   } else if (mine > 0) {
     pieces[base + total - 1 - atomicAdd(&s_n[1], 1)] = Piece{id_mine, start, mine, -1};
+  }
+  for (uint64_t m = __builtin_amdgcn_ballot_w64(np > 1); m != 0; m &= m - 1) {   // several pieces: by all lanes (one lane, 1024 of them: 45 us)
+    const int l = __builtin_ctzll(m);
+    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    for (int k = lane; k < of(np); k += kWave)
+      pieces[of(at) + k] = Piece{of(id_mine), of(start) + k * kPiece, min(kPiece, of(mine) - k * kPiece), of(row) + k};
   }
   __syncthreads();
   if (tid == 0) {
@@ -206,18 +228,19 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   if (total == 0) return;
   for (int64_t t0 = 0; t0 < T; t0 += kSortChunk) {
     if (T > kSortChunk) load(t0, false);   // a single chunk is still there
-    int ahead[kSortRuns];   // of the wave's own tokens of the run, those of the lanes in front
+    // own tokens of the run in the lanes in front, and in the wave: three runs to a word (a wave has 256 tokens of a run)
+    int ahead[kSortRuns];
 #pragma unroll
-    for (int r = 0; r < kSortRuns; ++r) {
-      int in_wave = 0;
-      ahead[r] = 0;
+    for (int r0 = 0; r0 < kSortRuns; r0 += 3) {
+      uint32_t mine3 = 0;
 #pragma unroll
-      for (int u = 0; u < kSortEach; ++u) {
-        const uint64_t m = __builtin_amdgcn_ballot_w64((own >> (kSortEach * r + u) & 1) != 0);
-        ahead[r] += __popcll(m & below);
-        in_wave += __popcll(m);
+      for (int r = r0; r < kSortRuns && r < r0 + 3; ++r) mine3 |= uint32_t(__popc(own >> (kSortEach * r) & ((1u << kSortEach) - 1))) << (10 * (r - r0));
+      const uint32_t up_to = wave_scan(mine3);
+#pragma unroll
+      for (int r = r0; r < kSortRuns && r < r0 + 3; ++r) {
+        ahead[r] = int((up_to - mine3) >> (10 * (r - r0)) & 1023);
+        if (lane == kWave - 1) s_run[r * kSortWaves + wave] = int(up_to >> (10 * (r - r0)) & 1023);
       }
-      if (lane == 0) s_run[r * kSortWaves + wave] = in_wave;
     }
     __syncthreads();
     static_assert(kSortRuns * kSortWaves == 2 * kWave, "two counts per lane");
@@ -239,39 +262,83 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
       if (own != 0) {
 #pragma unroll
         for (int r = 0; r < kSortRuns; ++r) {
+          if ((own >> (kSortEach * r) & ((1u << kSortEach) - 1)) == 0) continue;
           int at = s_run[r * kSortWaves + wave] + ahead[r] - from;
 #pragma unroll
           for (int u = 0; u < kSortEach; ++u) {
             if (own >> (kSortEach * r + u) & 1) {
-              if (at >= 0 && at < kListed) {
-                s_tok[at] = int32_t(t0 + r * kSortRun + tid * kSortEach + u);
-                s_bin[at] = uint16_t(id[r][u] >> log_owners);
-              }
+              if (at >= 0 && at < kListed)
+                s_list[at] = uint32_t(r * kSortRun + tid * kSortEach + u) << kLogBins | uint32_t(id[r][u] >> log_owners);
               ++at;
             }
           }
         }
       }
       __syncthreads();
-      // 64 at a time by the first wave: a token's place is its id's next one plus the lanes in front with the same id
+      // 64 at a time: a token's place is its id's next one plus the lanes in front with the same id
       const int listed = min(n - from, kListed);
-      if (wave == 0) {
-        for (int k0 = 0; k0 < listed; k0 += kWave) {
-          const int k = k0 + lane;
-          const bool in = k < listed;
-          const int bin = in ? s_bin[k] : 0;
-          uint64_t same = __builtin_amdgcn_ballot_w64(in);
+      auto same_id = [&](int k, int end, int& bin, int32_t& token) {   // lanes with the id of token k
+        const bool in = k < end;
+        const uint32_t x = in ? s_list[k] : 0;
+        bin = int(x & (kBins - 1));
+        token = int32_t(t0 + (x >> kLogBins));
+        uint64_t same = __builtin_amdgcn_ballot_w64(in);
 #pragma unroll
-          for (int bit = 0; bit < kLogBins; ++bit) {
-            const uint64_t m = __builtin_amdgcn_ballot_w64((bin >> bit & 1) != 0);
-            same &= (bin >> bit & 1) != 0 ? m : ~m;
+        for (int bit = 0; bit < kLogBins; ++bit) {
+          const uint64_t m = __builtin_amdgcn_ballot_w64((bin >> bit & 1) != 0);
+          same &= (bin >> bit & 1) != 0 ? m : ~m;
+        }
+        return same;
+      };
+      if (listed <= kWave) {
+        if (wave == 0) {
+          int bin, token;
+          const uint64_t same = same_id(lane, listed, bin, token);
+          if (lane < listed) {
+            const int rank = __popcll(same & below), at = s_at[bin];
+            order[at + rank] = token;
+            if (rank == 0) s_at[bin] = at + __popcll(same);   // behind the read by every lane of the id: one wave, in step
           }
-          if (in) {
-            const int rank = __popcll(same & below);
-            const int first = s_at[bin];
-            order[first + rank] = s_tok[k];
-            if (rank == 0) s_at[bin] = first + __popcll(same);   // behind the read by every lane of the id: one wave, in step
+        }
+      } else {
+        // A segment of the list to each wave, which counts its ids; a thread per two ids turns the counts into offsets.  (All by one wave:
+        // 253 us for 32768 tokens of one id, 28 instead of 19 for ids whose frequency falls as 1 / rank.)
+        const int each = (listed + kSortNT - 1) / kSortNT * kWave, segs = (listed + each - 1) / each;
+        const int k0 = wave * each, k1 = min(k0 + each, listed);
+        if (wave < segs) {
+#pragma unroll
+          for (int k = 0; k < kBins / 2 / kWave; ++k) s_seg[wave][k * kWave + lane] = 0;
+          __builtin_amdgcn_wave_barrier();
+          for (int k = k0 + lane; k < k1; k += kWave) {
+            const uint32_t bin = s_list[k] & (kBins - 1);
+            atomicAdd(&s_seg[wave][bin / 2], bin % 2 ? 0x10000u : 1u);
           }
+        }
+        __syncthreads();
+        uint32_t up_to = 0;
+        if (tid < kBins / 2)
+          for (int w = 0; w < segs; ++w) {
+            const uint32_t x = s_seg[w][tid];
+            s_seg[w][tid] = up_to;
+            up_to += x;   // at most kListed in either half
+          }
+        __syncthreads();
+        for (int k = k0; k < k1; k += kWave) {
+          int bin, token;
+          const uint64_t same = same_id(k + lane, k1, bin, token);
+          if (k + lane < k1) {
+            const int rank = __popcll(same & below), shift = bin % 2 * 16;
+            const uint32_t offset = s_seg[wave][bin / 2] >> shift & 0xffffu;
+            order[s_at[bin] + int(offset) + rank] = token;
+            __builtin_amdgcn_wave_barrier();   // behind the read by every lane of the word
+            if (rank == 0) atomicAdd(&s_seg[wave][bin / 2], uint32_t(__popcll(same)) << shift);
+          }
+          __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        if (tid < kBins / 2) {
+          s_at[2 * tid] += int(up_to & 0xffffu);
+          s_at[2 * tid + 1] += int(up_to >> 16);
         }
       }
       __syncthreads();
@@ -515,31 +582,37 @@ template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT, 6) voi
   }
 }
 
-// Ids with several pieces: workgroup by (id, kSumNT columns).
+// Ids with several pieces: workgroup by (id, kWave columns), a quarter of the pieces to each wave.
 template <int OUT>
 __global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a, const Whole* __restrict__ wholes) {
   extern __shared__ int s_end[];   // [owners]
   __shared__ int s_wave[kSumWaves];
-  const int blocks = (a.H + kSumNT - 1) / kSumNT;
+  __shared__ float s_sum[kSumWaves][kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int blocks = (a.H + kWave - 1) / kWave;
   const int64_t units = int64_t(scan_owners(a.n.whole, a.owners, s_end, s_wave)) * blocks;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     int k;
     const int g = find_owner(s_end, a.owners, int(u / blocks), k);
     const Whole w = wholes[a.n.base[g] + k];
-    const int c = int(u % blocks) * kSumNT + threadIdx.x;
-    if (c >= a.H) continue;
-    const float* const x = a.partial + size_t(w.row) * a.H + c;
-    float sum[1] = {0.f};
-    int r = 0;
-    for (; r + 8 <= w.pieces; r += 8) {
+    const int c = int(u % blocks) * kWave + lane;
+    const float* const x = a.partial + size_t(w.row) * a.H + min(c, a.H - 1);
+    const int each = (w.pieces + kSumWaves - 1) / kSumWaves, last = min((wave + 1) * each, w.pieces);
+    float sum = 0.f;
+    for (int r = wave * each; r < last; r += 8) {
       float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[size_t(r + e) * a.H];
+      for (int e = 0; e < 8; ++e) y[e] = x[size_t(min(r + e, last - 1)) * a.H];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[0] += y[e];
+      for (int e = 0; e < 8; ++e)
+        if (r + e < last) sum += y[e];
     }
-    for (; r < w.pieces; ++r) sum[0] += x[size_t(r) * a.H];
-    put_sums<OUT, 1>(row_ptr<OUT>(a.table, w.id, a.H, c), sum, 0, a.scale, a.accumulate != 0);
+    s_sum[wave][lane] = sum;
+    __syncthreads();
+    static_assert(kSumWaves == 4, "sums of a column");
+    const float all[1] = {(s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane])};
+    if (wave == 0 && c < a.H) put_sums<OUT, 1>(row_ptr<OUT>(a.table, w.id, a.H, c), all, 0, a.scale, a.accumulate != 0);
+    __syncthreads();   // s_sum is free again
   }
 }
 
