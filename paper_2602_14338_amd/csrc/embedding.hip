@@ -8,7 +8,6 @@
 // that no token has, 16 bytes a thread in the order of their addresses: that writes 6.5 TB/s, workgroups that walk over rows 5.2.
 // Ids with several pieces are joined in order in a third.
 #include <algorithm>
-#include <type_traits>
 
 #include "row_scan.h"
 
@@ -106,18 +105,6 @@ static EmbedWorkspace embed_workspace(void* base, int64_t T, int32_t V, int64_t 
 }
 size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H) {
   return embed_workspace(nullptr, T, V > 0 ? V : 1, H > 0 ? H : 0).bytes;
-}
-
-// Inclusive sums over the lanes of a wave, lane by lane in the registers (LDS is not taken).
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-  const auto plus = [&](auto ctrl, auto rows) { x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), ctrl.value, rows.value, 0xf, true)); };
-  plus(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // 1, 2, 4, 8 lanes along a row of 16
-  plus(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
-  plus(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
-  plus(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
-  plus(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // a row's last lane to the row behind it
-  plus(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // the first half's last lane to the second half
-  return x;
 }
 
 // Workgroup g owns the ids with id % owners == g.  A chunk of tokens is kSortRuns runs, of which a thread holds kSortEach tokens that follow

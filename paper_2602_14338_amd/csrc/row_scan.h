@@ -1,6 +1,8 @@
 // Rows of logits that may be masked: their log-partition, and walks over their vectors that a workgroup or a part of
 // one makes.  Shared by the calls around a drafter (top-K lists, distillation, verification).
 #pragma once
+#include <type_traits>
+
 #include "aero_device.h"
 
 namespace aero {
@@ -97,6 +99,18 @@ __device__ __forceinline__ double soft_lse(SoftSum st) {
   }
   const double lse = (double(st.o) + double(k) + double(logf(f)) * 1.4426950408889634) * (1.0 / double(kLog2e));
   return st.o < INFINITY && st.s == st.s ? lse : __builtin_nan("");
+}
+
+// Inclusive sums over the lanes of a wave, lane by lane in the registers (LDS is not taken).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  const auto plus = [&](auto ctrl, auto rows) { x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), ctrl.value, rows.value, 0xf, true)); };
+  plus(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // 1, 2, 4, 8 lanes along a row of 16
+  plus(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  plus(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  plus(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  plus(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // a row's last lane to the row behind it
+  plus(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // the first half's last lane to the second half
+  return x;
 }
 
 // An element as it is stored, to be widened where it is needed: a conversion next to the load waits for it there.

@@ -1,8 +1,8 @@
 // The K largest logits of each row with their log-probs, and the row's log-partition, in one pass over the row.
 //
-// While the row streams by, each thread notes the largest logit of every kGroup of its vectors in LDS, 16 bits of it (the maximum of a
-// vector is formed for the running offset anyway): 152K logits of 16 bits leave 9.5K numbers.  A threshold that at least
-// K logits reach follows from the threads' own maxima, joined into about 2 K of them: the K-th largest of these, found digit by digit by one wave.
+// A short row is held in registers.  While a long one streams by, each thread notes the largest logit of every kGroup of its vectors in
+// LDS, 16 bits of it (the maximum of a vector is formed for the running offset anyway): 152K logits of 16 bits leave 9.5K numbers.  A threshold that at least
+// K logits reach follows from the threads' own maxima, joined into about 2 K of them: the K-th largest of these, found bit by bit by one wave.
 // Groups that reach it, little more than K, are read again, all at once and out of the caches, and what reaches it among their logits are the
 // candidates.  A candidate's rank is the count of larger ones; pairs of value and id are distinct, so the order is total and ties
 // go to the lower id.
@@ -10,14 +10,16 @@
 // wave, 3.4 times the time of the whole call at 4096 x 151936 bf16.)
 // Rows with more candidates than fit (thousands of equal logits at the threshold) are selected digit by digit over their keys, nine more passes.
 #include <algorithm>
+#include <type_traits>
 
 #include "row_scan.h"
 
 namespace aero {
 
 constexpr int kGroup = 2, kAhead = 2;   // vectors of a group, groups of a batch
-constexpr int kGroupMax = 10240;      // maxima that are noted; longer rows note one for several groups
-constexpr int kCandidates = 1792, kHits = 1024;
+// Maxima that are noted; longer rows note one for several groups.
+constexpr int group_max(int threads) { return threads == 256 ? 2048 : 10240; }
+constexpr int kCandidates = 1536, kHits = 1024;
 
 // The order of floats as that of whole numbers; -0 and 0 are the same.
 __device__ __forceinline__ uint32_t float_order(float z) {
@@ -36,7 +38,7 @@ __device__ __forceinline__ int key_id(uint64_t key) { return int(~uint32_t(key))
 
 // A lower bound on the K-th largest of the NT numbers in `best` (-inf: none), -inf where there are no K of them; by one wave.  They are joined
 // into N x 64 maxima, K <= 32 N, of which at least as many reach it: for K = 64 joining 512 into 128 makes 89 of 68 candidates, and only
-// one wave counts (16 waves that each count their own lanes share the CU's one scalar unit: 6 times as long).  Digits of two bits, from the
+// one wave counts (16 waves that each count their own lanes share the CU's one scalar unit: 6 times as long).  Bit by bit, from the
 // counts of lanes that reach a number; 18 bits tell all 16- and 8-bit logits apart and leave a bound for the others.
 template <int NT, int N> __device__ __forceinline__ float top_threshold(const float* best, int K) {
   constexpr int kJoined = NT / (kWave * N);
@@ -50,16 +52,11 @@ template <int NT, int N> __device__ __forceinline__ float top_threshold(const fl
   }
   uint32_t reached = 0;
 #pragma unroll
-  for (int shift = 30; shift >= 14; shift -= 2) {
-    uint32_t digit = 0;
+  for (int shift = 31; shift >= 14; --shift) {
+    int lanes = 0;
 #pragma unroll
-    for (uint32_t d = 1; d < 4; ++d) {
-      int lanes = 0;
-#pragma unroll
-      for (int n = 0; n < N; ++n) lanes += __popcll(__builtin_amdgcn_ballot_w64(ord[n] >= (reached | d << shift)));
-      digit += lanes >= K;
-    }
-    reached |= digit << shift;
+    for (int n = 0; n < N; ++n) lanes += __popcll(__builtin_amdgcn_ballot_w64(ord[n] >= (reached | 1u << shift)));
+    if (lanes >= K) reached |= 1u << shift;
   }
   const float least = order_float(reached);   // without a logit: at or below -inf's bits
   return least > kMasked ? least : -INFINITY;
@@ -74,17 +71,47 @@ template <int NT> __device__ __forceinline__ float top_threshold_of(const float*
 
 struct TopBuffer {
   uint64_t key[kCandidates];
-  union {
-    uint16_t group[kGroupMax];   // upper halves of the maxima
-    uint32_t hist[256];
-  };
-  uint16_t hit[kHits];
-  int count, hits, digit, left;
+  uint32_t hist[256];
+  int count, digit, left;
 };
+// What is noted while a row streams by.
+template <int NT> struct TopGroups {
+  uint16_t most[group_max(NT)];   // upper halves of the maxima
+  uint16_t hit[kHits];
+  int hits;
+};
+struct NoGroups {};
 
 __device__ __forceinline__ void top_push(TopBuffer& b, uint64_t key) {
   const int at = atomicAdd(&b.count, 1);
   if (at < kCandidates) b.key[at] = key;
+}
+
+// Pushes the logits of U vectors (column -1: none) that reach `least`, behind one count of the wave's (a count for each: 150 cycles one
+// after the other).  By whole waves.
+template <int U, class View> __device__ __forceinline__ void top_push(TopBuffer& b, const View& row, const u32x4_t (&v)[U], const int (&column)[U], float least) {
+  constexpr int E = View::E;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float z[E];
+      row.unpack(v[u], z);
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (column[u] >= 0 && z[e] >= least && z[e] > kMasked) f(z[e], column[u] + e);
+    }
+  };
+  int n = 0;
+  each([&](float, int) { ++n; });
+  if (__builtin_amdgcn_ballot_w64(n > 0) == 0) return;
+  const int up_to = int(wave_scan(uint32_t(n)));
+  int at = 0;
+  if (threadIdx.x % kWave == kWave - 1) at = atomicAdd(&b.count, up_to);
+  at = __builtin_amdgcn_readlane(at, kWave - 1) + up_to - n;
+  each([&](float z, int j) {
+    if (at < kCandidates) b.key[at] = top_key(z, j);
+    ++at;
+  });
 }
 
 // Exactly the K largest keys of [first, last) of the row (fewer where fewer are unmasked), digit by digit.  In place: a call, rare as it
@@ -150,14 +177,182 @@ template <int NT, class Put> __device__ __forceinline__ void top_rank(const TopB
   }
 }
 
+// A part of a row that streams by: its sum, and the largest logit of every group noted.
+template <int NT, int DT, bool VEC> struct Streamed {
+  using View = RowView<DT, VEC>;
+  static constexpr int E = View::E;
+  const View& row;
+  const int first, last;
+  TopGroups<NT>& groups;
+  const int tid = threadIdx.x;
+  const int steps = (last - first + kGroup * NT - 1) / (kGroup * NT);                    // of the workgroup
+  const int fold = max((steps * NT + group_max(NT) - 1) / group_max(NT), 1);             // steps that share a maximum
+
+  __device__ __forceinline__ void read(SoftSum& st, float& best) {
+    float noted = -INFINITY;
+    int i = first + tid;
+    int step = 0, kept = 0, slot = tid;
+    auto note = [&]() {   // the end of a step
+      ++step;
+      if (++kept == fold || step == steps) {
+        groups.most[slot] = uint16_t(__float_as_uint(noted) >> 16);
+        slot += NT;
+        best = fmaxf(best, noted);
+        noted = -INFINITY;
+        kept = 0;
+      }
+    };
+    auto take = [&](const u32x4_t& x) {
+      float z[E];
+      row.unpack(x, z);
+      const float vm = vec_max<E>(z);
+      soft_update<E>(st, z, vm);
+      noted = fmaxf(noted, vm);
+    };
+    // batches of kAhead groups, the next one asked for before this one is used
+    constexpr int kBatch = kAhead * kGroup;
+    u32x4_t ahead[kBatch];
+    auto ask = [&](u32x4_t (&v)[kBatch]) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) v[u] = row.load(i + u * NT);
+    };
+    bool more = i + (kBatch - 1) * NT < last;
+    if (more) ask(ahead);
+    while (more) {
+      u32x4_t v[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) v[u] = ahead[u];
+      i += kBatch * NT;
+      more = i + (kBatch - 1) * NT < last;
+      if (more) ask(ahead);
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) {   // one test of the offset for a group
+        float z[kGroup * E];
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) {
+          float x[E];
+          row.unpack(v[g * kGroup + u], x);
+#pragma unroll
+          for (int e = 0; e < E; ++e) z[u * E + e] = x[e];
+        }
+        const float vm = vec_max<kGroup * E>(z);
+        soft_update<kGroup * E>(st, z, vm);
+        noted = fmaxf(noted, vm);
+        note();
+      }
+    }
+    while (step < steps) {   // note() counts
+      u32x4_t v[kGroup];
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u)
+        if (i + u * NT < last) v[u] = row.load(i + u * NT);
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u)
+        if (i + u * NT < last) take(v[u]);
+      note();
+      i += kGroup * NT;
+    }
+  }
+  // Pushes what reaches `least`; false where the groups that do are more than are listed.  By all threads.
+  __device__ __forceinline__ bool push(TopBuffer& buf, float best, float least) {
+    auto reaches = [&](float z) { return z >= least && z > kMasked; };
+    // ---- groups that reach the threshold: cutting off lower halves keeps the order ----
+    if (reaches(best)) {
+      const float bound = __uint_as_float(__float_as_uint(least) & 0xffff0000u);
+      const int mine = (steps + fold - 1) / fold;
+      for (int g0 = 0; g0 < mine; g0 += 4) {
+        uint32_t code[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) code[u] = groups.most[min(g0 + u, mine - 1) * NT + tid];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float most = __uint_as_float(code[u] << 16);
+          if (g0 + u < mine && most >= bound && most > kMasked) {
+            const int at = atomicAdd(&groups.hits, 1);
+            if (at < kHits) groups.hit[at] = uint16_t((g0 + u) * NT + tid);
+          }
+        }
+      }
+    }
+    __syncthreads();
+    // ---- their logits ----
+    const int hits = groups.hits, span = kGroup * fold;
+    if (hits > kHits) return false;
+    for (int k0 = 0; k0 < hits * span; k0 += 4 * NT) {
+      u32x4_t v[4];
+      int vec[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = min(k0 + u * NT + tid, hits * span - 1), slot = groups.hit[k / span];
+        vec[u] = first + slot % NT + ((slot / NT) * span + k % span) * NT;
+        if (k0 + u * NT + tid >= hits * span || vec[u] >= last) vec[u] = -1;
+        v[u] = row.load_again(max(vec[u], 0));
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float z[E];
+        row.unpack(v[u], z);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (vec[u] >= 0 && reaches(z[e])) top_push(buf, top_key(z[e], row.column(vec[u]) + e));
+      }
+    }
+    return true;
+  }
+};
+
+// A part of at most N vectors per thread, which hold it.
+template <int NT, int DT, bool VEC, int N> struct Held {
+  using View = RowView<DT, VEC>;
+  static constexpr int E = View::E;
+  const View& row;
+  const int first, last;
+  NoGroups& groups;
+  u32x4_t v[N];
+
+  template <class F> __device__ __forceinline__ void each(F f) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int k = first + int(threadIdx.x) + u * NT;
+      if (k < last) f(v[u], k);
+    }
+  }
+  __device__ __forceinline__ void read(SoftSum& st, float& best) {
+    each([&](u32x4_t& x, int k) { x = row.load(k); });
+    float z[E];
+    each([&](const u32x4_t& x, int) {
+      row.unpack(x, z);
+      best = fmaxf(best, vec_max<E>(z));
+    });
+    if (best > kMasked) st.o = soft_offset(best);
+    each([&](const u32x4_t& x, int) {
+      row.unpack(x, z);
+      soft_add<E>(st, z);
+    });
+  }
+  __device__ __forceinline__ bool push(TopBuffer& buf, float best, float least) {
+    if (__builtin_amdgcn_ballot_w64(best >= least && best > kMasked) == 0) return true;
+    int column[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int k = first + int(threadIdx.x) + u * NT;
+      column[u] = k < last ? row.column(k) : -1;
+    }
+    top_push(buf, row, v, column, least);
+    return true;
+  }
+};
+
 // Workgroup (t, part): part of the row's vectors.  With one part the outputs; with several the part's keys in descending order (0:
 // fewer) and sum for k_topk_join.
-template <int NT, int DT, bool VEC>
+template <int NT, int DT, bool VEC, int HELD>   // vectors that a thread holds, 0: the row streams by
 __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, int V, int64_t ld, const uint8_t* __restrict__ row_active,
                                              int K, int32_t* __restrict__ index, float* __restrict__ logprob,
                                              float* __restrict__ lse, uint64_t* __restrict__ part_keys, SoftSum* __restrict__ part_sums) {
-  constexpr int E = RowView<DT, VEC>::E, kWaves = NT / kWave;
+  constexpr int kWaves = NT / kWave;
+  using Part = std::conditional_t<HELD != 0, Held<NT, DT, VEC, HELD>, Streamed<NT, DT, VEC>>;
   __shared__ TopBuffer buf;
+  __shared__ std::conditional_t<HELD != 0, NoGroups, TopGroups<NT>> groups;
   __shared__ float s_best[NT], s_least;
   __shared__ SoftSum s_sum[kWaves];
   const int64_t t = blockIdx.x;
@@ -177,76 +372,14 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   const int first = min(part * per, row.nvec), last = min(first + per, row.nvec);
   if (tid == 0) {
     buf.count = 0;
-    buf.hits = 0;
+    if constexpr (HELD == 0) groups.hits = 0;
   }
-  const int steps = (last - first + kGroup * NT - 1) / (kGroup * NT);          // of the workgroup
-  const int fold = max((steps * NT + kGroupMax - 1) / kGroupMax, 1);           // steps that share a maximum
   const int jr = part == 0 ? row.ragged() : -1;
   const float zr = jr >= 0 ? row.at(jr) : -INFINITY;
   SoftSum st = soft_identity();
-  float best = -INFINITY, noted = -INFINITY;
-  int i = first + tid;
-  int step = 0, kept = 0, slot = tid;
-  auto note = [&]() {   // the end of a step
-    ++step;
-    if (++kept == fold || step == steps) {
-      buf.group[slot] = uint16_t(__float_as_uint(noted) >> 16);
-      slot += NT;
-      best = fmaxf(best, noted);
-      noted = -INFINITY;
-      kept = 0;
-    }
-  };
-  auto take = [&](const u32x4_t& x) {
-    float z[E];
-    row.unpack(x, z);
-    const float vm = vec_max<E>(z);
-    soft_update<E>(st, z, vm);
-    noted = fmaxf(noted, vm);
-  };
-  // batches of kAhead groups, the next one asked for before this one is used
-  constexpr int kBatch = kAhead * kGroup;
-  u32x4_t ahead[kBatch];
-  auto ask = [&](u32x4_t (&v)[kBatch]) {
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u] = row.load(i + u * NT);
-  };
-  bool more = i + (kBatch - 1) * NT < last;
-  if (more) ask(ahead);
-  while (more) {
-    u32x4_t v[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) v[u] = ahead[u];
-    i += kBatch * NT;
-    more = i + (kBatch - 1) * NT < last;
-    if (more) ask(ahead);
-#pragma unroll
-    for (int g = 0; g < kAhead; ++g) {   // one test of the offset for a group
-      float z[kGroup * E];
-#pragma unroll
-      for (int u = 0; u < kGroup; ++u) {
-        float x[E];
-        row.unpack(v[g * kGroup + u], x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) z[u * E + e] = x[e];
-      }
-      const float vm = vec_max<kGroup * E>(z);
-      soft_update<kGroup * E>(st, z, vm);
-      noted = fmaxf(noted, vm);
-      note();
-    }
-  }
-  while (step < steps) {   // note() counts
-    u32x4_t v[kGroup];
-#pragma unroll
-    for (int u = 0; u < kGroup; ++u)
-      if (i + u * NT < last) v[u] = row.load(i + u * NT);
-#pragma unroll
-    for (int u = 0; u < kGroup; ++u)
-      if (i + u * NT < last) take(v[u]);
-    note();
-    i += kGroup * NT;
-  }
+  float best = -INFINITY;
+  Part mine{row, first, last, groups};
+  mine.read(st, best);
   if (jr >= 0) {
     float z[1] = {zr};
     soft_update<1>(st, z);
@@ -261,51 +394,10 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   const double z0 = soft_lse(st);
   __syncthreads();
   const float least = s_least;
-  auto reaches = [&](float z) { return z >= least && z > kMasked; };
-  if (reaches(zr)) top_push(buf, top_key(zr, jr));
-  // ---- groups that reach the threshold: cutting off lower halves keeps the order ----
-  if (reaches(best)) {
-    const float bound = __uint_as_float(__float_as_uint(least) & 0xffff0000u);
-    const int groups = (steps + fold - 1) / fold;
-    for (int g0 = 0; g0 < groups; g0 += 4) {
-      uint32_t code[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) code[u] = buf.group[min(g0 + u, groups - 1) * NT + tid];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float most = __uint_as_float(code[u] << 16);
-        if (g0 + u < groups && most >= bound && most > kMasked) {
-          const int at = atomicAdd(&buf.hits, 1);
-          if (at < kHits) buf.hit[at] = uint16_t((g0 + u) * NT + tid);
-        }
-      }
-    }
-  }
+  if (zr >= least && zr > kMasked) top_push(buf, top_key(zr, jr));
+  const bool listed = mine.push(buf, best, least);
   __syncthreads();
-  // ---- their logits ----
-  const int hits = buf.hits, span = kGroup * fold;
-  if (hits <= kHits)
-    for (int k0 = 0; k0 < hits * span; k0 += 4 * NT) {
-      u32x4_t v[4];
-      int vec[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int k = min(k0 + u * NT + tid, hits * span - 1), slot = buf.hit[k / span];
-        vec[u] = first + slot % NT + ((slot / NT) * span + k % span) * NT;
-        if (k0 + u * NT + tid >= hits * span || vec[u] >= last) vec[u] = -1;
-        v[u] = row.load_again(max(vec[u], 0));
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float z[E];
-        row.unpack(v[u], z);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (vec[u] >= 0 && reaches(z[e])) top_push(buf, top_key(z[e], row.column(vec[u]) + e));
-      }
-    }
-  __syncthreads();
-  if (hits > kHits || buf.count > kCandidates) top_by_digits<NT>(row, first, last, K, buf);   // uniform
+  if (!listed || buf.count > kCandidates) top_by_digits<NT>(row, first, last, K, buf);   // uniform
   const int n = buf.count;
   if (parts > 1) {
     uint64_t* keys = part_keys + (t * parts + part) * K;
@@ -397,14 +489,21 @@ static void topk_launch(const void* logits, int64_t T, int V, int64_t ld, const 
   uint64_t* keys = reinterpret_cast<uint64_t*>(sums + (parts > 1 ? T * parts : 0));
   const dim3 grid{unsigned(T), unsigned(parts)};
   const int per = (nvec + parts - 1) / parts;
-  // 512 / 1024 threads (151936 bf16): 200 rows, K = 16, 64, 256: 21.0 / 19.1, 22.1 / 19.7, 33.5 / 25.8 us; 64 rows split in four 16.2 / 18.3, 17.6 /
-  // 19.3, 32.5 / 28.9; 300 rows 27.8 / 37.3, 4096 242 / 316 at K = 64
   auto launch = [&](auto kernel, int threads) {
     hipLaunchKernelGGL(kernel, grid, dim3(unsigned(threads)), 0, s, logits, V, ld, row_active, K, index, logprob, lse, keys, sums);
   };
-  if (per <= 4 * 256) launch(k_topk<256, DT, VEC>, 256);
-  else if (T * parts <= compute_units() && (parts == 1 || K > 128)) launch(k_topk<1024, DT, VEC>, 1024);
-  else launch(k_topk<512, DT, VEC>, 512);
+  // Held / streaming by: bf16 K = 64, 64 rows of 2399 6.7 / 7.2 us, 4000 of 1024 17.6 / 23.2; fp32, 4000 of 2399 19.6 / 25.2.  Where rows queue,
+  // waiting threads cost more than vectors in turn: 5000 rows of 14464 with 1024 / 256 threads 79 / 47 us, 40 rows 7.1 / 7.8.  Eight vectors held are
+  // no gain: 5000 of 14464 49.6 / 47.3.  More than 128 of 256 maxima would be no threshold.  151936, streaming by 512 / 1024: 200 rows, K = 16, 64,
+  // 256: 21.0 / 19.1, 22.1 / 19.7, 33.5 / 25.8 us; 300 rows 27.8 / 37.3, 4096 242 / 316 at K = 64.
+  const bool many = T > 2 * compute_units();
+  if (K <= 128 && per <= 2 * 256) launch(k_topk<256, DT, VEC, 2>, 256);
+  else if (K <= 128 && per <= 4 * 256 && many) launch(k_topk<256, DT, VEC, 4>, 256);
+  else if (per <= 2 * 512) launch(k_topk<512, DT, VEC, 2>, 512);
+  else if (per <= 2 * 1024 && !many) launch(k_topk<1024, DT, VEC, 2>, 1024);
+  else if (K <= 128 && per <= 4096 && many) launch(k_topk<256, DT, VEC, 0>, 256);
+  else if (T * parts <= compute_units() && (parts == 1 || K > 128)) launch(k_topk<1024, DT, VEC, 0>, 1024);
+  else launch(k_topk<512, DT, VEC, 0>, 512);
   if (parts > 1)
     hipLaunchKernelGGL(k_topk_join, dim3(unsigned(T)), dim3(kJoinNT), 0, s, row_active, K, parts, keys, sums, index, logprob, lse);
 }
@@ -422,7 +521,8 @@ extern "C" aero_status aero_topk_logprob(const void* logits, int32_t dtype, int6
   if (!logits || !index || !logprob) return AERO_ERR_NULL;
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 != 0 || workspace_bytes < topk_workspace_bytes(T, V, K))
     return AERO_ERR_WORKSPACE;
-  const bool vec = rows_alike(logits, nullptr, storage_bytes(dtype));
+  // Element by element where a row has few vectors for K: their maxima hardly make a threshold (64 rows of 2399, K = 256: 20 us for 255)
+  const bool vec = rows_alike(logits, nullptr, storage_bytes(dtype)) && int64_t(V) * storage_bytes(dtype) / 16 >= 2 * K;
   const hipStream_t s = as_stream(stream);
   auto launch = [&](auto dt) {
     constexpr int DT = decltype(dt)::value;

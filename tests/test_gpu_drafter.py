@@ -103,6 +103,16 @@ def test_top(gh, dtype, T, V, K, ld, off):
     check_top(normal([T, V, K], T, V), dtype, K, ld, off)
 
 
+@pytest.mark.parametrize("dtype,V,K", [
+    ("bf16", 2047, 128), ("bf16", 2049, 129), ("bf16", 4095, 256), ("bf16", 4098, 256), ("bf16", 4097, 17), ("bf16", 8193, 128), ("bf16", 8210, 129),
+    ("bf16", 16385, 100), ("bf16", 16400, 1), ("bf16", 32770, 64), ("bf16", 32790, 128), ("f32", 1023, 128), ("f32", 2051, 100), ("f32", 4099, 129),
+    ("f32", 8197, 60), ("f8", 4096, 128), ("f8", 8193, 200), ("f8", 16385, 128), ("f8", 33000, 7)])
+def test_top_where_its_forms_meet(gh, dtype, V, K):
+    """Lengths around what a workgroup holds in registers, with few rows and with more than two per compute unit."""
+    check_top(normal([V, K, 3], 3, V), dtype, K)
+    check_top(normal([V, K, 4], 521, V), dtype, K, ld=V + 1)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32", "f8"])
 @pytest.mark.parametrize("V", [300, 4000, 40000])
 def test_top_of_rows_without_order(gh, dtype, V):
