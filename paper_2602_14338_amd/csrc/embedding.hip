@@ -3,8 +3,9 @@
 // The sort is a launch of independent workgroups, each of which owns the ids that are alike modulo their number: it counts
 // its own ids one by one and the tokens of those in front of it as a whole, and places its tokens in ascending order within an id.
 // Every token is read by every workgroup, out of the caches; nothing passes between workgroups and there are no counters whose order
-// could show.  The sums are a second launch of workgroups that go over two kinds of work, found by halving in the owners' counts:
-// pieces of kPiece tokens of frequent ids by column blocks, and whole rows of the others; and of small workgroups that zero the rows of the ids
+// could show.  A sorted place holds its token and where its id's tokens start and how many they are, so that the sums, a second launch,
+// take the places as they lie: the places of kPiece tokens of an id share the row's columns among them, each of which it sums over all of
+// these tokens, and so every place has the same work, however often its id occurs.  Beside them small workgroups zero the rows of the ids
 // that no token has, 16 bytes a thread in the order of their addresses: that writes 6.5 TB/s, workgroups that walk over rows 5.2.
 // Ids with several pieces are joined in order in a third.
 #include <algorithm>
@@ -51,22 +52,12 @@ constexpr int kSortRuns = 8, kSortEach = 4, kSortRun = kSortNT * kSortEach, kSor
 constexpr int kListed = 16384;                           // of its own among them that it places at a time
 constexpr int kLogBins = 10, kBins = 1 << kLogBins;      // ids of a sorting workgroup
 constexpr int kMinOwners = 256;                          // sorting workgroups, a power of two
-constexpr int kPiece = 32;                               // tokens of a frequent id that one wave adds up
-constexpr int kFew = 4;                                  // up to so many tokens: a wave takes the whole row
+constexpr int kPiece = 32;                               // tokens of an id that are added up at a time
+constexpr int kFew = 4;                                  // up to so many: several column blocks of a wave at a time
 
-// Sorted tokens [start, start + count) of an id.  row: where the sum goes when the id has several pieces, -1: to the table.
-struct Piece {
-  int32_t id, start, count, row;
-};
-// An id with several pieces, whose sums are rows [row, row + pieces).
-struct Whole {
-  int32_t id, row, pieces, pad;
-};
-// How many of each a sorting workgroup has.  Its pieces lie from its first sorted position on: those of frequent ids in front, the
-// others behind, from the last position backwards; its wholes from the same position on.
-struct OwnerCounts {
-  int32_t *heavy, *few, *whole;   // [owners]
-  int32_t *base, *end;            // [owners] first sorted position, and the one behind the last
+// A sorted place: a token, and its id's places [start, start + count).
+struct Sorted {
+  int32_t token, id, start, count;
 };
 
 static int embed_owners(int32_t V) {
@@ -74,12 +65,13 @@ static int embed_owners(int32_t V) {
   while (int64_t(owners) * kBins < V) owners *= 2;
   return owners;
 }
+// First of the rows of partial sums of an id with several pieces; pieces <= 2 (count / kPiece), so that the next id's rows lie behind.
+__host__ __device__ constexpr int piece_row(int start) { return 2 * (start / kPiece); }
+
 struct EmbedWorkspace {
-  int32_t* order;   // [T] tokens sorted by id
-  Piece* piece;     // [T]
-  Whole* whole;     // [T]
+  Sorted* sorted;   // [T]
+  int32_t* n;       // places that are taken
   uint8_t* there;   // [V] a token has the id
-  OwnerCounts n;
   float* partial;   // [2 (T / kPiece + 1)][H]
   size_t bytes;
 };
@@ -91,14 +83,10 @@ static EmbedWorkspace embed_workspace(void* base, int64_t T, int32_t V, int64_t 
     at += (n + 255) / 256 * 256;
     return q;
   };
-  const size_t owners = embed_owners(V);
   EmbedWorkspace w;
-  w.order = reinterpret_cast<int32_t*>(take(size_t(T) * 4));
-  w.piece = reinterpret_cast<Piece*>(take(size_t(T) * sizeof(Piece)));
-  w.whole = reinterpret_cast<Whole*>(take(size_t(T) * sizeof(Whole)));
+  w.sorted = reinterpret_cast<Sorted*>(take(size_t(T) * sizeof(Sorted)));
+  w.n = reinterpret_cast<int32_t*>(take(4));
   w.there = reinterpret_cast<uint8_t*>(take(size_t(V)));
-  int32_t** const counts[] = {&w.n.heavy, &w.n.few, &w.n.whole, &w.n.base, &w.n.end};
-  for (int32_t** c : counts) *c = reinterpret_cast<int32_t*>(take(owners * 4));
   w.partial = reinterpret_cast<float*>(take(size_t(2 * (T / kPiece + 1)) * size_t(H) * 4));
   w.bytes = at + 256;
   return w;
@@ -110,11 +98,10 @@ size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H) {
 // Workgroup g owns the ids with id % owners == g.  A chunk of tokens is kSortRuns runs, of which a thread holds kSortEach tokens that follow
 // each other: (run, thread, number) is their order.
 __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restrict__ ids, int64_t T, int V, int log_owners,
-                                                        int32_t* __restrict__ order, Piece* __restrict__ pieces, Whole* __restrict__ wholes,
-                                                        uint8_t* __restrict__ there, OwnerCounts counts, int32_t* __restrict__ err_flag) {
-  __shared__ int s_count[kBins], s_at[kBins];
+                                                        Sorted* __restrict__ sorted, int32_t* __restrict__ n_sorted,
+                                                        uint8_t* __restrict__ there, int32_t* __restrict__ err_flag) {
+  __shared__ int s_count[kBins], s_start[kBins], s_at[kBins];   // an id's tokens, their first place, the next one's
   __shared__ int s_wave[2][kSortWaves], s_run[kSortRuns * kSortWaves], s_all;
-  __shared__ int s_n[3];
   __shared__ uint32_t s_list[kListed];                // own tokens in order: place in the chunk << kLogBins | id
   static_assert(uint64_t(kSortChunk) << kLogBins <= uint64_t(1) << 32 && kListed < 1 << 16, "a word each; counts of half a word");
   __shared__ uint32_t s_seg[kSortWaves][kBins / 2];   // listed tokens of an id in a wave's segment; ids 2 k and 2 k + 1 share a word
@@ -123,7 +110,6 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   const int bins = (V - g + mask) >> log_owners;   // ids g, g + owners, ... below V
   const uint64_t below = (uint64_t(1) << lane) - 1;
   s_count[tid] = 0;
-  if (tid < 3) s_n[tid] = 0;
   __syncthreads();
   // ---- count ----
   int id[kSortRuns][kSortEach];
@@ -183,34 +169,11 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
     total += s_wave[1][w];
   }
   start += base;
+  s_start[tid] = start;
   s_at[tid] = start;
-  // ---- pieces, in whatever order ----
-  const int id_mine = (tid << log_owners) + g;
-  if (tid < bins) there[id_mine] = mine > 0;
-  const int np = mine > kFew ? (mine + kPiece - 1) / kPiece : 0;
-  const int row = 2 * (start / kPiece);   // np <= 2 (mine / kPiece): the next id's rows lie behind
-  int at = 0;
-  if (mine > kFew) {
-    at = base + atomicAdd(&s_n[0], np);
-    if (np > 1) wholes[base + atomicAdd(&s_n[2], 1)] = Whole{id_mine, row, np, 0};
-    else pieces[at] = Piece{id_mine, start, mine, -1};
-  } else if (mine > 0) {
-    pieces[base + total - 1 - atomicAdd(&s_n[1], 1)] = Piece{id_mine, start, mine, -1};
-  }
-  for (uint64_t m = __builtin_amdgcn_ballot_w64(np > 1); m != 0; m &= m - 1) {   // several pieces: by all lanes (one lane, 1024 of them: 45 us)
-    const int l = __builtin_ctzll(m);
-    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-    for (int k = lane; k < of(np); k += kWave)
-      pieces[of(at) + k] = Piece{of(id_mine), of(start) + k * kPiece, min(kPiece, of(mine) - k * kPiece), of(row) + k};
-  }
+  if (tid < bins) there[(tid << log_owners) + g] = mine > 0;
+  if (tid == 0 && g == mask) *n_sorted = base + total;
   __syncthreads();
-  if (tid == 0) {
-    counts.heavy[g] = s_n[0];
-    counts.few[g] = s_n[1];
-    counts.whole[g] = s_n[2];
-    counts.base[g] = base;
-    counts.end[g] = base + total;
-  }
   // ---- place, in order ----
   if (total == 0) return;
   for (int64_t t0 = 0; t0 < T; t0 += kSortChunk) {
@@ -264,6 +227,10 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
       __syncthreads();
       // 64 at a time: a token's place is its id's next one plus the lanes in front with the same id
       const int listed = min(n - from, kListed);
+      auto put = [&](int place, int token, int bin) {
+        const u32x4_t x = {uint32_t(token), uint32_t((bin << log_owners) + g), uint32_t(s_start[bin]), uint32_t(s_count[bin])};
+        reinterpret_cast<u32x4_t*>(sorted)[place] = x;
+      };
       auto same_id = [&](int k, int end, int& bin, int32_t& token) {   // lanes with the id of token k
         const bool in = k < end;
         const uint32_t x = in ? s_list[k] : 0;
@@ -283,7 +250,7 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
           const uint64_t same = same_id(lane, listed, bin, token);
           if (lane < listed) {
             const int rank = __popcll(same & below), at = s_at[bin];
-            order[at + rank] = token;
+            put(at + rank, token, bin);
             if (rank == 0) s_at[bin] = at + __popcll(same);   // behind the read by every lane of the id: one wave, in step
           }
         }
@@ -316,7 +283,7 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
           if (k + lane < k1) {
             const int rank = __popcll(same & below), shift = bin % 2 * 16;
             const uint32_t offset = s_seg[wave][bin / 2] >> shift & 0xffffu;
-            order[s_at[bin] + int(offset) + rank] = token;
+            put(s_at[bin] + int(offset) + rank, token, bin);
             __builtin_amdgcn_wave_barrier();   // behind the read by every lane of the word
             if (rank == 0) atomicAdd(&s_seg[wave][bin / 2], uint32_t(__popcll(same)) << shift);
           }
@@ -334,45 +301,7 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   }
 }
 
-// Inclusive sums of the owners' counts in LDS, and the owner that the u-th of all lies with (and which of its own it is).
 constexpr int kSumNT = 256, kSumWaves = kSumNT / kWave;
-__device__ __forceinline__ int scan_owners(const int32_t* __restrict__ n, int owners, int* s_end /*[owners]*/, int* s_wave /*[kSumWaves]*/) {
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  int total = 0;
-  __syncthreads();   // s_end may still be in use
-  for (int g0 = 0; g0 < owners; g0 += kSumNT) {   // owners is a multiple of kSumNT
-    int incl = n[g0 + tid];
-#pragma unroll
-    for (int m = 1; m < kWave; m <<= 1) {
-      const int y = __shfl_up(incl, m, kWave);
-      if (lane >= m) incl += y;
-    }
-    if (lane == kWave - 1) s_wave[wave] = incl;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < kSumWaves; ++w) {
-      if (w < wave) incl += s_wave[w];
-      all += s_wave[w];
-    }
-    s_end[g0 + tid] = total + incl;
-    total += all;
-    __syncthreads();
-  }
-  return total;
-}
-__device__ __forceinline__ int find_owner(const int* s_end, int owners, int u, int& own) {
-  int lo = 0, hi = owners - 1;   // the first owner whose end is behind u
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (s_end[mid] > u) hi = mid;
-    else lo = mid + 1;
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  own = u - (lo > 0 ? __builtin_amdgcn_readfirstlane(s_end[lo - 1]) : 0);
-  return lo;
-}
-
 // N sums, scaled, to consecutive columns of the table from the skip-th on: added to what is there, or in its place.
 template <int OUT, int N> __device__ __forceinline__ void put_sums(char* at, const float (&sum)[N], int skip, float scale, bool accumulate) {
   float x[N];
@@ -401,15 +330,15 @@ template <int OUT, int N> __device__ __forceinline__ void put_sums(char* at, con
 struct EmbedSums {
   const void* dout;
   int64_t ld;
-  int H, owners;
-  const int32_t* order;
-  const Piece* piece;
+  int H;
+  const Sorted* sorted;
+  const int32_t* n;
   const uint8_t* there;
-  OwnerCounts n;
   float scale;
   int accumulate;
   double per_width;      // 1 / H
   int V, workers;        // workgroups that go over the sums; others zero the table in the order of its addresses
+  int log_split;         // waves that a place's columns are split over
   uint64_t zeros_from;   // the first of those
   float* partial;
   void* table;
@@ -422,9 +351,9 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
   struct Raw {
     uint32_t w[(E * Storage<DT>::kBytes + 3) / 4];
   };
-  // Column blocks of `rows` rows that are asked for at a time: at most 32 registers of them.
+  // Column blocks of `rows` rows that are asked for at a time: at most 24 registers of them.
   static constexpr int blocks(int rows) {
-    const int n = 32 / (rows * int(sizeof(Raw) / 4));
+    const int n = 24 / (rows * int(sizeof(Raw) / 4));
     return n < 1 ? 1 : n > 8 ? 8 : n;
   }
   __device__ __forceinline__ static int column(const EmbedSums& a, int c) { return min(c, a.H - E); }
@@ -449,14 +378,14 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
     if constexpr (Storage<DT>::kBytes == 4) return __uint_as_float(r.w[e]);
     else return widen<DT>(e % 2 ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xffffu);
   }
-  // R rows, of which `count` are there, C column blocks, all asked for before any is used
+  // R rows, of which `count` are there, C column blocks from c0 on, up to column `last`, all asked for before any is used
   template <int R, int C>
-  __device__ __forceinline__ static void add(const EmbedSums& a, const int (&token)[R], int count, int c0, float (&sum)[C][E]) {
+  __device__ __forceinline__ static void add(const EmbedSums& a, const int (&token)[R], int count, int c0, int last, float (&sum)[C][E]) {
     Raw v[C][R];
 #pragma unroll
     for (int b = 0; b < C; ++b)
 #pragma unroll
-      for (int k = 0; k < R; ++k) v[b][k] = load(a, token[k], column(a, c0 + b * kBlock));
+      for (int k = 0; k < R; ++k) v[b][k] = load(a, token[k], min(c0 + b * kBlock, last));
 #pragma unroll
     for (int b = 0; b < C; ++b)
 #pragma unroll
@@ -471,16 +400,24 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
     const int at = column(a, c);
     put_sums<OUT, E>(row_ptr<OUT>(a.table, id, a.H, at), sum, c - at, a.scale, a.accumulate != 0);
   }
-  // the whole row of an id with R tokens
-  template <int R, int C> __device__ __forceinline__ static void row(const EmbedSums& a, const Piece& p, int own) {
+  // a row of the joined sums
+  __device__ __forceinline__ static void keep(const EmbedSums& a, int row, int c, const float (&sum)[E]) {
+    if (c >= a.H) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) a.partial[size_t(row) * a.H + column(a, c) + e] = sum[e];   // columns that overlap have the same sums
+  }
+  // column blocks [block, end) of an id with R tokens
+  template <int R, int C> __device__ __forceinline__ static void columns(const EmbedSums& a, int id, int own, int block, int end) {
     int token[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) token[k] = __builtin_amdgcn_readlane(own, k);
-    for (int c0 = threadIdx.x % kWave * E; c0 < a.H; c0 += C * kBlock) {
+    const int lane = threadIdx.x % kWave * E, last = column(a, (end - 1) * kBlock + lane);
+    for (; block < end; block += C) {   // uniform
       float sum[C][E] = {};
-      add<R, C>(a, token, R, c0, sum);
+      add<R, C>(a, token, R, block * kBlock + lane, last, sum);
 #pragma unroll
-      for (int b = 0; b < C; ++b) put(a, p.id, c0 + b * kBlock, sum[b]);
+      for (int b = 0; b < C; ++b)
+        if (block + b < end) put(a, id, (block + b) * kBlock + lane, sum[b]);
     }
   }
 };
@@ -516,90 +453,95 @@ template <int OUT> __device__ __forceinline__ void put_zeros(const EmbedSums& a,
   }
 }
 
-// 80 registers, six workgroups to a CU: 16384 tokens of width 1536 in bf16, 69 us; eight workgroups, with registers spilled, 74; five, 71.
-template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT, 6) void k_embed_sum(EmbedSums a) {
+// 64 registers, eight workgroups to a CU.  (With 32 registers of column blocks, six: one token of 151936 x 1536 fp32 142 us instead of 136.)
+template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT, 8) void k_embed_sum(EmbedSums a) {
   using Sums = ColumnSums<DT, OUT, VEC>;
   constexpr int E = Sums::E, Z = Storage<OUT>::kPerVec;
-  extern __shared__ int s_end[];   // [owners]
-  __shared__ int s_wave[kSumWaves];
   const int lane = threadIdx.x % kWave;
   if (int(blockIdx.x) >= a.workers) {
     put_zeros<OUT>(a, (a.zeros_from + (blockIdx.x - uint32_t(a.workers))) * (kSumNT * Z));
     return;
   }
   const int first = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kSumWaves + int(threadIdx.x) / kWave), waves = a.workers * kSumWaves;
-  // ---- pieces of frequent ids, by column blocks ----
-  const int blocks = (a.H + Sums::kBlock - 1) / Sums::kBlock;
-  int64_t units = int64_t(scan_owners(a.n.heavy, a.owners, s_end, s_wave)) * blocks;
+  const int units = *a.n << a.log_split, blocks = (a.H + Sums::kBlock - 1) / Sums::kBlock;
+  const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  // a place's record and its piece's tokens are asked for one and two turns ahead
+  const auto record = [&](int64_t u) { return u < units ? a.sorted[u >> a.log_split] : Sorted{0, 0, 0, 0}; };
+  const auto first_of = [&](int64_t u, int start) { return (int(u >> a.log_split) - start) / kPiece * kPiece; };   // of the piece's, from the id's
+  const auto tokens = [&](int64_t u, const Sorted& x) {   // lane r: the piece's r-th token
+    const int k = first_of(u, x.start);
+    return lane < min(x.count - k, kPiece) ? a.sorted[x.start + k + lane].token : 0;
+  };
+  Sorted next = record(first), after = record(int64_t(first) + waves);
+  int own = tokens(first, next);
   for (int64_t u = first; u < units; u += waves) {
-    int k;
-    const int g = find_owner(s_end, a.owners, int(u / blocks), k);
-    const Piece p = a.piece[a.n.base[g] + k];
-    const int own = lane < p.count ? a.order[p.start + lane] : 0;   // lane k: the piece's k-th token
-    const int c = int(u % blocks) * Sums::kBlock + lane * E;
-    float sum[1][E] = {};
-    constexpr int R = sizeof(typename Sums::Raw) > 16 ? 4 : 8;
-    for (int k0 = 0; k0 < p.count; k0 += R) {
-      int token[R];
-#pragma unroll
-      for (int r = 0; r < R; ++r) token[r] = __builtin_amdgcn_readlane(own, min(k0 + r, p.count - 1));
-      Sums::template add<R, 1>(a, token, p.count - k0, c, sum);
-    }
-    if (p.row < 0) {
-      Sums::put(a, p.id, c, sum[0]);
-    } else if (c < a.H) {   // columns that overlap have the same sums
-#pragma unroll
-      for (int e = 0; e < E; ++e) a.partial[size_t(p.row) * a.H + Sums::column(a, c) + e] = sum[0][e];
-    }
-  }
-  // ---- whole rows of the others ----
-  units = scan_owners(a.n.few, a.owners, s_end, s_wave);
-  for (int64_t u = first; u < units; u += waves) {
-    int k;
-    const int g = find_owner(s_end, a.owners, int(u), k);
-    const Piece p = a.piece[a.n.end[g] - 1 - k];
-    const int own = lane < p.count ? a.order[p.start + lane] : 0;
+    const Sorted at{0, uniform(next.id), uniform(next.start), uniform(next.count)};
+    const int own_next = tokens(u + waves, after);
+    next = after;
+    after = record(u + 2 * waves);
+    const int k = first_of(u, at.start), place = int(u >> a.log_split) - at.start - k, count = min(at.count - k, kPiece);
+    // the piece's column blocks are dealt out over its places and their waves, evenly spaced
+    const int share = count << a.log_split, mine = place << a.log_split | (int(u) & ((1 << a.log_split) - 1));
+    const int block = mine * blocks / share, end = (mine + 1) * blocks / share;
     static_assert(kFew == 4, "cases below");
-    switch (p.count) {   // uniform
-      case 1: Sums::template row<1, Sums::blocks(1)>(a, p, own); break;
-      case 2: Sums::template row<2, Sums::blocks(2)>(a, p, own); break;
-      case 3: Sums::template row<3, Sums::blocks(3)>(a, p, own); break;
-      default: Sums::template row<4, Sums::blocks(4)>(a, p, own);
+    switch (at.count <= kPiece ? count : kPiece) {   // uniform; a short last piece goes with the others of its id
+      case 1: Sums::template columns<1, Sums::blocks(1)>(a, at.id, own, block, end); break;
+      case 2: Sums::template columns<2, Sums::blocks(2)>(a, at.id, own, block, end); break;
+      case 3: Sums::template columns<3, Sums::blocks(3)>(a, at.id, own, block, end); break;
+      case 4: Sums::template columns<4, Sums::blocks(4)>(a, at.id, own, block, end); break;
+      default:
+        for (int b = block; b < end; ++b) {   // uniform
+          const int c = b * Sums::kBlock + lane * E;
+          float sum[1][E] = {};
+          constexpr int R = sizeof(typename Sums::Raw) > 16 ? 4 : 8;
+          for (int k0 = 0; k0 < count; k0 += R) {
+            int token[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) token[r] = __builtin_amdgcn_readlane(own, min(k0 + r, count - 1));
+            Sums::template add<R, 1>(a, token, count - k0, c, a.H - E, sum);
+          }
+          if (at.count <= kPiece) Sums::put(a, at.id, c, sum[0]);
+          else Sums::keep(a, piece_row(at.start) + k / kPiece, c, sum[0]);
+        }
     }
+    own = own_next;
   }
 }
 
-// Ids with several pieces: workgroup by (id, kWave columns), a quarter of the pieces to each wave.
+// Ids with several pieces: their places take turns at kWave columns, a workgroup at a place; a quarter of the pieces to each of its waves.
 template <int OUT>
-__global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a, const Whole* __restrict__ wholes) {
-  extern __shared__ int s_end[];   // [owners]
-  __shared__ int s_wave[kSumWaves];
+__global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a) {
   __shared__ float s_sum[kSumWaves][kWave];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int blocks = (a.H + kWave - 1) / kWave;
-  const int64_t units = int64_t(scan_owners(a.n.whole, a.owners, s_end, s_wave)) * blocks;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    int k;
-    const int g = find_owner(s_end, a.owners, int(u / blocks), k);
-    const Whole w = wholes[a.n.base[g] + k];
-    const int c = int(u % blocks) * kWave + lane;
-    const float* const x = a.partial + size_t(w.row) * a.H + min(c, a.H - 1);
-    const int each = (w.pieces + kSumWaves - 1) / kSumWaves, last = min((wave + 1) * each, w.pieces);
-    float sum = 0.f;
-    for (int r = wave * each; r < last; r += 8) {
-      float y[8];
+  const int n = *a.n;
+  for (int64_t p0 = blockIdx.x; p0 < n; p0 += int64_t(kWave) * gridDim.x) {   // a place by each lane, the same ones in every wave
+    const int64_t p = p0 + int64_t(lane) * gridDim.x;
+    Sorted x{0, 0, 0, 0};
+    if (p < n) x = a.sorted[p];
+    for (uint64_t m = __builtin_amdgcn_ballot_w64(x.count > kPiece); m != 0; m &= m - 1) {   // uniform
+      const int l = __builtin_ctzll(m);
+      const int id = __builtin_amdgcn_readlane(x.id, l), start = __builtin_amdgcn_readlane(x.start, l), count = __builtin_amdgcn_readlane(x.count, l);
+      const int pieces = (count + kPiece - 1) / kPiece, each = (pieces + kSumWaves - 1) / kSumWaves, last = min((wave + 1) * each, pieces);
+      for (int64_t c0 = (p0 + int64_t(l) * gridDim.x - start) * kWave; c0 < a.H; c0 += int64_t(count) * kWave) {
+        const int c = int(c0) + lane;
+        const float* const from = a.partial + size_t(piece_row(start)) * a.H + min(c, a.H - 1);
+        float sum = 0.f;
+        for (int r = wave * each; r < last; r += 8) {
+          float y[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[size_t(min(r + e, last - 1)) * a.H];
+          for (int e = 0; e < 8; ++e) y[e] = from[size_t(min(r + e, last - 1)) * a.H];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (r + e < last) sum += y[e];
+          for (int e = 0; e < 8; ++e)
+            if (r + e < last) sum += y[e];
+        }
+        s_sum[wave][lane] = sum;
+        __syncthreads();
+        static_assert(kSumWaves == 4, "sums of a column");
+        const float all[1] = {(s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane])};
+        if (wave == 0 && c < a.H) put_sums<OUT, 1>(row_ptr<OUT>(a.table, id, a.H, c), all, 0, a.scale, a.accumulate != 0);
+        __syncthreads();   // s_sum is free again
+      }
     }
-    s_sum[wave][lane] = sum;
-    __syncthreads();
-    static_assert(kSumWaves == 4, "sums of a column");
-    const float all[1] = {(s_sum[0][lane] + s_sum[1][lane]) + (s_sum[2][lane] + s_sum[3][lane])};
-    if (wave == 0 && c < a.H) put_sums<OUT, 1>(row_ptr<OUT>(a.table, w.id, a.H, c), all, 0, a.scale, a.accumulate != 0);
-    __syncthreads();   // s_sum is free again
   }
 }
 
@@ -616,28 +558,30 @@ struct EmbedArgs {
   int32_t* err_flag;
 };
 
-constexpr int kWorkers = 6;                       // to a CU: 16384 tokens of 1000 ids, width 3584, 4 / 6 / 8: 67.7 / 63.3 / 63.1 us
+constexpr int kWorkers = 8;                       // to a CU: 16384 tokens of 1000 ids, width 3584, 6 / 8 / 12: 62.4 / 56.1 / 57.7 us
 constexpr int64_t kMaxZeros = int64_t(1) << 23;   // workgroups of a launch: half of the threads that a grid may have
 template <int DT, int OUT> static void embed_bwd_launch(const EmbedArgs& a, void* workspace, hipStream_t s) {
   const EmbedWorkspace w = embed_workspace(workspace, a.T, a.V, a.H);
   const int owners = embed_owners(a.V), log_owners = __builtin_ctz(unsigned(owners));
-  hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.order, w.piece, w.whole,
-                     w.there, w.n, a.err_flag);
+  hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.sorted, w.n, w.there, a.err_flag);
   constexpr int E = Storage<OUT>::kPerVec;
   const bool vec = a.H >= E;
-  const int workers = kWorkers * compute_units();
+  const int blocks = vec ? (a.H + kWave * E - 1) / (kWave * E) : 1;
+  const int64_t most = int64_t(kWorkers) * compute_units() * kSumWaves;   // waves
+  int log_split = 0;
+  while ((2 << log_split) <= blocks && (a.T << (log_split + 1)) <= most) ++log_split;
+  const int workers = int(std::min(most, std::max<int64_t>(a.T << log_split, 1)) + kSumWaves - 1) / kSumWaves;
   const int64_t zeros = a.accumulate ? 0 : (int64_t(a.V) * a.H + int64_t(kSumNT) * E - 1) / (int64_t(kSumNT) * E);
-  EmbedSums sums{a.dout, a.ld, a.H, owners, w.order, w.piece, w.there, w.n, a.scale, a.accumulate, 1.0 / a.H, a.V, workers, 0, w.partial, a.table};
+  EmbedSums sums{a.dout, a.ld, a.H, w.sorted, w.n, w.there, a.scale, a.accumulate, 1.0 / a.H, a.V, workers, log_split, 0, w.partial, a.table};
   const auto sum = vec ? k_embed_sum<DT, OUT, true> : k_embed_sum<DT, OUT, false>;
-  const size_t lds = size_t(owners) * 4;   // at most 64 KB
-  hipLaunchKernelGGL(sum, dim3(unsigned(workers + std::min(zeros, kMaxZeros))), dim3(kSumNT), lds, s, sums);
+  hipLaunchKernelGGL(sum, dim3(unsigned(workers + std::min(zeros, kMaxZeros))), dim3(kSumNT), 0, s, sums);
   sums.workers = 0;
   for (int64_t from = kMaxZeros; from < zeros; from += kMaxZeros) {
     sums.zeros_from = uint64_t(from);
-    hipLaunchKernelGGL(sum, dim3(unsigned(std::min(zeros - from, kMaxZeros))), dim3(kSumNT), lds, s, sums);
+    hipLaunchKernelGGL(sum, dim3(unsigned(std::min(zeros - from, kMaxZeros))), dim3(kSumNT), 0, s, sums);
   }
   if (a.T > kPiece)
-    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(4 * compute_units())), dim3(kSumNT), lds, s, sums, w.whole);
+    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(4 * compute_units())), dim3(kSumNT), 0, s, sums);
 }
 
 template <int DT>
