@@ -14,35 +14,41 @@
 
 namespace aero {
 
-// One workgroup per token row.  VEC: rows of a vector and more, at any alignment; the last vector ends where the row ends and overlaps the one in
-// front.
-template <int DT, bool VEC>
-__global__ __launch_bounds__(256) void k_embed_fwd(const void* __restrict__ table, int V, int H, const int32_t* __restrict__ ids,
-                                                   float scale, void* __restrict__ out, int64_t ld_out,
-                                                   int32_t* __restrict__ err_flag) {
-  constexpr int E = VEC ? Storage<DT>::kPerVec : 1;
-  const int64_t t = blockIdx.x;
-  const int id = ids[t];
-  if (id >= V && threadIdx.x == 0 && err_flag) atomicOr(err_flag, AERO_DERR_BAD_TARGET);
-  const bool there = id >= 0 && id < V;
-  for (int c0 = threadIdx.x * E; c0 < H; c0 += 256 * E) {
-    const int c = min(c0, H - E);
-    const char* const src = row_ptr<DT>(table, there ? id : 0, H, c);
-    char* const dst = row_ptr<DT>(out, t, ld_out, c);
-    if constexpr (VEC) {
-      u32x4_t v = {0u, 0u, 0u, 0u};
-      if (there) {
-        float x[E];
-        const u32x4_t in = *reinterpret_cast<const u32x4_any_t*>(src);
-        unpack_vec<DT>(in, x);
+// scale * E elements from src on, or zeros.
+template <int DT, int E> __device__ __forceinline__ void look_up(const char* src, bool there, float scale, char* dst) {
+  if constexpr (E > 1) {
+    u32x4_t v = {0u, 0u, 0u, 0u};
+    if (there) {
+      float x[E];
+      const u32x4_t in = *reinterpret_cast<const u32x4_any_t*>(src);
+      unpack_vec<DT>(in, x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] *= scale;
-        v = pack_vec<DT>(x);
-      }
-      *reinterpret_cast<u32x4_any_t*>(dst) = v;
-    } else {
-      store_elt<DT>(dst, 0, there ? scale * load_elt<DT>(src, 0) : 0.f);
+      for (int e = 0; e < E; ++e) x[e] *= scale;
+      v = pack_vec<DT>(x);
     }
+    *reinterpret_cast<u32x4_any_t*>(dst) = v;
+  } else {
+    store_elt<DT>(dst, 0, there ? scale * load_elt<DT>(src, 0) : 0.f);
+  }
+}
+// A workgroup per token row, or (NARROW) per `rows` of them, a thread a vector (32768 rows of 64 bf16: one a workgroup 9.0 us, 32 3.3; a row's
+// address is scalar where it is the only one: 16384 rows of 1536 12.8 us for 13.5).  VEC: rows of a vector and more, at any alignment; the last
+// vector ends where the row ends and overlaps the one in front.
+constexpr int kLookNT = 256;
+template <int DT, bool VEC, bool NARROW>
+__global__ __launch_bounds__(kLookNT) void k_embed_fwd(const void* __restrict__ table, int V, int H, const int32_t* __restrict__ ids, int64_t T,
+                                                       int rows, float scale, void* __restrict__ out, int64_t ld_out,
+                                                       int32_t* __restrict__ err_flag) {
+  constexpr int E = VEC ? Storage<DT>::kPerVec : 1;
+  const uint32_t per = uint32_t(H + E - 1) / E, r = NARROW ? threadIdx.x / per : 0;
+  const int64_t t = NARROW ? int64_t(blockIdx.x) * rows + r : blockIdx.x;
+  if (NARROW && (r >= uint32_t(rows) || t >= T)) return;
+  const int first = int((threadIdx.x - r * per) * E), id = ids[t];
+  if (id >= V && first == 0 && err_flag) atomicOr(err_flag, AERO_DERR_BAD_TARGET);
+  const bool there = id >= 0 && id < V;
+  for (int c0 = first; c0 < H; c0 += kLookNT * E) {   // one turn where NARROW
+    const int c = min(c0, H - E);
+    look_up<DT, E>(row_ptr<DT>(table, there ? id : 0, H, c), there, scale, row_ptr<DT>(out, t, ld_out, c));
   }
 }
 
@@ -588,8 +594,9 @@ template <int DT>
 static void embed_fwd_launch(const void* table, int V, int H, const int32_t* ids, int64_t T, float scale, void* out, int64_t ld_out,
                              int32_t* err_flag, hipStream_t s) {
   const bool vec = H >= Storage<DT>::kPerVec;
-  const auto fwd = vec ? k_embed_fwd<DT, true> : k_embed_fwd<DT, false>;
-  hipLaunchKernelGGL(fwd, dim3(unsigned(T)), dim3(256), 0, s, table, V, H, ids, scale, out, ld_out, err_flag);
+  const int per = vec ? (H + Storage<DT>::kPerVec - 1) / Storage<DT>::kPerVec : H, rows = std::max(kLookNT / per, 1);
+  const auto fwd = rows == 1 ? k_embed_fwd<DT, true, false> : vec ? k_embed_fwd<DT, true, true> : k_embed_fwd<DT, false, true>;
+  hipLaunchKernelGGL(fwd, dim3(unsigned((T + rows - 1) / rows)), dim3(kLookNT), 0, s, table, V, H, ids, T, rows, scale, out, ld_out, err_flag);
 }
 
 constexpr int kMaxWidth = 1 << 20;
