@@ -328,7 +328,7 @@ aero_status aero_topk_logprob(
  * logits / dlogits [T, ld], same dtype and ld; dlogits may alias logits (in place), NULL: loss only.
  * teacher_index i32[T, K], teacher_logprob f32[T, K], 1 <= K <= AERO_TOPK_MAX (AERO_ERR_LIMIT beyond); token_weight f32[T].
  * loss f32[1] (fixed-order sum), row_loss f32[T] or NULL.
- * The lists' probabilities are formed in 32 bits, their sums and the loss terms in 64, everything per logit in 32.
+ * The lists' probabilities, what is added up across threads, logarithms and loss terms are formed in 64 bits, everything per logit in 32.
  * workspace: aero_workspace_bytes(AERO_OP_DISTILL_LOSS_BWD, T, V, 0, 0, 0).
  */
 aero_status aero_distill_loss_bwd(

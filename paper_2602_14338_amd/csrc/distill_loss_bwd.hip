@@ -54,7 +54,7 @@ struct ListEntry {
 };
 struct ListSums {
   double mass, p_lp_z;   // sum p, sum p (ln p - z)
-  SoftSum own;           // of the listed logits
+  SoftTotal own;         // of the listed logits
   int32_t any, bad;      // entries; ids outside the vocabulary, or the same place twice
 };
 
@@ -115,19 +115,32 @@ template <int N, int E> struct PlaceBits {
   }
 };
 
-// Probability of a listed log-prob: where it is near 1, what it lacks of 1 keeps its own precision (p_r is formed from it).
-__device__ __forceinline__ double list_prob(float lp) { return lp > -0.5f ? 1.0 + double(expm1f(lp)) : double(expf(lp)); }
+// Probability of a listed log-prob, exp(lp) = 2^n exp(r) with |r| <= ln 2 / 2 and the exponential series up to r^8 / 8! (the next term is
+// under 2e-10): a loss is a small difference, and what p_k rounds by is what it is off by.
+__device__ __forceinline__ double list_prob(float lp) {
+  const float n = rintf(lp * kLog2e);
+  const double r = fma(double(n), -0.69314718055994531, double(lp));
+  double x = 1.0 / 40320;
+  x = fma(x, r, 1.0 / 5040);
+  x = fma(x, r, 1.0 / 720);
+  x = fma(x, r, 1.0 / 120);
+  x = fma(x, r, 1.0 / 24);
+  x = fma(x, r, 1.0 / 6);
+  x = fma(x, r, 0.5);
+  x = fma(x, r, 1.0);
+  return lp < -103.97f ? 0.0 : ldexp(fma(x, r, 1.0), int(n));
+}
 
 // Sums over the entries of a wave, left in s[wave] by its first lane.
 __device__ __forceinline__ void list_sum(const ListEntry& e, bool bad, ListSums* s) {
   ListSums sum;
   const bool there = e.j >= 0;
-  sum.own = soft_identity();
+  SoftSum own = soft_identity();
   if (there && !(e.z <= kMasked)) {
     float z[1] = {e.z};
-    soft_update<1>(sum.own, z);
+    soft_update<1>(own, z);
   }
-  sum.own = soft_reduce<true>(sum.own);
+  sum.own = soft_reduce<true>(soft_total(own));
   sum.mass = wave_sum_d(there ? e.p : 0.0);
   sum.p_lp_z = wave_sum_d(there && e.p != 0.0 ? e.p * (e.lp - (e.z <= kMasked ? -INFINITY : double(e.z))) : 0.0);
   sum.any = __builtin_amdgcn_ballot_w64(there) != 0;
@@ -150,10 +163,10 @@ struct RowGrad {
   bool quiet;   // no loss, no gradient
 };
 // What the sum over the other places and the list come to; one thread writes the loss (a quiet row's too).  By all threads.
-__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftSum rest, const ListSums* s, int waves, bool bad = false,
+__device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, float w, SoftTotal rest, const ListSums* s, int waves, bool bad = false,
                                               bool report = true) {
   double mass = 0.0, p_lp_z = 0.0;
-  SoftSum all = rest;
+  SoftTotal all = rest;
   bool any = false;
   for (int k = 0; k < waves; ++k) {   // uniform
     mass += s[k].mass;
@@ -162,28 +175,28 @@ __device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, fl
     any |= s[k].any != 0;
     bad |= s[k].bad != 0;
   }
-  const bool has_rest = rest.s != 0.f, renorm = a.tail == AERO_TAIL_RENORM;
-  const float rest_q = has_rest ? rest.s / all.s * exp2_fast(rest.o - all.o) : 0.f;
+  const bool has_rest = rest.s != 0.0, renorm = a.tail == AERO_TAIL_RENORM;
+  const float rest_q = has_rest ? float(rest.s) / float(all.s) * exp2_fast(rest.o - all.o) : 0.f;
   const double g = double(w) * double(a.grad_scale);
   const double rest_p = renorm || !has_rest || mass >= 1.0 ? 0.0 : 1.0 - mass;
   const double total = renorm ? 1.0 : mass + rest_p;
   RowGrad r;
-  r.quiet = bad || !any || all.s == 0.f || (renorm && mass == 0.0);
+  r.quiet = bad || !any || all.s == 0.0 || (renorm && mass == 0.0);
   r.scale_p = uniform(float(renorm ? g / mass : g));
-  r.at_listed = uniform(float(g * total) / all.s);
+  r.at_listed = uniform(float(g * total) / float(all.s));
   r.o_all = uniform(all.o);
-  r.at_other = uniform(has_rest ? float(g * (total * double(rest_q) - rest_p)) / rest.s : 0.f);
+  r.at_other = uniform(has_rest ? float(g * (total * double(rest_q) - rest_p)) / float(rest.s) : 0.f);
   r.o_rest = uniform(rest.o);
   if (report && threadIdx.x == blockDim.x - 1) {   // the first wave has the list to look after
     if (bad && a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_TEACHER);
     double loss = 0.0;
-    if (!r.quiet) {   // logarithms of 32-bit numbers: 2^-24 of the logarithm
+    if (!r.quiet) {
       const double lse = soft_lse(all);
       if (renorm) {
-        loss = p_lp_z / mass - double(logf(float(mass))) + lse;
+        loss = p_lp_z / mass - log_of(mass) + lse;
       } else {
         loss = p_lp_z + (mass != 0.0 ? mass * lse : 0.0);
-        if (rest_p != 0.0) loss += rest_p * (double(logf(float(rest_p))) - (soft_lse(rest) - lse));
+        if (rest_p != 0.0) loss += rest_p * (log_of(rest_p) - (soft_lse(rest) - lse));
       }
     }
     put_loss(a, t, w, float(loss));
@@ -213,7 +226,7 @@ __device__ __forceinline__ void put_listed(const ListPlaces<NT>& list, const Row
 enum { kWhole, kSums, kGradient };
 constexpr int kMaxParts = 16;
 struct RowSplit {
-  SoftSum part[kMaxParts];
+  SoftTotal part[kMaxParts];
   ListSums list;
 };
 template <int STEP, int NT, int DT, bool VEC>
@@ -222,7 +235,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a, int summed, R
   constexpr int E = View::E, kAhead = 4, kWaves = NT / kWave;
   static_assert(NT >= kListMax, "an entry per thread");
   __shared__ ListPlaces<NT> list;
-  __shared__ SoftSum s_sum[kWaves];
+  __shared__ SoftTotal s_sum[kWaves];
   __shared__ ListSums s_list[kListWaves];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, K = a.K, part = blockIdx.y, parts = gridDim.y;
@@ -273,6 +286,7 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a, int summed, R
   __syncthreads();
   const float zr = jr >= 0 ? row.at(jr) : 0.f;
   SoftSum st = soft_identity();
+  SoftTotal total = soft_total(st);
   if constexpr (STEP != kGradient) {
     if (tid < kListMax) {   // whole waves
       if (entry.j >= 0) bad |= list_twice(list, tid);
@@ -303,11 +317,11 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a, int summed, R
       each_listed(list, [&](int, int place) { z[0] = place == kRagged ? -INFINITY : z[0]; });
       soft_update<1>(st, z);
     }
-    st = soft_block_reduce<NT>(st, s_sum);   // its barrier: s_list
+    total = soft_block_total<NT>(st, s_sum);   // its barrier: s_list
   }
   if constexpr (STEP == kSums) {
     if (tid == 0) {
-      split->part[part] = st;
+      split->part[part] = total;
       if (part == 0) {
         ListSums all = s_list[0];
 #pragma unroll
@@ -324,10 +338,10 @@ __global__ __launch_bounds__(NT) void k_distill_row(DistillArgs a, int summed, R
     return;
   }
   if constexpr (STEP == kGradient) {
-    if (tid % 16 < summed) st = split->part[tid % 16];
-    st = soft_reduce<false>(st);
+    if (tid % 16 < summed) total = split->part[tid % 16];
+    total = soft_reduce<false>(total);
   }
-  const RowGrad r = row_terms(a, t, w, st, STEP == kGradient ? &split->list : s_list, STEP == kGradient ? 1 : kListWaves, false, part == 0);
+  const RowGrad r = row_terms(a, t, w, total, STEP == kGradient ? &split->list : s_list, STEP == kGradient ? 1 : kListWaves, false, part == 0);
   if (!drow) return;
   if (r.quiet) {   // uniform
     zero_fill();
@@ -360,7 +374,7 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
   using View = RowView<DT, true>;
   constexpr int E = View::E, kWaves = NT / kWave;
   __shared__ ListPlaces<NT> list;
-  __shared__ SoftSum s_sum[kWaves];
+  __shared__ SoftTotal s_sum[kWaves];
   __shared__ ListSums s_list[kListWaves];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, K = a.K;
@@ -428,9 +442,9 @@ __global__ __launch_bounds__(NT) void k_distill_held(DistillArgs a) {
   }
   // orders the loads of the row before the stores over it, for a gradient in place: by its barrier, and with one wave because
   // every lane's result needs every lane's loads
-  st = soft_block_reduce<NT>(st, s_sum);
+  const SoftTotal rest = soft_block_total<NT>(st, s_sum);
   if constexpr (kWaves == 1) __syncthreads();
-  const RowGrad r = row_terms(a, t, w, st, s_list, list_waves);
+  const RowGrad r = row_terms(a, t, w, rest, s_list, list_waves);
   if (!drow) return;
   if (r.quiet) {   // uniform
     zero_fill();
@@ -497,7 +511,7 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
   using View = RowView<DT, true>;
   constexpr int E = View::E, NT = kStreamNT, NL = kStreamLds, NR = kStreamVecs - kStreamLds;
   __shared__ ListPlaces<NT> lists[2];          // by the row's parity, like everything below
-  __shared__ SoftSum s_sum[2][NT / kWave];
+  __shared__ SoftTotal s_sum[2][NT / kWave];
   __shared__ ListSums s_list[2][kListWaves];
   __shared__ int s_twice[2][kListWaves];
   extern __shared__ __align__(16) u32x4_t slots_raw[];   // NL x NT vectors
@@ -619,10 +633,10 @@ __global__ __launch_bounds__(kStreamNT) void k_distill_stream(DistillArgs a, con
         list_sum(entry, bad, s_list[par ^ 1]);
       }
       have = entry.j >= 0;
-      st = soft_block_reduce<NT>(st, s_sum[par]);   // its barrier also orders loads before stores over them
+      const SoftTotal rest = soft_block_total<NT>(st, s_sum[par]);   // its barrier also orders loads before stores over them
       bool twice = false;
       for (int k = 0; k < list_waves; ++k) twice |= s_twice[par][k] != 0;
-      const RowGrad r = row_terms(a, t, w, st, s_list[par], list_waves, twice);
+      const RowGrad r = row_terms(a, t, w, rest, s_list[par], list_waves, twice);
       if (!r.quiet) {
         zeros = false;
         uint32_t voff_st = voff;

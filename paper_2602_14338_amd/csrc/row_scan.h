@@ -87,19 +87,67 @@ template <int NT> __device__ __forceinline__ SoftSum soft_block_reduce(SoftSum a
   return a;
 }
 
-// log sum exp in 64 bits: (o + k + log2 f) / log2 e with s = 2^k f, f in [1/sqrt 2, sqrt 2), whose logarithm rounds by 2^-26 at most; log2 e is
-// the rounded one that the sums were formed with.  -inf for an empty row, NaN for one with a NaN or +inf logit.
-__device__ __forceinline__ double soft_lse(SoftSum st) {
-  if (st.s == 0.f) return -INFINITY;
-  float f = __builtin_amdgcn_frexp_mantf(st.s);
-  int k = __builtin_amdgcn_frexp_expf(st.s);
-  if (f < 0.70710678f) {
-    f *= 2.f;
+// The same with the sums of the threads added up in 64 bits: what is left of an error is their own, which differs from thread to thread and
+// evens out, where the last few of 32-bit additions do not.
+struct SoftTotal {
+  float o;
+  double s;
+};
+__device__ __forceinline__ SoftTotal soft_total(SoftSum a) { return SoftTotal{a.o, double(a.s)}; }
+__device__ __forceinline__ double soft_rescaled(SoftTotal a, float o) { return a.s * double(exp2_fast(a.o - o)); }
+__device__ __forceinline__ SoftTotal soft_merge(SoftTotal a, SoftTotal b) {
+  const float o = fmaxf(a.o, b.o);
+  return SoftTotal{o, soft_rescaled(a, o) + soft_rescaled(b, o)};
+}
+// Over 16 lanes in a row.
+__device__ __forceinline__ double row16_sum_d(double v) {
+  const auto moved = [](auto ctrl, double x) {
+    return __hiloint2double(dpp_move_i<ctrl.value>(__double2hiint(x)), dpp_move_i<ctrl.value>(__double2loint(x)));
+  };
+  v += moved(std::integral_constant<int, 0xB1>{}, v);
+  v += moved(std::integral_constant<int, 0x4E>{}, v);
+  v += moved(std::integral_constant<int, 0x141>{}, v);
+  return v + moved(std::integral_constant<int, 0x140>{}, v);
+}
+template <bool WAVE> __device__ __forceinline__ SoftTotal soft_reduce(SoftTotal a) {
+  const auto most = [](float x, float y) { return fmaxf(x, y); };
+  const float o = WAVE ? wave_reduce(a.o, most) : row16_reduce(a.o, most);
+  const double s = soft_rescaled(a, o);
+  return SoftTotal{o, WAVE ? wave_sum_d(s) : row16_sum_d(s)};
+}
+template <int NT> __device__ __forceinline__ SoftTotal soft_block_total(SoftSum mine, SoftTotal* lds /*[NT/64]*/) {
+  SoftTotal a = soft_reduce<true>(soft_total(mine));
+  constexpr int kWaves = NT / kWave;
+  static_assert(kWaves <= 16, "one lane per wave in the second step");
+  if constexpr (kWaves > 1) {
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if (lane == 0) lds[wave] = a;
+    __syncthreads();
+    a = soft_reduce<false>(lane % 16 < kWaves ? lds[lane % 16] : soft_total(soft_identity()));
+  }
+  return a;
+}
+
+// Logarithm of a positive number x = 2^k f, f in [1/sqrt 2, sqrt 2), in 64 bits: of f's 32-bit rounding, whose logarithm rounds by 2^-26 at most, and
+// of what that leaves.
+__device__ __forceinline__ double log_of(double x) {
+  double f = __builtin_amdgcn_frexp_mant(x);
+  int k = __builtin_amdgcn_frexp_exp(x);
+  if (f < 0.70710678) {
+    f *= 2.0;
     --k;
   }
-  const double lse = (double(st.o) + double(k) + double(logf(f)) * 1.4426950408889634) * (1.0 / double(kLog2e));
+  const float g = float(f);
+  return double(k) * 0.69314718055994531 + (double(logf(g)) + double(float(f - double(g)) / g));
+}
+// log sum exp in 64 bits: (o + log2 s) / log2 e; log2 e is the rounded one that the sums were formed with.  -inf for an empty row, NaN for one with a
+// NaN or +inf logit.
+__device__ __forceinline__ double soft_lse(SoftTotal st) {
+  if (st.s == 0.0) return -INFINITY;
+  const double lse = (double(st.o) + log_of(st.s) * 1.4426950408889634) * (1.0 / double(kLog2e));
   return st.o < INFINITY && st.s == st.s ? lse : __builtin_nan("");
 }
+__device__ __forceinline__ double soft_lse(SoftSum st) { return soft_lse(soft_total(st)); }
 
 // Inclusive sums over the lanes of a wave, lane by lane in the registers (LDS is not taken).
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
