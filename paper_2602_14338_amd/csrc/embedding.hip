@@ -587,7 +587,7 @@ template <int DT, int OUT> static void embed_bwd_launch(const EmbedArgs& a, void
     hipLaunchKernelGGL(sum, dim3(unsigned(std::min(zeros - from, kMaxZeros))), dim3(kSumNT), 0, s, sums);
   }
   if (a.T > kPiece)
-    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(4 * compute_units())), dim3(kSumNT), 0, s, sums);
+    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(kWorkers * compute_units())), dim3(kSumNT), 0, s, sums);
 }
 
 template <int DT>
