@@ -163,12 +163,7 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
   // ---- where each id starts ----
   static_assert(kBins == kSortNT, "a thread per id");
   const int mine = s_count[tid];
-  int incl = mine;
-#pragma unroll
-  for (int m = 1; m < kWave; m <<= 1) {
-    const int y = __shfl_up(incl, m, kWave);
-    if (lane >= m) incl += y;
-  }
+  const int incl = int(wave_scan(uint32_t(mine)));
   if (lane == kWave - 1) s_wave[1][wave] = incl;
   __syncthreads();
   int base = 0, start = incl - mine, total = 0;
@@ -206,12 +201,7 @@ __global__ __launch_bounds__(kSortNT) void k_embed_sort(const int32_t* __restric
     static_assert(kSortRuns * kSortWaves == 2 * kWave, "two counts per lane");
     if (wave == 0) {
       const int x = s_run[2 * lane], y = s_run[2 * lane + 1];
-      int sum = x + y;
-#pragma unroll
-      for (int m = 1; m < kWave; m <<= 1) {
-        const int z = __shfl_up(sum, m, kWave);
-        if (lane >= m) sum += z;
-      }
+      const int sum = int(wave_scan(uint32_t(x + y)));
       s_run[2 * lane] = sum - x - y;
       s_run[2 * lane + 1] = sum - y;
       if (lane == kWave - 1) s_all = sum;
