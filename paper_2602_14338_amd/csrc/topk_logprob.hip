@@ -356,6 +356,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   __shared__ TopBuffer buf;
   __shared__ std::conditional_t<HELD != 0, NoGroups, TopGroups<NT>> groups;
   __shared__ float s_best[NT], s_least;
+  __shared__ double s_lse;
   __shared__ SoftSum s_sum[kWaves];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, parts = gridDim.y, part = blockIdx.y;
@@ -392,8 +393,10 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   if (tid < kWave) {
     const float reached = top_threshold_of<NT>(s_best, K);
     if (tid == 0) s_least = reached;
+  } else if (tid >= NT - kWave) {   // beside it
+    const double z0 = soft_lse(st);
+    if (tid == NT - 1) s_lse = z0;
   }
-  const double z0 = soft_lse(st);
   __syncthreads();
   const float least = s_least;
   if (zr >= least && zr > kMasked) top_push(buf, top_key(zr, jr));
@@ -408,6 +411,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
     if (tid == 0) part_sums[t * parts + part] = st;
     return;
   }
+  const double z0 = s_lse;
   top_rank<NT>(buf, n, K, [&](int r, uint64_t key) {
     index[t * K + r] = key_id(key);
     logprob[t * K + r] = float(double(key_logit(key)) - z0);
@@ -427,17 +431,21 @@ __global__ __launch_bounds__(kJoinNT) void k_topk_join(const uint8_t* __restrict
                                                        int32_t* __restrict__ index, float* __restrict__ logprob,
                                                        float* __restrict__ lse) {
   __shared__ uint64_t s_key[kMaxParts * AERO_TOPK_MAX];
+  __shared__ double s_lse;
   __shared__ int s_n;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
   if (row_active && row_active[t] == 0) return;   // uniform; its outputs were written by its first part
   SoftSum st = soft_identity();
-  if (tid % 16 < parts) st = part_sums[t * parts + tid % 16];
+  if (tid >= kJoinNT - kWave && tid % 16 < parts) st = part_sums[t * parts + tid % 16];
   if (tid == 0) s_n = 0;
   for (int k = tid; k < parts * K; k += kJoinNT) s_key[k] = part_keys[t * parts * K + k];
-  st = soft_reduce<false>(st);   // over 16 lanes, the same in each row of them
+  if (tid >= kJoinNT - kWave) {   // the last wave, which has the fewest keys
+    const double z0 = soft_lse(soft_reduce<false>(st));   // over 16 lanes, the same in each row of them
+    if (tid == kJoinNT - 1) s_lse = z0;
+  }
   __syncthreads();
-  const double z0 = soft_lse(st);
+  const double z0 = s_lse;
   int mine = 0, top_step = 1;
   while (2 * top_step <= K) top_step *= 2;
   for (int k = tid; k < parts * K; k += kJoinNT) {
