@@ -4,8 +4,9 @@
 // LDS, 16 bits of it (the maximum of a vector is formed for the running offset anyway): 152K logits of 16 bits leave 9.5K numbers.  A threshold that at least
 // K logits reach follows from the threads' own maxima, joined into about 2 K of them: the K-th largest of these, found bit by bit by one wave.
 // Groups that reach it, little more than K, are read again, all at once and out of the caches, and what reaches it among their logits are the
-// candidates.  A candidate's rank is the count of larger ones; pairs of value and id are distinct, so the order is total and ties
-// go to the lower id.
+// candidates.  A candidate's rank is the count of larger ones, of which only those in its own interval of values are gone through where there
+// are many (all pairs instead: 4000 rows of 2399, K = 120 and 256, 35 and 101 us for 20 and 41); pairs of value and id are distinct, so the order is
+// total and ties go to the lower id.
 // (Comparing every vector with a threshold from the row's first vectors instead: 900 candidates, a branch in nearly every step of a
 // wave, 3.4 times the time of the whole call at 4096 x 151936 bf16.)
 // Rows with more candidates than fit (thousands of equal logits at the threshold) are selected digit by digit over their keys, nine more passes.
@@ -22,6 +23,8 @@ constexpr int kGroup = 2, kAhead = 2;   // vectors of a group, groups of a batch
 // Maxima that are noted; longer rows note one for several groups.
 constexpr int group_max(int threads) { return threads == 256 ? 2048 : 10240; }
 constexpr int kCandidates = 1536, kHits = 1024;
+constexpr int kBins = 256;
+constexpr int kPairs = 16;   // comparisons of a thread up to which all pairs of candidates are as fast as intervals
 
 // The order of floats as that of whole numbers; -0 and 0 are the same.
 __device__ __forceinline__ uint32_t float_order(float z) {
@@ -73,7 +76,7 @@ template <int NT> __device__ __forceinline__ float top_threshold_of(const float*
 
 struct TopBuffer {
   uint64_t key[kCandidates];
-  uint32_t hist[256];
+  alignas(16) uint32_t hist[kBins];
   int count, digit, left;
 };
 // What is noted while a row streams by.
@@ -136,7 +139,7 @@ __device__ __forceinline__ void top_by_digits(const RowView<DT, VEC>& row, int f
   int left = K;          // how many keys with this prefix are among the K largest
   for (int shift = 56; shift >= 0; shift -= 8) {
     __syncthreads();
-    for (int k = tid; k < 256; k += NT) b.hist[k] = 0;
+    for (int k = tid; k < kBins; k += NT) b.hist[k] = 0;
     __syncthreads();
     each([&](uint64_t key) {
       if (key != 0 && (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&b.hist[(key >> shift) & 255], 1u);
@@ -345,6 +348,50 @@ template <int NT, int DT, bool VEC, int N> struct Held {
   }
 };
 
+// The same for many keys: they are dealt out over kBins intervals of [least, most], largest first, and ranked within theirs.
+template <int NT, class Put> __device__ __forceinline__ void top_rank_binned(TopBuffer& b, int n, int K, float least, float most, Put put) {
+  constexpr int kEach = (kCandidates + NT - 1) / NT;
+  const int tid = threadIdx.x;
+  const float scale = float(kBins) / (most - least);
+  uint64_t key[kEach];
+  int bin[kEach], at[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int i = tid + u * NT;
+    if (i < n) {
+      key[u] = b.key[i];
+      bin[u] = int(fminf(fmaxf((most - key_logit(key[u])) * scale, 0.f), float(kBins - 1)));   // falls with the logit; NaN: 0
+      at[u] = atomicAdd(&b.hist[bin[u]], 1u);
+    }
+  }
+  __syncthreads();
+  if (tid < kWave) {   // counts into the first places
+    static_assert(kBins == 4 * kWave, "four intervals a lane");
+    u32x4_t* const mine = reinterpret_cast<u32x4_t*>(b.hist) + tid;
+    const u32x4_t x = *mine;
+    const uint32_t all = x.x + x.y + x.z + x.w, before = wave_scan(all) - all;
+    *mine = u32x4_t{before, before + x.x, before + x.x + x.y, before + x.x + x.y + x.z};
+  }
+  __syncthreads();
+  int first[kEach], end[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u)
+    if (tid + u * NT < n) {
+      first[u] = int(b.hist[bin[u]]);
+      end[u] = bin[u] + 1 < kBins ? int(b.hist[bin[u] + 1]) : n;
+      b.key[first[u] + at[u]] = key[u];
+    }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kEach; ++u)
+    if (tid + u * NT < n) {
+      int rank = first[u];
+#pragma unroll 4
+      for (int k = first[u]; k < end[u]; ++k) rank += b.key[k] > key[u];
+      if (rank < K) put(rank, key[u]);
+    }
+}
+
 // Workgroup (t, part): part of the row's vectors.  With one part the outputs; with several the part's keys in descending order (0:
 // fewer) and sum for k_topk_join.
 template <int NT, int DT, bool VEC, int HELD>   // vectors that a thread holds, 0: the row streams by
@@ -355,7 +402,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   using Part = std::conditional_t<HELD != 0, Held<NT, DT, VEC, HELD>, Streamed<NT, DT, VEC>>;
   __shared__ TopBuffer buf;
   __shared__ std::conditional_t<HELD != 0, NoGroups, TopGroups<NT>> groups;
-  __shared__ float s_best[NT], s_least;
+  __shared__ float s_best[NT], s_least, s_most;
   __shared__ double s_lse;
   __shared__ SoftSum s_sum[kWaves];
   const int64_t t = blockIdx.x;
@@ -373,6 +420,7 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   const RowView<DT, VEC> row(logits, t, ld, V);
   const int per = (row.nvec + parts - 1) / parts;
   const int first = min(part * per, row.nvec), last = min(first + per, row.nvec);
+  for (int k = tid; k < kBins; k += NT) buf.hist[k] = 0;
   if (tid == 0) {
     buf.count = 0;
     if constexpr (HELD == 0) groups.hits = 0;
@@ -396,23 +444,34 @@ __global__ __launch_bounds__(NT) void k_topk(const void* __restrict__ logits, in
   } else if (tid >= NT - kWave) {   // beside it
     const double z0 = soft_lse(st);
     if (tid == NT - 1) s_lse = z0;
+  } else if (tid >= NT - 2 * kWave) {
+    float most = s_best[tid % kWave];
+#pragma unroll
+    for (int k = 1; k < NT / kWave; ++k) most = fmaxf(most, s_best[k * kWave + tid % kWave]);
+    most = wave_reduce(most, [](float x, float y) { return fmaxf(x, y); });
+    if (tid == NT - 2 * kWave) s_most = most;
   }
   __syncthreads();
   const float least = s_least;
   if (zr >= least && zr > kMasked) top_push(buf, top_key(zr, jr));
   const bool listed = mine.push(buf, best, least);
   __syncthreads();
-  if (!listed || buf.count > kCandidates) top_by_digits<NT>(row, first, last, K, buf);   // uniform
+  const bool digits = !listed || buf.count > kCandidates;   // uniform
+  if (digits) top_by_digits<NT>(row, first, last, K, buf);
   const int n = buf.count;
+  auto rank = [&](auto put) {
+    if (digits || n * n < kPairs * NT) top_rank<NT>(buf, n, K, put);
+    else top_rank_binned<NT>(buf, n, K, least, s_most, put);
+  };
   if (parts > 1) {
     uint64_t* keys = part_keys + (t * parts + part) * K;
-    top_rank<NT>(buf, n, K, [&](int r, uint64_t key) { keys[r] = key; });
+    rank([&](int r, uint64_t key) { keys[r] = key; });
     for (int k = n + tid; k < K; k += NT) keys[k] = 0;
     if (tid == 0) part_sums[t * parts + part] = st;
     return;
   }
   const double z0 = s_lse;
-  top_rank<NT>(buf, n, K, [&](int r, uint64_t key) {
+  rank([&](int r, uint64_t key) {
     index[t * K + r] = key_id(key);
     logprob[t * K + r] = float(double(key_logit(key)) - z0);
   });
