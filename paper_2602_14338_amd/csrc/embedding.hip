@@ -9,8 +9,8 @@
 // that no token has, 16 bytes a thread in the order of their addresses: that writes 6.5 TB/s, workgroups that walk over rows 5.2.
 // Ids with several pieces are joined in order in a third.
 //
-// The lookup is bound by its bytes: 16384 rows of 1536 bf16 14.4 us (6.8 TB/s).  The gradient by the table's: 600 tokens, 151936 x 1536 bf16 77 us (6.1 TB/s,
-// the sort's 8 and the join's 4.5 included), 32768 tokens, 32000 x 3584 fp32 152 us (4.5 TB/s: sort 17, sums and zeros 126, join 9.6); of a
+// The lookup is bound by its bytes: 16384 rows of 1536 bf16 14.4 us (6.8 TB/s).  The gradient by the table's: 600 tokens, 151936 x 1536 bf16 76 us (6.1 TB/s,
+// the sort's 7.4 and the join's 4.5 included), 32768 tokens, 32000 x 3584 fp32 149 us (4.6 TB/s: sort 17, sums and zeros 126, join 8.5); of a
 // small table by three launches (600 tokens of 1000 x 64 15 us).
 #include <algorithm>
 

@@ -11,7 +11,7 @@
 // wave, 3.4 times the time of the whole call at 4096 x 151936 bf16.)
 // Rows with more candidates than fit (thousands of equal logits at the threshold) are selected digit by digit over their keys, nine more passes.
 // Bound by the row's bytes where there are many: 4096 x 151936 bf16, K = 64, 201 us (6.2 TB/s); by the chain of load, threshold, candidates and
-// ranks (13000 cycles of a short row) and a second launch where there are few: 64 such rows, in four parts each, 16.7 us.
+// ranks (10000 cycles of a short row) and a second launch where there are few: 64 such rows, in four parts each, 16.3 us.
 #include <algorithm>
 #include <type_traits>
 
