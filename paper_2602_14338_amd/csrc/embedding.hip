@@ -7,11 +7,11 @@
 // take the places as they lie: the places of kPiece tokens of an id share the row's columns among them, each of which it sums over all of
 // these tokens, and so every place has the same work, however often its id occurs.  Beside them small workgroups zero the rows of the ids
 // that no token has, 16 bytes a thread in the order of their addresses: that writes 6.5 TB/s, workgroups that walk over rows 5.2.
-// Ids with several pieces are joined in order in a third.
+// Ids with several pieces are joined in order in a third.  A few hundred tokens take one launch instead (k_embed_few).
 //
 // The lookup is bound by its bytes: 16384 rows of 1536 bf16 14.4 us (6.8 TB/s).  The gradient by the table's: 600 tokens, 151936 x 1536 bf16 76 us (6.1 TB/s,
 // the sort's 7.4 and the join's 4.5 included), 32768 tokens, 32000 x 3584 fp32 149 us (4.6 TB/s: sort 17, sums and zeros 126, join 8.5); of a
-// small table by three launches (600 tokens of 1000 x 64 15 us).
+// small table by three launches (600 tokens of 1000 x 64 15 us), or by one (97 of 2589 x 367 4.2).
 #include <algorithm>
 
 #include "row_scan.h"
@@ -422,44 +422,48 @@ template <int DT, int OUT, bool VEC> struct ColumnSums {
   }
 };
 
+// The table's row with an element: by a reciprocal and a correction.
+__device__ __forceinline__ uint32_t row_of(const EmbedSums& a, uint64_t element) {
+  const uint32_t row = uint32_t(double(element) * a.per_width);
+  const int64_t rest = int64_t(element) - int64_t(uint64_t(row) * uint32_t(a.H));
+  return rest < 0 ? row - 1 : rest >= a.H ? row + 1 : row;
+}
 // A vector of the table by each thread of the workgroup, from element `before` on: zeros where no token has the row's id.  A vector that spans
-// two rows is stored whole where both are empty, and otherwise element by element.
-template <int OUT> __device__ __forceinline__ void put_zeros(const EmbedSums& a, uint64_t before) {
+// two rows is stored whole where both are empty, and otherwise element by element.  (Two or four vectors a thread: 600 tokens, 151936 x 1536 bf16
+// 89 and 96 us for 76.)
+template <int OUT> constexpr uint64_t kZeroElts = uint64_t(kSumNT) * Storage<OUT>::kPerVec;   // of a workgroup
+template <int OUT, class There> __device__ __forceinline__ void put_zeros(const EmbedSums& a, uint64_t before, There there) {
   constexpr int Z = Storage<OUT>::kPerVec;
   const uint32_t H = uint32_t(a.H);
   const uint64_t all = uint64_t(a.V) * H, from = before + threadIdx.x * Z;
   if (from >= all) return;
   char* const at = reinterpret_cast<char*>(a.table) + from * Storage<OUT>::kBytes;
-  // row and column of the vector, by reciprocals and a correction (whole-number division: a third of the time of a narrow table)
-  uint32_t base = uint32_t(double(before) * a.per_width);
-  int64_t rest = int64_t(before) - int64_t(uint64_t(base) * H);
-  if (rest < 0) rest += H, --base;
-  if (rest >= int64_t(H)) rest -= H, ++base;
-  const uint32_t in = uint32_t(rest) + threadIdx.x * Z;
+  const uint32_t base = row_of(a, before);
+  const uint32_t in = uint32_t(before - uint64_t(base) * H) + threadIdx.x * Z;
   uint32_t more = uint32_t(float(in) * float(a.per_width));
   int32_t column = int32_t(in - more * H);
   if (column < 0) column += H, --more;
   if (column >= int32_t(H)) column -= H, ++more;
   const uint32_t row = base + more, left = H - uint32_t(column);   // columns of the row from here on
   const bool spans = left < Z;
-  const bool none = !a.there[row], next_none = !a.there[min(row + 1, uint32_t(a.V) - 1)];   // asked for together
+  const bool none = !there(row), next_none = !there(min(row + 1, uint32_t(a.V) - 1));   // asked for together
   if (none && (!spans || (next_none && H >= Z && from + Z <= all))) {
     const u32x4_any_t zero = {0u, 0u, 0u, 0u};
     __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_any_t*>(at));
   } else if (spans) {
 #pragma unroll
     for (int e = 0; e < Z; ++e)
-      if (from + e < all && (e < int(left) ? none : H >= Z ? next_none : !a.there[row + 1 + (e - left) / H])) store_elt<OUT>(at, e, 0.f);
+      if (from + e < all && (e < int(left) ? none : H >= Z ? next_none : !there(row + 1 + (e - left) / H))) store_elt<OUT>(at, e, 0.f);
   }
 }
 
 // 64 registers, eight workgroups to a CU.  (With 32 registers of column blocks, six: one token of 151936 x 1536 fp32 142 us instead of 136.)
 template <int DT, int OUT, bool VEC> __global__ __launch_bounds__(kSumNT, 8) void k_embed_sum(EmbedSums a) {
   using Sums = ColumnSums<DT, OUT, VEC>;
-  constexpr int E = Sums::E, Z = Storage<OUT>::kPerVec;
+  constexpr int E = Sums::E;
   const int lane = threadIdx.x % kWave;
   if (int(blockIdx.x) >= a.workers) {
-    put_zeros<OUT>(a, (a.zeros_from + (blockIdx.x - uint32_t(a.workers))) * (kSumNT * Z));
+    put_zeros<OUT>(a, (a.zeros_from + (blockIdx.x - uint32_t(a.workers))) * kZeroElts<OUT>, [&](uint32_t row) { return a.there[row] != 0; });
     return;
   }
   const int first = __builtin_amdgcn_readfirstlane(int(blockIdx.x) * kSumWaves + int(threadIdx.x) / kWave), waves = a.workers * kSumWaves;
@@ -545,6 +549,102 @@ __global__ __launch_bounds__(kSumNT) void k_embed_join(EmbedSums a) {
   }
 }
 
+// A few hundred tokens need no sort: one launch, in which a workgroup per token and column block sums up the tokens with its id, 64 to a wave in turn, if
+// it is the first of them, and those that zero the table see from the ids whether one has a row of theirs.  Sorted / so: 97 tokens, 2589 x 367
+// 13.2 / 4.2 us; 256 of 151936 x 1536 bf16 75 / 72; 500 of 20000 x 368 20 / 10.8.  Every zeroing wave reads the ids, so that more than 256 take it for
+// tables of up to 64 MB only: 500 of 33 MB 21 / 13.5 us, of 123 MB 29.9 / 30.9, 300 of 467 MB 75 / 95.
+constexpr int kFewWords = 4, kMoreWords = 8;   // of 64 tokens
+constexpr int64_t kMoreZeros = 16384;          // workgroups
+template <int DT, int OUT, bool VEC, int WORDS>
+__global__ __launch_bounds__(kSumNT) void k_embed_few(EmbedSums a, const int32_t* __restrict__ ids, int T, int blocks, int32_t* __restrict__ err_flag) {
+  using Sums = ColumnSums<DT, OUT, VEC>;
+  constexpr int E = Sums::E;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  if (int(blockIdx.x) >= a.workers) {   // each wave by itself
+    const uint64_t before = (a.zeros_from + (blockIdx.x - uint32_t(a.workers))) * kZeroElts<OUT>;
+    const uint32_t r0 = row_of(a, before), r1 = row_of(a, before + kZeroElts<OUT> - 1);
+    int own[WORDS];
+    uint64_t meant[WORDS], any = 0;   // tokens with a row of the workgroup's
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) own[w] = w * kWave + lane < T ? ids[w * kWave + lane] : -1;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+      meant[w] = __builtin_amdgcn_ballot_w64(own[w] >= 0 && uint32_t(own[w]) >= r0 && uint32_t(own[w]) <= r1);
+      any |= meant[w];
+    }
+    if (any == 0) {   // uniform
+      put_zeros<OUT>(a, before, [](uint32_t) { return false; });
+    } else {
+      put_zeros<OUT>(a, before, [&](uint32_t row) {
+        bool yes = false;
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w)
+          for (uint64_t m = meant[w]; m != 0;) {   // an id once
+            const int one = __builtin_amdgcn_readlane(own[w], __builtin_ctzll(m));
+            yes |= uint32_t(one) == row;
+            m &= (m - 1) & ~__builtin_amdgcn_ballot_w64(own[w] == one);
+          }
+        return yes;
+      });
+    }
+    return;
+  }
+  __shared__ uint64_t s_same[WORDS];
+  __shared__ float s_sum[kSumWaves][E][kWave];
+  const int t = int(blockIdx.x) / blocks, block = int(blockIdx.x) % blocks;
+  const int own = ids[t];
+  uint64_t same[WORDS / kSumWaves], mine = 0;   // tokens with the id, 64 in a word: the wave's are every fourth
+#pragma unroll
+  for (int k = 0; k < WORDS / kSumWaves; ++k) {
+    const int w = k * kSumWaves + wave, id = w * kWave + lane < T ? ids[w * kWave + lane] : -1;
+    if (blockIdx.x == 0 && id >= a.V && err_flag) atomicOr(err_flag, AERO_DERR_BAD_TARGET);
+    same[k] = __builtin_amdgcn_ballot_w64(id == own);
+    mine |= same[k];
+    if (lane == 0) s_same[w] = same[k];
+  }
+  if (own < 0 || own >= a.V) return;   // uniform
+  __syncthreads();
+  bool has[kSumWaves] = {};   // waves with tokens of the id
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w) {
+    const uint64_t m = s_same[w], in_front = t / kWave > w ? ~uint64_t(0) : t / kWave == w ? (uint64_t(1) << (t % kWave)) - 1 : 0;
+    if ((m & in_front) != 0) return;   // uniform: not the first
+    has[w % kSumWaves] |= m != 0;
+  }
+  const int waves = has[0] + has[1] + has[2] + has[3];
+  const int c = block * Sums::kBlock + lane * E;
+  float sum[1][E] = {};
+  constexpr int R = sizeof(typename Sums::Raw) > 16 ? 4 : sizeof(typename Sums::Raw) > 8 ? 8 : 16;
+#pragma unroll
+  for (int k = 0; k < WORDS / kSumWaves; ++k)
+    for (uint64_t rest = same[k]; rest != 0;) {   // uniform in the wave; R tokens in ascending order
+      int token[R], count = 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (rest != 0) {
+          token[r] = (k * kSumWaves + wave) * kWave + __builtin_ctzll(rest);
+          rest &= rest - 1;
+          ++count;
+        } else {
+          token[r] = token[0];
+        }
+      }
+      Sums::template add<R, 1>(a, token, count, c, a.H - E, sum);
+    }
+  if (waves == 1) {   // uniform
+    if (mine != 0) Sums::put(a, own, c, sum[0]);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_sum[wave][e][lane] = sum[0][e];
+  __syncthreads();
+  if (wave != 0) return;
+  static_assert(kSumWaves == 4, "sums of a column");
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[0][e] = (s_sum[0][e][lane] + s_sum[1][e][lane]) + (s_sum[2][e][lane] + s_sum[3][e][lane]);
+  Sums::put(a, own, c, sum[0]);
+}
+
 struct EmbedArgs {
   const void* dout;
   int64_t T;
@@ -562,26 +662,37 @@ constexpr int kWorkers = 8;                       // to a CU: 16384 tokens of 10
 constexpr int64_t kMaxZeros = int64_t(1) << 23;   // workgroups of a launch: half of the threads that a grid may have
 template <int DT, int OUT> static void embed_bwd_launch(const EmbedArgs& a, void* workspace, hipStream_t s) {
   const EmbedWorkspace w = embed_workspace(workspace, a.T, a.V, a.H);
-  const int owners = embed_owners(a.V), log_owners = __builtin_ctz(unsigned(owners));
-  hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.sorted, w.n, w.there, a.err_flag);
   constexpr int E = Storage<OUT>::kPerVec;
   const bool vec = a.H >= E;
-  const int blocks = vec ? (a.H + kWave * E - 1) / (kWave * E) : 1;
+  const int blocks = (a.H + kWave * (vec ? E : 1) - 1) / (kWave * (vec ? E : 1));
+  const int64_t zeros = a.accumulate ? 0 : int64_t((uint64_t(a.V) * a.H + kZeroElts<OUT> - 1) / kZeroElts<OUT>);
+  EmbedSums sums{a.dout, a.ld, a.H, w.sorted, w.n, w.there, a.scale, a.accumulate, 1.0 / a.H, a.V, 0, 0, 0, w.partial, a.table};
+  const bool more = a.T > kFewWords * kWave;
+  if (a.T <= kMoreWords * kWave && (!more || zeros <= kMoreZeros)) {
+    const auto few = more ? (vec ? k_embed_few<DT, OUT, true, kMoreWords> : k_embed_few<DT, OUT, false, kMoreWords>)
+                          : (vec ? k_embed_few<DT, OUT, true, kFewWords> : k_embed_few<DT, OUT, false, kFewWords>);
+    sums.workers = int(a.T) * blocks;
+    for (int64_t from = 0; from == 0 || from < zeros; from += kMaxZeros) {
+      sums.zeros_from = uint64_t(from);
+      const int64_t n = sums.workers + std::min(zeros - from, kMaxZeros);
+      if (n > 0) hipLaunchKernelGGL(few, dim3(unsigned(n)), dim3(kSumNT), 0, s, sums, a.ids, int(a.T), blocks, a.err_flag);
+      sums.workers = 0;
+    }
+    return;
+  }
+  const int owners = embed_owners(a.V), log_owners = __builtin_ctz(unsigned(owners));
+  hipLaunchKernelGGL(k_embed_sort, dim3(unsigned(owners)), dim3(kSortNT), 0, s, a.ids, a.T, a.V, log_owners, w.sorted, w.n, w.there, a.err_flag);
   const int64_t most = int64_t(kWorkers) * compute_units() * kSumWaves;   // waves
-  int log_split = 0;
-  while ((2 << log_split) <= blocks && (a.T << (log_split + 1)) <= most) ++log_split;
-  const int workers = int(std::min(most, std::max<int64_t>(a.T << log_split, 1)) + kSumWaves - 1) / kSumWaves;
-  const int64_t zeros = a.accumulate ? 0 : (int64_t(a.V) * a.H + int64_t(kSumNT) * E - 1) / (int64_t(kSumNT) * E);
-  EmbedSums sums{a.dout, a.ld, a.H, w.sorted, w.n, w.there, a.scale, a.accumulate, 1.0 / a.H, a.V, workers, log_split, 0, w.partial, a.table};
+  while ((2 << sums.log_split) <= blocks && (a.T << (sums.log_split + 1)) <= most) ++sums.log_split;
+  sums.workers = int(std::min(most, std::max<int64_t>(a.T << sums.log_split, 1)) + kSumWaves - 1) / kSumWaves;
   const auto sum = vec ? k_embed_sum<DT, OUT, true> : k_embed_sum<DT, OUT, false>;
-  hipLaunchKernelGGL(sum, dim3(unsigned(workers + std::min(zeros, kMaxZeros))), dim3(kSumNT), 0, s, sums);
+  hipLaunchKernelGGL(sum, dim3(unsigned(sums.workers + std::min(zeros, kMaxZeros))), dim3(kSumNT), 0, s, sums);
   sums.workers = 0;
   for (int64_t from = kMaxZeros; from < zeros; from += kMaxZeros) {
     sums.zeros_from = uint64_t(from);
     hipLaunchKernelGGL(sum, dim3(unsigned(std::min(zeros - from, kMaxZeros))), dim3(kSumNT), 0, s, sums);
   }
-  if (a.T > kPiece)
-    hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(kWorkers * compute_units())), dim3(kSumNT), 0, s, sums);
+  hipLaunchKernelGGL(k_embed_join<OUT>, dim3(unsigned(kWorkers * compute_units())), dim3(kSumNT), 0, s, sums);
 }
 
 template <int DT>

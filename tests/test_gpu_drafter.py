@@ -582,16 +582,27 @@ def test_embedding_gradient_within_its_table(gh, T, V, H, off, grad):
     assert bool((buf[:off] == 7.0).all()) and bool((buf[off + V * H:] == 7.0).all())
 
 
+@pytest.mark.parametrize("H", [1, 3, 40, 1001])
+@pytest.mark.parametrize("T", [2, 64, 65, 256, 257, 512, 513])
+def test_embedding_gradient_of_few_tokens(gh, T, H):
+    """Around as many tokens as need no sort: ids that meet across the waves of a workgroup, all the same, none, outside the table."""
+    V = 700
+    t = np.arange(T)
+    for kind, ids in enumerate((np.full(T, 699), t % 2 * 64, t * 5 % V, np.where(t % 3 == 0, V + t, t % 7), np.full(T, -1), t // 2)):
+        check_embed_bwd(T, V, H, H, "bf16", "f32" if kind % 2 else "bf16", kind % 3 == 0, ids.astype(np.int32), err=2 if kind == 3 else 0)
+
+
 def test_embedding_gradient_of_large_tables(gh):
     """More ids than 256 workgroups count, and lengths around a workgroup's step."""
     for T, V in ((4096, 300000), (4097, 262145), (8191, 151936)):
         check_embed_bwd(T, V, 8, 8, "bf16", "f32", False, token_ids(3, T, V))
 
 
-def test_embedding_gradient_of_a_table_past_32_bits(gh):
+@pytest.mark.parametrize("T", [40, 300])
+def test_embedding_gradient_of_a_table_past_32_bits(gh, T):
     """Elements and bytes past 2^32, and more zeros than one launch writes; rows looked up from it at the same places."""
     import paper_2602_14338_amd as aero
-    T, V, H = 40, 1 << 24, 513
+    V, H = 1 << 24, 513
     ids = np.random.default_rng(5).integers(0, V, T).astype(np.int32)
     ids[:4] = (0, V - 1, V - 2, V // 2)
     dout, host = stored(normal([T, H], T, H, 1.0), "f32")
