@@ -5,7 +5,7 @@
 // rows behind a refusal are mostly left out.  The second finds the first position whose uniform number is not below p / q, and in every
 // slice of the vocabulary the largest max(0, p - q) / noise there.  The third joins a sequence's slices: the larger score, the lower id
 // where equal, which does not depend on their order.  (Joining in the second launch by atomics takes a device-wide fence per workgroup, 50 of 129
-// us for 128 sequences.)  Bound by the rows' and the noise's bytes (151936 bf16: 128 sequences of up to 5 drafted tokens 71 us, of which the sums 41 at 5.6 TB/s and
+// us for 128 sequences.)  Short rows take one launch, in which a workgroup does all of that for a sequence.  Bound by the rows' and the noise's bytes (151936 bf16: 128 sequences of up to 5 drafted tokens 71 us, of which the sums 41 at 5.6 TB/s and
 // the draw 28; 256 of 3 copied tokens 86 us) and, for few sequences, by three launches (8 of 4 tokens 16.8 us).
 #include <algorithm>
 
@@ -260,9 +260,40 @@ __device__ __forceinline__ void put_drawn(const VerifyArgs& a, int b, int n, dou
   }
 }
 
-// DECIDED: k_verify_positions has been there.  With one slice the drawn token too, else what k_verify_end needs.
-template <int NT, int DT, bool VEC, bool DECIDED>
+// The sum of a row by a wave.
+template <int DT, bool VEC> __device__ __forceinline__ SoftSum wave_row(const RowView<DT, VEC>& row) {
+  constexpr int E = RowView<DT, VEC>::E, kAhead = 4;
+  const int lane = threadIdx.x % kWave;
+  SoftSum st = soft_identity();
+  auto fold = [&](const u32x4_t& v) {
+    float z[E];
+    row.unpack(v, z);
+    soft_update<E>(st, z);
+  };
+  const int jr = VEC ? ragged_elt<DT>(RowGeom{row.head, row.nvec}, row.V, lane) : -1;
+  if (jr >= 0) {
+    float z[1] = {row.at(jr)};
+    soft_update<1>(st, z);
+  }
+  int k = lane;
+  for (; k + (kAhead - 1) * kWave < row.nvec; k += kAhead * kWave) {
+    u32x4_t v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = row.load_again(k + u * kWave);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) fold(v[u]);
+  }
+  for (; k < row.nvec; k += kWave) fold(row.load_again(k));
+  return soft_reduce<true>(st);
+}
+
+// What is known before: the rows' sums by k_verify_rows, decisions too by k_verify_positions, or nothing (short rows: a wave forms the sum of a row,
+// and one launch does everything).  With one slice the drawn token too, else what k_verify_end needs.
+enum { kSummed, kDecided, kAlone };
+template <int NT, int DT, bool VEC, int KNOWN>
 __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
+  constexpr bool DECIDED = KNOWN == kDecided;
+  __shared__ SoftSum s_row[KNOWN == kAlone ? 2 * AERO_DRAFT_MAX + 1 : 1];
   constexpr int E = RowView<DT, VEC>::E;
   __shared__ uint64_t s_key[NT / kWave];
   const int tid = threadIdx.x, lane = tid % kWave, b = blockIdx.x, slice = blockIdx.y, slices = gridDim.y;
@@ -272,8 +303,10 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
   const int64_t my_t = int64_t(b) * (a.G + 1) + min(lane, a.G), my_d = int64_t(b) * a.G + min(lane, a.G - 1);
   const bool minus = a.draft != nullptr;   // and so G > 0
   RowParts pp, qp;
-  pp.load(a, my_t);
-  if (minus) qp.load(a, n_target + my_d);
+  if constexpr (KNOWN != kAlone) {
+    pp.load(a, my_t);
+    if (minus) qp.load(a, n_target + my_d);
+  }
   double lp = 0.0;
   float u = 0.f;
   if constexpr (DECIDED) lp = a.lp[my_t];
@@ -293,7 +326,22 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
     return;
   }
   const bool on = lane < count;
-  const SoftSum sp = pp.sum(), sq = minus ? qp.sum() : soft_identity();
+  SoftSum sp, sq;
+  if constexpr (KNOWN == kAlone) {
+    const int rows = count + 1 + (minus ? count : 0);   // target rows, then draft rows
+    for (int r = tid / kWave; r < rows; r += NT / kWave) {
+      const bool of_draft = r > count;
+      const RowView<DT, VEC> row(of_draft ? a.draft : a.target, of_draft ? int64_t(b) * a.G + r - count - 1 : int64_t(b) * (a.G + 1) + r, a.ld, a.V);
+      const SoftSum st = wave_row(row);
+      if (lane == 0) s_row[r] = st;
+    }
+    __syncthreads();
+    sp = lane <= count ? s_row[lane] : soft_identity();
+    sq = minus && on ? s_row[count + 1 + lane] : soft_identity();
+  } else {
+    sp = pp.sum();
+    sq = minus ? qp.sum() : soft_identity();
+  }
   bool ok;
   if constexpr (DECIDED) {
     ok = on && lp == lp;
@@ -437,16 +485,23 @@ template <int DT, bool VEC> static void verify_launch(VerifyArgs a, hipStream_t 
   const dim3 draw{unsigned(a.B), unsigned(a.slices)};
   // four positions to a CU and more: rows one by one / by position, 256 sequences x 8 drafted tokens 260 / 192 us, x 3 142 / 134, x 3 copied
   // ones 94.0 / 91.8; fewer: 128 x 5 102 / 100, with drawn counts 75 / 85, 64 x 4 49.9 / 53.4
-  if (a.G > 0 && positions >= 4 * compute_units()) {
+  // Vectors that a lane goes through where a wave takes a row: few enough, or more where the sequences alone fill the CUs.  Two or three launches / one:
+  // bf16, 1 sequence x 3 copied tokens of 1024 7.0 / 5.7 us, 8 x 4 of 3000 (6 vectors) 9.2 / 8.3, of 11000 (22) 13.4 / 14.1, 256 x 3 of 1024 16.3 / 7.4, of
+  // 16000 (32) 26.6 / 19.6, 1 x 8 of 5586 (22) 9.3 / 11.6.  (Rows split over the waves that have none: 1 us more at 1024, nothing gained below 32000.)
+  const int waves = 1024 / kWave, each = int((rows / a.B + waves - 1) / waves) * ((nvec + kWave - 1) / kWave);
+  if (each <= 12 + a.B / 8) {
+    a.slices = 1;
+    hipLaunchKernelGGL((k_verify_draw<1024, DT, VEC, kAlone>), dim3(unsigned(a.B)), dim3(1024), 0, s, a);
+  } else if (a.G > 0 && positions >= 4 * compute_units()) {
     a.parts = 1;
     hipLaunchKernelGGL(k_verify_start, dim3(unsigned((a.B + 255) / 256)), dim3(256), 0, s, a.refused, a.B);
     // 1024 threads, so that two positions are under way on a CU (512, four: 223 / 141 / 97.2 us)
     hipLaunchKernelGGL((k_verify_positions<1024, DT, VEC>), dim3(unsigned(positions)), dim3(1024), 0, s, a);
-    hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC, true>), draw, dim3(NT), 0, s, a);
+    hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC, kDecided>), draw, dim3(NT), 0, s, a);
   } else {
     a.parts = verify_parts(rows, nvec, NT);
     hipLaunchKernelGGL((k_verify_rows<NT, DT, VEC>), dim3(unsigned(rows), unsigned(a.parts)), dim3(NT), 0, s, a);
-    hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC, false>), draw, dim3(NT), 0, s, a);
+    hipLaunchKernelGGL((k_verify_draw<NT, DT, VEC, kSummed>), draw, dim3(NT), 0, s, a);
   }
   if (a.slices > 1) hipLaunchKernelGGL((k_verify_end<DT>), dim3(unsigned(a.B)), dim3(kEndNT), 0, s, a);
 }

@@ -807,6 +807,31 @@ def test_verify_of_many_sequences(gh, dtype, V, ld, probs):
     check_verify(draft_case(12, 1100, 0, 40, dtype, probs), 1100, 0, 40, 40, None)      # nothing drafted, one slice
 
 
+@pytest.mark.parametrize("probs", [True, False])
+@pytest.mark.parametrize("dtype,B,G,V", [("bf16", 40, 5, 20001), ("f32", 260, 3, 12001), ("bf16", 260, 3, 23001), ("f32", 9, 2, 9001)])
+def test_verify_of_longer_rows(gh, dtype, B, G, V, probs):
+    """Rows too long for one launch, of few sequences and of many: ragged counts, idle and bad sequences, masked, empty and NaN rows."""
+    case = draft_case(13, B, G, V, dtype, probs)
+    count = np.random.default_rng(13).integers(0, G + 1, size=B).astype(np.int32)
+    count[3], count[4], count[5:9] = -1, G + 1, G
+    case["tokens"][5, 1] = -4
+    case["tokens"][6, 0] = V
+    zt = np.asarray(case["th"], np.float32).reshape(B, G + 1, V).copy()
+    zt[7, 0, ::3] = -np.inf
+    zt[8, 0] = -np.inf
+    zt[0, 0, V - 1] = np.nan
+    zt[1, 0, :V - 2] = np.finfo(np.float32).min if dtype == "f32" else -3.0e38
+    case["t"], host = stored(zt.reshape(-1, V), dtype)
+    case["th"] = host.reshape(B, G + 1, V)
+    if probs:
+        zd = np.asarray(case["dh"], np.float32).reshape(B, G, V).copy()
+        zd[2, 0] = -np.inf
+        case["d"], host = stored(zd.reshape(-1, V), dtype)
+        case["dh"] = host.reshape(B, G, V)
+    ref = check_verify(case, B, G, V, V, count, err=2 | 16)
+    assert ref["tokens"][0, 0] == -1 and ref["tokens"][8, 0] == -1 and ref["tokens"][1, 0] >= V - 2
+
+
 def test_verify_of_equal_rows_that_are_refused(gh):
     """Where the residual vanishes the token is drawn from p: the drafter's rows are the policy's and the drafted token is masked in both,
     so that it is refused; with one slice per sequence and with several."""
