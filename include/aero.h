@@ -380,8 +380,8 @@ aero_status aero_embedding_fwd(
 /*
  * Its gradient: dtable[v, :] = scale * sum over the tokens t with ids[t] == v of dout[t, :], rows without a token +0; with
  * AERO_DW_ACCUMULATE in dtable_dtype the sum is added to what dtable holds (for a table that is the LM head too: onto
- * the dweight of aero_lmhead_logprob_fused) and rows without a token are not touched.  Tokens are sorted by id first; a row's
- * sum is formed in fp32 in an order that the ids alone determine (the same bits every time) and rounded once.
+ * the dweight of aero_lmhead_logprob_fused) and rows without a token are not touched.  A row's sum is formed in fp32 in an order
+ * that the ids alone determine (the same bits every time) and rounded once.
  * dout [T, ld_dout] of dtype AERO_F32, AERO_BF16 or AERO_F16; dtable [V, H] contiguous, AERO_F32 or AERO_BF16.  ids, V, H as above
  * (ids outside [0, V) take no part).  T = 0 is valid.
  * workspace: aero_workspace_bytes(AERO_OP_EMBEDDING_BWD, T, V, H, 0, 0).
