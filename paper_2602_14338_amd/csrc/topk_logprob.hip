@@ -536,8 +536,8 @@ __global__ __launch_bounds__(kJoinNT) void k_topk_join(const uint8_t* __restrict
   if (tid == 0 && lse) lse[t] = float(z0);
 }
 
-// Parts of a row: a workgroup per CU in all.  (151936 bf16, K = 64, one / two / four workgroups per CU: 64 rows 17.8 / 20.8 / 20.9 us,
-// 200 26.6 / 30.0 / 36.8, 300 28.8 / 37.4 / 38.8.)
+// Parts of a row: a workgroup per CU in all.  (151936 bf16, K = 64, one / two / four workgroups per CU: 64 rows 15.4 / 17.0 / 16.9 us,
+// 200 17.5 / 24.7 / 26.0, 300 26.7 / 26.6 / 30.5.)
 static int topk_parts(int64_t T, int nvec, int cus) {
   if (T > cus / 2 || nvec < 2 * 4 * 256) return 1;
   return int(std::min<int64_t>({kMaxParts, cus / T, nvec / (4 * 256)}));
@@ -564,7 +564,7 @@ static void topk_launch(const void* logits, int64_t T, int V, int64_t ld, const 
   // Held / streaming by: bf16 K = 64, 64 rows of 2399 6.7 / 7.2 us, 4000 of 1024 17.6 / 23.2; fp32, 4000 of 2399 19.6 / 25.2.  Where rows queue,
   // waiting threads cost more than vectors in turn: 5000 rows of 14464 with 1024 / 256 threads 79 / 47 us, 40 rows 7.1 / 7.8.  Eight vectors held are
   // no gain: 5000 of 14464 49.6 / 47.3.  More than 128 of 256 maxima would be no threshold.  151936, streaming by 512 / 1024: 200 rows, K = 16, 64,
-  // 256: 21.0 / 19.1, 22.1 / 19.7, 33.5 / 25.8 us; 300 rows 27.8 / 37.3, 4096 242 / 316 at K = 64.
+  // 256: 16.8 / 16.5, 18.0 / 17.5, 21.2 / 20.1 us; 300 rows 26.7 / 28.8, 4096 203 / 214 at K = 64.
   const bool many = T > 2 * compute_units();
   if (K <= 128 && per <= 2 * 256) launch(k_topk<256, DT, VEC, 2>, 256);
   else if (K <= 128 && per <= 4 * 256 && many) launch(k_topk<256, DT, VEC, 4>, 256);
