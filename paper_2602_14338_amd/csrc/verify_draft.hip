@@ -115,8 +115,19 @@ __device__ __forceinline__ SoftSum from_lane(SoftSum s, int lane) {
                  __int_as_float(__builtin_amdgcn_readlane(__float_as_int(s.s), lane))};
 }
 
-// Is the drafted token accepted: u q < p, from ln p and ln(p / q).
-__device__ __forceinline__ bool accept(float u, double ratio) {
+// Is a drafted token accepted, u q < p (has_q: q is the softmax of a row, else 1), from its logits and its rows' sums?  lp: its ln p.  Masks are looked
+// at first: the differences of masked logits, or of one and an empty row's -inf, say nothing about the probabilities, which are 0.
+__device__ __forceinline__ bool accept(float u, float zp, SoftSum p, bool has_q, float zq, SoftSum q, double& lp) {
+  const double lse_p = soft_lse(p);
+  lp = double(zp) - lse_p;
+  if (!(zp > kMasked) || !(lse_p - lse_p == 0.0)) return false;   // p = 0, or the row is empty or has a NaN
+  double ratio = lp;
+  if (has_q) {   // uniform
+    const double lse_q = soft_lse(q);
+    if (!(lse_q - lse_q == 0.0)) return false;
+    if (!(zq > kMasked)) return true;   // u 0 < p
+    ratio -= double(zq) - lse_q;
+  }
   const float coarse = float(ratio);
   const double fine = fabsf(coarse) < INFINITY ? 1.0 + (ratio - double(coarse)) : 1.0;
   return double(u) < double(expf(coarse)) * fine;
@@ -187,8 +198,8 @@ __global__ __launch_bounds__(NT) void k_verify_positions(VerifyArgs a) {
     a.sums[rt] = p;
     if (minus) a.sums[n_target + rd] = q;
     if (i < n) {
-      const double lp = double(zp) - soft_lse(p);
-      const bool ok = accept(u, minus ? lp - (double(zq) - soft_lse(q)) : lp);
+      double lp;
+      const bool ok = accept(u, zp, p, minus, zq, q, lp);
       a.lp[rt] = ok ? lp : __builtin_nan("");
       if (!ok) atomicMin(a.refused + b, i);
     }
@@ -351,8 +362,7 @@ __global__ __launch_bounds__(NT) void k_verify_draw(VerifyArgs a) {
     const int column = on ? token : 0;
     const float zp = load_elt<DT>(row_ptr<DT>(a.target, my_t, a.ld), column);
     const float zq = minus ? load_elt<DT>(row_ptr<DT>(a.draft, my_d, a.ld), column) : 0.f;
-    lp = double(zp) - soft_lse(sp);
-    ok = on && accept(u, minus ? lp - (double(zq) - soft_lse(sq)) : lp);
+    ok = accept(u, zp, sp, minus, zq, sq, lp) && on;
   }
   const int n = __builtin_ctzll(~__builtin_amdgcn_ballot_w64(ok));   // at most 63 positions
   const bool refused = n < count;

@@ -1,0 +1,65 @@
+"""The calls around a drafter on logits that masks and other callers write: finite masks, logits far from 0, probabilities that vanish.
+Helpers, checks and tolerances are those of test_gpu_drafter."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_drafter import check_verify, draft_case, gh, stored  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = {"f32": float(torch.finfo(torch.float32).min), "bf16": float(torch.finfo(torch.bfloat16).min)}
+
+# sequences, drafted tokens and logits for which verification takes one launch, decides by sequence, and decides by position
+FORMS = [(12, 2, 500), (12, 2, 7001), (16, 63, 1100)]
+
+
+def parts(case, B, G, V):
+    zt = np.asarray(case["th"], np.float32).reshape(B, G + 1, V).copy()
+    return zt, None if case["dh"] is None else np.asarray(case["dh"], np.float32).reshape(B, G, V).copy()
+
+
+def put(case, zt, zd, dtype):
+    V = zt.shape[2]
+    case["t"], host = stored(zt.reshape(-1, V), dtype)
+    case["th"] = host.reshape(zt.shape)
+    if zd is not None:
+        case["d"], host = stored(zd.reshape(-1, V), dtype)
+        case["dh"] = host.reshape(zd.shape)
+
+
+@pytest.mark.parametrize("uniform", [1e-30, 0.25])
+@pytest.mark.parametrize("mask", ["lowest", -1e30, -np.inf])
+@pytest.mark.parametrize("probs", [True, False])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,G,V", FORMS)
+def test_verify_decides_on_masks(gh, B, G, V, dtype, probs, mask, uniform):   # noqa: F811
+    """A masked token has probability 0 whatever it is masked with: it is refused where the policy's row masks it (u 0 < 0 is false), also
+    where the drafter's does so, and accepted where only the drafter's does; an empty row of the policy accepts nothing."""
+    mask = LOWEST[dtype] if mask == "lowest" else mask
+    case = draft_case(21, B, G, V, dtype, probs)
+    zt, zd = parts(case, B, G, V)
+    x = case["tokens"][:, 0]
+    for b in range(B):
+        zt[b, 0, x[b]] += 2.0   # sequences of their own otherwise
+    for b in range(6):
+        zt[b, 0, x[b]] = mask
+    zt[1, 0] = mask                                     # an empty row
+    zt[2, 0] = np.where(np.arange(V) % 3 == 0, -np.inf, np.where(np.arange(V) % 3 == 1, -1e30, LOWEST[dtype]))
+    zt[6, 0] = mask
+    zt[6, 0, (x[6] + 1) % V] = -3.0                      # one choice, not the drafted token
+    if probs:
+        zd[0, 0, x[0]] = mask                           # masked in both rows, with the same and with other numbers
+        zd[3, 0, x[3]] = -np.inf
+        zd[4, 0, x[4]] = LOWEST[dtype]
+        zd[5, 0, x[5]] = -1e30
+        zd[7, 0, x[7]] = mask                           # by the drafter alone
+        zd[8, 0] = mask                                 # an empty row of the drafter's
+        zd[9, 0] = mask
+        zt[9, 0] = mask
+    put(case, zt, zd, dtype)
+    case["u"][:10, 0] = uniform
+    ref = check_verify(case, B, G, V, V, None)
+    assert not ref["accepted"][:7].any() and (ref["tokens"][1:3, 0] == -1).all() and ref["tokens"][6, 0] == (x[6] + 1) % V
+    if probs:
+        assert ref["accepted"][7] > 0 and ref["accepted"][8] == 0 and ref["tokens"][8, 0] >= 0 and ref["tokens"][9, 0] == -1
