@@ -111,13 +111,15 @@ def verify(target, draft, V, draft_tokens, draft_count, uniform, noise):
         n = 0
         while n < count:
             x = int(draft_tokens[b][n])
-            p = np.exp(log_softmax(target[b][n][:V])[x])
-            q = np.exp(log_softmax(draft[b][n][:V])[x]) if draft is not None else 1.0
+            lp = log_softmax(target[b][n][:V])[x]
+            lq = log_softmax(draft[b][n][:V])[x] if draft is not None else 0.0
+            p, q = np.exp(lp), np.exp(lq)
             usable = np.isfinite(log_partition(draft[b][n][:V])) if draft is not None else True
             if usable and np.isfinite(p):
                 margin = min(margin, abs(float(uniform[b][n]) * q - p) / max(p, 1e-300) if p > 0 or q > 0 else np.inf)
-            if usable and float(uniform[b][n]) * q < p:
-                lps[b, n] = log_softmax(target[b][n][:V])[x]
+            lu = np.log(float(uniform[b][n])) if uniform[b][n] > 0 else -np.inf
+            if usable and lu + lq < lp:   # u q < p, also where 64 bits hold neither
+                lps[b, n] = lp
                 tokens[b, n] = x
                 n += 1
             else:

@@ -119,20 +119,11 @@ template <int N, int E> struct PlaceBits {
   }
 };
 
-// Probability of a listed log-prob, exp(lp) = 2^n exp(r) with |r| <= ln 2 / 2 and the exponential series up to r^8 / 8! (the next term is
-// under 2e-10): a loss is a small difference, and what p_k rounds by is what it is off by.
+// Probability of a listed log-prob, in 64 bits: a loss is a small difference, and what p_k rounds by is what it is off by.  0 where 32 bits hold
+// no probability.
 __device__ __forceinline__ double list_prob(float lp) {
-  const float n = rintf(lp * kLog2e);
-  const double r = fma(double(n), -0.69314718055994531, double(lp));
-  double x = 1.0 / 40320;
-  x = fma(x, r, 1.0 / 5040);
-  x = fma(x, r, 1.0 / 720);
-  x = fma(x, r, 1.0 / 120);
-  x = fma(x, r, 1.0 / 24);
-  x = fma(x, r, 1.0 / 6);
-  x = fma(x, r, 0.5);
-  x = fma(x, r, 1.0);
-  return lp < -103.97f ? 0.0 : ldexp(fma(x, r, 1.0), int(n));
+  const double p = exp_of(double(lp));
+  return lp < -103.97f ? 0.0 : p;
 }
 
 // Sums over the entries of a wave, left in s[wave] by its first lane.

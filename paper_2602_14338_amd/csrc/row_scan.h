@@ -128,6 +128,21 @@ template <int NT> __device__ __forceinline__ SoftTotal soft_block_total(SoftSum 
   return a;
 }
 
+// e^x for a 32-bit x, or a 64-bit one within +-800, in 64 bits: 2^n e^r with |r| <= ln 2 / 2 and the exponential series up to r^8 / 8! (the next term is under
+// 2e-10).
+__device__ __forceinline__ double exp_of(double x) {
+  const float n = rintf(float(x) * kLog2e);
+  const double r = fma(double(n), -0.69314718055994531, x);
+  double y = 1.0 / 40320;
+  y = fma(y, r, 1.0 / 5040);
+  y = fma(y, r, 1.0 / 720);
+  y = fma(y, r, 1.0 / 120);
+  y = fma(y, r, 1.0 / 24);
+  y = fma(y, r, 1.0 / 6);
+  y = fma(y, r, 0.5);
+  y = fma(y, r, 1.0);
+  return ldexp(fma(y, r, 1.0), int(n));
+}
 // Logarithm of a positive number x = 2^k f, f in [1/sqrt 2, sqrt 2), in 64 bits: of f's 32-bit rounding, whose logarithm rounds by 2^-26 at most, and
 // of what that leaves.
 __device__ __forceinline__ double log_of(double x) {

@@ -128,9 +128,8 @@ __device__ __forceinline__ bool accept(float u, float zp, SoftSum p, bool has_q,
     if (!(zq > kMasked)) return true;   // u 0 < p
     ratio -= double(zq) - lse_q;
   }
-  const float coarse = float(ratio);
-  const double fine = fabsf(coarse) < INFINITY ? 1.0 + (ratio - double(coarse)) : 1.0;
-  return double(u) < double(expf(coarse)) * fine;
+  // beyond +-800 the ratio is past every number that u may be: a number of 0 is below any ratio, any other above e^-800
+  return u == 0.f || double(u) < exp_of(fmin(fmax(ratio, -800.0), 800.0));
 }
 
 // Many sequences: a workgroup per position, which goes over its target row and its draft row together and decides.  Positions

@@ -63,3 +63,31 @@ def test_verify_decides_on_masks(gh, B, G, V, dtype, probs, mask, uniform):   # 
     assert not ref["accepted"][:7].any() and (ref["tokens"][1:3, 0] == -1).all() and ref["tokens"][6, 0] == (x[6] + 1) % V
     if probs:
         assert ref["accepted"][7] > 0 and ref["accepted"][8] == 0 and ref["tokens"][8, 0] >= 0 and ref["tokens"][9, 0] == -1
+
+
+@pytest.mark.parametrize("B,G,V", FORMS)
+def test_verify_of_ratios_past_32_bits(gh, B, G, V):   # noqa: F811
+    """p / q beyond what a 32-bit exponential holds, either way, and a ratio whose logarithm 32 bits round by more than 1."""
+    case = draft_case(22, B, G, V, "f32", True)
+    zt, zd = parts(case, B, G, V)
+    x = case["tokens"][:, 0]
+    u = case["u"]
+    u[:8, 0] = 0.999
+    zd[0, 0, x[0]] = -1e9                               # a mask that is an ordinary logit: q = 0 nearly, accepted
+    zd[1, 0, x[1]] = -1e9
+    zt[1, 0] -= np.float32(2.5) + np.log(np.exp(zt[1, 0].astype(np.float64)).sum()).astype(np.float32)
+    zd[2, 0, x[2]] = -3e8
+    zd[3, 0, x[3]] = -200.0                             # e^200
+    zt[4, 0, x[4]] = -1e9                               # p = 0 nearly, refused
+    zt[5, 0, x[5]] = zt[5, 0].max() - 120.0             # p > 0, which a number of 0 is below
+    u[5, 0] = 0.0
+    zt[6, 0, x[6]] = zd[6, 0, x[6]] - 110.0             # e^-110 of about 1.7e-48: the smallest 32-bit number is above it,
+    u[6, 0] = 2.0 ** -149
+    zt[7, 0, x[7]] = zd[7, 0, x[7]] - 95.0              # and below e^-95
+    u[7, 0] = 2.0 ** -149
+    put(case, zt, zd, "f32")
+    ref = check_verify(case, B, G, V, V, None)
+    assert (ref["accepted"][[0, 1, 2, 3, 5, 7]] > 0).all() and not ref["accepted"][[4, 6]].any()
+    bare = dict(case, d=None, dh=None)                  # without the drafter's rows: p itself
+    ref = check_verify(bare, B, G, V, V, None)
+    assert ref["accepted"][5] > 0 and not ref["accepted"][4]
