@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_drafter import check_verify, draft_case, gh, stored  # noqa: F401
+from test_gpu_drafter import check_distill, check_verify, draft_case, gh, normal, stored  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +91,21 @@ def test_verify_of_ratios_past_32_bits(gh, B, G, V):   # noqa: F811
     bare = dict(case, d=None, dh=None)                  # without the drafter's rows: p itself
     ref = check_verify(bare, B, G, V, V, None)
     assert ref["accepted"][5] > 0 and not ref["accepted"][4]
+
+
+@pytest.mark.parametrize("V", [200, 5000, 40003])
+def test_distill_of_lists_that_leave_little(gh, V):   # noqa: F811
+    """A teacher whose list leaves 1e-9 to 1e-7 of its probability, and a student that leaves less outside it: the others' gradient is that small
+    difference alone, to the accuracy of everything else."""
+    T, K = 6, 12
+    rng = np.random.default_rng(V)
+    z = normal([V, 6], T, V, 1.0)
+    index = np.stack([rng.permutation(V)[:K] for _ in range(T)]).astype(np.int32)
+    for t in range(T):
+        z[t, index[t]] += 60.0
+    lists = []
+    while len(lists) < T:
+        lp = np.log(rng.dirichlet(np.ones(K))).astype(np.float32)
+        if 1e-9 < 1.0 - np.exp(lp.astype(np.float64)).sum() < 1e-7:
+            lists.append(lp)
+    check_distill(z, "f32", K, 1, w=np.ones(T, np.float32), lists=(index, np.stack(lists)))
