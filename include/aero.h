@@ -285,13 +285,15 @@ aero_status aero_lmhead_logprob_fused(
  * of are cheaper to generate when a small model proposes tokens and the policy's rows verify several of them at once.
  * Their common conventions, besides those at the top of this file:
  *   - Temperature 1, as for the policy (Table 8).
- *   - Masked logits are allowed here: a logit of -inf or at or below -1e30 (such as the lowest value of fp32 or bf16, as
- *     masks write it) has probability 0.  A row without any other logit is empty: its lse is -inf.  A NaN or +inf logit
- *     makes the row's lse NaN.
+ *   - Masked logits are allowed here: a logit at or below -AERO_LOGIT_LIMIT (-inf, the lowest value of fp32 or bf16, -1e10, as
+ *     masks write it) has probability 0.  A row without any other logit is empty: its lse is -inf.  A NaN logit, or one at or
+ *     above AERO_LOGIT_LIMIT (+inf), makes the row's lse NaN.
  *   - logits [T, ld] row-major in the four storage types, ld >= V, columns >= V never touched, any alignment; rows are
  *     moved as 16-byte vectors between their ragged ends unless a base is not a multiple of the element size.
  *     1 <= V <= 2^24, T < 2^22 rows.
  */
+
+#define AERO_LOGIT_LIMIT 1.2e9f
 
 /*
  * The K largest logits of each row: what a teacher's distribution is handed on as.
@@ -351,7 +353,7 @@ aero_status aero_distill_loss_bwd(
  *          NULL: ln p_i(token) - the old_logprob that the update needs - and 0 behind the drawn token.
  * A drafted id outside [0, V) ends the sequence's drafted tokens in front of it (an id >= V raises AERO_DERR_BAD_TARGET).
  * draft_count[b] < 0: the sequence is idle (nothing read; accepted 0, tokens -1, logprob 0); > G: the same, and
- * AERO_DERR_BAD_COUNT.  A position whose target row is empty or has a NaN or +inf logit accepts nothing and draws
+ * AERO_DERR_BAD_COUNT.  A position whose target row is empty or has a NaN logit or one at or above the limit accepts nothing and draws
  * -1 (logprob 0); one whose draft row has is refused and drawn from p.
  *
  * target_logits [B, G+1, ld], draft_logits [B, G, ld] of the same dtype; draft_tokens i32[B, G], draft_count i32[B] or

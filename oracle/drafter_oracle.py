@@ -1,15 +1,15 @@
 """Float64 checker of the calls around a drafter: a teacher's lists, distillation, verification, embedding.  Plain loops over
-rows, by the definitions; shares no code with the product.  Logits are widened float64 rows; a logit of -inf or at or below
--1e30 is masked."""
+rows, by the definitions; shares no code with the product.  Logits are widened float64 rows; a logit at or below -1.2e9 (-inf,
+say) is masked, one at or above 1.2e9 makes its row NaN as +inf does."""
 import numpy as np
 
-MASKED = -1e30
+MASKED, TOO_LARGE = -1.2e9, 1.2e9
 
 
 def log_partition(z):
-    """log sum exp over the unmasked logits; -inf without any, NaN with a NaN or +inf among them."""
+    """log sum exp over the unmasked logits; -inf without any, NaN with a NaN or too large one among them."""
     z = np.asarray(z, np.float64)
-    if np.isnan(z).any() or np.isposinf(z).any():
+    if np.isnan(z).any() or (z >= TOO_LARGE).any():
         return np.nan
     z = z[z > MASKED]
     if z.size == 0:

@@ -19,6 +19,7 @@ OP_GROUP_ADVANTAGE, OP_LOGPROB_FWD, OP_GRPO_LOSS_BWD, OP_LMHEAD_FUSED = 0, 1, 2,
 OP_TOPK_LOGPROB, OP_DISTILL_LOSS_BWD, OP_VERIFY_DRAFT, OP_EMBEDDING_BWD = 4, 5, 6, 7
 AERO_TAIL_RENORM, AERO_TAIL_BUCKET = 0, 1
 AERO_TOPK_MAX, AERO_DRAFT_MAX = 256, 63
+AERO_LOGIT_LIMIT = 1.2e9   # of the calls around a drafter: masked at or below its negative, NaN at or above
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libaero_hip.so")
 

@@ -7,22 +7,26 @@
 
 namespace aero {
 
-// A logit at or below this is masked (-inf, or the lowest value of fp32 / bf16, as masks write it).
-constexpr float kMasked = -1e30f;
-// Where a running offset starts, in units of log 2 and a little above the masked logits: their exponentials are 0 by
-// themselves, and never exp(inf - inf).
-constexpr float kMaskedLog2 = -1.4426e30f;
+// A logit at or below this is masked (-inf, the lowest value of fp32 or bf16, -1e10, as masks write it); one at or above its negative makes the row NaN, as
+// +inf does.  In between an offset of 32 bits, whose unit is at most 128, is within 64 of its logit's z log2 e, so that no exponential that is kept
+// overflows, or vanishes beside its own offset; beyond (z = -1e10: 440 off) sums would be inf or 0.
+constexpr float kMasked = -AERO_LOGIT_LIMIT, kTooLarge = AERO_LOGIT_LIMIT;
+// Where a running offset starts, in units of log 2: the largest masked logit's exponent is 234 below it, so that those of masked logits are 0 by
+// themselves, and the smallest other one's (128 more, the logits' own unit there) 49 below.
+constexpr float kMaskedLog2 = -1731233792.f;
+static_assert(AERO_LOGIT_LIMIT == 1.2e9f, "kMaskedLog2 goes with it");
 
 // 2^o s = sum of 2^(z log2 e) over the logits, o a whole number near the largest z log2 e.  Being whole, it is subtracted inside the fused
 // multiply-add without a rounding of its own, and sums with different offsets meet without one either: the error of an exponential is
-// that of its argument near the offset, whatever the size of the logits.  (An offset in the logits' own units costs
-// 2^-24 |z| in every probability, 3 times the error of a gradient in fp32.)  s == 0: nothing but masked logits.  A NaN or +inf logit
+// that of its argument near the offset, whatever the size of the logits up to 2^23 (and 2^-18 up to the limit).  (An offset in the logits' own units costs
+// 2^-24 |z| in every probability, 3 times the error of a gradient in fp32.)  s == 0: nothing but masked logits.  A NaN or too large logit
 // makes s NaN.
 struct SoftSum {
   float o, s;
 };
 __device__ __forceinline__ SoftSum soft_identity() { return SoftSum{kMaskedLog2, 0.f}; }
-__device__ __forceinline__ float soft_offset(float z) { return rintf(z * kLog2e); }
+// The offset for a logit; NaN where it is too large, which makes s, and whatever the sum meets, NaN.
+__device__ __forceinline__ float soft_offset(float z) { return z < kTooLarge ? rintf(z * kLog2e) : __builtin_nanf(""); }
 
 // The largest of a vector's logits (NaN are passed over).
 template <int N> __device__ __forceinline__ float vec_max(const float (&z)[N]) {
@@ -158,11 +162,11 @@ __device__ __forceinline__ double log_of(double x) {
   return double(k) * 0.69314718055994531 + (double(logf(g)) + double(float(f - double(g)) / g));
 }
 // log sum exp in 64 bits: (o + log2 s) / log2 e; log2 e is the rounded one that the sums were formed with.  -inf for an empty row, NaN for one with a
-// NaN or +inf logit.
+// NaN or too large logit.
 __device__ __forceinline__ double soft_lse(SoftTotal st) {
   if (st.s == 0.0) return -INFINITY;
   const double lse = (double(st.o) + log_of(st.s) * 1.4426950408889634) * (1.0 / double(kLog2e));
-  return st.o < INFINITY && st.s == st.s ? lse : __builtin_nan("");
+  return st.s == st.s ? lse : __builtin_nan("");
 }
 __device__ __forceinline__ double soft_lse(SoftSum st) { return soft_lse(soft_total(st)); }
 

@@ -250,25 +250,35 @@ template <int E> __device__ __forceinline__ void load_floats(const float* x, flo
   }
 }
 // The sequence's drawn token from its best key, which the first thread has.  Where the residual vanishes (rows that are the same but for
-// roundings) it is drawn from p, by this workgroup alone.
+// roundings) it is drawn from p, by this workgroup alone; so it does where what is left is a masked logit's exponential, which beside logits next to
+// AERO_LOGIT_LIMIT may be 2^-120 for 0.
 template <int NT, int DT>
 __device__ __forceinline__ void put_drawn(const VerifyArgs& a, int b, int n, double lse, uint64_t key, uint64_t* lds /*[NT/64]*/) {
   __shared__ uint64_t s_best;
-  if (threadIdx.x == 0) s_best = key;
-  __syncthreads();
-  key = s_best;
   const int64_t rt = int64_t(b) * (a.G + 1) + n;
   const char* const row = row_ptr<DT>(a.target, rt, a.ld);
-  if (key == 0 && lse - lse == 0.0) {   // uniform
+  float z = 0.f;
+  const auto look = [&]() {   // the first thread's token's logit; no key where it is masked
+    z = key ? load_elt<DT>(row, int(~uint32_t(key))) : 0.f;
+    if (z <= kMasked) key = 0;
+  };
+  if (threadIdx.x == 0) {
+    look();
+    s_best = key;
+  }
+  __syncthreads();
+  if (s_best == 0 && lse - lse == 0.0) {   // uniform
     Drawn d{0.f, 0};
-    for (int j = threadIdx.x; j < a.V; j += NT)
-      race(d, expf(float(double(load_elt<DT>(row, j)) - lse)) * __builtin_amdgcn_rcpf(a.noise[int64_t(b) * a.V + j]), j);
+    for (int j = threadIdx.x; j < a.V; j += NT) {
+      const float y = load_elt<DT>(row, j);
+      if (y > kMasked) race(d, expf(float(double(y) - lse)) * __builtin_amdgcn_rcpf(a.noise[int64_t(b) * a.V + j]), j);
+    }
     key = block_drawn<NT>(d, lds);   // the barrier above lies between two uses of lds
+    if (threadIdx.x == 0) look();
   }
   if (threadIdx.x == 0) {
-    const int drawn = key ? int(~uint32_t(key)) : -1;
-    a.out[rt] = drawn;
-    if (a.logprob) a.logprob[rt] = drawn >= 0 ? float(double(load_elt<DT>(row, drawn)) - lse) : 0.f;
+    a.out[rt] = key ? int(~uint32_t(key)) : -1;
+    if (a.logprob) a.logprob[rt] = key ? float(double(z) - lse) : 0.f;
   }
 }
 
