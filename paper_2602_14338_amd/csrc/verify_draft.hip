@@ -509,8 +509,11 @@ template <int DT, bool VEC> static void verify_launch(VerifyArgs a, hipStream_t 
   // Vectors that a lane goes through where a wave takes a row: few enough, or more where the sequences alone fill the CUs.  Two or three launches / one:
   // bf16, 1 sequence x 3 copied tokens of 1024 7.0 / 5.7 us, 8 x 4 of 3000 (6 vectors) 9.2 / 8.3, of 11000 (22) 13.4 / 14.1, 256 x 3 of 1024 16.3 / 7.4, of
   // 16000 (32) 26.6 / 19.6, 1 x 8 of 5586 (22) 9.3 / 11.6.  (Rows split over the waves that have none: 1 us more at 1024, nothing gained below 32000.)
+  // Past one workgroup to a CU the bound stays, and falls where many queue, since a wave reads all rows and by position those behind a refusal are mostly left
+  // out: 8192 (16 vectors), 1024 x 5 69 / 56, 4096 x 5 246 / 228; 16384 (32), 1024 x 5 93 / 97, 4096 x 3 259 / 285; 32000 (63), 256 x 5 49 / 41, 512 x 5 82 / 91,
+  // 4096 x 5 513 / 651; 65536 x 8 (256), 4096 sequences 1016 / 1872.
   const int waves = 1024 / kWave, each = int((rows / a.B + waves - 1) / waves) * ((nvec + kWave - 1) / kWave);
-  if (each <= 12 + a.B / 8) {
+  if (each <= (a.B <= 1024 ? 12 + std::min(a.B, 256) / 8 : 24)) {
     a.slices = 1;
     hipLaunchKernelGGL((k_verify_draw<1024, DT, VEC, kAlone>), dim3(unsigned(a.B)), dim3(1024), 0, s, a);
   } else if (a.G > 0 && positions >= 4 * compute_units()) {

@@ -269,3 +269,14 @@ def test_no_masked_token_is_drawn(gh, B, G, V):   # noqa: F811
     put(case, zt, zd, "f32")
     ref = check_verify(case, B, G, V, V, None)
     assert not ref["accepted"].any() and (ref["tokens"][:, 0] % 50 == 3).all()
+
+
+# ------------------------------------------------------------------------------------------------ many sequences
+@pytest.mark.parametrize("probs", [True, False])
+@pytest.mark.parametrize("B,G,V", [(1030, 1, 13001), (1030, 1, 5000), (420, 2, 24001)])
+def test_verify_of_many_sequences_of_longer_rows(gh, B, G, V, probs):   # noqa: F811
+    """On both sides of the lengths up to which a workgroup takes a whole sequence, where there are more sequences than compute units."""
+    case = draft_case(25, B, G, V, "bf16", probs)
+    count = np.full(B, G, np.int32)
+    count[5], count[6], count[7] = -1, 0, G + 1
+    check_verify(case, B, G, V, V, count, err=16)
