@@ -71,7 +71,10 @@ class Drafter:
         binding.aero_distill_loss_bwd(z, T, self.V, self.V, teacher.index, teacher.logprob, K, token_weight, tail, grad_scale, loss, None,
                                       dz, _workspace(binding.OP_DISTILL_LOSS_BWD, dev, T=T, V=self.V), self.err)
         if dtable is not None:
-            dtable.copy_(dz.t() @ x)
+            if dtable.dtype == torch.float32 and dz.dtype != torch.float32:
+                torch.mm(dz.t(), x, out_dtype=torch.float32, out=dtable)   # as it is summed up: not rounded to the rows' type in between
+            else:
+                dtable.copy_(dz.t() @ x)
             dx = dz @ self.table
             binding.aero_embedding_bwd(dx, T, self.H, self.H, ids, self.V, self.scale, dtable,
                                        _workspace(binding.OP_EMBEDDING_BWD, dev, T=T, V=self.V, H=self.H), True, self.err)

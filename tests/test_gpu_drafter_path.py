@@ -238,3 +238,31 @@ def test_example(gh, monkeypatch, capsys):
     lines = capsys.readouterr().out.strip().splitlines()
     first, final = ([float(x.split()[-1 if "divergence" in x else 0]) for x in lines[i].split(", ")] for i in (0, -1))
     assert final[0] < 0.2 * first[0] and first[1] < 1.0 and final[1] > 2.0
+
+
+def test_head_gradient_is_summed_in_32_bits(gh):
+    """An fp32 table gradient is the head's product and the lookup's sums of the rounded dz and dx in 32 bits, which the same calls give here: sums of T
+    products, n tokens of an id, and the addition."""
+    from paper_2602_14338_amd import drafter as d
+    rng = np.random.default_rng(8)
+    T, V, H, K, scale = 300, 900, 48, 7, 2.0
+    table = device(rng.normal(0, 0.3, size=(V, H)).astype(np.float32)).bfloat16()
+    ids = rng.integers(0, V, size=T).astype(np.int32)
+    index = np.stack([rng.permutation(V)[:K] for _ in range(T)]).astype(np.int32)
+    lp = np.log(rng.dirichlet(np.ones(K + 1), size=T)[:, :K]).astype(np.float32)
+    teacher = d.TeacherLists(device(index), device(lp), None)
+    weight = device(rng.random(T).astype(np.float32))
+    drafter = d.Drafter(table, scale)
+    dtable = torch.full((V, H), 7.0, device="cuda")
+    drafter.loss_bwd(device(ids), teacher, weight, dtable)
+    x = drafter.hidden(device(ids))
+    dz = x @ table.t()
+    gh.aero.aero_distill_loss_bwd(dz, T, V, V, teacher.index, teacher.logprob, K, weight, 1, 1.0, torch.empty(1, device="cuda"), None, dz,
+                                  torch.empty(gh.aero.aero_workspace_bytes(gh.aero.binding.OP_DISTILL_LOSS_BWD, T=T, V=V), dtype=torch.uint8, device="cuda"))
+    dx = dz @ table
+    z64, x64 = wide(dz), wide(x)
+    lookup, size = orc.embedding_grad(wide(dx), ids, V, scale)
+    n = np.bincount(ids, minlength=V)[:, None]
+    head, head_size = z64.T @ x64, np.abs(z64.T) @ np.abs(x64)
+    bound = 2.0 ** -24 * ((T + 2) * head_size + (n + 2) * size + 2 * np.abs(head + lookup)) + 2.0 ** -126
+    assert (np.abs(wide(dtable) - head - lookup) <= bound).all()
