@@ -171,7 +171,8 @@ __device__ __forceinline__ RowGrad row_terms(const DistillArgs& a, int64_t t, fl
     bad |= s[k].bad != 0;
   }
   const bool has_rest = rest.s != 0.0, renorm = a.tail == AERO_TAIL_RENORM;
-  const float rest_q = has_rest ? float(rest.s) / float(all.s) * exp2_fast(rest.o - all.o) : 0.f;
+  // the difference of the offsets first: far from 0 a sum may be 2^64 and more, or 2^-64, for a logit (see kMasked)
+  const float rest_q = has_rest ? float(rest.s) * exp2_fast(rest.o - all.o) / float(all.s) : 0.f;
   const double g = double(w) * double(a.grad_scale);
   const double rest_p = renorm || !has_rest || mass >= 1.0 ? 0.0 : 1.0 - mass;
   const double total = renorm ? 1.0 : mass + rest_p;

@@ -228,6 +228,36 @@ def test_distill_of_rows_far_from_zero(gh, V, copies, tail):   # noqa: F811
     assert np.isnan(got[:3]).all() and np.isfinite(got[3:]).all()
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("V", [3000, 40003, 100003])
+def test_distill_of_offsets_off_either_way(gh, V, tail, sign):   # noqa: F811
+    """Offsets that are 60 above the others' exponents and 60 below the listed ones': each sum keeps what its offset leaves, 2^60 and 2^-60 a logit, and
+    the others' share of the whole is 0, not the infinite ratio of those times 0."""
+    k = float(np.float32(1.4426950408889634))
+    far = (np.float32(1.1e9) + 128 * np.arange(4000)).astype(np.float32) * np.float32(sign)
+    residual = far.astype(np.float64) * k - np.rint((far.astype(np.float64) * k).astype(np.float32).astype(np.float64))
+    others = far[residual > 60].min()
+    listed = far[(residual < -60) & (far > others)].min()
+    T, K = 3, 5
+    rng = np.random.default_rng(V)
+    index = np.stack([rng.permutation(V)[:K] for _ in range(T)]).astype(np.int32)
+    lp = np.log(rng.dirichlet(np.ones(K + 1), size=T)[:, :K]).astype(np.float32)
+    z = np.full((T, V), others, np.float32)
+    for t in range(T):
+        z[t, index[t]] = listed
+    dev, host = stored(z, "f32")
+    ref = orc.distill(host - float(listed), V, index, lp, np.ones(T), tail, 1.0)
+    dz = sevens(T, V, "f32")
+    _, rows, _ = run_distill(dev, T, V, V, index, lp, np.ones(T, np.float32), tail, 1.0, dz)
+    total, rest_p, _ = ref["masses"].T
+    share = np.full((T, V), 1.0 / (V - K))
+    np.put_along_axis(share, index, 0.0, 1)
+    size = total[:, None] * ref["q"] + ref["p"] + rest_p[:, None] * share
+    assert (np.abs(rows - ref["row_loss"]) <= 4 * 2.0 ** -18 + 2.0 ** -22 * np.abs(ref["row_loss"])).all()
+    assert (np.abs(wide(dz).reshape(T, V) - ref["dlogits"]) <= 4 * 2.0 ** -18 * size + 2.0 ** -126).all()
+
+
 @pytest.mark.parametrize("mask", MASKS)
 @pytest.mark.parametrize("probs", [True, False])
 @pytest.mark.parametrize("B,G,V", FORMS)
