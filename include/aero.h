@@ -23,9 +23,10 @@
  *     index, or row_active == 0.  It is not read, its outputs are 0 (gradient rows +0, or left as
  *     they are when the rollout index is AERO_ROW_UNTOUCHED), and nothing about it is flagged,
  *     whatever its other fields hold.
- *   - Logits (and hidden states / weights) must be finite.  An infinite or NaN logit gives NaN
- *     statistics for its row (the entropy term contains 0 * inf); vocabulary masking with -inf
- *     is not part of the policy the paper defines (App. C).
+ *   - Logits (and hidden states / weights) of the calls up to aero_lmhead_logprob_fused must be
+ *     finite.  An infinite or NaN logit gives NaN statistics for its row (the entropy term contains
+ *     0 * inf); vocabulary masking with -inf is not part of the policy the paper defines (App. C).
+ *     The calls around a drafter, at the end of this file, take masked logits.
  */
 #ifndef AERO_H
 #define AERO_H
@@ -49,13 +50,14 @@ enum {
   AERO_ERR_LIMIT = 7       /* size beyond the fixed capacity of an entry point that owns its scratch */
 };
 
-/* Storage types of logits / dlogits.  AERO_F16 (IEEE binary16) and AERO_F8E4M3 are accepted by
- * aero_logprob_fwd and aero_grpo_loss_bwd only.  fp16 gradient entries round to the fp16 grid (subnormals
+/* Storage types.  AERO_F16 (IEEE binary16) and AERO_F8E4M3 are accepted by the calls that take logits (logits and
+ * dlogits of aero_logprob_fwd, aero_grpo_loss_bwd, aero_topk_logprob, aero_distill_loss_bwd, aero_verify_draft),
+ * AERO_F16 by the embedding calls as well (table, out, dout).  fp16 gradient entries round to the fp16 grid (subnormals
  * below 6.1e-5, zero below 3e-8): pass a grad_scale that lifts them, as with any fp16 gradient.
  * AERO_F8E4M3 is the 8-bit float with 4 exponent bits (bias 7) and 3 mantissa bits in the variant without
  * infinities (sign.1111.111 is NaN, largest finite value 448, subnormals are multiples of 2^-9); gradient
  * entries are rounded to nearest even on that grid and saturate at +-448, so a grad_scale is needed all the
- * more.  All arithmetic is fp32 whatever the storage type. */
+ * more.  Arithmetic per element is fp32 whatever the storage type; what is formed in 64 bits is said at its call. */
 enum { AERO_F32 = 0, AERO_BF16 = 1, AERO_F16 = 2, AERO_F8E4M3 = 3 };
 
 /* OR-ed into the dweight_dtype argument of aero_lmhead_logprob_fused: dweight += dz^T hidden instead of
@@ -281,9 +283,9 @@ aero_status aero_lmhead_logprob_fused(
     void* workspace, size_t workspace_bytes, void* stream);
 
 /*
- * The four calls below keep a drafter close to the policy and draft with it: the rollouts that this update is made
+ * The five calls below keep a drafter close to the policy and draft with it: the rollouts that this update is made
  * of are cheaper to generate when a small model proposes tokens and the policy's rows verify several of them at once.
- * Their common conventions, besides those at the top of this file:
+ * Conventions of the three that take logits, besides those at the top of this file:
  *   - Temperature 1, as for the policy (Table 8).
  *   - Masked logits are allowed here: a logit at or below -AERO_LOGIT_LIMIT (-inf, the lowest value of fp32 or bf16, -1e10, as
  *     masks write it) has probability 0.  A row without any other logit is empty: its lse is -inf.  A NaN logit, or one at or
@@ -293,7 +295,7 @@ aero_status aero_lmhead_logprob_fused(
  *     1 <= V <= 2^24, T < 2^22 rows.
  */
 
-#define AERO_LOGIT_LIMIT 1.2e9f
+#define AERO_LOGIT_LIMIT 1.2e9f   /* logits at or below its negative are masked, at or above it make their row NaN */
 
 /*
  * The K largest logits of each row: what a teacher's distribution is handed on as.
@@ -357,7 +359,7 @@ aero_status aero_distill_loss_bwd(
  * -1 (logprob 0); one whose draft row has is refused and drawn from p.
  *
  * target_logits [B, G+1, ld], draft_logits [B, G, ld] of the same dtype; draft_tokens i32[B, G], draft_count i32[B] or
- * NULL (= G for all), uniform f32[B, G] in [0, 1), noise f32[B, V], > 0.  0 <= G <= AERO_DRAFT_MAX (AERO_ERR_LIMIT beyond);
+ * NULL (= G for all), uniform f32[B, G] in [0, 1), noise f32[B, V], > 0 (normal numbers).  0 <= G <= AERO_DRAFT_MAX (AERO_ERR_LIMIT beyond);
  * with G = 0 draft_tokens, uniform and draft_logits may be NULL.  B = 0 is valid.
  * workspace: aero_workspace_bytes(AERO_OP_VERIFY_DRAFT, B * (G + 1), V, 0, 0, B).
  */
@@ -373,7 +375,7 @@ aero_status aero_verify_draft(
  * Embedding rows: out[t, :] = scale * table[ids[t], :], formed in fp32 and rounded once.
  * table [V, H] contiguous, out [T, ld_out] (ld_out >= H, columns >= H untouched: rows of a wider buffer), both of dtype AERO_F32, AERO_BF16
  * or AERO_F16; ids i32[T].  A negative id is padding: its row is +0; an id >= V likewise, and raises
- * AERO_DERR_BAD_TARGET.  1 <= V <= 2^24, 1 <= H <= 2^20; any element's alignment.
+ * AERO_DERR_BAD_TARGET.  T < 2^22, 1 <= V <= 2^24, 1 <= H <= 2^20; any element's alignment.
  */
 aero_status aero_embedding_fwd(
     const void* table, int32_t dtype, int32_t V, int32_t H, const int32_t* ids, int64_t T, float scale,
@@ -384,7 +386,7 @@ aero_status aero_embedding_fwd(
  * AERO_DW_ACCUMULATE in dtable_dtype the sum is added to what dtable holds (for a table that is the LM head too: onto
  * the dweight of aero_lmhead_logprob_fused) and rows without a token are not touched.  A row's sum is formed in fp32 in an order
  * that the ids alone determine (the same bits every time) and rounded once.
- * dout [T, ld_dout] of dtype AERO_F32, AERO_BF16 or AERO_F16; dtable [V, H] contiguous, AERO_F32 or AERO_BF16.  ids, V, H as above
+ * dout [T, ld_dout] of dtype AERO_F32, AERO_BF16 or AERO_F16; dtable [V, H] contiguous, AERO_F32 or AERO_BF16.  ids, T, V, H as above
  * (ids outside [0, V) take no part).  T = 0 is valid.
  * workspace: aero_workspace_bytes(AERO_OP_EMBEDDING_BWD, T, V, H, 0, 0).
  */

@@ -4,11 +4,12 @@
 // the draft rows in front of it), a row split over several workgroups; with many sequences it also decides position by position, so that
 // rows behind a refusal are mostly left out.  The second finds the first position whose uniform number is not below p / q, and in every
 // slice of the vocabulary the largest max(0, p - q) / noise there.  The third joins a sequence's slices: the larger score, the lower id
-// where equal, which does not depend on their order.  (Joining in the second launch by atomics takes a device-wide fence per workgroup, 50 of 129
-// us for 128 sequences.)  Short rows take one launch, in which a workgroup does all of that for a sequence.
+// where equal, which does not depend on their order.  (Joining in the second launch by its last workgroup, with the slices' keys as plain
+// stores, takes a device-wide fence per workgroup, 50 of 129 us for 128 sequences; keys that are atomics themselves have not been measured.)  Short rows take one launch, in which a workgroup does all of that for a sequence.
 //
 // Bound by the rows' and the noise's bytes (151936 bf16: 128 sequences of up to 5 drafted tokens 71 us, of which the sums 41 at 5.6 TB/s and
-// the draw 28; 256 of 3 copied tokens 86 us) and, for few sequences, by three launches (8 of 4 tokens 16.9 us).
+// the draw 28; 256 of 3 copied tokens 86 us) and, for few sequences, by three launches (8 of 4 tokens 16.9 us).  The noise is the
+// caller's: a [B, V] fp32 row a sequence, 31 and 44 % of the bytes of those two.
 #include <algorithm>
 
 #include "row_scan.h"

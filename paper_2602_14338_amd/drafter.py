@@ -114,8 +114,8 @@ def verify(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tokens: Op
 def generate(drafter: Drafter, policy: Callable[[torch.Tensor], torch.Tensor], last: torch.Tensor, G: int,
              generator: Optional[torch.Generator] = None):
     """One turn of drafting for each sequence: the policy is asked once for the rows behind the last token and the G drafted ones
-    (``policy``: i32 [B, G+1] -> rows [B, G+1, ld]).  Returns accepted, tokens, logprob and the policy's rows, from which the
-    drafter can learn."""
+    (``policy``: i32 [B, G+1] -> rows [B, G+1, ld]).  Returns accepted, tokens, logprob, the policy's rows, from which the
+    drafter can learn, and the drafted tokens i32 [B, G], which with ``last`` are the tokens in front of those rows."""
     tokens, rows = drafter.propose(last, G, generator)
     target = policy(torch.cat((last.view(-1, 1), tokens), 1))
     if target.shape[2] != drafter.V:   # rows with padding columns: the drafter's get them as well
