@@ -499,22 +499,30 @@ size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B) {
   return verify_workspace(nullptr, rows, B > 0 ? B : 0).bytes;
 }
 
+// One launch, a workgroup a sequence and a wave a row?  By the vectors that a lane goes through: few enough, or more where the sequences alone fill the CUs.  Two
+// or three launches / one, bf16 (vectors): 1 sequence x 3 copied tokens of 1024 (2) 7.0 / 5.7 us, 8 x 4 of 3000 (6) 9.2 / 8.3, of 11000 (22) 13.4 / 14.1, 256 x 3 of
+// 1024 16.3 / 7.4, of 16000 (32) 26.6 / 19.6, 1 x 8 of 5586 (22) 9.3 / 11.6.  (Rows split over the waves that have none: 1 us more at 1024, nothing gained below
+// 32000.)  Where workgroups queue the bound falls, since all rows are read and by position those behind a refusal mostly are not: 512 x 5 of 16384 (32) 49 / 45, of
+// 32000 (63) 82 / 91, 1024 x 5 of 8192 (16) 69 / 56, of 16384 93 / 97, 4096 x 5 of 8192 246 / 228, of 16384 316 / 361, of 32000 513 / 651; and so it does, further, for fewer
+// rows than four, which leave most waves idle: nothing drafted, 512 x 4096 (8) 11.4 / 12.1, 1024 x 2048 (4) 14.3 / 19.0, 4096 x 8192 59 / 126; one token with the drafter's
+// rows, 512 x 8192 0.85 of the time, 1024 x 8192 37 / 40, 4096 x 4096 99 / 107.
+static bool verify_alone(int64_t B, int64_t rows, int nvec) {
+  constexpr int kWaves = 1024 / kWave;
+  const int64_t each = (rows + kWaves - 1) / kWaves * ((nvec + kWave - 1) / kWave);
+  if (B <= 256) return each <= 12 + B / 8;
+  if (rows < 4) return each <= (rows == 1 ? 2048 : 10240) / B;
+  return each <= (B <= 1024 ? 32 : 20);
+}
+
 template <int DT, bool VEC> static void verify_launch(VerifyArgs a, hipStream_t s) {
   constexpr int NT = 512;
   const int64_t positions = int64_t(a.B) * (a.G + 1), rows = positions + (a.draft ? int64_t(a.B) * a.G : 0);
   const int nvec = a.V / RowView<DT, VEC>::E;
   a.slices = verify_slices(a.B, nvec, NT);
   const dim3 draw{unsigned(a.B), unsigned(a.slices)};
-  // four positions to a CU and more: rows one by one / by position, 256 sequences x 8 drafted tokens 260 / 192 us, x 3 142 / 134, x 3 copied
+  // Otherwise, from four positions to a CU on: rows one by one / by position, 256 sequences x 8 drafted tokens 260 / 192 us, x 3 142 / 134, x 3 copied
   // ones 94.0 / 91.8; fewer: 128 x 5 102 / 100, with drawn counts 75 / 85, 64 x 4 49.9 / 53.4
-  // Vectors that a lane goes through where a wave takes a row: few enough, or more where the sequences alone fill the CUs.  Two or three launches / one:
-  // bf16, 1 sequence x 3 copied tokens of 1024 7.0 / 5.7 us, 8 x 4 of 3000 (6 vectors) 9.2 / 8.3, of 11000 (22) 13.4 / 14.1, 256 x 3 of 1024 16.3 / 7.4, of
-  // 16000 (32) 26.6 / 19.6, 1 x 8 of 5586 (22) 9.3 / 11.6.  (Rows split over the waves that have none: 1 us more at 1024, nothing gained below 32000.)
-  // Past one workgroup to a CU the bound stays, and falls where many queue, since a wave reads all rows and by position those behind a refusal are mostly left
-  // out: 8192 (16 vectors), 1024 x 5 69 / 56, 4096 x 5 246 / 228; 16384 (32), 1024 x 5 93 / 97, 4096 x 3 259 / 285; 32000 (63), 256 x 5 49 / 41, 512 x 5 82 / 91,
-  // 4096 x 5 513 / 651; 65536 x 8 (256), 4096 sequences 1016 / 1872.
-  const int waves = 1024 / kWave, each = int((rows / a.B + waves - 1) / waves) * ((nvec + kWave - 1) / kWave);
-  if (each <= (a.B <= 1024 ? 12 + std::min(a.B, 256) / 8 : 24)) {
+  if (verify_alone(a.B, rows / a.B, nvec)) {
     a.slices = 1;
     hipLaunchKernelGGL((k_verify_draw<1024, DT, VEC, kAlone>), dim3(unsigned(a.B)), dim3(1024), 0, s, a);
   } else if (a.G > 0 && positions >= 4 * compute_units()) {

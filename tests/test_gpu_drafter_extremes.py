@@ -310,3 +310,14 @@ def test_verify_of_many_sequences_of_longer_rows(gh, B, G, V, probs):   # noqa: 
     count = np.full(B, G, np.int32)
     count[5], count[6], count[7] = -1, 0, G + 1
     check_verify(case, B, G, V, V, count, err=16)
+
+
+@pytest.mark.parametrize("B,G,V", [(1100, 0, 700), (1100, 0, 3001), (600, 0, 2001), (1100, 1, 3001), (1100, 1, 6001), (300, 2, 9001)])
+def test_verify_of_many_sequences_of_few_rows(gh, B, G, V):   # noqa: F811
+    """Few rows a sequence, which leave most of a workgroup's waves idle: on both sides of where one launch ends."""
+    for dtype, probs in (("bf16", True), ("f32", False)):
+        count = None
+        if G:
+            count = np.full(B, G, np.int32)
+            count[3], count[4] = -1, 0
+        check_verify(draft_case(26, B, G, V, dtype, probs), B, G, V, V, count)
