@@ -86,7 +86,8 @@ enum { AERO_CAT_ZERO = 0, AERO_CAT_PARTIAL = 1, AERO_CAT_GOOD = 2, AERO_CAT_PERF
 
 enum { AERO_OP_GROUP_ADVANTAGE = 0, AERO_OP_LOGPROB_FWD = 1, AERO_OP_GRPO_LOSS_BWD = 2,
        AERO_OP_LMHEAD_FUSED = 3, AERO_OP_TOPK_LOGPROB = 4, AERO_OP_DISTILL_LOSS_BWD = 5,
-       AERO_OP_VERIFY_DRAFT = 6, AERO_OP_EMBEDDING_BWD = 7 };
+       AERO_OP_VERIFY_DRAFT = 6, AERO_OP_EMBEDDING_BWD = 7, AERO_OP_PREFERENCE_LOSS = 8,
+       AERO_OP_PREFERENCE_LOSS_BWD = 9, AERO_OP_GRAD_NORM = 10 };
 
 /* Hyper-parameters of the curation step (Table 8; Sec. 4.2). */
 typedef struct {
@@ -394,6 +395,145 @@ aero_status aero_embedding_bwd(
     const void* dout, int32_t dtype, int64_t T, int32_t H, int64_t ld_dout, const int32_t* ids, int32_t V, float scale,
     void* dtable, int32_t dtable_dtype, int32_t* err_flag /*nullable*/,
     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A loss on pairs of rollouts, the first of which is to be preferred (a right and a wrong one of the same query: with k_ratio = 1 the
+ * curation keeps as many of either), and its gradient.
+ *   log ratio of a rollout   s_r = sum over its tokens t of (logprob[t] - ref_logprob[t]), with `average` divided by their number;
+ *                            ref_logprob == NULL counts as 0; a rollout without tokens has s_r = 0
+ *   pair p, c = pair_chosen[p], j = pair_rejected[p]:  m_p = beta (s_c - s_j),  x_p = m_p - margin
+ *   AERO_PAIR_LOGISTIC       l(x) = (1 - smoothing) ln(1 + e^-x) + smoothing ln(1 + e^x)
+ *   AERO_PAIR_HINGE          l(x) = max(0, 1 - x)
+ *   AERO_PAIR_SQUARE         l(x) = ((x - 1/2) / beta)^2
+ *   loss = sum_p w_p l(x_p),  w_p = pair_weight[p], or 1 / P with pair_weight == NULL
+ *   drollout[r] = dloss / ds_r (with `average` divided by the number of tokens: the derivative by each token's log-prob)
+ *   dlogits[t, j] = grad_scale drollout[token_rollout[t]] (1[j == targets[t]] - softmax(z[t])_j)
+ * A rollout may be in any number of pairs.  Pairs with w_p == 0 or a negative index take no part, nor do those with an index >= R, which raise
+ * AERO_DERR_BAD_ROLLOUT; their pair_margin is 0.
+ * Log ratios, margins, losses and derivatives are formed in 64 bits from log-probs of 32 (of 64 in the call that takes logits); sums over the tokens and the pairs of
+ * a rollout do not depend on their order: the same bits every time.
+ * A token's logprob - ref_logprob that is infinite makes its rollout's s_r infinite, NaN (or infinities of both signs) NaN.  A
+ * margin of +-inf has the loss's limit, and the derivative's; NaN makes the loss, the pair's margin and what derives from it NaN.
+ *
+ * token_rollout i32[T] (as elsewhere: negative = no rollout, an index >= R the same and raises AERO_DERR_BAD_ROLLOUT); tokens of a rollout may
+ * stand anywhere.  pair_chosen, pair_rejected i32[P], pair_weight f32[P] or NULL, ref_logprob f32[T] or NULL.
+ * T < 2^25 (2^22 rows of logits), 0 <= R < 2^22, 0 <= P < 2^22; T = 0, R = 0 and P = 0 are valid (arrays without entries may be NULL).
+ * params is a host pointer, read before the call returns: beta > 0 and finite, 0 <= smoothing <= 1/2 (looked at by AERO_PAIR_LOGISTIC alone), margin finite.
+ */
+enum { AERO_PAIR_LOGISTIC = 0, AERO_PAIR_HINGE = 1, AERO_PAIR_SQUARE = 2 };
+typedef struct {
+  int32_t kind;      /* AERO_PAIR_* */
+  int32_t average;   /* 0: log ratios are sums over a rollout's tokens, 1: means */
+  float beta, smoothing, margin;
+} aero_preference_params;
+
+/*
+ * The loss from log-probs (those of aero_logprob_fwd or aero_lmhead_logprob_fused over all micro-batches of a step: a rollout's log ratio needs all
+ * of its tokens).  The gradient of a micro-batch is then aero_grpo_loss_bwd's, or aero_lmhead_logprob_fused's, with adv[r] = -drollout[r],
+ * weight[r] = 1 and old_logprob the log-probs themselves (a ratio of 1).
+ * logprob f32[T] (not read where token_rollout is negative).  Outputs loss f32[1], pair_margin f32[P] (m_p) or NULL, rollout_ratio f32[R] (s_r) or
+ * NULL, drollout f32[R] or NULL.
+ * workspace: aero_workspace_bytes(AERO_OP_PREFERENCE_LOSS, T, 0, 0, R, P) (P in the place of Q).
+ */
+aero_status aero_preference_loss(
+    const float* logprob, int64_t T, const float* ref_logprob /*nullable*/, const int32_t* token_rollout, int32_t R,
+    const int32_t* pair_chosen, const int32_t* pair_rejected, const float* pair_weight /*nullable*/, int32_t P,
+    const aero_preference_params* params,
+    float* loss, float* pair_margin /*nullable*/, float* rollout_ratio /*nullable*/, float* drollout /*nullable*/,
+    int32_t* err_flag /*nullable*/, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same from logits, with the gradient, where all rollouts of a pair are in one batch of rows.  Conventions of the calls that take masked logits: a sampled token
+ * whose logit is masked has log-prob -inf; rows without an unmasked logit take no part (log-prob 0, gradient +0); a row with a NaN or too
+ * large logit has log-prob NaN, and NaN makes its gradient row NaN.  A sampled-token id >= V raises AERO_DERR_BAD_TARGET and its row is ignored, as rows with
+ * a negative id or rollout index are; dlogits rows marked AERO_ROW_UNTOUCHED are left as they are, other ignored rows are +0.
+ * logits / dlogits [T, ld], same dtype and ld; dlogits may alias logits (in place), NULL: loss only.  logprob_out f32[T] or
+ * NULL (0 for rows that take no part).
+ * workspace: aero_workspace_bytes(AERO_OP_PREFERENCE_LOSS_BWD, T, V, 0, R, P) (P in the place of Q).
+ */
+aero_status aero_preference_loss_bwd(
+    const void* logits, int32_t dtype, int64_t T, int32_t V, int64_t ld, const int32_t* targets,
+    const float* ref_logprob /*nullable*/, const int32_t* token_rollout, int32_t R,
+    const int32_t* pair_chosen, const int32_t* pair_rejected, const float* pair_weight /*nullable*/, int32_t P,
+    const aero_preference_params* params, float grad_scale,
+    float* loss, float* pair_margin /*nullable*/, float* rollout_ratio /*nullable*/, float* logprob_out /*nullable*/,
+    void* dlogits /*nullable*/, int32_t* err_flag /*nullable*/, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Many tensors at once: their description, laid out once.  aero_tensor_table writes an image of aero_tensor_table_bytes(list, count) bytes to HOST
+ * memory; the caller keeps it and copies it to the device (16-byte aligned), and hands both to the calls below.  The image holds the
+ * pointers, not what they point to; the device copy also holds a counter, so that calls on one table have to be ordered on one stream.
+ *   - Tensors are contiguous, any element's alignment, 0 <= n < 2^32 elements each; count < 2^20.  They do not overlap.
+ *   - grad and param f32, bf16 or fp16.  param == NULL: the gradient takes part in the norm alone (the moments are not looked at).
+ *   - master f32[n] or NULL: the weights the step is made on; param is then its rounding.  fp16 parameters need one, fp32 ones have none
+ *     (AERO_ERR_DTYPE).
+ *   - Moments: f32[n] where the scales are NULL, otherwise 8 bits (see aero_adamw_step).  Both moments alike.
+ *   - decay multiplies the step's weight_decay (0 for a tensor that does not decay).
+ * NULL where a pointer is needed: AERO_ERR_NULL; element alignment: AERO_ERR_ALIGN; count or n out of range: AERO_ERR_SHAPE; an image too small:
+ * AERO_ERR_WORKSPACE.
+ */
+typedef struct {
+  void* param;
+  const void* grad;
+  float* master;
+  void *exp_avg, *exp_avg_sq;               /* f32[n], or codes int8[n] and uint8[n] */
+  float *exp_avg_scale, *exp_avg_sq_scale;  /* NULL, or f32[(n + 255) / 256] */
+  int64_t n;
+  int32_t param_dtype, grad_dtype;
+  float decay;
+} aero_tensor;
+#define AERO_MOMENT_BLOCK 256
+size_t aero_tensor_table_bytes(const aero_tensor* list, int32_t count);
+aero_status aero_tensor_table(const aero_tensor* list, int32_t count, void* image, size_t image_bytes);
+
+/*
+ * Norm of all gradients of a table, and the factor that a step multiplies them with:
+ *   norm[0] = |grad_scale| sqrt(sum of g^2),   factor[0] = grad_scale min(1, max_norm / norm), max_norm <= 0: grad_scale.
+ * grad_scale undoes a scale that the loss was given.  A NaN or infinite gradient makes norm that and factor NaN, at
+ * which aero_adamw_step leaves everything as it is.  Squares and sums in 64 bits, in an order that the table alone determines.
+ * norm, factor f32[1], either may be NULL.  grad_scale finite, max_norm not NaN (AERO_ERR_SHAPE).  An empty table has norm 0.
+ * workspace: aero_workspace_bytes(AERO_OP_GRAD_NORM, 0, 0, 0, 0, 0).
+ */
+aero_status aero_grad_norm(
+    const void* image, void* table, float grad_scale, float max_norm, float* norm /*nullable*/, float* factor /*nullable*/,
+    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One step of Adam with decoupled weight decay on every tensor of a table that has parameters.  With t = step[0] + 1, per element:
+ *   g = factor grad,   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = p - rate (decay weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)),   rate = lr lr_factor,
+ * then step[0] = t.  factor f32[1] or NULL (1), lr_factor f32[1] or NULL (1), step i32[1] (>= 0) are device words, so that a captured call
+ * follows a schedule and counts its replays.  factor NaN or infinite: the step does not take place, step included.
+ * Per element in 32 bits, every product and sum of m and v rounded by itself; 1 - beta^t in 64.
+ *
+ * Moments in 8 bits: blocks of 256 elements of a tensor share a scale S,
+ *   m = c |c| S, c = -127 .. 127, S = max|m| / 127^2;    v = c^4 S, c = 0 .. 255, S = max v / 255^4
+ * (steps that grow with the value: 1.6 % at the top of a block, 16 % at a hundredth of it, a smallest m of 6.2e-5 and a smallest sqrt(v) of 1.5e-5 of the
+ * largest).  The parameters are stepped with the moments as formed; stored is the code next in value, or with `stochastic` one of the two neighbours at
+ * random, so that the stored value's expectation is the moment: v changes by a thousandth a step, which rounding to nearest
+ * loses.  A v > 0 is never stored as 0.  S below 2^-126 counts as 0 (all of the block's moments as 0), a block with a moment that is not finite has S = NaN.
+ *   y = min(|m| (1 / S), 127^2), c the largest with c^2 <= y, one more if u (2 c + 1) < y - c^2;  for v alike with c^4;  u = 1/2, or at random
+ * `stochastic` also rounds bf16 parameters without a master at random (to the neighbour that the added low bits carry to).
+ * Random bits: h of the seed, t - 1, the tensor's place k in the list and the element's place i in it, with mix(x): x = (x ^ x >> 16) 0x6A09E667,
+ * x = (x ^ x >> 15) 0xBB67AE85, x ^ x >> 16 (32 bits; fractions of sqrt 2 and sqrt 3):
+ *   h = mix(mix(mix(seed_lo ^ mix(seed_hi ^ mix(t - 1))) + k) + i);   u = (low half of h + 1/2) / 2^16 for m, of the high half for v; the
+ *   parameter's 16 bits are the high half of h 0x9E3779B1.
+ * params is a host pointer, read before the call returns: 0 <= beta < 1, eps > 0 (as fp32 too), lr >= 0 and weight_decay finite (AERO_ERR_SHAPE).
+ */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  uint64_t seed;
+  int32_t stochastic;
+} aero_adamw_params;
+aero_status aero_adamw_step(
+    const void* image, void* table, const aero_adamw_params* params, int32_t* step,
+    const float* factor /*nullable*/, const float* lr_factor /*nullable*/, void* stream);
+
+/*
+ * The moments of a table's tensors as numbers (for a checkpoint, say), one tensor behind the other in the list's order (those without parameters
+ * have none): avg, avg_sq [sum of n], both of dtype AERO_F32 (exactly what is stored) or AERO_BF16 (rounded once).
+ */
+aero_status aero_adamw_moments(const void* image, void* table, int32_t dtype, void* avg, void* avg_sq, void* stream);
 
 #ifdef __cplusplus
 }

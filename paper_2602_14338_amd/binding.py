@@ -17,7 +17,10 @@ AERO_ROW_PADDING, AERO_ROW_UNTOUCHED = -1, -2
 AERO_DW_ACCUMULATE = 0x100
 OP_GROUP_ADVANTAGE, OP_LOGPROB_FWD, OP_GRPO_LOSS_BWD, OP_LMHEAD_FUSED = 0, 1, 2, 3
 OP_TOPK_LOGPROB, OP_DISTILL_LOSS_BWD, OP_VERIFY_DRAFT, OP_EMBEDDING_BWD = 4, 5, 6, 7
+OP_PREFERENCE_LOSS, OP_PREFERENCE_LOSS_BWD, OP_GRAD_NORM = 8, 9, 10
 AERO_TAIL_RENORM, AERO_TAIL_BUCKET = 0, 1
+AERO_PAIR_LOGISTIC, AERO_PAIR_HINGE, AERO_PAIR_SQUARE = 0, 1, 2
+AERO_MOMENT_BLOCK = 256
 AERO_TOPK_MAX, AERO_DRAFT_MAX = 256, 63
 AERO_LOGIT_LIMIT = 1.2e9   # of the calls around a drafter: masked at or below its negative, NaN at or above
 
@@ -49,6 +52,47 @@ class AdvParams:
     def to_c(self) -> _AdvParamsC:
         return _AdvParamsC(self.k_ratio, self.s_rescue, self.tau_num, self.tau_den, self.zero_keep,
                            self.reject_enable, self.posterior_mode, self.alpha0, self.beta0)
+
+
+class _PreferenceParamsC(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("average", C.c_int32), ("beta", C.c_float), ("smoothing", C.c_float), ("margin", C.c_float)]
+
+
+@dataclass
+class PreferenceParams:
+    kind: int = AERO_PAIR_LOGISTIC
+    average: int = 0
+    beta: float = 0.1
+    smoothing: float = 0.0
+    margin: float = 0.0
+
+    def to_c(self) -> _PreferenceParamsC:
+        return _PreferenceParamsC(self.kind, self.average, self.beta, self.smoothing, self.margin)
+
+
+class _AdamWParamsC(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("seed", C.c_uint64), ("stochastic", C.c_int32)]
+
+
+@dataclass
+class AdamWParams:
+    lr: float = 1e-3
+    beta1: float = 0.9
+    beta2: float = 0.999
+    eps: float = 1e-8
+    weight_decay: float = 0.01
+    seed: int = 0
+    stochastic: bool = False
+
+    def to_c(self) -> _AdamWParamsC:
+        return _AdamWParamsC(self.lr, self.beta1, self.beta2, self.eps, self.weight_decay, self.seed, int(bool(self.stochastic)))
+
+
+class _TensorC(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("exp_avg_scale", C.c_void_p), ("exp_avg_sq_scale", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("decay", C.c_float)]
 
 
 def library_path() -> str:
@@ -87,6 +131,21 @@ def _load() -> C.CDLL:
     lib.aero_embedding_fwd.argtypes = [p, i32, i32, i32, p, i64, f32, p, i64, p, p]
     lib.aero_embedding_bwd.restype = i32
     lib.aero_embedding_bwd.argtypes = [p, i32, i64, i32, i64, p, i32, f32, p, i32, p, p, sz, p]
+    lib.aero_preference_loss.restype = i32
+    lib.aero_preference_loss.argtypes = [p, i64, p, p, i32, p, p, p, i32, C.POINTER(_PreferenceParamsC), p, p, p, p, p, p, sz, p]
+    lib.aero_preference_loss_bwd.restype = i32
+    lib.aero_preference_loss_bwd.argtypes = [p, i32, i64, i32, i64, p, p, p, i32, p, p, p, i32, C.POINTER(_PreferenceParamsC), f32, p, p, p,
+                                             p, p, p, p, sz, p]
+    lib.aero_tensor_table_bytes.restype = sz
+    lib.aero_tensor_table_bytes.argtypes = [C.POINTER(_TensorC), i32]
+    lib.aero_tensor_table.restype = i32
+    lib.aero_tensor_table.argtypes = [C.POINTER(_TensorC), i32, p, sz]
+    lib.aero_grad_norm.restype = i32
+    lib.aero_grad_norm.argtypes = [p, p, f32, f32, p, p, p, sz, p]
+    lib.aero_adamw_step.restype = i32
+    lib.aero_adamw_step.argtypes = [p, p, C.POINTER(_AdamWParamsC), p, p, p, p]
+    lib.aero_adamw_moments.restype = i32
+    lib.aero_adamw_moments.argtypes = [p, p, i32, p, p, p]
     return lib
 
 
@@ -128,7 +187,7 @@ class _Marshal:
 
     def __getattr__(self, name):
         if name not in ("pointers", "group_advantage", "logprob_fwd", "loss_bwd", "fused", "topk", "distill", "verify", "embed_fwd",
-                        "embed_bwd"):
+                        "embed_bwd", "pair", "pair_bwd", "norm", "adamw"):
             raise AttributeError(name)
         try:
             from . import _marshal
@@ -140,8 +199,9 @@ class _Marshal:
         else:
             entries = (_lib.aero_group_advantage, _lib.aero_logprob_fwd, _lib.aero_grpo_loss_bwd,
                        _lib.aero_grpo_loss_bwd_noalloc, _lib.aero_lmhead_logprob_fused, _lib.aero_topk_logprob,
-                       _lib.aero_distill_loss_bwd, _lib.aero_verify_draft, _lib.aero_embedding_fwd, _lib.aero_embedding_bwd)
-            _marshal.bind(torch._C._cuda_getCurrentRawStream, AdvParams, *(C.cast(f, C.c_void_p).value for f in entries))
+                       _lib.aero_distill_loss_bwd, _lib.aero_verify_draft, _lib.aero_embedding_fwd, _lib.aero_embedding_bwd,
+                       _lib.aero_preference_loss, _lib.aero_preference_loss_bwd, _lib.aero_grad_norm, _lib.aero_adamw_step)
+            _marshal.bind(torch._C._cuda_getCurrentRawStream, AdvParams, PreferenceParams, AdamWParams, *(C.cast(f, C.c_void_p).value for f in entries))
         fn = getattr(_marshal, name)
         setattr(self, name, fn)
         return fn
@@ -342,3 +402,123 @@ def aero_embedding_bwd(dout, T: int, H: int, ld_dout: int, ids, V: int, scale: f
     code = _dtype_code(dtable) | (AERO_DW_ACCUMULATE if accumulate else 0)
     st = _lib.aero_embedding_bwd(d, _dtype_code(dout), T, H, ld_dout, i, V, scale, g, code, err, ws, _bytes(workspace), _stream(dout))
     _check(st, "aero_embedding_bwd")
+
+
+def aero_preference_loss(logprob, T: int, ref_logprob, token_rollout, R: int, pair_chosen, pair_rejected, pair_weight, P: int,
+                         params: PreferenceParams, loss, pair_margin, rollout_ratio, drollout, workspace, err_flag=None) -> None:
+    st = _m.pair(logprob, T, ref_logprob, token_rollout, R, pair_chosen, pair_rejected, pair_weight, P, params, loss, pair_margin,
+                 rollout_ratio, drollout, err_flag, workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_preference_loss")
+    lp, ref, owner, c, j, w, *p = _m.pointers(
+        logprob, _F32, "logprob", ref_logprob, _F32, "ref_logprob", token_rollout, _I32, "token_rollout", pair_chosen, _I32, "pair_chosen",
+        pair_rejected, _I32, "pair_rejected", pair_weight, _F32, "pair_weight", loss, _F32, "loss", pair_margin, _F32, "pair_margin",
+        rollout_ratio, _F32, "rollout_ratio", drollout, _F32, "drollout", err_flag, _I32, "err_flag", workspace, None, "workspace")
+    on = next((t for t in (loss, logprob, workspace) if t is not None), None)
+    st = _lib.aero_preference_loss(lp, T, ref, owner, R, c, j, w, P, C.byref(params.to_c()), *p, _bytes(workspace),
+                                   _stream(on) if on is not None else None)
+    _check(st, "aero_preference_loss")
+
+
+def aero_preference_loss_bwd(logits, T: int, V: int, ld: int, targets, ref_logprob, token_rollout, R: int, pair_chosen, pair_rejected,
+                             pair_weight, P: int, params: PreferenceParams, grad_scale: float, loss, pair_margin, rollout_ratio,
+                             logprob_out, dlogits, workspace, err_flag=None) -> None:
+    st = _m.pair_bwd(logits, T, V, ld, targets, ref_logprob, token_rollout, R, pair_chosen, pair_rejected, pair_weight, P, params,
+                     grad_scale, loss, pair_margin, rollout_ratio, logprob_out, dlogits, err_flag, workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_preference_loss_bwd")
+    if dlogits is not None and dlogits.dtype != logits.dtype:
+        raise AeroError("dlogits must have the dtype of logits")
+    z, y, ref, owner, c, j, w, *p = _m.pointers(
+        logits, None, "logits", targets, _I32, "targets", ref_logprob, _F32, "ref_logprob", token_rollout, _I32, "token_rollout",
+        pair_chosen, _I32, "pair_chosen", pair_rejected, _I32, "pair_rejected", pair_weight, _F32, "pair_weight", loss, _F32, "loss",
+        pair_margin, _F32, "pair_margin", rollout_ratio, _F32, "rollout_ratio", logprob_out, _F32, "logprob_out", dlogits, None, "dlogits",
+        err_flag, _I32, "err_flag", workspace, None, "workspace")
+    st = _lib.aero_preference_loss_bwd(z, _dtype_code(logits), T, V, ld, y, ref, owner, R, c, j, w, P, C.byref(params.to_c()), grad_scale, *p,
+                                       _bytes(workspace), _stream(logits))
+    _check(st, "aero_preference_loss_bwd")
+
+
+class TensorTable:
+    """The tensors that norm, step and moments work on, described once.  Entries: dicts of the tensors ``param``, ``grad``, ``master``,
+    ``exp_avg``, ``exp_avg_sq``, ``exp_avg_scale``, ``exp_avg_sq_scale`` (``grad`` alone: it takes part in the norm) and the number
+    ``decay``.  Keeps the tensors alive; calls on one table have to be ordered on one stream."""
+
+    _NAMES = ("param", "grad", "master", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")
+
+    def __init__(self, entries):
+        self.entries = [dict(e) for e in entries]
+        if not self.entries:
+            raise AeroError("a table needs a tensor")
+        self.device = None
+        self.n_moments = 0
+        rows = (_TensorC * len(self.entries))()
+        for k, e in enumerate(self.entries):
+            self._fill(rows[k], e, f"entry {k}")
+        size = int(_lib.aero_tensor_table_bytes(rows, len(self.entries)))
+        self._host = torch.empty(size + 16, dtype=torch.uint8)
+        self.image = (self._host.data_ptr() + 15) & ~15
+        _check(_lib.aero_tensor_table(rows, len(self.entries), self.image, size), "aero_tensor_table")
+        at = self.image - self._host.data_ptr()
+        with torch.cuda.device(self.device):
+            self.table = torch.empty(size, dtype=torch.uint8, device=self.device)
+            self.table.copy_(self._host[at:at + size])
+
+    def _fill(self, row: _TensorC, e: dict, where: str) -> None:
+        unknown = set(e) - set(self._NAMES) - {"decay"}
+        if unknown:
+            raise AeroError(f"{where}: unknown {', '.join(sorted(unknown))}")
+        if e.get("grad") is None:
+            raise AeroError(f"{where}: grad is missing")
+        n = e["grad"].numel()
+        small = e.get("exp_avg_scale") is not None
+        blocks = (n + AERO_MOMENT_BLOCK - 1) // AERO_MOMENT_BLOCK
+        for name in self._NAMES:
+            t = e.get(name)
+            if t is None:
+                continue
+            dtype = {"master": _F32, "exp_avg": torch.int8 if small else _F32, "exp_avg_sq": _U8 if small else _F32,
+                     "exp_avg_scale": _F32, "exp_avg_sq_scale": _F32}.get(name)
+            address = _ptr(t, dtype, f"{where}: {name}")
+            if t.numel() != (blocks if name.endswith("scale") else n):
+                raise AeroError(f"{where}: {name} has {t.numel()} elements, grad {n}")
+            if self.device is None:
+                self.device = t.device
+            if t.device != self.device:
+                raise AeroError(f"{where}: {name} is on {t.device}, the table on {self.device}")
+            setattr(row, name, address)
+        row.n = n
+        row.grad_dtype = _dtype_code(e["grad"])
+        if e.get("param") is not None:
+            row.param_dtype = _dtype_code(e["param"])
+            self.n_moments += n
+        row.decay = e.get("decay", 1.0)
+
+
+def aero_grad_norm(table: TensorTable, grad_scale: float, max_norm: float, norm, factor, workspace) -> None:
+    st = _m.norm(table.image, table.table, grad_scale, max_norm, norm, factor, workspace)
+    if st is not NotImplemented:
+        return _check(st, "aero_grad_norm")
+    p = _m.pointers(table.table, None, "table", norm, _F32, "norm", factor, _F32, "factor", workspace, None, "workspace")
+    st = _lib.aero_grad_norm(table.image, p[0], grad_scale, max_norm, *p[1:], _bytes(workspace), _stream(table.table))
+    _check(st, "aero_grad_norm")
+
+
+def aero_adamw_step(table: TensorTable, params: AdamWParams, step, factor=None, lr_factor=None) -> None:
+    st = _m.adamw(table.image, table.table, params, step, factor, lr_factor)
+    if st is not NotImplemented:
+        return _check(st, "aero_adamw_step")
+    p = _m.pointers(table.table, None, "table", step, _I32, "step", factor, _F32, "factor", lr_factor, _F32, "lr_factor")
+    st = _lib.aero_adamw_step(table.image, p[0], C.byref(params.to_c()), *p[1:], _stream(table.table))
+    _check(st, "aero_adamw_step")
+
+
+def aero_adamw_moments(table: TensorTable, avg, avg_sq) -> None:
+    if avg.dtype != avg_sq.dtype:
+        raise AeroError("avg and avg_sq must have the same dtype")
+    for name, t in (("avg", avg), ("avg_sq", avg_sq)):
+        if t.numel() != table.n_moments:
+            raise AeroError(f"{name} has {t.numel()} elements, the table's moments {table.n_moments}")
+    p = _m.pointers(table.table, None, "table", avg, None, "avg", avg_sq, None, "avg_sq")
+    st = _lib.aero_adamw_moments(table.image, p[0], _dtype_code(avg), *p[1:], _stream(table.table))
+    _check(st, "aero_adamw_moments")

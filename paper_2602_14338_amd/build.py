@@ -9,7 +9,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libaero_hip.so")
 MARSHAL = os.path.join(PKG, "_marshal.so")
 SOURCES = ["aero_api.hip", "group_advantage.hip", "logprob_fwd.hip", "grpo_loss_bwd.hip", "grpo_single_pass.hip",
-           "lmhead_fused.hip", "topk_logprob.hip", "distill_loss_bwd.hip", "verify_draft.hip", "embedding.hip"]
+           "lmhead_fused.hip", "topk_logprob.hip", "distill_loss_bwd.hip", "verify_draft.hip", "embedding.hip",
+           "preference_loss.hip", "optimizer.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-shared",
          # keep the compiler from forming packed-fp32 VALU ops from scalar float code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

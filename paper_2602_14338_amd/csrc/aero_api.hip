@@ -8,6 +8,8 @@ size_t topk_workspace_bytes(int64_t T, int32_t V, int32_t K);
 size_t distill_workspace_bytes(int64_t T, int32_t V);
 size_t verify_workspace_bytes(int64_t rows, int32_t V, int32_t B);
 size_t embedding_workspace_bytes(int64_t T, int32_t V, int32_t H);
+size_t preference_workspace_bytes(int64_t T, int32_t R, int32_t P, bool rows);
+size_t grad_norm_workspace_bytes();
 }  // namespace aero
 
 extern "C" const char* aero_status_string(aero_status s) {
@@ -25,7 +27,6 @@ extern "C" const char* aero_status_string(aero_status s) {
 }
 
 extern "C" size_t aero_workspace_bytes(int32_t op, int64_t T, int32_t V, int32_t H, int32_t R, int32_t Q) {
-  (void)R;
   if (T < 0) return 0;
   switch (op) {
     case AERO_OP_GRPO_LOSS_BWD: return aero::loss_workspace_bytes(T);
@@ -34,6 +35,9 @@ extern "C" size_t aero_workspace_bytes(int32_t op, int64_t T, int32_t V, int32_t
     case AERO_OP_DISTILL_LOSS_BWD: return aero::distill_workspace_bytes(T, V);
     case AERO_OP_VERIFY_DRAFT: return aero::verify_workspace_bytes(T, V, Q);
     case AERO_OP_EMBEDDING_BWD: return aero::embedding_workspace_bytes(T, V, H);
+    case AERO_OP_PREFERENCE_LOSS: return aero::preference_workspace_bytes(T, R, Q, false);
+    case AERO_OP_PREFERENCE_LOSS_BWD: return aero::preference_workspace_bytes(T, R, Q, true);
+    case AERO_OP_GRAD_NORM: return aero::grad_norm_workspace_bytes();
     default: return 0;
   }
 }

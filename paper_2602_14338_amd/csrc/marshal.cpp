@@ -77,6 +77,8 @@ PyObject* pointers(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
 // ---- whole calls ----
 PyObject* g_stream = nullptr;     // torch's current raw stream of a device index
 PyObject* g_params = nullptr;     // class of group_advantage's parameters
+PyObject* g_pair_params = nullptr;    // of the preference losses'
+PyObject* g_adamw_params = nullptr;   // of the AdamW step's
 decltype(&aero_group_advantage) g_group_advantage = nullptr;
 decltype(&aero_logprob_fwd) g_logprob_fwd = nullptr;
 decltype(&aero_grpo_loss_bwd) g_loss_bwd = nullptr;
@@ -87,16 +89,25 @@ decltype(&aero_distill_loss_bwd) g_distill = nullptr;
 decltype(&aero_verify_draft) g_verify = nullptr;
 decltype(&aero_embedding_fwd) g_embed_fwd = nullptr;
 decltype(&aero_embedding_bwd) g_embed_bwd = nullptr;
+decltype(&aero_preference_loss) g_pair = nullptr;
+decltype(&aero_preference_loss_bwd) g_pair_bwd = nullptr;
+decltype(&aero_grad_norm) g_norm = nullptr;
+decltype(&aero_adamw_step) g_adamw = nullptr;
 
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *stream, *params;
-  unsigned long long f[10];
-  if (!PyArg_ParseTuple(args, "OOKKKKKKKKKK", &stream, &params, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9]))
+  PyObject *stream, *params, *pair_params, *adamw_params;
+  unsigned long long f[14];
+  if (!PyArg_ParseTuple(args, "OOOOKKKKKKKKKKKKKK", &stream, &params, &pair_params, &adamw_params, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5],
+                        &f[6], &f[7], &f[8], &f[9], &f[10], &f[11], &f[12], &f[13]))
     return nullptr;
   Py_INCREF(stream);
   Py_INCREF(params);
+  Py_INCREF(pair_params);
+  Py_INCREF(adamw_params);
   Py_XSETREF(g_stream, stream);
   Py_XSETREF(g_params, params);
+  Py_XSETREF(g_pair_params, pair_params);
+  Py_XSETREF(g_adamw_params, adamw_params);
   g_group_advantage = reinterpret_cast<decltype(g_group_advantage)>(f[0]);
   g_logprob_fwd = reinterpret_cast<decltype(g_logprob_fwd)>(f[1]);
   g_loss_bwd = reinterpret_cast<decltype(g_loss_bwd)>(f[2]);
@@ -107,6 +118,10 @@ PyObject* bind(PyObject*, PyObject* args) {
   g_verify = reinterpret_cast<decltype(g_verify)>(f[7]);
   g_embed_fwd = reinterpret_cast<decltype(g_embed_fwd)>(f[8]);
   g_embed_bwd = reinterpret_cast<decltype(g_embed_bwd)>(f[9]);
+  g_pair = reinterpret_cast<decltype(g_pair)>(f[10]);
+  g_pair_bwd = reinterpret_cast<decltype(g_pair_bwd)>(f[11]);
+  g_norm = reinterpret_cast<decltype(g_norm)>(f[12]);
+  g_adamw = reinterpret_cast<decltype(g_adamw)>(f[13]);
   Py_RETURN_NONE;
 }
 
@@ -466,13 +481,149 @@ PyObject* embed_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// The next argument, an object of exactly the given class: its attributes, each handed to take(index, value).
+template <int N, class Take> void attributes(Plain& p, PyObject* cls, PyObject* (&names)[N], const char* const (&text)[N], Take take) {
+  PyObject* params = *p.next++;
+  if (reinterpret_cast<PyObject*>(Py_TYPE(params)) != cls) {
+    p.ok = false;
+    return;
+  }
+  for (int k = 0; k < N; ++k) {
+    if (!names[k] && !(names[k] = PyUnicode_InternFromString(text[k]))) throw python_error();
+    THPObjectPtr v(PyObject_GetAttr(params, names[k]));
+    if (!v) {   // no such attribute: the general way raises
+      PyErr_Clear();
+      p.ok = false;
+      return;
+    }
+    take(k, v.get());
+  }
+}
+
+aero_preference_params pair_params(Plain& p) {
+  static PyObject* names[5];
+  static const char* const text[5] = {"kind", "average", "beta", "smoothing", "margin"};
+  int32_t whole[2] = {};
+  float real[3] = {};
+  attributes(p, g_pair_params, names, text, [&](int k, PyObject* v) {
+    if (k < 2) whole[k] = int32_t(p.integer_of(v, INT32_MIN, INT32_MAX));
+    else real[k - 2] = p.real_of(v);
+  });
+  return aero_preference_params{whole[0], whole[1], real[0], real[1], real[2]};
+}
+
+// pair(logprob, T, ref_logprob, token_rollout, R, chosen, rejected, weight, P, params, loss, margin, ratio, drollout, err_flag, workspace)
+PyObject* pair(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 16 || !g_pair) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const float* logprob = p.f32();
+  const int64_t T = p.int64();
+  const float* ref = p.f32();
+  const int32_t* owner = p.i32();
+  const int32_t R = p.int32();
+  const int32_t *chosen = p.i32(), *rejected = p.i32();
+  const float* weight = p.f32();
+  const int32_t P = p.int32();
+  const aero_preference_params c = pair_params(p);
+  const at::Tensor* on = peek(*p.next);
+  float *loss = p.f32(), *margin = p.f32(), *ratio = p.f32(), *slope = p.f32();
+  int32_t* err = p.i32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) {
+    return g_pair(logprob, T, ref, owner, R, chosen, rejected, weight, P, &c, loss, margin, ratio, slope, err, ws, bytes, s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// pair_bwd(logits, T, V, ld, targets, ref_logprob, token_rollout, R, chosen, rejected, weight, P, params, grad_scale, loss, margin, ratio,
+//          logprob, dlogits, err_flag, workspace)
+PyObject* pair_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 21 || !g_pair_bwd) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const at::Tensor* on = peek(*p.next);
+  const void* logits = p.any();
+  const int32_t dtype = on ? dtype_code(*on) : -1;
+  if (dtype < 0) p.ok = false;
+  const int64_t T = p.int64();
+  const int32_t V = p.int32();
+  const int64_t ld = p.int64();
+  const int32_t* targets = p.i32();
+  const float* ref = p.f32();
+  const int32_t* owner = p.i32();
+  const int32_t R = p.int32();
+  const int32_t *chosen = p.i32(), *rejected = p.i32();
+  const float* weight = p.f32();
+  const int32_t P = p.int32();
+  const aero_preference_params c = pair_params(p);
+  const float scale = p.real();
+  float *loss = p.f32(), *margin = p.f32(), *ratio = p.f32(), *lp_out = p.f32();
+  const at::Tensor* d = peek(*p.next);
+  void* dlogits = p.any();
+  if (d && on && d->scalar_type() != on->scalar_type()) p.ok = false;
+  int32_t* err = p.i32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) {
+    return g_pair_bwd(logits, dtype, T, V, ld, targets, ref, owner, R, chosen, rejected, weight, P, &c, scale, loss, margin, ratio, lp_out,
+                      dlogits, err, ws, bytes, s);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// norm(image address, table, grad_scale, max_norm, norm, factor, workspace)
+PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 7 || !g_norm) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const void* image = reinterpret_cast<const void*>(p.int64());
+  const at::Tensor* on = peek(*p.next);
+  void* table = p.any();
+  const float scale = p.real(), most = p.real();
+  float *out = p.f32(), *factor = p.f32();
+  const at::Tensor* w = peek(*p.next);
+  void* ws = p.any();
+  const size_t bytes = w ? w->nbytes() : 0;
+  return finish(p, on, [&](void* s) { return g_norm(image, table, scale, most, out, factor, ws, bytes, s); });
+  END_HANDLE_TH_ERRORS
+}
+
+// adamw(image address, table, params, step, factor, lr_factor)
+PyObject* adamw(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 6 || !g_adamw) Py_RETURN_NOTIMPLEMENTED;
+  Plain p{args};
+  const void* image = reinterpret_cast<const void*>(p.int64());
+  const at::Tensor* on = peek(*p.next);
+  void* table = p.any();
+  static PyObject* names[7];
+  static const char* const text[7] = {"lr", "beta1", "beta2", "eps", "weight_decay", "seed", "stochastic"};
+  aero_adamw_params c{};
+  double* const real[5] = {&c.lr, &c.beta1, &c.beta2, &c.eps, &c.weight_decay};
+  attributes(p, g_adamw_params, names, text, [&](int k, PyObject* v) {
+    if (k < 5 && PyFloat_CheckExact(v)) *real[k] = PyFloat_AS_DOUBLE(v);
+    else if (k < 5) *real[k] = double(p.integer_of(v, -(1 << 24), 1 << 24));
+    else if (k == 5) c.seed = uint64_t(p.integer_of(v, 0, INT64_MAX));
+    else if (v == Py_True || v == Py_False) c.stochastic = v == Py_True;
+    else p.ok = false;
+  });
+  int32_t* step = p.i32();
+  const float *factor = p.f32(), *lr_factor = p.f32();
+  return finish(p, on, [&](void* s) { return g_adamw(image, table, &c, step, factor, lr_factor, s); });
+  END_HANDLE_TH_ERRORS
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> constexpr PyCFunction fast() {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F));
 }
 
 PyMethodDef methods[] = {
     {"setup", setup, METH_VARARGS, "setup(error class, pointer function for other kinds of tensors)"},
-    {"bind", bind, METH_VARARGS, "bind(raw stream function, parameter class, ten entry points' addresses)"},
+    {"bind", bind, METH_VARARGS, "bind(raw stream function, three parameter classes, fourteen entry points' addresses)"},
     {"pointers", fast<pointers>(), METH_FASTCALL, "pointers(t0, dtype0, name0, ...) -> tuple of addresses"},
     {"group_advantage", fast<group_advantage>(), METH_FASTCALL, "status, or NotImplemented"},
     {"logprob_fwd", fast<logprob_fwd>(), METH_FASTCALL, "status, or NotImplemented"},
@@ -483,6 +634,10 @@ PyMethodDef methods[] = {
     {"verify", fast<verify>(), METH_FASTCALL, "status, or NotImplemented"},
     {"embed_fwd", fast<embed_fwd>(), METH_FASTCALL, "status, or NotImplemented"},
     {"embed_bwd", fast<embed_bwd>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"pair", fast<pair>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"pair_bwd", fast<pair_bwd>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"norm", fast<norm>(), METH_FASTCALL, "status, or NotImplemented"},
+    {"adamw", fast<adamw>(), METH_FASTCALL, "status, or NotImplemented"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,658 @@
+// Loss on pairs of rollouts (the first of a pair to be preferred) and its gradient: from log-probs, or from logits.
+//
+//   s_r = sum over r's tokens of (ln pi - ln ref),  x_p = beta (s_c - s_j) - margin,  loss = sum_p w_p l(x_p),
+//   D_r = dloss / ds_r = beta sum_p w_p l'(x_p) (1[r = c_p] - 1[r = j_p]),  dz_t = g D_r (onehot(y_t) - softmax(z_t))
+//
+// A gradient row needs both rollouts of its pairs whole, so logits are read twice: once for the rows' statistics, once for the gradient.
+// In between stand sums over tokens (by rollout) and over pairs (by rollout), in whatever order a batch brings them.  They are formed
+// exactly, in whole numbers, so that order does not matter: a 32-bit float is m 2^(p - 149) with a 24-bit m, and goes into two of nine
+// 64-bit limbs that stand for 2^(32 k - 149) (the low 32 bits of m 2^(p mod 32) and what is above), each below 2^32, so that 2^31 of them fit.
+#include "row_scan.h"
+
+namespace aero {
+
+// ---------------------------------------------------------------------------------- exact sums
+enum { kPlusInf = 1, kMinusInf = 2, kNan = 4 };
+constexpr int kLimbs = 9;
+struct ExactSum {
+  unsigned long long limb[kLimbs];
+  uint32_t flags;   // of what is not finite
+  int32_t count;
+};
+static_assert(sizeof(ExactSum) == 80, "cleared in 16-byte pieces");
+
+__device__ __forceinline__ void exact_add(ExactSum* s, float x) {
+  const uint32_t bits = __float_as_uint(x), e = bits >> 23 & 0xff;
+  if (e == 0xff) {
+    atomicOr(&s->flags, uint32_t(bits & 0x7fffff ? kNan : bits >> 31 ? kMinusInf : kPlusInf));
+    return;
+  }
+  const uint32_t m = (bits & 0x7fffff) | (e ? 0x800000u : 0u), p = e ? e - 1 : 0;
+  if (m == 0) return;
+  const uint64_t at = uint64_t(m) << (p & 31);
+  const uint64_t low = at & 0xffffffffu, high = at >> 32;
+  const uint64_t sign = bits >> 31 ? ~uint64_t(0) : 0;
+  unsigned long long* limb = s->limb + (p >> 5);
+  if (low) atomicAdd(limb, (unsigned long long)((low ^ sign) - sign));
+  if (high) atomicAdd(limb + 1, (unsigned long long)((high ^ sign) - sign));
+}
+// A 64-bit number to 48 bits.
+__device__ __forceinline__ void exact_add(ExactSum* s, double x) {
+  const float hi = float(x);
+  exact_add(s, hi);
+  if (fabsf(hi) < INFINITY) exact_add(s, float(x - double(hi)));
+}
+__device__ __forceinline__ double exact_value(const ExactSum& s) {
+  if (s.flags) {
+    if (s.flags == kPlusInf) return INFINITY;
+    if (s.flags == kMinusInf) return -INFINITY;
+    return __builtin_nan("");
+  }
+  int64_t l[kLimbs];
+#pragma unroll
+  for (int k = 0; k < kLimbs; ++k) l[k] = int64_t(s.limb[k]);
+#pragma unroll
+  for (int k = 0; k + 1 < kLimbs; ++k) {   // digits of 32 bits, the sign in the last
+    l[k + 1] += l[k] >> 32;
+    l[k] &= 0xffffffff;
+  }
+  // a negative sum as its magnitude, or its digits would cancel
+  const bool negative = l[kLimbs - 1] < 0;
+  if (negative) {
+#pragma unroll
+    for (int k = 0; k < kLimbs; ++k) l[k] = (k + 1 < kLimbs ? int64_t(0xffffffff) : int64_t(-1)) - l[k];
+    l[0] += 1;
+  }
+  double v = double(l[kLimbs - 1]);
+#pragma unroll
+  for (int k = kLimbs - 2; k >= 0; --k) v = fma(v, 4294967296.0, double(l[k]));
+  v = ldexp(v, -149);
+  return negative ? -v : v;
+}
+
+// ---------------------------------------------------------------------------------- arguments and workspace
+struct PairLoss {
+  const int32_t *chosen, *rejected;
+  const float* weight;
+  int32_t P, R;
+  int32_t kind, average;
+  float beta, smoothing, margin;
+  float *loss, *pair_margin, *rollout_ratio, *drollout;
+  int32_t* err_flag;
+};
+
+// What a row leaves for the steps behind it, and what they make of it for its gradient.
+struct RowRecord {
+  int32_t rollout;   // AERO_ROW_PADDING, AERO_ROW_UNTOUCHED: takes no part   ->  gradient by the log-prob (-0: not to be written)
+  float d;           // logprob - ref                                          ->  factor of the row's exponentials
+  float offset;      // of the row's exponentials, in powers of two
+  float inv;         // 1 / their sum
+};
+struct GradRecord {
+  float g, k, offset;
+  int32_t y;
+};
+static_assert(sizeof(RowRecord) == 16 && sizeof(GradRecord) == 16, "one takes the other's place");
+
+struct PairWorkspace {
+  ExactSum *ratio, *slope;   // [R]
+  double* part;              // [ceil(P / 64)] of the loss
+  RowRecord* rows;           // [T]
+};
+constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+static PairWorkspace carve(void* ws, int64_t T, int32_t R, int32_t P, size_t* bytes) {
+  char* p = static_cast<char*>(ws);
+  PairWorkspace w;
+  const size_t sums = up256(size_t(R) * 2 * sizeof(ExactSum)), part = up256((size_t(P) + 63) / 64 * 8), rows = up256(size_t(T) * 16);
+  w.ratio = reinterpret_cast<ExactSum*>(p);
+  w.slope = w.ratio + R;
+  w.part = reinterpret_cast<double*>(p + sums);
+  w.rows = reinterpret_cast<RowRecord*>(p + sums + part);
+  if (bytes) *bytes = sums + part + rows;
+  return w;
+}
+size_t preference_workspace_bytes(int64_t T, int32_t R, int32_t P, bool rows) {
+  if (R < 0 || P < 0) return 0;
+  size_t bytes = 0;
+  carve(nullptr, rows ? T : 0, R, P, &bytes);
+  return bytes + 256;   // never 0
+}
+
+// ---------------------------------------------------------------------------------- a pair
+struct PairTerm {
+  double value, slope;
+};
+__device__ __forceinline__ PairTerm pair_term(const PairLoss& a, double x) {
+  if (a.kind == AERO_PAIR_HINGE) {
+    if (x != x) return PairTerm{x, x};
+    return x < 1.0 ? PairTerm{1.0 - x, -1.0} : PairTerm{0.0, 0.0};
+  }
+  if (a.kind == AERO_PAIR_SQUARE) {
+    const double u = (x - 0.5) / double(a.beta);
+    return PairTerm{u * u, 2.0 * u / double(a.beta)};
+  }
+  if (x != x) return PairTerm{x, x};
+  const double e = double(a.smoothing), away = exp(-fabs(x)), low = log1p(away);
+  double value = (1.0 - e) * (x < 0.0 ? -x + low : low);
+  if (e != 0.0) value += e * (x > 0.0 ? x + low : low);
+  const double sigma = x > 0.0 ? away / (1.0 + away) : 1.0 / (1.0 + away);   // of -x
+  return PairTerm{value, e - sigma};
+}
+
+__device__ __forceinline__ double ratio_of(const PairLoss& a, const ExactSum& s) {
+  const double v = exact_value(s);
+  return a.average && s.count > 1 ? v / double(s.count) : v;
+}
+// Derivative by a rollout's log ratio, or with `average` by the log-prob of each of its tokens.
+__device__ __forceinline__ float slope_of(const PairLoss& a, const ExactSum& slope, int32_t count) {
+  const double v = exact_value(slope);
+  return float(a.average && count > 1 ? v / double(count) : v);
+}
+
+// One pair: its share goes to its rollouts' slopes, its term is returned.
+__device__ __forceinline__ double pair_step(const PairLoss& a, int p, const ExactSum* ratio, ExactSum* slope) {
+  const int c = a.chosen[p], j = a.rejected[p];
+  const float w = a.weight ? a.weight[p] : 1.f / float(a.P);
+  double term = 0.0, m = 0.0;
+  if (c >= 0 && j >= 0 && (c >= a.R || j >= a.R)) {
+    if (a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_ROLLOUT);
+  } else if (c >= 0 && j >= 0 && w != 0.f) {
+    m = double(a.beta) * (ratio_of(a, ratio[c]) - ratio_of(a, ratio[j]));
+    const PairTerm t = pair_term(a, m - double(a.margin));
+    term = double(w) * t.value;
+    const float share = float(double(a.beta) * double(w) * t.slope);
+    exact_add(&slope[c], share);
+    exact_add(&slope[j], -share);
+  }
+  if (a.pair_margin) a.pair_margin[p] = float(m);
+  return term;
+}
+
+// ---------------------------------------------------------------------------------- tokens
+// Sums of tokens by rollout, a wave at a time over 64 tokens in a row: as long as they are one rollout's (a rollout's tokens usually stand together), lanes
+// add up by themselves and the wave at the end; otherwise rollout by rollout for up to four of them and lane by lane for the others.
+struct TokenSums {
+  ExactSum* sums;
+  int rollout;   // uniform; -1: nothing held
+  double held;
+  int count;
+
+  __device__ __forceinline__ void put(int r, double total, int n) {   // total and n: the same in every lane
+    if (threadIdx.x % kWave == 0) {
+      exact_add(&sums[r], total);
+      atomicAdd(&sums[r].count, n);
+    }
+  }
+  __device__ __forceinline__ void flush() {
+    if (rollout >= 0) put(rollout, wave_sum_d(held), count);
+    rollout = -1;
+    held = 0.0;
+    count = 0;
+  }
+  __device__ __forceinline__ void add(int r, float d) {   // r < 0: no token
+    uint64_t left = __ballot(r >= 0);
+    if (left == 0) return;
+    const int first = __shfl(r, __ffsll((unsigned long long)left) - 1, kWave);
+    if (__ballot(r == first) == left) {
+      if (first != rollout) {
+        flush();
+        rollout = first;
+      }
+      held += r >= 0 ? double(d) : 0.0;
+      count += __popcll(left);
+      return;
+    }
+    flush();
+    for (int turn = 0; turn < 4 && left; ++turn) {
+      const int one = __shfl(r, __ffsll((unsigned long long)left) - 1, kWave);
+      const uint64_t same = __ballot(r == one);
+      put(one, wave_sum_d(r == one ? double(d) : 0.0), __popcll(same));
+      left &= ~same;
+    }
+    if (left >> (threadIdx.x % kWave) & 1) {
+      exact_add(&sums[r], d);
+      atomicAdd(&sums[r].count, 1);
+    }
+  }
+};
+
+// The tokens of the call without logits.
+struct Tokens {
+  const float *logprob, *ref;
+  const int32_t* rollout;
+  int64_t T;
+};
+__device__ __forceinline__ void token_at(const Tokens& k, int64_t t, int R, int32_t* err_flag, int& r, float& d) {
+  r = -1;
+  d = 0.f;
+  if (t >= k.T) return;
+  r = k.rollout[t];
+  if (r >= R) {
+    if (err_flag) atomicOr(err_flag, AERO_DERR_BAD_ROLLOUT);
+    r = -1;
+  }
+  if (r < 0) {
+    r = -1;
+    return;
+  }
+  d = k.logprob[t] - (k.ref ? k.ref[t] : 0.f);
+}
+
+constexpr int kTokenRounds = 16, kTokenNT = 256;
+__global__ __launch_bounds__(kTokenNT) void k_pair_tokens(Tokens k, PairLoss a, ExactSum* ratio) {
+  const int wave = blockIdx.x * (kTokenNT / kWave) + threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  TokenSums sums{ratio, -1, 0.0, 0};
+  for (int u = 0; u < kTokenRounds; ++u) {
+    int r;
+    float d;
+    token_at(k, (int64_t(wave) * kTokenRounds + u) * kWave + lane, a.R, a.err_flag, r, d);
+    sums.add(r, d);
+  }
+  sums.flush();
+}
+
+__global__ __launch_bounds__(256) void k_pair_clear(u32x4_t* p, int64_t n) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i < n) p[i] = u32x4_t{0u, 0u, 0u, 0u};
+}
+
+__global__ __launch_bounds__(256) void k_pair_terms(PairLoss a, const ExactSum* __restrict__ ratio, ExactSum* slope, double* __restrict__ part) {
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  const double term = wave_sum_d(p < a.P ? pair_step(a, p, ratio, slope) : 0.0);
+  if (threadIdx.x % kWave == 0 && p < a.P) part[p / kWave] = term;
+}
+
+// What a row's gradient is made with.
+__device__ __forceinline__ GradRecord grad_record(const RowRecord& row, int y, float slope, float grad_scale) {
+  float g = row.rollout >= 0 ? slope * grad_scale : 0.f;
+  if (g == 0.f) g = row.rollout == AERO_ROW_UNTOUCHED ? -0.f : 0.f;
+  return GradRecord{g, -g * row.inv, row.offset, y};
+}
+
+// The rollouts' outputs and the rows' records; the first workgroup adds up the loss.
+__global__ __launch_bounds__(256) void k_pair_finish(PairLoss a, const ExactSum* __restrict__ ratio, const ExactSum* __restrict__ slope,
+                                                     const double* __restrict__ part, RowRecord* rows, const int32_t* __restrict__ targets,
+                                                     int64_t T, float grad_scale) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i < a.R) {
+    if (a.rollout_ratio) a.rollout_ratio[i] = float(ratio_of(a, ratio[i]));
+    if (a.drollout) a.drollout[i] = slope_of(a, slope[i], ratio[i].count);
+  }
+  if (rows && i < T) {
+    const RowRecord row = rows[i];
+    const float d = row.rollout >= 0 ? slope_of(a, slope[row.rollout], ratio[row.rollout].count) : 0.f;
+    reinterpret_cast<GradRecord*>(rows)[i] = grad_record(row, targets[i], d, grad_scale);
+  }
+  if (blockIdx.x != 0) return;
+  __shared__ double s_part[4];
+  double sum = 0.0;
+  const int n = (a.P + kWave - 1) / kWave;
+  for (int k = threadIdx.x; k < n; k += 256) sum += part[k];
+  sum = wave_sum_d(sum);
+  if (threadIdx.x % kWave == 0) s_part[threadIdx.x / kWave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) a.loss[0] = float(s_part[0] + s_part[1] + s_part[2] + s_part[3]);
+}
+
+// All of the above by one workgroup, the sums in LDS: for as many tokens, pairs and rollouts as take it less time than the launches.
+constexpr int kSmallNT = 1024, kSmallR = 256, kSmallP = 4096;
+constexpr int64_t kSmallT = 16384;
+template <bool ROWS>
+__global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, RowRecord* rows, const int32_t* __restrict__ targets, float grad_scale) {
+  __shared__ ExactSum s_ratio[kSmallR], s_slope[kSmallR];
+  __shared__ double s_part[kSmallNT / kWave];
+  const int tid = threadIdx.x;
+  {
+    u32x4_t *p = reinterpret_cast<u32x4_t*>(s_ratio), *q = reinterpret_cast<u32x4_t*>(s_slope);
+    const int n = a.R * int(sizeof(ExactSum) / 16);
+    for (int i = tid; i < n; i += kSmallNT) p[i] = q[i] = u32x4_t{0u, 0u, 0u, 0u};
+  }
+  __syncthreads();
+  {
+    TokenSums sums{s_ratio, -1, 0.0, 0};
+    for (int64_t t0 = 0; t0 < k.T; t0 += kSmallNT) {
+      const int64_t t = t0 + tid;
+      int r = -1;
+      float d = 0.f;
+      if constexpr (ROWS) {
+        if (t < k.T) {
+          r = max(rows[t].rollout, -1);
+          d = rows[t].d;
+        }
+      } else {
+        token_at(k, t, a.R, a.err_flag, r, d);
+      }
+      sums.add(r, d);
+    }
+    sums.flush();
+  }
+  __syncthreads();
+  double sum = 0.0;
+  for (int p = tid; p < a.P; p += kSmallNT) sum += pair_step(a, p, s_ratio, s_slope);
+  sum = wave_sum_d(sum);
+  if (tid % kWave == 0) s_part[tid / kWave] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    double total = 0.0;
+    for (int w = 0; w < kSmallNT / kWave; ++w) total += s_part[w];
+    a.loss[0] = float(total);
+  }
+  __shared__ float s_d[kSmallR];
+  for (int r = tid; r < a.R; r += kSmallNT) {
+    const float d = slope_of(a, s_slope[r], s_ratio[r].count);
+    s_d[r] = d;
+    if (a.rollout_ratio) a.rollout_ratio[r] = float(ratio_of(a, s_ratio[r]));
+    if (a.drollout) a.drollout[r] = d;
+  }
+  if constexpr (ROWS) {
+    __syncthreads();
+    for (int64_t t = tid; t < k.T; t += kSmallNT) {
+      const RowRecord row = rows[t];
+      reinterpret_cast<GradRecord*>(rows)[t] = grad_record(row, targets[t], row.rollout >= 0 ? s_d[row.rollout] : 0.f, grad_scale);
+    }
+  }
+}
+
+static bool is_small(int64_t T, int32_t R, int32_t P) { return T <= kSmallT && R <= kSmallR && P <= kSmallP; }
+static unsigned blocks_of(int64_t n, int nt) { return unsigned((n + nt - 1) / nt); }
+
+// Everything behind the sums over the tokens.
+static void launch_pairs(const PairLoss& a, const PairWorkspace& w, RowRecord* rows, const int32_t* targets, int64_t T, float grad_scale,
+                         hipStream_t s) {
+  if (a.P > 0) hipLaunchKernelGGL(k_pair_terms, dim3(blocks_of(a.P, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part);
+  int64_t n = a.R > 1 ? a.R : 1;
+  if (rows && T > n) n = T;
+  hipLaunchKernelGGL(k_pair_finish, dim3(blocks_of(n, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part, rows, targets, T, grad_scale);
+}
+static void launch_clear(const PairWorkspace& w, int32_t R, hipStream_t s) {
+  const int64_t n = int64_t(R) * 2 * int64_t(sizeof(ExactSum)) / 16;
+  if (n > 0) hipLaunchKernelGGL(k_pair_clear, dim3(blocks_of(n, 256)), dim3(256), 0, s, reinterpret_cast<u32x4_t*>(w.ratio), n);
+}
+
+// ---------------------------------------------------------------------------------- rows of logits
+struct PairRows {
+  const void* logits;
+  int64_t T;
+  int V;
+  int64_t ld;
+  const int32_t* targets;
+  const float* ref;
+  const int32_t* rollout;
+  int R;
+  RowRecord* rows;
+  ExactSum* ratio;      // NULL: the sums are formed later
+  float* logprob_out;
+  int32_t* err_flag;
+};
+
+// A row's sum of exponentials, to 3e-8 where hundreds of tokens add up what is off.  Three errors go the same way in every row otherwise (1e-7 a token each, a
+// log ratio of 5 over 256 tokens to 5e-6 of itself):
+//   - beside a sampled token that has half of the row, a thread's other exponentials are mostly less than half a unit of its sum, which stays where it is:
+//     a vector's are added up first;
+//   - log2 e in 32 bits is off by a relative d = -1.3e-8, and the log-partition by d times the mean logit: the sum of e^z z sets it right;
+//   - an argument is rounded at its own size, and stored logits of 16 bits have few values, whose roundings do not even out: the offset
+//     follows the largest logit closely, so that the arguments that count are near 0.
+struct RowSum {
+  SoftSum st;
+  float sz;   // the exponentials times their logits
+};
+constexpr float kRowAbove = 2.f;
+constexpr double kLog2eOff = (1.4426950408889634074 - double(kLog2e)) * 0.69314718055994531;
+template <int N> __device__ __forceinline__ void row_update(RowSum& r, const float (&z)[N]) {
+  const float vm = vec_max<N>(z);
+  const bool grow = fmaf(vm, kLog2e, -r.st.o) > kRowAbove;
+  if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+    asm volatile("" ::: "memory");   // stays a branch
+    if (grow) {
+      const float o = soft_offset(vm), f = exp2_fast(r.st.o - o);
+      r.st = SoftSum{o, r.st.s * f};
+      r.sz *= f;
+    }
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const float e = exp2_fast(fmaf(z[k], kLog2e, -r.st.o));
+    s += e;
+    r.sz = fmaf(e, fmaxf(z[k], kMasked), r.sz);   // 0 times a masked logit's -inf would be NaN
+  }
+  r.st.s += s;
+}
+// Over the workgroup, with the sums of the threads added up in 64 bits.
+template <int NT> __device__ __forceinline__ SoftTotal row_total(const RowSum& r, SoftTotal* lds) {
+  const SoftTotal whole{r.st.o, double(r.st.s) + kLog2eOff * double(r.sz)};
+  SoftTotal a = soft_reduce<true>(whole);
+  constexpr int kWaves = NT / kWave;
+  if constexpr (kWaves > 1) {
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if (lane == 0) lds[wave] = a;
+    __syncthreads();
+    a = soft_reduce<false>(lane % 16 < kWaves ? lds[lane % 16] : soft_total(soft_identity()));
+  }
+  return a;
+}
+__device__ __forceinline__ double row_lse(SoftTotal st) {
+  if (st.s == 0.0) return -INFINITY;
+  return st.s == st.s ? double(st.o) * 0.69314718055994531 + log_of(st.s) : __builtin_nan("");
+}
+
+// A row's log-partition and its sampled token's log-prob: one workgroup reads it once.
+template <int NT, int DT, bool VEC>
+__global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
+  constexpr int E = RowView<DT, VEC>::E, kAhead = 4;
+  __shared__ SoftTotal lds[NT / kWave];
+  const int64_t t = blockIdx.x;
+  const int tid = threadIdx.x;
+  const int r = a.rollout[t], y = a.targets[t];
+  if (r < 0 || y < 0 || r >= a.R || y >= a.V) {   // uniform
+    if (tid == 0) {
+      if (r >= 0 && y >= 0 && a.err_flag) atomicOr(a.err_flag, r >= a.R ? AERO_DERR_BAD_ROLLOUT : AERO_DERR_BAD_TARGET);
+      a.rows[t] = RowRecord{r == AERO_ROW_UNTOUCHED ? AERO_ROW_UNTOUCHED : AERO_ROW_PADDING, 0.f, 0.f, 0.f};
+      if (a.logprob_out) a.logprob_out[t] = 0.f;
+    }
+    return;
+  }
+  const RowView<DT, VEC> row(a.logits, t, a.ld, a.V);
+  const int jr = row.ragged();
+  const float zr = jr >= 0 ? row.at(jr) : 0.f, zy = row.at(y);
+  RowSum st{soft_identity(), 0.f};
+  int i = tid;
+  for (; i + (kAhead - 1) * NT < row.nvec; i += kAhead * NT) {
+    u32x4_t v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = row.load(i + u * NT);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      float z[E];
+      row.unpack(v[u], z);
+      row_update<E>(st, z);
+    }
+  }
+  for (; i < row.nvec; i += NT) {
+    float z[E];
+    row.unpack(row.load(i), z);
+    row_update<E>(st, z);
+  }
+  if (jr >= 0) {
+    float z[1] = {zr};
+    row_update<1>(st, z);
+  }
+  const SoftTotal sum = row_total<NT>(st, lds);
+  if (tid != 0) return;
+  const double lse = row_lse(sum);
+  const bool empty = sum.s == 0.0;
+  const double lp = empty ? 0.0 : zy <= kMasked ? (lse == lse ? -INFINITY : lse) : double(zy) - lse;
+  const float d = empty ? 0.f : float(a.ref ? lp - double(a.ref[t]) : lp);
+  a.rows[t] = RowRecord{empty ? AERO_ROW_PADDING : r, d, sum.o, float(1.0 / sum.s)};
+  if (a.logprob_out) a.logprob_out[t] = float(lp);
+  if (a.ratio && !empty) {
+    exact_add(&a.ratio[r], d);
+    atomicAdd(&a.ratio[r].count, 1);
+  }
+}
+
+// ---------------------------------------------------------------------------------- gradient rows
+template <int DT> __device__ __forceinline__ float grad_elt(const GradRecord& c, float z, int j) {
+  const float d = c.k * exp2_fast(fmaf(z, kLog2e, -c.offset));
+  return j == c.y ? d + c.g : d;
+}
+
+// (row, segment) per workgroup, a vector per thread, in the order of addresses from the end: what was read last is read first.
+template <int NT, int DT>
+__global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V, int64_t ld, int segs, const GradRecord* __restrict__ rows,
+                                                      void* dlogits) {
+  constexpr int E = Storage<DT>::kPerVec;
+  const unsigned block = gridDim.x - 1 - blockIdx.x;
+  const int64_t t = block / segs;
+  const int seg = block % segs;
+  const GradRecord c = rows[t];
+  const RowGeom geom = row_geom<DT>(logits, t, ld, V);
+  const char* zrow = row_ptr<DT>(logits, t, ld);
+  char* drow = row_ptr<DT>(dlogits, t, ld);
+  const u32x4_t* zv = reinterpret_cast<const u32x4_t*>(zrow + geom.head * Storage<DT>::kBytes);
+  u32x4_t* dv = reinterpret_cast<u32x4_t*>(drow + geom.head * Storage<DT>::kBytes);
+  const int k = seg * NT + threadIdx.x;
+  const bool in = k < geom.nvec;
+  const int jr = seg == 0 ? ragged_elt<DT>(geom, V, threadIdx.x) : -1;
+  if (c.g == 0.f) {   // uniform: nothing to read
+    if (__float_as_uint(c.g) >> 31) return;
+    if (in) dv[k] = u32x4_t{0u, 0u, 0u, 0u};
+    if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
+    return;
+  }
+  if (in) {
+    const u32x4_t v = zv[k];
+    float z[E], d[E];
+    unpack_vec<DT>(v, z);
+#pragma unroll
+    for (int e = 0; e < E; ++e) d[e] = c.k * exp2_fast(fmaf(z[e], kLog2e, -c.offset));
+    const int at = c.y - geom.head;
+    if (k == (at >> Storage<DT>::kLogPerVec)) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) d[e] += e == (at & (E - 1)) ? c.g : 0.f;
+    }
+    dv[k] = pack_vec<DT>(d);
+  }
+  if (jr >= 0) store_elt<DT>(drow, jr, grad_elt<DT>(c, load_elt<DT>(zrow, jr), jr));
+}
+
+// A row per workgroup, element by element: where logits and dlogits differ in their offset from 16 bytes, or a launch would not
+// hold the segments.
+template <int DT>
+__global__ __launch_bounds__(256) void k_pair_grad_row(const void* logits, int V, int64_t ld, const GradRecord* __restrict__ rows, void* dlogits) {
+  const int64_t t = blockIdx.x;
+  const GradRecord c = rows[t];
+  if (c.g == 0.f && __float_as_uint(c.g) >> 31) return;
+  const char* zrow = row_ptr<DT>(logits, t, ld);
+  char* drow = row_ptr<DT>(dlogits, t, ld);
+  for (int j = threadIdx.x; j < V; j += 256) store_elt<DT>(drow, j, c.g == 0.f ? 0.f : grad_elt<DT>(c, load_elt<DT>(zrow, j), j));
+}
+
+template <int DT> static void launch_rows(const PairRows& a, hipStream_t s) {
+  const bool vec = rows_alike(a.logits, nullptr, Storage<DT>::kBytes);
+  const int64_t work = vec ? (a.V + Storage<DT>::kPerVec - 1) / Storage<DT>::kPerVec : a.V;
+  const dim3 grid = dim3(unsigned(a.T));
+  auto launch = [&](auto nt) {
+    if (vec) hipLaunchKernelGGL((k_pair_rows<nt.value, DT, true>), grid, dim3(nt.value), 0, s, a);
+    else hipLaunchKernelGGL((k_pair_rows<nt.value, DT, false>), grid, dim3(nt.value), 0, s, a);
+  };
+  if (work <= 4 * 64) launch(std::integral_constant<int, 64>{});
+  else if (work <= 16 * 256) launch(std::integral_constant<int, 256>{});
+  else if (a.T <= compute_units()) launch(std::integral_constant<int, 1024>{});
+  else launch(std::integral_constant<int, 512>{});
+}
+
+template <int DT> static void launch_grad(const PairRows& a, void* dlogits, hipStream_t s) {
+  const GradRecord* rows = reinterpret_cast<const GradRecord*>(a.rows);
+  const int64_t nvec = a.V / Storage<DT>::kPerVec + 1;
+  const int nt = nvec <= 128 ? 64 : 256;
+  const int64_t segs = (nvec + nt - 1) / nt;
+  if (!rows_alike(a.logits, dlogits, Storage<DT>::kBytes) || !grid_fits(a.T * segs, nt)) {
+    hipLaunchKernelGGL(k_pair_grad_row<DT>, dim3(unsigned(a.T)), dim3(256), 0, s, a.logits, a.V, a.ld, rows, dlogits);
+    return;
+  }
+  const dim3 grid = dim3(unsigned(a.T * segs));
+  if (nt == 64) hipLaunchKernelGGL((k_pair_grad_seg<64, DT>), grid, dim3(64), 0, s, a.logits, a.V, a.ld, int(segs), rows, dlogits);
+  else hipLaunchKernelGGL((k_pair_grad_seg<256, DT>), grid, dim3(256), 0, s, a.logits, a.V, a.ld, int(segs), rows, dlogits);
+}
+
+template <int DT> static void run_rows(const PairRows& rows, const PairLoss& a, const PairWorkspace& w, float grad_scale, void* dlogits, hipStream_t s) {
+  const bool small = is_small(rows.T, a.R, a.P);
+  if (!small) launch_clear(w, a.R, s);
+  PairRows r = rows;
+  r.ratio = small ? nullptr : w.ratio;
+  if (r.T > 0) launch_rows<DT>(r, s);
+  if (small) {
+    hipLaunchKernelGGL(k_pair_small<true>, dim3(1), dim3(kSmallNT), 0, s, Tokens{nullptr, nullptr, nullptr, r.T}, a, r.rows, r.targets, grad_scale);
+  } else {
+    launch_pairs(a, w, dlogits ? r.rows : nullptr, r.targets, r.T, grad_scale, s);
+  }
+  if (dlogits && r.T > 0) launch_grad<DT>(r, dlogits, s);
+}
+
+// ---------------------------------------------------------------------------------- the calls' checks
+static bool finite(float x) { return x - x == 0.f; }
+static aero_status check_pairs(const aero_preference_params* p, int32_t R, int32_t P, const int32_t* chosen, const int32_t* rejected,
+                               const float* loss) {
+  if (!p || !loss) return AERO_ERR_NULL;
+  if (R < 0 || P < 0 || R >= (1 << 22) || P >= (1 << 22)) return AERO_ERR_SHAPE;
+  if (p->kind != AERO_PAIR_LOGISTIC && p->kind != AERO_PAIR_HINGE && p->kind != AERO_PAIR_SQUARE) return AERO_ERR_SHAPE;
+  if ((p->average != 0 && p->average != 1) || !(p->beta > 0.f) || !finite(p->beta) || !finite(p->margin)) return AERO_ERR_SHAPE;
+  if (p->kind == AERO_PAIR_LOGISTIC && !(p->smoothing >= 0.f && p->smoothing <= 0.5f)) return AERO_ERR_SHAPE;
+  if (P > 0 && (!chosen || !rejected)) return AERO_ERR_NULL;
+  return AERO_OK;
+}
+static bool workspace_ok(const void* ws, size_t bytes, size_t need) { return ws && reinterpret_cast<uintptr_t>(ws) % 256 == 0 && bytes >= need; }
+
+}  // namespace aero
+
+extern "C" aero_status aero_preference_loss(
+    const float* logprob, int64_t T, const float* ref_logprob, const int32_t* token_rollout, int32_t R, const int32_t* pair_chosen,
+    const int32_t* pair_rejected, const float* pair_weight, int32_t P, const aero_preference_params* params, float* loss, float* pair_margin,
+    float* rollout_ratio, float* drollout, int32_t* err_flag, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace aero;
+  if (T < 0 || T >= (int64_t(1) << 25)) return AERO_ERR_SHAPE;
+  const aero_status st = check_pairs(params, R, P, pair_chosen, pair_rejected, loss);
+  if (st != AERO_OK) return st;
+  if (T > 0 && (!logprob || !token_rollout)) return AERO_ERR_NULL;
+  if (!workspace_ok(workspace, workspace_bytes, preference_workspace_bytes(T, R, P, false))) return AERO_ERR_WORKSPACE;
+  const PairWorkspace w = carve(workspace, 0, R, P, nullptr);
+  const PairLoss a{pair_chosen, pair_rejected, pair_weight, P, R, params->kind, params->average, params->beta, params->smoothing, params->margin,
+                   loss, pair_margin, rollout_ratio, drollout, err_flag};
+  const Tokens k{logprob, ref_logprob, token_rollout, T};
+  hipStream_t s = as_stream(stream);
+  if (is_small(T, R, P)) {
+    hipLaunchKernelGGL(k_pair_small<false>, dim3(1), dim3(kSmallNT), 0, s, k, a, nullptr, nullptr, 0.f);
+    return launch_status();
+  }
+  launch_clear(w, R, s);
+  if (T > 0) hipLaunchKernelGGL(k_pair_tokens, dim3(blocks_of(T, kTokenNT * kTokenRounds)), dim3(kTokenNT), 0, s, k, a, w.ratio);
+  launch_pairs(a, w, nullptr, nullptr, 0, 0.f, s);
+  return launch_status();
+}
+
+extern "C" aero_status aero_preference_loss_bwd(
+    const void* logits, int32_t dtype, int64_t T, int32_t V, int64_t ld, const int32_t* targets, const float* ref_logprob,
+    const int32_t* token_rollout, int32_t R, const int32_t* pair_chosen, const int32_t* pair_rejected, const float* pair_weight, int32_t P,
+    const aero_preference_params* params, float grad_scale, float* loss, float* pair_margin, float* rollout_ratio, float* logprob_out,
+    void* dlogits, int32_t* err_flag, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace aero;
+  if (T < 0 || T >= (1 << 22) || V < 1 || V > (1 << 24) || ld < V) return AERO_ERR_SHAPE;
+  if (!storage_dtype_ok(dtype)) return AERO_ERR_DTYPE;
+  const aero_status st = check_pairs(params, R, P, pair_chosen, pair_rejected, loss);
+  if (st != AERO_OK) return st;
+  if (T > 0 && (!logits || !targets || !token_rollout)) return AERO_ERR_NULL;
+  if (!workspace_ok(workspace, workspace_bytes, preference_workspace_bytes(T, R, P, true))) return AERO_ERR_WORKSPACE;
+  const PairWorkspace w = carve(workspace, T, R, P, nullptr);
+  const PairLoss a{pair_chosen, pair_rejected, pair_weight, P, R, params->kind, params->average, params->beta, params->smoothing, params->margin,
+                   loss, pair_margin, rollout_ratio, nullptr, err_flag};
+  const PairRows rows{logits, T, V, ld, targets, ref_logprob, token_rollout, R, w.rows, nullptr, logprob_out, err_flag};
+  hipStream_t s = as_stream(stream);
+  switch (dtype) {
+    case AERO_BF16: run_rows<kBF16>(rows, a, w, grad_scale, dlogits, s); break;
+    case AERO_F16: run_rows<kF16>(rows, a, w, grad_scale, dlogits, s); break;
+    case AERO_F8E4M3: run_rows<kF8>(rows, a, w, grad_scale, dlogits, s); break;
+    default: run_rows<kF32>(rows, a, w, grad_scale, dlogits, s);
+  }
+  return launch_status();
+}

@@ -18,6 +18,7 @@ from typing import Callable, Optional, Tuple
 import torch
 
 from . import binding
+from .optim import AdamW
 
 
 def _workspace(op: int, device: torch.device, **sizes: int) -> torch.Tensor:
@@ -138,8 +139,8 @@ def main() -> None:
     gen = torch.Generator(device="cuda").manual_seed(0)
     new = lambda sigma: torch.randn((a.vocab, a.width), generator=gen, device="cuda") * sigma   # noqa: E731
     truth, drafter = new(0.35).bfloat16(), Drafter(new(0.1).bfloat16())
-    master, first, second = drafter.table.float(), torch.zeros_like(new(0.0)), torch.zeros_like(new(0.0))
-    dtable = torch.empty_like(master)
+    dtable = new(0.0)
+    optimizer = AdamW([drafter.table], [dtable], lr=a.rate, betas=(0.9, 0.99), eps=1e-12, weight_decay=0.0)
     last = torch.randint(0, a.vocab, (a.sequences,), generator=gen, device="cuda", dtype=torch.int32)
     for turn in range(a.turns):
         policy = lambda ids: (truth[ids.long()] @ truth.t())   # noqa: E731
@@ -148,13 +149,9 @@ def main() -> None:
         lists = teacher_lists(rows.view(-1, rows.shape[2]), a.vocab, a.top)
         weight = torch.full((seen.numel(),), 1.0 / seen.numel(), device="cuda")
         loss = drafter.loss_bwd(seen, lists, weight, dtable)
-        first.lerp_(dtable, 0.1)
-        second.lerp_(dtable * dtable, 0.01)
-        step = turn + 1
-        master -= a.rate * (first / (1 - 0.9 ** step)) / ((second / (1 - 0.99 ** step)).sqrt() + 1e-12)
-        drafter.table.copy_(master)
+        optimizer.step()
         last = tokens.gather(1, accepted.long().view(-1, 1)).view(-1)
-        if turn % 20 == 0 or step == a.turns:
+        if turn % 20 == 0 or turn + 1 == a.turns:
             print(f"turn {turn}: divergence {loss.item():.4f}, {accepted.float().mean().item():.2f} of {a.drafted} drafted tokens kept", flush=True)
     if drafter.err.item():
         raise SystemExit(f"error bits {drafter.err.item()}")
