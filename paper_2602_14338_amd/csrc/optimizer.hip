@@ -14,8 +14,8 @@
 namespace aero {
 
 // ---------------------------------------------------------------------------------- the table
-constexpr int kOptNT = 256, kPer = 8, kChunk = kOptNT * kPer, kBlock = AERO_MOMENT_BLOCK;
-static_assert(kBlock == 32 * kPer, "half a wave holds a block of moments");
+constexpr int kOptNT = 256, kPer = 4, kBlock = AERO_MOMENT_BLOCK, kUnit = kBlock * (kOptNT / kWave), kUnits = 2, kChunk = kUnit * kUnits;
+static_assert(kBlock == kWave * kPer, "a wave holds a block of moments");
 
 enum ParamKind { kNoParam, kParamF32, kParamBF16, kMasterBF16, kMasterF16, kParamKinds };
 constexpr int kGrads = 3, kClasses = kParamKinds * kGrads * 2;   // times the gradient's type, times the moments'
@@ -37,6 +37,13 @@ struct Tensor {
 };
 static_assert(sizeof(Tensor) % 16 == 0, "read in 16-byte pieces");
 
+// What a step has worked out before it looks at an element.
+struct StepScalars {
+  float factor, by_first, by_second;
+  uint32_t of_step;       // the random bits' part of seed and step
+  double weight_decay;    // times the rate
+};
+
 constexpr uint64_t kMagic = 0x41455254'61626c65ull;
 struct Table {
   uint64_t magic;
@@ -45,8 +52,9 @@ struct Table {
   uint32_t chunks;
   uint32_t ticket;        // of the step's workgroups (device copy)
   uint32_t pad;
+  StepScalars step;       // of the step under way (device copy)
   uint32_t class_first[kClasses + 1];   // chunks of class k: class_first[k] .. class_first[k + 1]
-  uint32_t pad2;
+  uint32_t pad2[3];
 };
 static_assert(sizeof(Table) % 16 == 0, "the tensors behind it are aligned");
 inline size_t map_offset(int32_t count) { return sizeof(Table) + size_t(count) * sizeof(Tensor); }
@@ -85,63 +93,80 @@ static int class_of(const aero_tensor& t) {
 static uint64_t chunks_of(const aero_tensor& t) { return (uint64_t(t.n) + kChunk - 1) / kChunk; }
 
 // ---------------------------------------------------------------------------------- elements
-// Eight stored elements at any alignment as 32-bit floats.
-template <int DT> __device__ __forceinline__ void load8(const void* base, uint64_t i, float (&x)[kPer]) {
-  const char* p = static_cast<const char*>(base) + i * Storage<DT>::kBytes;
-  if constexpr (DT == kF32) {
-    const f32x4_any_t a = reinterpret_cast<const f32x4_any_t*>(p)[0], b = reinterpret_cast<const f32x4_any_t*>(p)[1];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = a[k], x[4 + k] = b[k];
-  } else {
-    const u32x4_any_t a = *reinterpret_cast<const u32x4_any_t*>(p);
-    unpack_vec<DT>(u32x4_t{a.x, a.y, a.z, a.w}, x);
+// A thread's elements come in groups of four, the groups of a wave's lanes side by side: 64 lanes read and write 256 elements in a row.  Any
+// alignment, and past the caches: nothing is read twice.
+typedef uint32_t u32_any_t __attribute__((aligned(1)));
+// Waits for what this wave has under way in memory, if asked to.
+template <bool ASKED> __device__ __forceinline__ void arrived() {
+  if constexpr (ASKED) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
   }
 }
-template <int DT> __device__ __forceinline__ void store8(void* base, uint64_t i, const float (&x)[kPer]) {
-  char* p = static_cast<char*>(base) + i * Storage<DT>::kBytes;
-  if constexpr (DT == kF32) {
-    f32x4_any_t a, b;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = x[k], b[k] = x[4 + k];
-    reinterpret_cast<f32x4_any_t*>(p)[0] = a;
-    reinterpret_cast<f32x4_any_t*>(p)[1] = b;
-  } else {
-    const u32x4_t v = pack_vec<DT>(x);
-    *reinterpret_cast<u32x4_any_t*>(p) = u32x4_any_t{v.x, v.y, v.z, v.w};
+// How many of the four elements from i on a tensor of n has.
+__device__ __forceinline__ int have_of(int64_t n, uint64_t i) {
+  const int64_t behind = n - int64_t(i);
+  return behind >= kPer ? kPer : behind > 0 ? int(behind) : 0;
+}
+// Four stored elements: `have` of them are the tensor's, the others read as 0 and are not written.
+template <int DT> struct Four {
+  static constexpr bool kWide = DT == kF32;
+  using raw = std::conditional_t<kWide, f32x4_any_t, u32x2_any_t>;
+  __device__ __forceinline__ static raw load(const void* base, uint64_t i, int have) {
+    const char* p = static_cast<const char*>(base) + i * Storage<DT>::kBytes;
+    if (have >= kPer) return __builtin_nontemporal_load(reinterpret_cast<const raw*>(p));
+    if constexpr (kWide) {
+      const float* f = reinterpret_cast<const float*>(p);
+      return raw{have > 0 ? f[0] : 0.f, have > 1 ? f[1] : 0.f, have > 2 ? f[2] : 0.f, 0.f};
+    } else {
+      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+      return raw{(have > 0 ? uint32_t(h[0]) : 0u) | (have > 1 ? uint32_t(h[1]) << 16 : 0u), have > 2 ? uint32_t(h[2]) : 0u};
+    }
   }
-}
-// The same up to a tensor's end: `have` elements of the eight (others read as 0).
-template <int DT> __device__ __forceinline__ void load_upto(const void* base, uint64_t i, int have, float (&x)[kPer]) {
-  if (have >= kPer) return load8<DT>(base, i, x);
+  __device__ __forceinline__ static void widen(const raw& a, float (&x)[kPer]) {
+    if constexpr (kWide) {
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) x[k] = k < have ? load_elt<DT>(base, int64_t(i) + k) : 0.f;
-}
-template <int DT> __device__ __forceinline__ void store_upto(void* base, uint64_t i, int have, const float (&x)[kPer]) {
-  if (have >= kPer) return store8<DT>(base, i, x);
+      for (int k = 0; k < kPer; ++k) x[k] = a[k];
+    } else if constexpr (DT == kBF16) {
+      x[0] = bf16_lo(a.x), x[1] = bf16_hi(a.x), x[2] = bf16_lo(a.y), x[3] = bf16_hi(a.y);
+    } else {
+      x[0] = f16_to_f32(uint16_t(a.x)), x[1] = f16_to_f32(uint16_t(a.x >> 16));
+      x[2] = f16_to_f32(uint16_t(a.y)), x[3] = f16_to_f32(uint16_t(a.y >> 16));
+    }
+  }
+  __device__ __forceinline__ static void store(void* base, uint64_t i, int have, const float (&x)[kPer]) {
+    char* p = static_cast<char*>(base) + i * Storage<DT>::kBytes;
+    if (have < kPer) {
+#pragma unroll
+      for (int k = 0; k < kPer - 1; ++k)
+        if (k < have) store_elt<DT>(p, k, x[k]);
+      return;
+    }
+    if constexpr (kWide) {
+      __builtin_nontemporal_store((raw{x[0], x[1], x[2], x[3]}), reinterpret_cast<raw*>(p));
+    } else {
+      const auto pack = [](float lo, float hi) { return DT == kBF16 ? pack_bf16x2(lo, hi) : pack_f16x2(lo, hi); };
+      __builtin_nontemporal_store((raw{pack(x[0], x[1]), pack(x[2], x[3])}), reinterpret_cast<raw*>(p));
+    }
+  }
+};
+__device__ __forceinline__ uint32_t load_codes(const char* base, uint64_t i, int have) {
+  if (have >= kPer) return __builtin_nontemporal_load(reinterpret_cast<const u32_any_t*>(base + i));
+  uint32_t w = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k)
-    if (k < have) store_elt<DT>(base, int64_t(i) + k, x[k]);
+    if (k < have) w |= uint32_t(uint8_t(base[i + k])) << (8 * k);
+  return w;
 }
-__device__ __forceinline__ void load_codes(const char* base, uint64_t i, int have, uint32_t (&w)[2]) {
+__device__ __forceinline__ void store_codes(char* base, uint64_t i, int have, uint32_t w) {
   if (have >= kPer) {
-    const u32x2_any_t v = *reinterpret_cast<const u32x2_any_t*>(base + i);
-    w[0] = v.x;
-    w[1] = v.y;
+    __builtin_nontemporal_store(w, reinterpret_cast<u32_any_t*>(base + i));
     return;
   }
-  w[0] = w[1] = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k)
-    if (k < have) w[k / 4] |= uint32_t(uint8_t(base[i + k])) << (8 * (k % 4));
-}
-__device__ __forceinline__ void store_codes(char* base, uint64_t i, int have, const uint32_t (&w)[2]) {
-  if (have >= kPer) {
-    *reinterpret_cast<u32x2_any_t*>(base + i) = u32x2_any_t{w[0], w[1]};
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (k < have) base[i + k] = char(w[k / 4] >> (8 * (k % 4)));
+    if (k < have) base[i + k] = char(w >> (8 * k));
 }
 
 // ---------------------------------------------------------------------------------- moments in 8 bits
@@ -161,54 +186,85 @@ __device__ __forceinline__ float second_value(float c, float scale) {
 #pragma clang fp contract(off)
   return fourth(c) * scale;
 }
-template <bool FIRST> __device__ __forceinline__ void decode8(const uint32_t (&w)[2], float scale, float (&x)[kPer]) {
+template <bool FIRST> __device__ __forceinline__ void decode4(uint32_t w, float scale, float (&x)[kPer]) {
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
-    if constexpr (FIRST) x[k] = first_value(float(int8_t(w[k / 4] >> (8 * (k % 4)))), scale);
-    else x[k] = second_value(float(w[k / 4] >> (8 * (k % 4)) & 0xff), scale);
+    if constexpr (FIRST) x[k] = first_value(float(int8_t(w >> (8 * k))), scale);
+    else x[k] = second_value(float(w >> (8 * k) & 0xff), scale);
   }
 }
-// The largest of a block's 256 moments by its bits (as whole numbers infinities and NaN come out largest): half a wave.
-__device__ __forceinline__ uint32_t block_max(uint32_t x) {
-  auto most = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-  x = most(x, uint32_t(dpp_move_i<0xB1>(int(x))));
-  x = most(x, uint32_t(dpp_move_i<0x4E>(int(x))));
-  x = most(x, uint32_t(dpp_move_i<0x141>(int(x))));
-  x = most(x, uint32_t(dpp_move_i<0x140>(int(x))));
-  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return most(r[0], r[1]);
-}
-__device__ __forceinline__ float block_scale(const float (&x)[kPer], float inv_top) {
+// The scale of a block, four of whose moments each lane of a wave holds.  The largest by its bits: as whole numbers infinities and NaN come out largest.
+template <bool SIGNED> __device__ __forceinline__ float block_scale(const float (&x)[kPer], float inv_top) {
 #pragma clang fp contract(off)
-  uint32_t most = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const uint32_t b = __float_as_uint(x[k]) & 0x7fffffffu;
-    most = b > most ? b : most;
-  }
-  most = block_max(most);
-  if (most >= 0x7f800000u) return __builtin_nanf("");
-  const float s = __uint_as_float(most) * inv_top;
+  auto most = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  auto bits = [](float v) { return SIGNED ? __float_as_uint(v) & 0x7fffffffu : __float_as_uint(v); };
+  uint32_t m = most(most(bits(x[0]), bits(x[1])), most(bits(x[2]), bits(x[3])));
+  m = uint32_t(wave_reduce_i(int(m), [&](int a, int b) { return int(most(uint32_t(a), uint32_t(b))); }));
+  if (m >= 0x7f800000u) return __builtin_nanf("");
+  const float s = __uint_as_float(m) * inv_top;
   return s >= 1.17549435e-38f ? s : 0.f;
 }
-__device__ __forceinline__ int first_code(float x, float inv, float u) {
+// Codes of a block's moments, of which this lane has four.  The root that finds a code is an estimate from below, by more than its own error and by so little that
+// the next code is rarely the right one: a branch that few waves take.
+constexpr float kBelow = 1.f - 0x1p-21f;
+__device__ __forceinline__ uint32_t first_codes(const float (&x)[kPer], float inv, const float (&u)[kPer]) {
 #pragma clang fp contract(off)
-  const float y = fminf(fabsf(x) * inv, kTop1);
-  float c = floorf(__builtin_amdgcn_sqrtf(y));
-  if (c * c > y) c -= 1.f;
-  else if ((c + 1.f) * (c + 1.f) <= y) c += 1.f;
-  if (u * (2.f * c + 1.f) < y - c * c) c += 1.f;
-  return int(x < 0.f ? -c : c);
+  float y[kPer], c[kPer];
+  bool more = false;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    y[k] = fminf(fabsf(x[k]) * inv, kTop1);
+    c[k] = floorf(__builtin_amdgcn_sqrtf(y[k]) * kBelow);
+    const float next = c[k] + 1.f;
+    more |= next * next <= y[k];
+  }
+  if (__builtin_amdgcn_ballot_w64(more) != 0) {
+    asm volatile("" ::: "memory");   // stays a branch
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const float next = c[k] + 1.f;
+      if (next * next <= y[k]) c[k] = next;
+    }
+  }
+  uint32_t w = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (u[k] * (2.f * c[k] + 1.f) < y[k] - c[k] * c[k]) c[k] += 1.f;
+    w |= (uint32_t(int(x[k] < 0.f ? -c[k] : c[k])) & 0xff) << (8 * k);
+  }
+  return w;
 }
-__device__ __forceinline__ uint32_t second_code(float x, float inv, float u) {
+__device__ __forceinline__ uint32_t second_codes(const float (&x)[kPer], float inv, const float (&u)[kPer]) {
 #pragma clang fp contract(off)
-  const float y = fminf(x * inv, kTop2);
-  float c = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(y)));
-  if (fourth(c) > y) c -= 1.f;
-  else if (fourth(c + 1.f) <= y) c += 1.f;
-  const float at = fourth(c);
-  if (u * (fourth(c + 1.f) - at) < y - at) c += 1.f;
-  return uint32_t(y > 0.f ? fminf(fmaxf(c, 1.f), 255.f) : 0.f);
+  float y[kPer], c[kPer], at[kPer], next[kPer];
+  bool more = false;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    y[k] = fminf(x[k] * inv, kTop2);
+    c[k] = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(y[k])) * kBelow);
+    at[k] = fourth(c[k]);
+    next[k] = fourth(c[k] + 1.f);
+    more |= next[k] <= y[k];
+  }
+  if (__builtin_amdgcn_ballot_w64(more) != 0) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (next[k] <= y[k]) {
+        c[k] += 1.f;
+        at[k] = next[k];
+        next[k] = fourth(c[k] + 1.f);
+      }
+    }
+  }
+  uint32_t w = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    if (u[k] * (next[k] - at[k]) < y[k] - at[k]) c[k] += 1.f;
+    const float least = y[k] > 0.f ? 1.f : 0.f;   // a moment > 0 is not stored as 0
+    w |= uint32_t(__builtin_amdgcn_fmed3f(c[k], least, 255.f)) << (8 * k);
+  }
+  return w;
 }
 
 __device__ __forceinline__ uint32_t mix(uint32_t x) {
@@ -222,8 +278,7 @@ __device__ __forceinline__ float uniform16(uint32_t low16) { return fmaf(float(l
 struct StepArgs {
   void* table;
   int32_t count;
-  uint32_t first, chunks;   // of this launch's class
-  int32_t last;             // counts the step
+  uint32_t first, first_unit;   // chunk that this launch's class begins with; the launch's part of it
   float beta1, beta1c, beta2, beta2c, eps;
   double lr, weight_decay, dbeta1, dbeta2;
   uint32_t seed_lo, seed_hi;
@@ -240,169 +295,283 @@ __device__ __forceinline__ double power(double b, uint32_t t) {
   return r;
 }
 
-template <int KIND, int GRAD, bool SMALL>
-__global__ __launch_bounds__(kOptNT) void k_adamw(StepArgs a) {
-  const float factor = a.factor ? a.factor[0] : 1.f;
-  const int step = a.step[0];
-  if (!(fabsf(factor) < INFINITY)) return;   // uniform over the launch
-  const uint32_t t = uint32_t(step) + 1;
-  const double rate = a.lr * (a.lr_factor ? double(a.lr_factor[0]) : 1.0);
-  const float by_first = float(rate / (1.0 - power(a.dbeta1, t)));
-  const float by_second = float(1.0 / sqrt(1.0 - power(a.dbeta2, t)));
-  const uint32_t of_step = mix(a.seed_lo ^ mix(a.seed_hi ^ mix(uint32_t(step))));
-  const Tensor* tensors = tensors_of(a.table);
-  const uint32_t* map = map_of(a.table, a.count);
-  constexpr bool kMaster = KIND == kMasterBF16 || KIND == kMasterF16;
-  constexpr int kStored = KIND == kParamF32 ? kF32 : KIND == kMasterF16 ? kF16 : kBF16;
-  for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
-    const Tensor& e = tensors[__builtin_amdgcn_readfirstlane(map[a.first + c])];
-    const uint64_t i = uint64_t(a.first + c - e.first_chunk) * kChunk + threadIdx.x * kPer;
-    const int64_t behind = e.n - int64_t(i);
-    const int have = behind >= kPer ? kPer : behind > 0 ? int(behind) : 0;
-    float p[kPer], g[kPer], m[kPer], v[kPer];
-    load_upto<GRAD>(e.grad, i, have, g);
-    if constexpr (kMaster) load_upto<kF32>(e.master, i, have, p);
-    else load_upto<kStored>(e.param, i, have, p);
+// What a lane has of an element group, as it is stored: to be widened when it is worked on, so that the loads of a group are under way together, and those of
+// the next one while this one is stepped.
+template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
+  static constexpr bool kOrdered = !SMALL && !ALONE;
+  static constexpr bool kMaster = KIND == kMasterBF16 || KIND == kMasterF16;
+  static constexpr int kStored = KIND == kParamF32 ? kF32 : KIND == kMasterF16 ? kF16 : kBF16, kRead = kMaster ? kF32 : kStored;
+  typename Four<GRAD>::raw g;
+  typename Four<kRead>::raw p;
+  Four<kF32>::raw m, v;       // 32-bit moments
+  uint32_t wm, wv;            // codes
+  float scale_m, scale_v;
+
+  __device__ __forceinline__ void load(const Tensor& e, uint64_t from, int lane, int have) {
+    const uint64_t i = from + lane * kPer;
+    g = Four<GRAD>::load(e.grad, i, have);
+    arrived<kOrdered>();
+    if constexpr (kMaster) p = Four<kF32>::load(e.master, i, have);
+    else p = Four<kRead>::load(e.param, i, have);
+    arrived<kOrdered>();
     if constexpr (SMALL) {
-      uint32_t wm[2], wv[2];
-      load_codes(e.avg, i, have, wm);
-      load_codes(e.sq, i, have, wv);
-      const uint64_t block = i / kBlock;
-      const bool in = have > 0;
-      decode8<true>(wm, in ? e.avg_scale[block] : 0.f, m);
-      decode8<false>(wv, in ? e.sq_scale[block] : 0.f, v);
+      wm = load_codes(e.avg, i, have);
+      wv = load_codes(e.sq, i, have);
+      const bool in = from < uint64_t(e.n);
+      scale_m = in ? e.avg_scale[from / kBlock] : 0.f;
+      scale_v = in ? e.sq_scale[from / kBlock] : 0.f;
     } else {
-      load_upto<kF32>(e.avg, i, have, m);
-      load_upto<kF32>(e.sq, i, have, v);
+      m = Four<kF32>::load(e.avg, i, have);
+      arrived<kOrdered>();
+      v = Four<kF32>::load(e.sq, i, have);
     }
-    const float keep = float(1.0 - rate * a.weight_decay * double(e.decay));
+  }
+  // The step of the group, and its results to where they belong.
+  __device__ __forceinline__ void step(const Tensor& e, const StepArgs& a, const StepScalars& s, uint64_t from, int lane, int have) const {
+    const uint64_t i = from + lane * kPer;
+    const float keep = float(s.weight_decay);
+    const uint32_t of_tensor = mix(s.of_step + uint32_t(e.ordinal));
+    float xg[kPer], xp[kPer], xm[kPer], xv[kPer];
+    Four<GRAD>::widen(g, xg);
+    Four<kRead>::widen(p, xp);
+    if constexpr (SMALL) {
+      decode4<true>(wm, scale_m, xm);
+      decode4<false>(wv, scale_v, xv);
+    } else {
+      Four<kF32>::widen(m, xm);
+      Four<kF32>::widen(v, xv);
+    }
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
+      {
 #pragma clang fp contract(off)
-      const float x = g[k] * factor;
-      m[k] = m[k] * a.beta1 + x * a.beta1c;
-      v[k] = v[k] * a.beta2 + (x * x) * a.beta2c;
-      const float away = sqrtf(v[k]) * by_second + a.eps;
-      p[k] = p[k] * keep - m[k] / away * by_first;
+        const float x = xg[k] * s.factor;
+        xm[k] = xm[k] * a.beta1 + x * a.beta1c;
+        xv[k] = xv[k] * a.beta2 + (x * x) * a.beta2c;
+      }
+      const float away = fmaf(__builtin_amdgcn_sqrtf(xv[k]), s.by_second, a.eps);
+      xp[k] = fmaf(xp[k], keep, -(xm[k] * s.by_first) * __builtin_amdgcn_rcpf(away));
     }
-    const bool random_param = KIND == kParamBF16 && a.stochastic;
     uint32_t bits[kPer];
     if ((SMALL || KIND == kParamBF16) && a.stochastic) {
-      const uint32_t of_tensor = mix(of_step + uint32_t(e.ordinal));
 #pragma unroll
       for (int k = 0; k < kPer; ++k) bits[k] = mix(of_tensor + uint32_t(i) + uint32_t(k));
     }
+    if constexpr (!SMALL) {
+      Four<kF32>::store(e.avg, i, have, xm);
+      arrived<kOrdered>();
+      Four<kF32>::store(e.sq, i, have, xv);
+      arrived<kOrdered>();
+    }
+    if constexpr (kMaster) {
+      Four<kF32>::store(e.master, i, have, xp);
+      arrived<kOrdered>();
+    }
+    if (KIND == kParamBF16 && a.stochastic) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        const uint32_t raw = __float_as_uint(xp[k]), up = (raw + (bits[k] * 0x9E3779B1u >> 16)) & 0xffff0000u;
+        xp[k] = __uint_as_float(fabsf(xp[k]) < INFINITY ? up : raw);
+      }
+    }
+    Four<kStored>::store(e.param, i, have, xp);
     if constexpr (SMALL) {
-      const float sm = block_scale(m, kInvTop1), sv = block_scale(v, kInvTop2);
+      const float sm = block_scale<true>(xm, kInvTop1), sv = block_scale<false>(xv, kInvTop2);
       const float im = sm > 0.f ? 1.f / sm : 0.f, iv = sv > 0.f ? 1.f / sv : 0.f;
-      uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+      float um[kPer], uv[kPer];
 #pragma unroll
       for (int k = 0; k < kPer; ++k) {
-        const float um = a.stochastic ? uniform16(bits[k] & 0xffff) : 0.5f, uv = a.stochastic ? uniform16(bits[k] >> 16) : 0.5f;
-        wm[k / 4] |= (uint32_t(first_code(m[k], im, um)) & 0xff) << (8 * (k % 4));
-        wv[k / 4] |= second_code(v[k], iv, uv) << (8 * (k % 4));
+        um[k] = a.stochastic ? uniform16(bits[k] & 0xffff) : 0.5f;
+        uv[k] = a.stochastic ? uniform16(bits[k] >> 16) : 0.5f;
       }
-      store_codes(e.avg, i, have, wm);
-      store_codes(e.sq, i, have, wv);
-      if (have > 0 && threadIdx.x % 32 == 0) {
-        e.avg_scale[i / kBlock] = sm;
-        e.sq_scale[i / kBlock] = sv;
+      store_codes(e.avg, i, have, first_codes(xm, im, um));
+      store_codes(e.sq, i, have, second_codes(xv, iv, uv));
+      if (lane == 0 && have > 0) {
+        e.avg_scale[from / kBlock] = sm;
+        e.sq_scale[from / kBlock] = sv;
       }
-    } else {
-      store_upto<kF32>(e.avg, i, have, m);
-      store_upto<kF32>(e.sq, i, have, v);
     }
-    if constexpr (kMaster) store_upto<kF32>(e.master, i, have, p);
-    if (random_param) {
+  }
+};
+
+// Where a wave's group of a unit is: units are the halves, quarters, ... of chunks that a workgroup takes at a time.  The table is read as constant memory, which
+// makes it scalar loads; stores that might be to it, for all the compiler knows, would have every pointer read again by vector loads behind them.
+struct Place {
+  Tensor e;
+  uint64_t from;
+  bool full;   // the tensor has all of the workgroup's unit
+};
+template <class T> using Constant = const __attribute__((address_space(4))) T*;
+template <class T> __device__ __forceinline__ T constant_copy(const T* p) {
+  struct Words {
+    uint32_t w[sizeof(T) / 4];
+  } words;
+  const auto from = (Constant<uint32_t>)reinterpret_cast<uintptr_t>(p);
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        const uint32_t raw = __float_as_uint(p[k]);
-        if ((raw & 0x7f800000u) != 0x7f800000u) p[k] = __uint_as_float((raw + (bits[k] * 0x9E3779B1u >> 16)) & 0xffff0000u);
-      }
-    }
-    store_upto<kStored>(e.param, i, have, p);
-  }
-  // the last workgroup to end counts the step: by then every wave of every workgroup has read it
-  if (!a.last) return;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    uint32_t* ticket = &static_cast<Table*>(a.table)->ticket;
-    if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
-      *ticket = 0;
-      a.step[0] = step + 1;
-    }
-  }
+  for (size_t i = 0; i < sizeof(T) / 4; ++i) words.w[i] = from[i];
+  return __builtin_bit_cast(T, words);
+}
+__device__ __forceinline__ Place place_of(const void* table, int32_t count, uint32_t first, uint32_t unit, int wave) {
+  const uint32_t chunk = first + unit / kUnits;
+  Place p;
+  p.e = constant_copy(tensors_of(table) + constant_copy(map_of(table, count) + chunk));
+  const uint64_t at = uint64_t(chunk - p.e.first_chunk) * kChunk + unit % kUnits * kUnit;
+  p.from = at + uint64_t(wave) * kBlock;
+  p.full = at + kUnit <= uint64_t(p.e.n);
+  return p;
 }
 
-// A table without parameters still counts its steps.
-__global__ void k_count_step(int32_t* step, const float* factor) {
-  if (!factor || fabsf(factor[0]) < INFINITY) step[0] += 1;
+// Works out a step's scalars, counts it, and leaves them in the table for a launch of many workgroups.
+__device__ __forceinline__ StepScalars step_scalars(const StepArgs& a, float factor, int step) {
+  const uint32_t t = uint32_t(step) + 1;
+  const double rate = a.lr * (a.lr_factor ? double(a.lr_factor[0]) : 1.0);
+  return StepScalars{factor, float(rate / (1.0 - power(a.dbeta1, t))), float(1.0 / sqrt(1.0 - power(a.dbeta2, t))),
+                     mix(a.seed_lo ^ mix(a.seed_hi ^ mix(uint32_t(step)))), rate * a.weight_decay};
+}
+__global__ void k_step_begin(StepArgs a) {
+  const float factor = a.factor ? a.factor[0] : 1.f;
+  static_cast<Table*>(a.table)->step = step_scalars(a, factor, a.step[0]);
+  if (fabsf(factor) < INFINITY) a.step[0] += 1;
+}
+
+// A workgroup steps 1024 elements and ends.  ALONE: it works the scalars out itself, and the last workgroup to end counts the step.
+template <int KIND, int GRAD, bool SMALL, bool ALONE>
+__global__ __launch_bounds__(kOptNT) void k_adamw(StepArgs a) {
+  int step = 0;
+  StepScalars s;
+  if constexpr (ALONE) {
+    step = a.step[0];
+    s = step_scalars(a, a.factor ? a.factor[0] : 1.f, step);
+  } else {
+    s = constant_copy<StepScalars>(&static_cast<const Table*>(a.table)->step);
+  }
+  if (!(fabsf(s.factor) < INFINITY)) return;   // uniform over the launch
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const Place p = place_of(a.table, a.count, a.first, a.first_unit + blockIdx.x, wave);
+  s.weight_decay = 1.0 - s.weight_decay * double(p.e.decay);
+  Held<KIND, GRAD, SMALL, ALONE> h;
+  if (p.full) {
+    h.load(p.e, p.from, lane, kPer);
+    h.step(p.e, a, s, p.from, lane, kPer);
+  } else {
+    const int have = have_of(p.e.n, p.from + lane * kPer);
+    h.load(p.e, p.from, lane, have);
+    h.step(p.e, a, s, p.from, lane, have);
+  }
+  if constexpr (ALONE) {
+    __syncthreads();   // every wave of this workgroup has read the step by now
+    if (threadIdx.x == 0) {
+      uint32_t* ticket = &static_cast<Table*>(a.table)->ticket;
+      if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
+        *ticket = 0;
+        a.step[0] = step + 1;
+      }
+    }
+  }
 }
 
 using StepKernel = void (*)(StepArgs);
-template <int KIND, int GRAD> static StepKernel step_kernel(bool small) { return small ? k_adamw<KIND, GRAD, true> : k_adamw<KIND, GRAD, false>; }
-template <int KIND> static StepKernel step_kernel(int grad, bool small) {
-  return grad == 0 ? step_kernel<KIND, kF32>(small) : grad == 1 ? step_kernel<KIND, kBF16>(small) : step_kernel<KIND, kF16>(small);
+template <int KIND, int GRAD> static StepKernel step_kernel(bool small, bool alone) {
+  return small ? (alone ? k_adamw<KIND, GRAD, true, true> : k_adamw<KIND, GRAD, true, false>)
+               : (alone ? k_adamw<KIND, GRAD, false, true> : k_adamw<KIND, GRAD, false, false>);
 }
-static StepKernel step_kernel(int cls) {
+template <int KIND> static StepKernel step_kernel(int grad, bool small, bool alone) {
+  return grad == 0 ? step_kernel<KIND, kF32>(small, alone) : grad == 1 ? step_kernel<KIND, kBF16>(small, alone) : step_kernel<KIND, kF16>(small, alone);
+}
+static StepKernel step_kernel(int cls, bool alone) {
   const int kind = cls / 2 / kGrads, grad = cls / 2 % kGrads;
   const bool small = cls % 2;
   switch (kind) {
-    case kParamF32: return step_kernel<kParamF32>(grad, small);
-    case kParamBF16: return step_kernel<kParamBF16>(grad, small);
-    case kMasterBF16: return step_kernel<kMasterBF16>(grad, small);
-    default: return step_kernel<kMasterF16>(grad, small);
+    case kParamF32: return step_kernel<kParamF32>(grad, small, alone);
+    case kParamBF16: return step_kernel<kParamBF16>(grad, small, alone);
+    case kMasterBF16: return step_kernel<kMasterBF16>(grad, small, alone);
+    default: return step_kernel<kMasterF16>(grad, small, alone);
   }
 }
+// Up to so many workgroups a step is one launch; of more, working its scalars out and counting off in every one would cost more than a launch of its own.
+constexpr uint32_t kAloneUnits = 1024;
 
 // ---------------------------------------------------------------------------------- moments as numbers
-template <bool SMALL, int DT>
-__global__ __launch_bounds__(kOptNT) void k_moments(void* table, int32_t count, uint32_t first, uint32_t chunks, void* avg, void* sq) {
-  const Tensor* tensors = tensors_of(table);
-  const uint32_t* map = map_of(table, count);
-  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Tensor& e = tensors[__builtin_amdgcn_readfirstlane(map[first + c])];
-    const uint64_t i = uint64_t(first + c - e.first_chunk) * kChunk + threadIdx.x * kPer;
-    const int64_t behind = e.n - int64_t(i);
-    const int have = behind >= kPer ? kPer : behind > 0 ? int(behind) : 0;
-    if (have == 0) continue;
-    float m[kPer], v[kPer];
+template <bool SMALL> struct HeldMoments {
+  Four<kF32>::raw m, v;
+  uint32_t wm, wv;
+  float scale_m, scale_v;
+  __device__ __forceinline__ void load(const Tensor& e, uint64_t from, int lane, int have) {
+    const uint64_t i = from + lane * kPer;
     if constexpr (SMALL) {
-      uint32_t w[2];
-      load_codes(e.avg, i, have, w);
-      decode8<true>(w, e.avg_scale[i / kBlock], m);
-      load_codes(e.sq, i, have, w);
-      decode8<false>(w, e.sq_scale[i / kBlock], v);
+      wm = load_codes(e.avg, i, have);
+      wv = load_codes(e.sq, i, have);
+      const bool in = from < uint64_t(e.n);
+      scale_m = in ? e.avg_scale[from / kBlock] : 0.f;
+      scale_v = in ? e.sq_scale[from / kBlock] : 0.f;
     } else {
-      load_upto<kF32>(e.avg, i, have, m);
-      load_upto<kF32>(e.sq, i, have, v);
+      m = Four<kF32>::load(e.avg, i, have);
+      v = Four<kF32>::load(e.sq, i, have);
     }
-    store_upto<DT>(avg, uint64_t(e.out) + i, have, m);
-    store_upto<DT>(sq, uint64_t(e.out) + i, have, v);
+  }
+  template <int DT> __device__ __forceinline__ void store(void* avg, void* sq, uint64_t i, int have) const {
+    float xm[kPer], xv[kPer];
+    if constexpr (SMALL) {
+      decode4<true>(wm, scale_m, xm);
+      decode4<false>(wv, scale_v, xv);
+    } else {
+      Four<kF32>::widen(m, xm);
+      Four<kF32>::widen(v, xv);
+    }
+    Four<DT>::store(avg, i, have, xm);
+    Four<DT>::store(sq, i, have, xv);
+  }
+};
+template <bool SMALL, int DT>
+__global__ __launch_bounds__(kOptNT) void k_moments(void* table, int32_t count, uint32_t first, void* avg, void* sq) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  {
+    HeldMoments<SMALL> h[kUnits];
+    const Place p = place_of(table, count, first, blockIdx.x * kUnits, wave);
+    const bool full = p.from - uint64_t(wave) * kBlock + kChunk <= uint64_t(p.e.n);
+    const auto all = [&](auto have) {
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) h[u].load(p.e, p.from + u * kUnit, lane, have(p.from + u * kUnit + lane * kPer));
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+        h[u].template store<DT>(avg, sq, uint64_t(p.e.out) + p.from + u * kUnit + lane * kPer, have(p.from + u * kUnit + lane * kPer));
+    };
+    if (full) all([](uint64_t) { return kPer; });
+    else all([&](uint64_t i) { return have_of(p.e.n, i); });
   }
 }
 
 // ---------------------------------------------------------------------------------- norm
 constexpr int kNormMax = 2048;   // workgroups
-template <int DT> __device__ __forceinline__ void add_squares(const Tensor& e, uint64_t i, int have, double& sum) {
-  float g[kPer];
-  load_upto<DT>(e.grad, i, have, g);
+template <int DT, class Have> __device__ __forceinline__ void add_squares(const Place& p, int lane, Have have, double& sum) {
+  typename Four<DT>::raw g[kUnits];
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) sum = fma(double(g[k]), double(g[k]), sum);
+  for (int u = 0; u < kUnits; ++u) {
+    const uint64_t i = p.from + u * kUnit + lane * kPer;
+    g[u] = Four<DT>::load(p.e.grad, i, have(i));
+  }
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    float x[kPer];
+    Four<DT>::widen(g[u], x);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) sum = fma(double(x[k]), double(x[k]), sum);
+  }
 }
 __global__ __launch_bounds__(kOptNT) void k_norm_parts(const void* table, int32_t count, uint32_t chunks, double* __restrict__ part) {
-  const Tensor* tensors = tensors_of(table);
-  const uint32_t* map = map_of(table, count);
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   double sum = 0.0;
   for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Tensor& e = tensors[__builtin_amdgcn_readfirstlane(map[c])];
-    const uint64_t i = uint64_t(c - e.first_chunk) * kChunk + threadIdx.x * kPer;
-    const int64_t behind = e.n - int64_t(i);
-    const int have = behind >= kPer ? kPer : behind > 0 ? int(behind) : 0;
-    const int grad = e.kind / 2 % kGrads;
-    if (grad == 0) add_squares<kF32>(e, i, have, sum);
-    else if (grad == 1) add_squares<kBF16>(e, i, have, sum);
-    else add_squares<kF16>(e, i, have, sum);
+    const Place p = place_of(table, count, 0, c * kUnits, wave);
+    const bool full = p.from - uint64_t(wave) * kBlock + kChunk <= uint64_t(p.e.n);
+    const int grad = p.e.kind / 2 % kGrads;
+    const auto add = [&](auto have) {
+      if (grad == 0) add_squares<kF32>(p, lane, have, sum);
+      else if (grad == 1) add_squares<kBF16>(p, lane, have, sum);
+      else add_squares<kF16>(p, lane, have, sum);
+    };
+    if (full) add([](uint64_t) { return kPer; });
+    else add([&](uint64_t i) { return have_of(p.e.n, i); });
   }
   sum = wave_sum_d(sum);
   __shared__ double s_sum[kOptNT / kWave];
@@ -431,6 +600,8 @@ __global__ __launch_bounds__(kOptNT) void k_norm_end(const double* __restrict__ 
   else if (max_norm > 0.f && x > double(max_norm)) f *= double(max_norm) / x;
   factor[0] = float(f);
 }
+
+constexpr uint32_t kMostUnits = (1u << 24) - 1;   // workgroups of 256 threads that a launch has at most
 
 size_t grad_norm_workspace_bytes() { return kNormMax * sizeof(double); }
 
@@ -463,7 +634,7 @@ extern "C" aero_status aero_tensor_table(const aero_tensor* list, int32_t count,
     chunks += chunks_of(list[k]);
     of_class[class_of(list[k])] += chunks_of(list[k]);
   }
-  if (chunks >= (uint64_t(1) << 31)) return AERO_ERR_SHAPE;
+  if (chunks * kUnits >= (uint64_t(1) << 31)) return AERO_ERR_SHAPE;
   const size_t bytes = aero_tensor_table_bytes(list, count);
   if (image_bytes < bytes) return AERO_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(image) % 16 != 0) return AERO_ERR_ALIGN;
@@ -540,19 +711,29 @@ extern "C" aero_status aero_adamw_step(const void* image, void* table, const aer
   a.step = step;
   a.factor = factor;
   a.lr_factor = lr_factor;
-  int last = -1;
-  for (int k = class_of(kParamF32, 0, 0); k < kClasses; ++k)
-    if (t->class_first[k + 1] > t->class_first[k]) last = k;
-  if (last < 0) {
-    hipLaunchKernelGGL(k_count_step, dim3(1), dim3(1), 0, s, step, factor);
+  constexpr int kFirst = class_of(kParamF32, 0, 0);
+  int classes = 0, only = 0;
+  for (int k = kFirst; k < kClasses; ++k) {
+    if (t->class_first[k + 1] > t->class_first[k]) {
+      ++classes;
+      only = k;
+    }
+  }
+  const uint64_t units = uint64_t(t->class_first[kClasses] - t->class_first[kFirst]) * kUnits;
+  if (classes == 1 && units <= kAloneUnits) {
+    a.first = t->class_first[only];
+    hipLaunchKernelGGL(step_kernel(only, true), dim3(unsigned(units)), dim3(kOptNT), 0, s, a);
     return launch_status();
   }
-  for (int k = class_of(kParamF32, 0, 0); k <= last; ++k) {
+  hipLaunchKernelGGL(k_step_begin, dim3(1), dim3(1), 0, s, a);
+  for (int k = kFirst; k < kClasses; ++k) {
+    const uint64_t of_class = uint64_t(t->class_first[k + 1] - t->class_first[k]) * kUnits;
     a.first = t->class_first[k];
-    a.chunks = t->class_first[k + 1] - a.first;
-    if (a.chunks == 0) continue;
-    a.last = k == last;
-    hipLaunchKernelGGL(step_kernel(k), dim3(opt_grid(a.chunks, 8)), dim3(kOptNT), 0, s, a);
+    for (uint64_t from = 0; from < of_class; from += kMostUnits) {
+      const uint64_t n = of_class - from < kMostUnits ? of_class - from : kMostUnits;
+      a.first_unit = uint32_t(from);
+      hipLaunchKernelGGL(step_kernel(k, false), dim3(unsigned(n)), dim3(kOptNT), 0, s, a);
+    }
   }
   return launch_status();
 }
@@ -574,7 +755,10 @@ extern "C" aero_status aero_adamw_moments(const void* image, void* table, int32_
     if (chunks == 0) continue;
     const auto kernel = k % 2 ? (dtype == AERO_F32 ? k_moments<true, kF32> : k_moments<true, kBF16>)
                               : (dtype == AERO_F32 ? k_moments<false, kF32> : k_moments<false, kBF16>);
-    hipLaunchKernelGGL(kernel, dim3(opt_grid(chunks, 8)), dim3(kOptNT), 0, s, table, t->count, first, chunks, avg, avg_sq);
+    for (uint32_t from = 0; from < chunks; from += kMostUnits) {
+      const unsigned n = unsigned(chunks - from < kMostUnits ? chunks - from : kMostUnits);
+      hipLaunchKernelGGL(kernel, dim3(n), dim3(kOptNT), 0, s, table, t->count, first + from, avg, avg_sq);
+    }
   }
   return launch_status();
 }
