@@ -14,8 +14,10 @@
 namespace aero {
 
 // ---------------------------------------------------------------------------------- the table
-constexpr int kOptNT = 256, kPer = 4, kBlock = AERO_MOMENT_BLOCK, kUnit = kBlock * (kOptNT / kWave), kUnits = 2, kChunk = kUnit * kUnits;
-static_assert(kBlock == kWave * kPer, "a wave holds a block of moments");
+constexpr int kOptNT = 256, kChunk = 2048, kBlock = AERO_MOMENT_BLOCK;
+// Elements of a lane, side by side: of 32-bit arrays four, 16 bytes; eight where moments are codes, so that half a wave holds a block of them.
+constexpr int kWideLane = 4, kCodeLane = 8;
+static_assert(kBlock == kWave / 2 * kCodeLane && kChunk == kOptNT * kCodeLane, "a chunk is blocks of half a wave each");
 
 enum ParamKind { kNoParam, kParamF32, kParamBF16, kMasterBF16, kMasterF16, kParamKinds };
 constexpr int kGrads = 3, kClasses = kParamKinds * kGrads * 2;   // times the gradient's type, times the moments'
@@ -93,9 +95,10 @@ static int class_of(const aero_tensor& t) {
 static uint64_t chunks_of(const aero_tensor& t) { return (uint64_t(t.n) + kChunk - 1) / kChunk; }
 
 // ---------------------------------------------------------------------------------- elements
-// A thread's elements come in groups of four, the groups of a wave's lanes side by side: 64 lanes read and write 256 elements in a row.  Any
-// alignment, and past the caches: nothing is read twice.
-typedef uint32_t u32_any_t __attribute__((aligned(1)));
+// At any alignment, and past the caches: nothing is read twice.
+typedef uint32_t u32x4_at_t __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32x2_at_t __attribute__((ext_vector_type(2), aligned(1)));
+
 // Waits for what this wave has under way in memory, if asked to.
 template <bool ASKED> __device__ __forceinline__ void arrived() {
   if constexpr (ASKED) {
@@ -104,76 +107,95 @@ template <bool ASKED> __device__ __forceinline__ void arrived() {
     asm volatile("" ::: "memory");
   }
 }
-// How many of the four elements from i on a tensor of n has.
-__device__ __forceinline__ int have_of(int64_t n, uint64_t i) {
+// How many of the N elements from i on a tensor of n has.
+template <int N> __device__ __forceinline__ int have_of(int64_t n, uint64_t i) {
   const int64_t behind = n - int64_t(i);
-  return behind >= kPer ? kPer : behind > 0 ? int(behind) : 0;
+  return behind >= N ? N : behind > 0 ? int(behind) : 0;
 }
-// Four stored elements: `have` of them are the tensor's, the others read as 0 and are not written.
-template <int DT> struct Four {
-  static constexpr bool kWide = DT == kF32;
-  using raw = std::conditional_t<kWide, f32x4_any_t, u32x2_any_t>;
-  __device__ __forceinline__ static raw load(const void* base, uint64_t i, int have) {
-    const char* p = static_cast<const char*>(base) + i * Storage<DT>::kBytes;
-    if (have >= kPer) return __builtin_nontemporal_load(reinterpret_cast<const raw*>(p));
-    if constexpr (kWide) {
-      const float* f = reinterpret_cast<const float*>(p);
-      return raw{have > 0 ? f[0] : 0.f, have > 1 ? f[1] : 0.f, have > 2 ? f[2] : 0.f, 0.f};
-    } else {
-      const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-      return raw{(have > 0 ? uint32_t(h[0]) : 0u) | (have > 1 ? uint32_t(h[1]) << 16 : 0u), have > 2 ? uint32_t(h[2]) : 0u};
-    }
-  }
-  __device__ __forceinline__ static void widen(const raw& a, float (&x)[kPer]) {
-    if constexpr (kWide) {
+// N stored elements of BYTES each, as words: `have` of them are the tensor's, the others read as 0 and are not written.
+template <int BYTES, int N> struct Words {
+  static constexpr int kWords = BYTES * N / 4;
+  static_assert(kWords == 2 || kWords == 4 || kWords == 8, "one or two vectors");
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const void* base, uint64_t i, int have) {
+    const char* p = static_cast<const char*>(base) + i * BYTES;
+    if (have >= N) {
+      if constexpr (kWords == 2) {
+        const u32x2_at_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_at_t*>(p));
+        w[0] = v.x, w[1] = v.y;
+      } else {
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) x[k] = a[k];
-    } else if constexpr (DT == kBF16) {
-      x[0] = bf16_lo(a.x), x[1] = bf16_hi(a.x), x[2] = bf16_lo(a.y), x[3] = bf16_hi(a.y);
-    } else {
-      x[0] = f16_to_f32(uint16_t(a.x)), x[1] = f16_to_f32(uint16_t(a.x >> 16));
-      x[2] = f16_to_f32(uint16_t(a.y)), x[3] = f16_to_f32(uint16_t(a.y >> 16));
-    }
-  }
-  __device__ __forceinline__ static void store(void* base, uint64_t i, int have, const float (&x)[kPer]) {
-    char* p = static_cast<char*>(base) + i * Storage<DT>::kBytes;
-    if (have < kPer) {
-#pragma unroll
-      for (int k = 0; k < kPer - 1; ++k)
-        if (k < have) store_elt<DT>(p, k, x[k]);
+        for (int k = 0; k < kWords; k += 4) {
+          const u32x4_at_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_at_t*>(p + 4 * k));
+          w[k] = v.x, w[k + 1] = v.y, w[k + 2] = v.z, w[k + 3] = v.w;
+        }
+      }
       return;
     }
-    if constexpr (kWide) {
-      __builtin_nontemporal_store((raw{x[0], x[1], x[2], x[3]}), reinterpret_cast<raw*>(p));
-    } else {
-      const auto pack = [](float lo, float hi) { return DT == kBF16 ? pack_bf16x2(lo, hi) : pack_f16x2(lo, hi); };
-      __builtin_nontemporal_store((raw{pack(x[0], x[1]), pack(x[2], x[3])}), reinterpret_cast<raw*>(p));
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) w[k] = 0;
+#pragma unroll
+    for (int k = 0; k < N - 1; ++k) {
+      if (k >= have) continue;
+      if constexpr (BYTES == 4) w[k] = reinterpret_cast<const uint32_t*>(p)[k];
+      else if constexpr (BYTES == 2) w[k / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[k]) << (16 * (k % 2));
+      else w[k / 4] |= uint32_t(reinterpret_cast<const uint8_t*>(p)[k]) << (8 * (k % 4));
+    }
+  }
+  __device__ __forceinline__ void store(void* base, uint64_t i, int have) const {
+    char* p = static_cast<char*>(base) + i * BYTES;
+    if (have >= N) {
+      if constexpr (kWords == 2) {
+        __builtin_nontemporal_store((u32x2_at_t{w[0], w[1]}), reinterpret_cast<u32x2_at_t*>(p));
+      } else {
+#pragma unroll
+        for (int k = 0; k < kWords; k += 4)
+          __builtin_nontemporal_store((u32x4_at_t{w[k], w[k + 1], w[k + 2], w[k + 3]}), reinterpret_cast<u32x4_at_t*>(p + 4 * k));
+      }
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < N - 1; ++k) {
+      if (k >= have) continue;
+      if constexpr (BYTES == 4) reinterpret_cast<uint32_t*>(p)[k] = w[k];
+      else if constexpr (BYTES == 2) reinterpret_cast<uint16_t*>(p)[k] = uint16_t(w[k / 2] >> (16 * (k % 2)));
+      else reinterpret_cast<uint8_t*>(p)[k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
     }
   }
 };
-__device__ __forceinline__ uint32_t load_codes(const char* base, uint64_t i, int have) {
-  if (have >= kPer) return __builtin_nontemporal_load(reinterpret_cast<const u32_any_t*>(base + i));
-  uint32_t w = 0;
+// The same as numbers of a storage type.
+template <int DT, int N> struct Numbers : Words<Storage<DT>::kBytes, N> {
+  using Words<Storage<DT>::kBytes, N>::w;
+  __device__ __forceinline__ void widen(float (&x)[N]) const {
+    if constexpr (DT == kF32) {
 #pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (k < have) w |= uint32_t(uint8_t(base[i + k])) << (8 * k);
-  return w;
-}
-__device__ __forceinline__ void store_codes(char* base, uint64_t i, int have, uint32_t w) {
-  if (have >= kPer) {
-    __builtin_nontemporal_store(w, reinterpret_cast<u32_any_t*>(base + i));
-    return;
+      for (int k = 0; k < N; ++k) x[k] = __uint_as_float(w[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; k += 2) {
+        x[k] = DT == kBF16 ? bf16_lo(w[k / 2]) : f16_to_f32(uint16_t(w[k / 2]));
+        x[k + 1] = DT == kBF16 ? bf16_hi(w[k / 2]) : f16_to_f32(uint16_t(w[k / 2] >> 16));
+      }
+    }
   }
+  __device__ __forceinline__ static void store_rounded(void* base, uint64_t i, int have, const float (&x)[N]) {
+    Numbers v;
+    if constexpr (DT == kF32) {
 #pragma unroll
-  for (int k = 0; k < kPer; ++k)
-    if (k < have) base[i + k] = char(w >> (8 * k));
-}
+      for (int k = 0; k < N; ++k) v.w[k] = __float_as_uint(x[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; k += 2) v.w[k / 2] = DT == kBF16 ? pack_bf16x2(x[k], x[k + 1]) : pack_f16x2(x[k], x[k + 1]);
+    }
+    v.store(base, i, have);
+  }
+};
+using Codes = Words<1, kCodeLane>;
 
 // ---------------------------------------------------------------------------------- moments in 8 bits
 // Codes and values as aero.h defines them; each product, sum and quotient rounded by itself (no fused multiply-add), so that the codes are a
 // function of the definition alone.
-constexpr float kTop1 = 16129.f, kTop2 = 4228250625.f;   // 127^2, 255^4
-constexpr float kInvTop1 = float(1.0 / 16129.0), kInvTop2 = float(1.0 / 4228250625.0);
+constexpr float kInvTop1 = float(1.0 / 16129.0), kInvTop2 = float(1.0 / 4228250625.0);   // of 127^2, 255^4
 __device__ __forceinline__ float first_value(float c, float scale) {
 #pragma clang fp contract(off)
   return (c * fabsf(c)) * scale;
@@ -186,62 +208,91 @@ __device__ __forceinline__ float second_value(float c, float scale) {
 #pragma clang fp contract(off)
   return fourth(c) * scale;
 }
-template <bool FIRST> __device__ __forceinline__ void decode4(uint32_t w, float scale, float (&x)[kPer]) {
+__device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0x6A09E667u;
+  x = (x ^ (x >> 15)) * 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+__device__ __forceinline__ float uniform16(uint32_t low16) { return fmaf(float(low16), 0x1p-16f, 0x1p-17f); }   // exact
+
+template <bool FIRST> __device__ __forceinline__ void decode(const Codes& codes, float scale, float (&x)[kCodeLane]) {
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if constexpr (FIRST) x[k] = first_value(float(int8_t(w >> (8 * k))), scale);
-    else x[k] = second_value(float(w >> (8 * k) & 0xff), scale);
+  for (int k = 0; k < kCodeLane; ++k) {
+    const uint32_t w = codes.w[k / 4] >> (8 * (k % 4));
+    x[k] = FIRST ? first_value(float(int8_t(w)), scale) : second_value(float(w & 0xff), scale);
   }
 }
-// The scale of a block, four of whose moments each lane of a wave holds.  The largest by its bits: as whole numbers infinities and NaN come out largest.
-template <bool SIGNED> __device__ __forceinline__ float block_scale(const float (&x)[kPer], float inv_top) {
+// The scale of a block, eight of whose moments each lane of half a wave holds.  The largest by its bits: as whole numbers infinities and NaN come out largest.
+template <bool SIGNED> __device__ __forceinline__ float block_scale(const float (&x)[kCodeLane], float inv_top) {
 #pragma clang fp contract(off)
   auto most = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-  auto bits = [](float v) { return SIGNED ? __float_as_uint(v) & 0x7fffffffu : __float_as_uint(v); };
-  uint32_t m = most(most(bits(x[0]), bits(x[1])), most(bits(x[2]), bits(x[3])));
-  m = uint32_t(wave_reduce_i(int(m), [&](int a, int b) { return int(most(uint32_t(a), uint32_t(b))); }));
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < kCodeLane; ++k) m = most(m, SIGNED ? __float_as_uint(x[k]) & 0x7fffffffu : __float_as_uint(x[k]));
+  m = most(m, uint32_t(dpp_move_i<0xB1>(int(m))));
+  m = most(m, uint32_t(dpp_move_i<0x4E>(int(m))));
+  m = most(m, uint32_t(dpp_move_i<0x141>(int(m))));
+  m = most(m, uint32_t(dpp_move_i<0x140>(int(m))));
+  const auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  m = most(r[0], r[1]);
   if (m >= 0x7f800000u) return __builtin_nanf("");
   const float s = __uint_as_float(m) * inv_top;
   return s >= 1.17549435e-38f ? s : 0.f;
 }
-// Codes of a block's moments, of which this lane has four.  The root that finds a code is an estimate from below, by more than its own error and by so little that
-// the next code is rarely the right one: a branch that few waves take.
+__device__ __forceinline__ float inverse_of(float scale) { return scale > 0.f ? 1.f / scale : 0.f; }
+// Codes of a block's moments, of which this lane has eight, in the form of aero.h but for what makes no difference:
+//   - the root that a code is found by is estimated from below (kBelow: by more than the estimate's own error, 2^-22), so that the next code may be the right one
+//     but the one before never is, and that rarely: a branch that few waves take;
+//   - a y above the top is not cut down to it first: it rounds to at most one code more, which is cut off at the end.
+// `random`: of which `shift` of the bits u is made.
 constexpr float kBelow = 1.f - 0x1p-21f;
-__device__ __forceinline__ uint32_t first_codes(const float (&x)[kPer], float inv, const float (&u)[kPer]) {
+template <int SHIFT> __device__ __forceinline__ float random_or_half(bool stochastic, uint32_t bits) {
+  return stochastic ? uniform16(bits >> SHIFT & 0xffff) : 0.5f;
+}
+__device__ __forceinline__ Codes first_codes(const float (&x)[kCodeLane], float inv, bool stochastic, const uint32_t (&bits)[kCodeLane]) {
 #pragma clang fp contract(off)
-  float y[kPer], c[kPer];
+  float c[kCodeLane], left[kCodeLane], step[kCodeLane];   // code, y - c^2 and (c + 1)^2 - c^2, both exact
+  const float below = inv * (kBelow * kBelow);
   bool more = false;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    y[k] = fminf(fabsf(x[k]) * inv, kTop1);
-    c[k] = floorf(__builtin_amdgcn_sqrtf(y[k]) * kBelow);
-    const float next = c[k] + 1.f;
-    more |= next * next <= y[k];
+  for (int k = 0; k < kCodeLane; ++k) {
+    const float y = fabsf(x[k]) * inv;
+    c[k] = floorf(__builtin_amdgcn_sqrtf(fabsf(x[k]) * below));
+    left[k] = fmaf(-c[k], c[k], y);
+    step[k] = fmaf(2.f, c[k], 1.f);
+    more |= left[k] >= step[k];
   }
   if (__builtin_amdgcn_ballot_w64(more) != 0) {
     asm volatile("" ::: "memory");   // stays a branch
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const float next = c[k] + 1.f;
-      if (next * next <= y[k]) c[k] = next;
+    for (int k = 0; k < kCodeLane; ++k) {
+      if (left[k] >= step[k]) {
+        left[k] -= step[k];
+        c[k] += 1.f;
+        step[k] += 2.f;
+      }
     }
   }
-  uint32_t w = 0;
+  Codes out{};
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if (u[k] * (2.f * c[k] + 1.f) < y[k] - c[k] * c[k]) c[k] += 1.f;
-    w |= (uint32_t(int(x[k] < 0.f ? -c[k] : c[k])) & 0xff) << (8 * k);
+  for (int k = 0; k < kCodeLane; ++k) {
+    const float next = c[k] + 1.f;
+    c[k] = fminf(random_or_half<0>(stochastic, bits[k]) * step[k] < left[k] ? next : c[k], 127.f);
+    out.w[k / 4] |= (uint32_t(int(copysignf(c[k], x[k]))) & 0xff) << (8 * (k % 4));
   }
-  return w;
+  return out;
 }
-__device__ __forceinline__ uint32_t second_codes(const float (&x)[kPer], float inv, const float (&u)[kPer]) {
+// root: about the roots of the moments, of which a step has made use already.
+__device__ __forceinline__ Codes second_codes(const float (&x)[kCodeLane], const float (&root)[kCodeLane], float inv, bool stochastic,
+                                              const uint32_t (&bits)[kCodeLane]) {
 #pragma clang fp contract(off)
-  float y[kPer], c[kPer], at[kPer], next[kPer];
+  float y[kCodeLane], c[kCodeLane], at[kCodeLane], next[kCodeLane];
+  const float below = __builtin_amdgcn_sqrtf(inv) * (kBelow * kBelow);
   bool more = false;
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    y[k] = fminf(x[k] * inv, kTop2);
-    c[k] = floorf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(y[k])) * kBelow);
+  for (int k = 0; k < kCodeLane; ++k) {
+    y[k] = x[k] * inv;
+    c[k] = floorf(__builtin_amdgcn_sqrtf(root[k] * below));
     at[k] = fourth(c[k]);
     next[k] = fourth(c[k] + 1.f);
     more |= next[k] <= y[k];
@@ -249,7 +300,7 @@ __device__ __forceinline__ uint32_t second_codes(const float (&x)[kPer], float i
   if (__builtin_amdgcn_ballot_w64(more) != 0) {
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
+    for (int k = 0; k < kCodeLane; ++k) {
       if (next[k] <= y[k]) {
         c[k] += 1.f;
         at[k] = next[k];
@@ -257,22 +308,15 @@ __device__ __forceinline__ uint32_t second_codes(const float (&x)[kPer], float i
       }
     }
   }
-  uint32_t w = 0;
+  Codes out{};
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    if (u[k] * (next[k] - at[k]) < y[k] - at[k]) c[k] += 1.f;
+  for (int k = 0; k < kCodeLane; ++k) {
+    if (random_or_half<16>(stochastic, bits[k]) * (next[k] - at[k]) < y[k] - at[k]) c[k] += 1.f;
     const float least = y[k] > 0.f ? 1.f : 0.f;   // a moment > 0 is not stored as 0
-    w |= uint32_t(__builtin_amdgcn_fmed3f(c[k], least, 255.f)) << (8 * k);
+    out.w[k / 4] |= uint32_t(__builtin_amdgcn_fmed3f(c[k], least, 255.f)) << (8 * (k % 4));
   }
-  return w;
+  return out;
 }
-
-__device__ __forceinline__ uint32_t mix(uint32_t x) {
-  x = (x ^ (x >> 16)) * 0x6A09E667u;
-  x = (x ^ (x >> 15)) * 0xBB67AE85u;
-  return x ^ (x >> 16);
-}
-__device__ __forceinline__ float uniform16(uint32_t low16) { return fmaf(float(low16), 0x1p-16f, 0x1p-17f); }   // exact
 
 // ---------------------------------------------------------------------------------- the step
 struct StepArgs {
@@ -295,130 +339,120 @@ __device__ __forceinline__ double power(double b, uint32_t t) {
   return r;
 }
 
-// What a lane has of an element group, as it is stored: to be widened when it is worked on, so that the loads of a group are under way together, and those of
-// the next one while this one is stepped.
+// What a lane has of a tensor, as it is stored until it is worked on, so that a wave's loads can be under way together.
 template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
-  static constexpr bool kOrdered = !SMALL && !ALONE;
   static constexpr bool kMaster = KIND == kMasterBF16 || KIND == kMasterF16;
   static constexpr int kStored = KIND == kParamF32 ? kF32 : KIND == kMasterF16 ? kF16 : kBF16, kRead = kMaster ? kF32 : kStored;
-  typename Four<GRAD>::raw g;
-  typename Four<kRead>::raw p;
-  Four<kF32>::raw m, v;       // 32-bit moments
-  uint32_t wm, wv;            // codes
+  static constexpr int N = SMALL ? kCodeLane : kWideLane;
+  static constexpr bool kOrdered = !SMALL && !ALONE;
+  Numbers<GRAD, N> g;
+  Numbers<kRead, N> p;
+  std::conditional_t<SMALL, Codes, Numbers<kF32, N>> m, v;
   float scale_m, scale_v;
 
-  __device__ __forceinline__ void load(const Tensor& e, uint64_t from, int lane, int have) {
-    const uint64_t i = from + lane * kPer;
-    g = Four<GRAD>::load(e.grad, i, have);
+  __device__ __forceinline__ void load(const Tensor& e, uint64_t i, int have) {
+    g.load(e.grad, i, have);
     arrived<kOrdered>();
-    if constexpr (kMaster) p = Four<kF32>::load(e.master, i, have);
-    else p = Four<kRead>::load(e.param, i, have);
+    p.load(kMaster ? reinterpret_cast<const char*>(e.master) : e.param, i, have);
     arrived<kOrdered>();
+    m.load(e.avg, i, have);
+    arrived<kOrdered>();
+    v.load(e.sq, i, have);
     if constexpr (SMALL) {
-      wm = load_codes(e.avg, i, have);
-      wv = load_codes(e.sq, i, have);
-      const bool in = from < uint64_t(e.n);
-      scale_m = in ? e.avg_scale[from / kBlock] : 0.f;
-      scale_v = in ? e.sq_scale[from / kBlock] : 0.f;
-    } else {
-      m = Four<kF32>::load(e.avg, i, have);
-      arrived<kOrdered>();
-      v = Four<kF32>::load(e.sq, i, have);
+      scale_m = have > 0 ? e.avg_scale[i / kBlock] : 0.f;
+      scale_v = have > 0 ? e.sq_scale[i / kBlock] : 0.f;
     }
   }
-  // The step of the group, and its results to where they belong.
-  __device__ __forceinline__ void step(const Tensor& e, const StepArgs& a, const StepScalars& s, uint64_t from, int lane, int have) const {
-    const uint64_t i = from + lane * kPer;
-    const float keep = float(s.weight_decay);
-    const uint32_t of_tensor = mix(s.of_step + uint32_t(e.ordinal));
-    float xg[kPer], xp[kPer], xm[kPer], xv[kPer];
-    Four<GRAD>::widen(g, xg);
-    Four<kRead>::widen(p, xp);
+  // The step, and its results to where they belong.
+  __device__ __forceinline__ void step(const Tensor& e, const StepArgs& a, const StepScalars& s, uint64_t i, int have) const {
+    const float keep = float(1.0 - s.weight_decay * double(e.decay));
+    float xg[N], xp[N], xm[N], xv[N], root[N];
+    g.widen(xg);
+    p.widen(xp);
     if constexpr (SMALL) {
-      decode4<true>(wm, scale_m, xm);
-      decode4<false>(wv, scale_v, xv);
+      decode<true>(m, scale_m, xm);
+      decode<false>(v, scale_v, xv);
     } else {
-      Four<kF32>::widen(m, xm);
-      Four<kF32>::widen(v, xv);
+      m.widen(xm);
+      v.widen(xv);
     }
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
+    for (int k = 0; k < N; ++k) {
       {
 #pragma clang fp contract(off)
         const float x = xg[k] * s.factor;
         xm[k] = xm[k] * a.beta1 + x * a.beta1c;
         xv[k] = xv[k] * a.beta2 + (x * x) * a.beta2c;
       }
-      const float away = fmaf(__builtin_amdgcn_sqrtf(xv[k]), s.by_second, a.eps);
+      root[k] = __builtin_amdgcn_sqrtf(xv[k]);
+      const float away = fmaf(root[k], s.by_second, a.eps);
       xp[k] = fmaf(xp[k], keep, -(xm[k] * s.by_first) * __builtin_amdgcn_rcpf(away));
     }
-    uint32_t bits[kPer];
+    uint32_t bits[N] = {};
     if ((SMALL || KIND == kParamBF16) && a.stochastic) {
+      const uint32_t of_tensor = mix(s.of_step + uint32_t(e.ordinal));
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) bits[k] = mix(of_tensor + uint32_t(i) + uint32_t(k));
+      for (int k = 0; k < N; ++k) bits[k] = mix(of_tensor + uint32_t(i) + uint32_t(k));
     }
     if constexpr (!SMALL) {
-      Four<kF32>::store(e.avg, i, have, xm);
+      Numbers<kF32, N>::store_rounded(e.avg, i, have, xm);
       arrived<kOrdered>();
-      Four<kF32>::store(e.sq, i, have, xv);
+      Numbers<kF32, N>::store_rounded(e.sq, i, have, xv);
       arrived<kOrdered>();
     }
     if constexpr (kMaster) {
-      Four<kF32>::store(e.master, i, have, xp);
+      Numbers<kF32, N>::store_rounded(e.master, i, have, xp);
       arrived<kOrdered>();
     }
     if (KIND == kParamBF16 && a.stochastic) {
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
+      for (int k = 0; k < N; ++k) {
         const uint32_t raw = __float_as_uint(xp[k]), up = (raw + (bits[k] * 0x9E3779B1u >> 16)) & 0xffff0000u;
         xp[k] = __uint_as_float(fabsf(xp[k]) < INFINITY ? up : raw);
       }
     }
-    Four<kStored>::store(e.param, i, have, xp);
+    Numbers<kStored, N>::store_rounded(e.param, i, have, xp);
     if constexpr (SMALL) {
       const float sm = block_scale<true>(xm, kInvTop1), sv = block_scale<false>(xv, kInvTop2);
-      const float im = sm > 0.f ? 1.f / sm : 0.f, iv = sv > 0.f ? 1.f / sv : 0.f;
-      float um[kPer], uv[kPer];
-#pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        um[k] = a.stochastic ? uniform16(bits[k] & 0xffff) : 0.5f;
-        uv[k] = a.stochastic ? uniform16(bits[k] >> 16) : 0.5f;
-      }
-      store_codes(e.avg, i, have, first_codes(xm, im, um));
-      store_codes(e.sq, i, have, second_codes(xv, iv, uv));
-      if (lane == 0 && have > 0) {
-        e.avg_scale[from / kBlock] = sm;
-        e.sq_scale[from / kBlock] = sv;
+      first_codes(xm, inverse_of(sm), a.stochastic, bits).store(e.avg, i, have);
+      second_codes(xv, root, inverse_of(sv), a.stochastic, bits).store(e.sq, i, have);
+      if (i % kBlock == 0 && have > 0) {
+        e.avg_scale[i / kBlock] = sm;
+        e.sq_scale[i / kBlock] = sv;
       }
     }
   }
 };
 
-// Where a wave's group of a unit is: units are the halves, quarters, ... of chunks that a workgroup takes at a time.  The table is read as constant memory, which
-// makes it scalar loads; stores that might be to it, for all the compiler knows, would have every pointer read again by vector loads behind them.
+// Where a workgroup's elements are: chunks hold one unit or several.  The table is read as constant memory, which makes it scalar loads; stores that might
+// be to it, for all the compiler knows, would have every pointer read again by vector loads behind them.
 struct Place {
   Tensor e;
-  uint64_t from;
-  bool full;   // the tensor has all of the workgroup's unit
+  uint64_t at;
 };
 template <class T> using Constant = const __attribute__((address_space(4))) T*;
 template <class T> __device__ __forceinline__ T constant_copy(const T* p) {
-  struct Words {
+  struct Raw {
     uint32_t w[sizeof(T) / 4];
-  } words;
+  } raw;
   const auto from = (Constant<uint32_t>)reinterpret_cast<uintptr_t>(p);
 #pragma unroll
-  for (size_t i = 0; i < sizeof(T) / 4; ++i) words.w[i] = from[i];
-  return __builtin_bit_cast(T, words);
+  for (size_t i = 0; i < sizeof(T) / 4; ++i) raw.w[i] = from[i];
+  return __builtin_bit_cast(T, raw);
 }
-__device__ __forceinline__ Place place_of(const void* table, int32_t count, uint32_t first, uint32_t unit, int wave) {
+template <int UNIT> __device__ __forceinline__ Place place_of(const void* table, int32_t count, uint32_t first, uint32_t unit) {
+  constexpr uint32_t kUnits = kChunk / UNIT;
   const uint32_t chunk = first + unit / kUnits;
   Place p;
   p.e = constant_copy(tensors_of(table) + constant_copy(map_of(table, count) + chunk));
-  const uint64_t at = uint64_t(chunk - p.e.first_chunk) * kChunk + unit % kUnits * kUnit;
-  p.from = at + uint64_t(wave) * kBlock;
-  p.full = at + kUnit <= uint64_t(p.e.n);
+  p.at = uint64_t(chunk - p.e.first_chunk) * kChunk + unit % kUnits * UNIT;
   return p;
+}
+// Calls f(element, how many of N the tensor has) for this thread's N elements of a unit; in a unit that is whole, N is a constant.
+template <int N, class F> __device__ __forceinline__ void with_elements(const Place& p, F f) {
+  const uint64_t i = p.at + threadIdx.x * N;
+  if (p.at + kOptNT * N <= uint64_t(p.e.n)) f(i, std::integral_constant<int, N>{});
+  else f(i, have_of<N>(p.e.n, i));
 }
 
 // Works out a step's scalars, counts it, and leaves them in the table for a launch of many workgroups.
@@ -434,9 +468,12 @@ __global__ void k_step_begin(StepArgs a) {
   if (fabsf(factor) < INFINITY) a.step[0] += 1;
 }
 
-// A workgroup steps 1024 elements and ends.  ALONE: it works the scalars out itself, and the last workgroup to end counts the step.
+// A workgroup steps four or eight elements a thread and ends: new ones follow in the order of addresses, which the memory serves better than workgroups that walk
+// on and drift apart (28 bytes an element in seven streams: 6.3 against 4.3 TB/s), and better still where a wave waits for each access before the next (kOrdered;
+// 5.9 without; the 8-bit form is not bound by memory).  ALONE: it works the scalars out itself, and the last workgroup to end counts the step.
 template <int KIND, int GRAD, bool SMALL, bool ALONE>
 __global__ __launch_bounds__(kOptNT) void k_adamw(StepArgs a) {
+  using H = Held<KIND, GRAD, SMALL, ALONE>;
   int step = 0;
   StepScalars s;
   if constexpr (ALONE) {
@@ -446,18 +483,12 @@ __global__ __launch_bounds__(kOptNT) void k_adamw(StepArgs a) {
     s = constant_copy<StepScalars>(&static_cast<const Table*>(a.table)->step);
   }
   if (!(fabsf(s.factor) < INFINITY)) return;   // uniform over the launch
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const Place p = place_of(a.table, a.count, a.first, a.first_unit + blockIdx.x, wave);
-  s.weight_decay = 1.0 - s.weight_decay * double(p.e.decay);
-  Held<KIND, GRAD, SMALL, ALONE> h;
-  if (p.full) {
-    h.load(p.e, p.from, lane, kPer);
-    h.step(p.e, a, s, p.from, lane, kPer);
-  } else {
-    const int have = have_of(p.e.n, p.from + lane * kPer);
-    h.load(p.e, p.from, lane, have);
-    h.step(p.e, a, s, p.from, lane, have);
-  }
+  const Place p = place_of<kOptNT * H::N>(a.table, a.count, a.first, a.first_unit + blockIdx.x);
+  with_elements<H::N>(p, [&](uint64_t i, int have) {
+    H h;
+    h.load(p.e, i, have);
+    h.step(p.e, a, s, i, have);
+  });
   if constexpr (ALONE) {
     __syncthreads();   // every wave of this workgroup has read the step by now
     if (threadIdx.x == 0) {
@@ -492,86 +523,49 @@ static StepKernel step_kernel(int cls, bool alone) {
 constexpr uint32_t kAloneUnits = 1024;
 
 // ---------------------------------------------------------------------------------- moments as numbers
-template <bool SMALL> struct HeldMoments {
-  Four<kF32>::raw m, v;
-  uint32_t wm, wv;
-  float scale_m, scale_v;
-  __device__ __forceinline__ void load(const Tensor& e, uint64_t from, int lane, int have) {
-    const uint64_t i = from + lane * kPer;
-    if constexpr (SMALL) {
-      wm = load_codes(e.avg, i, have);
-      wv = load_codes(e.sq, i, have);
-      const bool in = from < uint64_t(e.n);
-      scale_m = in ? e.avg_scale[from / kBlock] : 0.f;
-      scale_v = in ? e.sq_scale[from / kBlock] : 0.f;
-    } else {
-      m = Four<kF32>::load(e.avg, i, have);
-      v = Four<kF32>::load(e.sq, i, have);
-    }
-  }
-  template <int DT> __device__ __forceinline__ void store(void* avg, void* sq, uint64_t i, int have) const {
-    float xm[kPer], xv[kPer];
-    if constexpr (SMALL) {
-      decode4<true>(wm, scale_m, xm);
-      decode4<false>(wv, scale_v, xv);
-    } else {
-      Four<kF32>::widen(m, xm);
-      Four<kF32>::widen(v, xv);
-    }
-    Four<DT>::store(avg, i, have, xm);
-    Four<DT>::store(sq, i, have, xv);
-  }
-};
 template <bool SMALL, int DT>
-__global__ __launch_bounds__(kOptNT) void k_moments(void* table, int32_t count, uint32_t first, void* avg, void* sq) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  {
-    HeldMoments<SMALL> h[kUnits];
-    const Place p = place_of(table, count, first, blockIdx.x * kUnits, wave);
-    const bool full = p.from - uint64_t(wave) * kBlock + kChunk <= uint64_t(p.e.n);
-    const auto all = [&](auto have) {
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u) h[u].load(p.e, p.from + u * kUnit, lane, have(p.from + u * kUnit + lane * kPer));
-#pragma unroll
-      for (int u = 0; u < kUnits; ++u)
-        h[u].template store<DT>(avg, sq, uint64_t(p.e.out) + p.from + u * kUnit + lane * kPer, have(p.from + u * kUnit + lane * kPer));
-    };
-    if (full) all([](uint64_t) { return kPer; });
-    else all([&](uint64_t i) { return have_of(p.e.n, i); });
-  }
+__global__ __launch_bounds__(kOptNT) void k_moments(void* table, int32_t count, uint32_t first, uint32_t first_unit, void* avg, void* sq) {
+  constexpr int N = SMALL ? kCodeLane : kWideLane;
+  const Place p = place_of<kOptNT * N>(table, count, first, first_unit + blockIdx.x);
+  const Tensor& e = p.e;
+  with_elements<N>(p, [&](uint64_t i, int have) {
+    std::conditional_t<SMALL, Codes, Numbers<kF32, N>> m, v;
+    float xm[N], xv[N];
+    m.load(e.avg, i, have);
+    v.load(e.sq, i, have);
+    if constexpr (SMALL) {
+      const float scale_m = have > 0 ? e.avg_scale[i / kBlock] : 0.f, scale_v = have > 0 ? e.sq_scale[i / kBlock] : 0.f;
+      decode<true>(m, scale_m, xm);
+      decode<false>(v, scale_v, xv);
+    } else {
+      m.widen(xm);
+      v.widen(xv);
+    }
+    Numbers<DT, N>::store_rounded(avg, uint64_t(e.out) + i, have, xm);
+    Numbers<DT, N>::store_rounded(sq, uint64_t(e.out) + i, have, xv);
+  });
 }
 
 // ---------------------------------------------------------------------------------- norm
 constexpr int kNormMax = 2048;   // workgroups
-template <int DT, class Have> __device__ __forceinline__ void add_squares(const Place& p, int lane, Have have, double& sum) {
-  typename Four<DT>::raw g[kUnits];
+template <int DT> __device__ __forceinline__ double squares(const Place& p) {
+  double sum = 0.0;
+  with_elements<kCodeLane>(p, [&](uint64_t i, int have) {
+    Numbers<DT, kCodeLane> g;
+    float x[kCodeLane];
+    g.load(p.e.grad, i, have);
+    g.widen(x);
 #pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    const uint64_t i = p.from + u * kUnit + lane * kPer;
-    g[u] = Four<DT>::load(p.e.grad, i, have(i));
-  }
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    float x[kPer];
-    Four<DT>::widen(g[u], x);
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) sum = fma(double(x[k]), double(x[k]), sum);
-  }
+    for (int k = 0; k < kCodeLane; ++k) sum = fma(double(x[k]), double(x[k]), sum);
+  });
+  return sum;
 }
 __global__ __launch_bounds__(kOptNT) void k_norm_parts(const void* table, int32_t count, uint32_t chunks, double* __restrict__ part) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   double sum = 0.0;
   for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Place p = place_of(table, count, 0, c * kUnits, wave);
-    const bool full = p.from - uint64_t(wave) * kBlock + kChunk <= uint64_t(p.e.n);
+    const Place p = place_of<kChunk>(table, count, 0, c);
     const int grad = p.e.kind / 2 % kGrads;
-    const auto add = [&](auto have) {
-      if (grad == 0) add_squares<kF32>(p, lane, have, sum);
-      else if (grad == 1) add_squares<kBF16>(p, lane, have, sum);
-      else add_squares<kF16>(p, lane, have, sum);
-    };
-    if (full) add([](uint64_t) { return kPer; });
-    else add([&](uint64_t i) { return have_of(p.e.n, i); });
+    sum += grad == 0 ? squares<kF32>(p) : grad == 1 ? squares<kBF16>(p) : squares<kF16>(p);
   }
   sum = wave_sum_d(sum);
   __shared__ double s_sum[kOptNT / kWave];
@@ -601,7 +595,18 @@ __global__ __launch_bounds__(kOptNT) void k_norm_end(const double* __restrict__ 
   factor[0] = float(f);
 }
 
+// Launches over the classes that have parameters, a workgroup to a unit: launch(class, its first unit, how many).
+constexpr int kFirstClass = class_of(kParamF32, 0, 0);
 constexpr uint32_t kMostUnits = (1u << 24) - 1;   // workgroups of 256 threads that a launch has at most
+static uint64_t units_of(const Table* t, int k) {
+  return uint64_t(t->class_first[k + 1] - t->class_first[k]) * (kChunk / (kOptNT * (k % 2 ? kCodeLane : kWideLane)));
+}
+template <class Launch> static void for_classes(const Table* t, Launch launch) {
+  for (int k = kFirstClass; k < kClasses; ++k) {
+    const uint64_t units = units_of(t, k);
+    for (uint64_t from = 0; from < units; from += kMostUnits) launch(k, uint32_t(from), unsigned(units - from < kMostUnits ? units - from : kMostUnits));
+  }
+}
 
 size_t grad_norm_workspace_bytes() { return kNormMax * sizeof(double); }
 
@@ -634,7 +639,7 @@ extern "C" aero_status aero_tensor_table(const aero_tensor* list, int32_t count,
     chunks += chunks_of(list[k]);
     of_class[class_of(list[k])] += chunks_of(list[k]);
   }
-  if (chunks * kUnits >= (uint64_t(1) << 31)) return AERO_ERR_SHAPE;
+  if (chunks >= (uint64_t(1) << 30)) return AERO_ERR_SHAPE;   // units of half a chunk count in 32 bits
   const size_t bytes = aero_tensor_table_bytes(list, count);
   if (image_bytes < bytes) return AERO_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(image) % 16 != 0) return AERO_ERR_ALIGN;
@@ -711,30 +716,25 @@ extern "C" aero_status aero_adamw_step(const void* image, void* table, const aer
   a.step = step;
   a.factor = factor;
   a.lr_factor = lr_factor;
-  constexpr int kFirst = class_of(kParamF32, 0, 0);
   int classes = 0, only = 0;
-  for (int k = kFirst; k < kClasses; ++k) {
+  for (int k = kFirstClass; k < kClasses; ++k) {
     if (t->class_first[k + 1] > t->class_first[k]) {
       ++classes;
       only = k;
     }
   }
-  const uint64_t units = uint64_t(t->class_first[kClasses] - t->class_first[kFirst]) * kUnits;
-  if (classes == 1 && units <= kAloneUnits) {
+  const uint64_t alone = classes == 1 ? units_of(t, only) : 0;
+  if (alone > 0 && alone <= kAloneUnits) {
     a.first = t->class_first[only];
-    hipLaunchKernelGGL(step_kernel(only, true), dim3(unsigned(units)), dim3(kOptNT), 0, s, a);
+    hipLaunchKernelGGL(step_kernel(only, true), dim3(unsigned(alone)), dim3(kOptNT), 0, s, a);
     return launch_status();
   }
   hipLaunchKernelGGL(k_step_begin, dim3(1), dim3(1), 0, s, a);
-  for (int k = kFirst; k < kClasses; ++k) {
-    const uint64_t of_class = uint64_t(t->class_first[k + 1] - t->class_first[k]) * kUnits;
+  for_classes(t, [&](int k, uint32_t first_unit, unsigned n) {
     a.first = t->class_first[k];
-    for (uint64_t from = 0; from < of_class; from += kMostUnits) {
-      const uint64_t n = of_class - from < kMostUnits ? of_class - from : kMostUnits;
-      a.first_unit = uint32_t(from);
-      hipLaunchKernelGGL(step_kernel(k, false), dim3(unsigned(n)), dim3(kOptNT), 0, s, a);
-    }
-  }
+    a.first_unit = first_unit;
+    hipLaunchKernelGGL(step_kernel(k, false), dim3(n), dim3(kOptNT), 0, s, a);
+  });
   return launch_status();
 }
 
@@ -744,21 +744,15 @@ extern "C" aero_status aero_adamw_moments(const void* image, void* table, int32_
   const Table* t = table_of(image);
   if (!t) return AERO_ERR_SHAPE;
   if (dtype != AERO_F32 && dtype != AERO_BF16) return AERO_ERR_DTYPE;
-  const uint32_t params = t->class_first[class_of(kParamF32, 0, 0)];
-  if (t->chunks == params) return AERO_OK;
+  if (t->chunks == t->class_first[kFirstClass]) return AERO_OK;
   if (!avg || !avg_sq) return AERO_ERR_NULL;
   const uintptr_t both = reinterpret_cast<uintptr_t>(avg) | reinterpret_cast<uintptr_t>(avg_sq);
   if (both % storage_bytes(dtype) != 0 || reinterpret_cast<uintptr_t>(table) % 16 != 0) return AERO_ERR_ALIGN;
   hipStream_t s = as_stream(stream);
-  for (int k = class_of(kParamF32, 0, 0); k < kClasses; ++k) {
-    const uint32_t first = t->class_first[k], chunks = t->class_first[k + 1] - first;
-    if (chunks == 0) continue;
+  for_classes(t, [&](int k, uint32_t first_unit, unsigned n) {
     const auto kernel = k % 2 ? (dtype == AERO_F32 ? k_moments<true, kF32> : k_moments<true, kBF16>)
                               : (dtype == AERO_F32 ? k_moments<false, kF32> : k_moments<false, kBF16>);
-    for (uint32_t from = 0; from < chunks; from += kMostUnits) {
-      const unsigned n = unsigned(chunks - from < kMostUnits ? chunks - from : kMostUnits);
-      hipLaunchKernelGGL(kernel, dim3(n), dim3(kOptNT), 0, s, table, t->count, first + from, avg, avg_sq);
-    }
-  }
+    hipLaunchKernelGGL(kernel, dim3(n), dim3(kOptNT), 0, s, table, t->count, t->class_first[k], first_unit, avg, avg_sq);
+  });
   return launch_status();
 }
