@@ -239,7 +239,11 @@ template <bool SIGNED> __device__ __forceinline__ float block_scale(const float 
   const float s = __uint_as_float(m) * inv_top;
   return s >= 1.17549435e-38f ? s : 0.f;
 }
-__device__ __forceinline__ float inverse_of(float scale) { return scale > 0.f ? 1.f / scale : 0.f; }
+// 1 / scale rounded once: the estimate is off by a unit at most, and one step with the exact remainder leaves none of it (for every mantissa, tried out).
+__device__ __forceinline__ float inverse_of(float scale) {
+  const float r = __builtin_amdgcn_rcpf(scale);
+  return scale > 0.f ? fmaf(fmaf(-scale, r, 1.f), r, r) : 0.f;
+}
 // Codes of a block's moments, of which this lane has eight, in the form of aero.h but for what makes no difference:
 //   - the root that a code is found by is estimated from below (kBelow: by more than the estimate's own error, 2^-22), so that the next code may be the right one
 //     but the one before never is, and that rarely: a branch that few waves take;
@@ -277,7 +281,7 @@ __device__ __forceinline__ Codes first_codes(const float (&x)[kCodeLane], float 
 #pragma unroll
   for (int k = 0; k < kCodeLane; ++k) {
     const float next = c[k] + 1.f;
-    c[k] = fminf(random_or_half<0>(stochastic, bits[k]) * step[k] < left[k] ? next : c[k], 127.f);
+    c[k] = __builtin_amdgcn_fmed3f(random_or_half<0>(stochastic, bits[k]) * step[k] < left[k] ? next : c[k], 0.f, 127.f);
     out.w[k / 4] |= (uint32_t(int(copysignf(c[k], x[k]))) & 0xff) << (8 * (k % 4));
   }
   return out;
@@ -286,15 +290,16 @@ __device__ __forceinline__ Codes first_codes(const float (&x)[kCodeLane], float 
 __device__ __forceinline__ Codes second_codes(const float (&x)[kCodeLane], const float (&root)[kCodeLane], float inv, bool stochastic,
                                               const uint32_t (&bits)[kCodeLane]) {
 #pragma clang fp contract(off)
-  float y[kCodeLane], c[kCodeLane], at[kCodeLane], next[kCodeLane];
+  float y[kCodeLane], c[kCodeLane], more_c[kCodeLane], at[kCodeLane], next[kCodeLane];   // code and the next one, what they stand for
   const float below = __builtin_amdgcn_sqrtf(inv) * (kBelow * kBelow);
   bool more = false;
 #pragma unroll
   for (int k = 0; k < kCodeLane; ++k) {
     y[k] = x[k] * inv;
     c[k] = floorf(__builtin_amdgcn_sqrtf(root[k] * below));
+    more_c[k] = c[k] + 1.f;
     at[k] = fourth(c[k]);
-    next[k] = fourth(c[k] + 1.f);
+    next[k] = fourth(more_c[k]);
     more |= next[k] <= y[k];
   }
   if (__builtin_amdgcn_ballot_w64(more) != 0) {
@@ -302,18 +307,19 @@ __device__ __forceinline__ Codes second_codes(const float (&x)[kCodeLane], const
 #pragma unroll
     for (int k = 0; k < kCodeLane; ++k) {
       if (next[k] <= y[k]) {
-        c[k] += 1.f;
+        c[k] = more_c[k];
         at[k] = next[k];
-        next[k] = fourth(c[k] + 1.f);
+        more_c[k] += 1.f;
+        next[k] = fourth(more_c[k]);
       }
     }
   }
   Codes out{};
 #pragma unroll
   for (int k = 0; k < kCodeLane; ++k) {
-    if (random_or_half<16>(stochastic, bits[k]) * (next[k] - at[k]) < y[k] - at[k]) c[k] += 1.f;
+    const float code = random_or_half<16>(stochastic, bits[k]) * (next[k] - at[k]) < y[k] - at[k] ? more_c[k] : c[k];
     const float least = y[k] > 0.f ? 1.f : 0.f;   // a moment > 0 is not stored as 0
-    out.w[k / 4] |= uint32_t(__builtin_amdgcn_fmed3f(c[k], least, 255.f)) << (8 * (k % 4));
+    out.w[k / 4] |= uint32_t(__builtin_amdgcn_fmed3f(code, least, 255.f)) << (8 * (k % 4));
   }
   return out;
 }
@@ -408,7 +414,7 @@ template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const uint32_t raw = __float_as_uint(xp[k]), up = (raw + (bits[k] * 0x9E3779B1u >> 16)) & 0xffff0000u;
-        xp[k] = __uint_as_float(fabsf(xp[k]) < INFINITY ? up : raw);
+        xp[k] = __uint_as_float(xp[k] == xp[k] ? up : raw);   // the sum leaves infinities what they are, but might carry a NaN beyond
       }
     }
     Numbers<kStored, N>::store_rounded(e.param, i, have, xp);
