@@ -337,14 +337,6 @@ struct StepArgs {
   const float *factor, *lr_factor;
 };
 
-// b^t for a whole t >= 1.
-__device__ __forceinline__ double power(double b, uint32_t t) {
-  double r = 1.0;
-  for (; t; t >>= 1, b *= b)
-    if (t & 1) r *= b;
-  return r;
-}
-
 // What a lane has of a tensor, as it is stored until it is worked on, so that a wave's loads can be under way together.
 template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
   static constexpr bool kMaster = KIND == kMasterBF16 || KIND == kMasterF16;
@@ -461,17 +453,26 @@ template <int N, class F> __device__ __forceinline__ void with_elements(const Pl
   else f(i, have_of<N>(p.e.n, i));
 }
 
-// Works out a step's scalars, counts it, and leaves them in the table for a launch of many workgroups.
-__device__ __forceinline__ StepScalars step_scalars(const StepArgs& a, float factor, int step) {
-  const uint32_t t = uint32_t(step) + 1;
+// A step's scalars: the two powers and quotients by two lanes at once.
+__device__ __forceinline__ StepScalars step_scalars(const StepArgs& a) {
+  const float factor = a.factor ? a.factor[0] : 1.f;
+  const int step = a.step[0];
   const double rate = a.lr * (a.lr_factor ? double(a.lr_factor[0]) : 1.0);
-  return StepScalars{factor, float(rate / (1.0 - power(a.dbeta1, t))), float(1.0 / sqrt(1.0 - power(a.dbeta2, t))),
+  const bool first = threadIdx.x % 2 == 0;
+  double by = first ? a.dbeta1 : a.dbeta2, power = 1.0;   // beta^t for t = step + 1
+  for (uint32_t t = uint32_t(step) + 1; t; t >>= 1, by *= by)
+    if (t & 1) power *= by;
+  const double under = first ? 1.0 - power : sqrt(1.0 - power);
+  const int quotient = __float_as_int(float((first ? rate : 1.0) / under));
+  return StepScalars{factor, __int_as_float(__builtin_amdgcn_readlane(quotient, 0)), __int_as_float(__builtin_amdgcn_readlane(quotient, 1)),
                      mix(a.seed_lo ^ mix(a.seed_hi ^ mix(uint32_t(step)))), rate * a.weight_decay};
 }
-__global__ void k_step_begin(StepArgs a) {
-  const float factor = a.factor ? a.factor[0] : 1.f;
-  static_cast<Table*>(a.table)->step = step_scalars(a, factor, a.step[0]);
-  if (fabsf(factor) < INFINITY) a.step[0] += 1;
+// In front of a launch of many workgroups: leaves the scalars in the table and counts the step.
+__global__ __launch_bounds__(kWave) void k_step_begin(StepArgs a) {
+  const StepScalars s = step_scalars(a);
+  if (threadIdx.x != 0) return;
+  static_cast<Table*>(a.table)->step = s;
+  if (fabsf(s.factor) < INFINITY) a.step[0] += 1;
 }
 
 // A workgroup steps four or eight elements a thread and ends: new ones follow in the order of addresses, which the memory serves better than workgroups that walk
@@ -480,28 +481,26 @@ __global__ void k_step_begin(StepArgs a) {
 template <int KIND, int GRAD, bool SMALL, bool ALONE>
 __global__ __launch_bounds__(kOptNT) void k_adamw(StepArgs a) {
   using H = Held<KIND, GRAD, SMALL, ALONE>;
-  int step = 0;
   StepScalars s;
-  if constexpr (ALONE) {
-    step = a.step[0];
-    s = step_scalars(a, a.factor ? a.factor[0] : 1.f, step);
-  } else {
+  if constexpr (!ALONE) {
     s = constant_copy<StepScalars>(&static_cast<const Table*>(a.table)->step);
+    if (!(fabsf(s.factor) < INFINITY)) return;   // uniform over the launch
   }
-  if (!(fabsf(s.factor) < INFINITY)) return;   // uniform over the launch
   const Place p = place_of<kOptNT * H::N>(a.table, a.count, a.first, a.first_unit + blockIdx.x);
   with_elements<H::N>(p, [&](uint64_t i, int have) {
     H h;
     h.load(p.e, i, have);
-    h.step(p.e, a, s, i, have);
+    if constexpr (ALONE) s = step_scalars(a);   // while the loads are under way
+    if (!ALONE || fabsf(s.factor) < INFINITY) h.step(p.e, a, s, i, have);
   });
   if constexpr (ALONE) {
+    if (!(fabsf(s.factor) < INFINITY)) return;
     __syncthreads();   // every wave of this workgroup has read the step by now
     if (threadIdx.x == 0) {
       uint32_t* ticket = &static_cast<Table*>(a.table)->ticket;
       if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
         *ticket = 0;
-        a.step[0] = step + 1;
+        a.step[0] += 1;
       }
     }
   }
@@ -735,7 +734,7 @@ extern "C" aero_status aero_adamw_step(const void* image, void* table, const aer
     hipLaunchKernelGGL(step_kernel(only, true), dim3(unsigned(alone)), dim3(kOptNT), 0, s, a);
     return launch_status();
   }
-  hipLaunchKernelGGL(k_step_begin, dim3(1), dim3(1), 0, s, a);
+  hipLaunchKernelGGL(k_step_begin, dim3(1), dim3(kWave), 0, s, a);
   for_classes(t, [&](int k, uint32_t first_unit, unsigned n) {
     a.first = t->class_first[k];
     a.first_unit = first_unit;
