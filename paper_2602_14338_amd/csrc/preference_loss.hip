@@ -81,34 +81,33 @@ struct PairLoss {
   int32_t* err_flag;
 };
 
-// What a row leaves for the steps behind it, and what they make of it for its gradient.
+// What a row leaves for the steps behind it.
 struct RowRecord {
-  int32_t rollout;   // AERO_ROW_PADDING, AERO_ROW_UNTOUCHED: takes no part   ->  gradient by the log-prob (-0: not to be written)
-  float d;           // logprob - ref                                          ->  factor of the row's exponentials
+  int32_t rollout;   // AERO_ROW_PADDING, AERO_ROW_UNTOUCHED: takes no part
+  float d;           // logprob - ref
   float offset;      // of the row's exponentials, in powers of two
   float inv;         // 1 / their sum
 };
-struct GradRecord {
-  float g, k, offset;
-  int32_t y;
-};
-static_assert(sizeof(RowRecord) == 16 && sizeof(GradRecord) == 16, "one takes the other's place");
+static_assert(sizeof(RowRecord) == 16, "one scalar load");
 
 struct PairWorkspace {
   ExactSum *ratio, *slope;   // [R]
   double* part;              // [ceil(P / 64)] of the loss
+  float* gradient;           // [R] of a rollout's log-probs, times grad_scale
   RowRecord* rows;           // [T]
 };
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 static PairWorkspace carve(void* ws, int64_t T, int32_t R, int32_t P, size_t* bytes) {
   char* p = static_cast<char*>(ws);
   PairWorkspace w;
-  const size_t sums = up256(size_t(R) * 2 * sizeof(ExactSum)), part = up256((size_t(P) + 63) / 64 * 8), rows = up256(size_t(T) * 16);
+  const size_t sums = up256(size_t(R) * 2 * sizeof(ExactSum)), part = up256((size_t(P) + 63) / 64 * 8);
+  const size_t gradient = T > 0 ? up256(size_t(R) * 4) : 0, rows = up256(size_t(T) * sizeof(RowRecord));
   w.ratio = reinterpret_cast<ExactSum*>(p);
   w.slope = w.ratio + R;
   w.part = reinterpret_cast<double*>(p + sums);
-  w.rows = reinterpret_cast<RowRecord*>(p + sums + part);
-  if (bytes) *bytes = sums + part + rows;
+  w.gradient = reinterpret_cast<float*>(p + sums + part);
+  w.rows = reinterpret_cast<RowRecord*>(p + sums + part + gradient);
+  if (bytes) *bytes = sums + part + gradient + rows;
   return w;
 }
 size_t preference_workspace_bytes(int64_t T, int32_t R, int32_t P, bool rows) {
@@ -119,6 +118,14 @@ size_t preference_workspace_bytes(int64_t T, int32_t R, int32_t P, bool rows) {
 }
 
 // ---------------------------------------------------------------------------------- a pair
+// ln(1 + x), 0 <= x <= 1: 2 artanh s with s = x / (2 + x) <= 1/3, to 1e-10 of itself behind s^18 / 19.
+__device__ __forceinline__ double log_1_and(double x) {
+  const double s = x / (2.0 + x), q = s * s;
+  double y = 1.0 / 17;
+#pragma unroll
+  for (int n = 15; n > 0; n -= 2) y = fma(y, q, 1.0 / n);
+  return 2.0 * s * y;
+}
 struct PairTerm {
   double value, slope;
 };
@@ -132,7 +139,7 @@ __device__ __forceinline__ PairTerm pair_term(const PairLoss& a, double x) {
     return PairTerm{u * u, 2.0 * u / double(a.beta)};
   }
   if (x != x) return PairTerm{x, x};
-  const double e = double(a.smoothing), away = exp(-fabs(x)), low = log1p(away);
+  const double e = double(a.smoothing), away = exp_of(-fmin(fabs(x), 700.0)), low = log_1_and(away);
   double value = (1.0 - e) * (x < 0.0 ? -x + low : low);
   if (e != 0.0) value += e * (x > 0.0 ? x + low : low);
   const double sigma = x > 0.0 ? away / (1.0 + away) : 1.0 / (1.0 + away);   // of -x
@@ -149,10 +156,17 @@ __device__ __forceinline__ float slope_of(const PairLoss& a, const ExactSum& slo
   return float(a.average && count > 1 ? v / double(count) : v);
 }
 
+struct Pair {
+  int c, j;
+  float w;
+};
+__device__ __forceinline__ Pair pair_at(const PairLoss& a, int p) {
+  return p < a.P ? Pair{a.chosen[p], a.rejected[p], a.weight ? a.weight[p] : 1.f / float(a.P)} : Pair{-1, -1, 0.f};
+}
 // One pair: its share goes to its rollouts' slopes, its term is returned.
-__device__ __forceinline__ double pair_step(const PairLoss& a, int p, const ExactSum* ratio, ExactSum* slope) {
-  const int c = a.chosen[p], j = a.rejected[p];
-  const float w = a.weight ? a.weight[p] : 1.f / float(a.P);
+__device__ __forceinline__ double pair_step(const PairLoss& a, int p, const Pair& pair, const ExactSum* ratio, ExactSum* slope) {
+  const int c = pair.c, j = pair.j;
+  const float w = pair.w;
   double term = 0.0, m = 0.0;
   if (c >= 0 && j >= 0 && (c >= a.R || j >= a.R)) {
     if (a.err_flag) atomicOr(a.err_flag, AERO_DERR_BAD_ROLLOUT);
@@ -192,7 +206,7 @@ struct TokenSums {
   __device__ __forceinline__ void add(int r, float d) {   // r < 0: no token
     uint64_t left = __ballot(r >= 0);
     if (left == 0) return;
-    const int first = __shfl(r, __ffsll((unsigned long long)left) - 1, kWave);
+    const int first = __builtin_amdgcn_readlane(r, __builtin_ctzll(left));
     if (__ballot(r == first) == left) {
       if (first != rollout) {
         flush();
@@ -204,7 +218,7 @@ struct TokenSums {
     }
     flush();
     for (int turn = 0; turn < 4 && left; ++turn) {
-      const int one = __shfl(r, __ffsll((unsigned long long)left) - 1, kWave);
+      const int one = __builtin_amdgcn_readlane(r, __builtin_ctzll(left));
       const uint64_t same = __ballot(r == one);
       put(one, wave_sum_d(r == one ? double(d) : 0.0), __popcll(same));
       left &= ~same;
@@ -227,27 +241,24 @@ __device__ __forceinline__ void token_at(const Tokens& k, int64_t t, int R, int3
   d = 0.f;
   if (t >= k.T) return;
   r = k.rollout[t];
-  if (r >= R) {
-    if (err_flag) atomicOr(err_flag, AERO_DERR_BAD_ROLLOUT);
+  d = k.logprob[t] - (k.ref ? k.ref[t] : 0.f);   // asked for with the index; no use is made of it where that says so
+  if (r >= R && err_flag) atomicOr(err_flag, AERO_DERR_BAD_ROLLOUT);
+  if (r < 0 || r >= R) {
     r = -1;
+    d = 0.f;
   }
-  if (r < 0) {
-    r = -1;
-    return;
-  }
-  d = k.logprob[t] - (k.ref ? k.ref[t] : 0.f);
 }
 
-constexpr int kTokenRounds = 16, kTokenNT = 256;
+constexpr int kTokenRounds = 8, kTokenNT = 256;
 __global__ __launch_bounds__(kTokenNT) void k_pair_tokens(Tokens k, PairLoss a, ExactSum* ratio) {
-  const int wave = blockIdx.x * (kTokenNT / kWave) + threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int64_t from = (int64_t(blockIdx.x) * kTokenNT + threadIdx.x / kWave * kWave) * kTokenRounds + threadIdx.x % kWave;
+  int r[kTokenRounds];
+  float d[kTokenRounds];
+#pragma unroll
+  for (int u = 0; u < kTokenRounds; ++u) token_at(k, from + u * kWave, a.R, a.err_flag, r[u], d[u]);
   TokenSums sums{ratio, -1, 0.0, 0};
-  for (int u = 0; u < kTokenRounds; ++u) {
-    int r;
-    float d;
-    token_at(k, (int64_t(wave) * kTokenRounds + u) * kWave + lane, a.R, a.err_flag, r, d);
-    sums.add(r, d);
-  }
+#pragma unroll
+  for (int u = 0; u < kTokenRounds; ++u) sums.add(r[u], d[u]);
   sums.flush();
 }
 
@@ -258,30 +269,19 @@ __global__ __launch_bounds__(256) void k_pair_clear(u32x4_t* p, int64_t n) {
 
 __global__ __launch_bounds__(256) void k_pair_terms(PairLoss a, const ExactSum* __restrict__ ratio, ExactSum* slope, double* __restrict__ part) {
   const int p = blockIdx.x * 256 + threadIdx.x;
-  const double term = wave_sum_d(p < a.P ? pair_step(a, p, ratio, slope) : 0.0);
+  const double term = wave_sum_d(p < a.P ? pair_step(a, p, pair_at(a, p), ratio, slope) : 0.0);
   if (threadIdx.x % kWave == 0 && p < a.P) part[p / kWave] = term;
 }
 
-// What a row's gradient is made with.
-__device__ __forceinline__ GradRecord grad_record(const RowRecord& row, int y, float slope, float grad_scale) {
-  float g = row.rollout >= 0 ? slope * grad_scale : 0.f;
-  if (g == 0.f) g = row.rollout == AERO_ROW_UNTOUCHED ? -0.f : 0.f;
-  return GradRecord{g, -g * row.inv, row.offset, y};
-}
-
-// The rollouts' outputs and the rows' records; the first workgroup adds up the loss.
+// The rollouts' outputs (gradient: NULL without logits); the first workgroup adds up the loss.
 __global__ __launch_bounds__(256) void k_pair_finish(PairLoss a, const ExactSum* __restrict__ ratio, const ExactSum* __restrict__ slope,
-                                                     const double* __restrict__ part, RowRecord* rows, const int32_t* __restrict__ targets,
-                                                     int64_t T, float grad_scale) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (i < a.R) {
-    if (a.rollout_ratio) a.rollout_ratio[i] = float(ratio_of(a, ratio[i]));
-    if (a.drollout) a.drollout[i] = slope_of(a, slope[i], ratio[i].count);
-  }
-  if (rows && i < T) {
-    const RowRecord row = rows[i];
-    const float d = row.rollout >= 0 ? slope_of(a, slope[row.rollout], ratio[row.rollout].count) : 0.f;
-    reinterpret_cast<GradRecord*>(rows)[i] = grad_record(row, targets[i], d, grad_scale);
+                                                     const double* __restrict__ part, float* __restrict__ gradient, float grad_scale) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r < a.R) {
+    const float d = slope_of(a, slope[r], ratio[r].count);
+    if (a.rollout_ratio) a.rollout_ratio[r] = float(ratio_of(a, ratio[r]));
+    if (a.drollout) a.drollout[r] = d;
+    if (gradient) gradient[r] = d * grad_scale;
   }
   if (blockIdx.x != 0) return;
   __shared__ double s_part[4];
@@ -298,10 +298,33 @@ __global__ __launch_bounds__(256) void k_pair_finish(PairLoss a, const ExactSum*
 constexpr int kSmallNT = 1024, kSmallR = 256, kSmallP = 4096;
 constexpr int64_t kSmallT = 16384;
 template <bool ROWS>
-__global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, RowRecord* rows, const int32_t* __restrict__ targets, float grad_scale) {
+__global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, const RowRecord* __restrict__ rows, float* __restrict__ gradient,
+                                                         float grad_scale) {
+  constexpr int kAhead = 8;
   __shared__ ExactSum s_ratio[kSmallR], s_slope[kSmallR];
   __shared__ double s_part[kSmallNT / kWave];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  // each wave takes tokens that stand together, in as many rounds as it takes
+  const int64_t rounds = (k.T + kSmallNT - 1) / kSmallNT, from = wave * rounds * kWave + lane, end = min(k.T, (wave + 1) * rounds * kWave);
+  int r[kAhead];
+  float d[kAhead];
+  const auto load = [&](int64_t round) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t t = from + (round + u) * kWave;
+      r[u] = -1;
+      d[u] = 0.f;
+      if (t >= end) continue;
+      if constexpr (ROWS) {
+        r[u] = max(rows[t].rollout, -1);
+        d[u] = rows[t].d;
+      } else {
+        token_at(k, t, a.R, a.err_flag, r[u], d[u]);
+      }
+    }
+  };
+  load(0);
+  const Pair first_pair = pair_at(a, tid);   // on its way with the tokens
   {
     u32x4_t *p = reinterpret_cast<u32x4_t*>(s_ratio), *q = reinterpret_cast<u32x4_t*>(s_slope);
     const int n = a.R * int(sizeof(ExactSum) / 16);
@@ -310,46 +333,29 @@ __global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, R
   __syncthreads();
   {
     TokenSums sums{s_ratio, -1, 0.0, 0};
-    for (int64_t t0 = 0; t0 < k.T; t0 += kSmallNT) {
-      const int64_t t = t0 + tid;
-      int r = -1;
-      float d = 0.f;
-      if constexpr (ROWS) {
-        if (t < k.T) {
-          r = max(rows[t].rollout, -1);
-          d = rows[t].d;
-        }
-      } else {
-        token_at(k, t, a.R, a.err_flag, r, d);
-      }
-      sums.add(r, d);
+    for (int64_t round = 0; round < rounds; round += kAhead) {
+      if (round > 0) load(round);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) sums.add(r[u], d[u]);
     }
     sums.flush();
   }
   __syncthreads();
   double sum = 0.0;
-  for (int p = tid; p < a.P; p += kSmallNT) sum += pair_step(a, p, s_ratio, s_slope);
+  if (tid < a.P) sum = pair_step(a, tid, first_pair, s_ratio, s_slope);
+  for (int p = tid + kSmallNT; p < a.P; p += kSmallNT) sum += pair_step(a, p, pair_at(a, p), s_ratio, s_slope);
   sum = wave_sum_d(sum);
-  if (tid % kWave == 0) s_part[tid / kWave] = sum;
+  if (lane == 0) s_part[wave] = sum;
   __syncthreads();
-  if (tid == 0) {
-    double total = 0.0;
-    for (int w = 0; w < kSmallNT / kWave; ++w) total += s_part[w];
-    a.loss[0] = float(total);
+  for (int i = tid; i < a.R; i += kSmallNT) {
+    const float slope = slope_of(a, s_slope[i], s_ratio[i].count);
+    if (a.rollout_ratio) a.rollout_ratio[i] = float(ratio_of(a, s_ratio[i]));
+    if (a.drollout) a.drollout[i] = slope;
+    if constexpr (ROWS) gradient[i] = slope * grad_scale;
   }
-  __shared__ float s_d[kSmallR];
-  for (int r = tid; r < a.R; r += kSmallNT) {
-    const float d = slope_of(a, s_slope[r], s_ratio[r].count);
-    s_d[r] = d;
-    if (a.rollout_ratio) a.rollout_ratio[r] = float(ratio_of(a, s_ratio[r]));
-    if (a.drollout) a.drollout[r] = d;
-  }
-  if constexpr (ROWS) {
-    __syncthreads();
-    for (int64_t t = tid; t < k.T; t += kSmallNT) {
-      const RowRecord row = rows[t];
-      reinterpret_cast<GradRecord*>(rows)[t] = grad_record(row, targets[t], row.rollout >= 0 ? s_d[row.rollout] : 0.f, grad_scale);
-    }
+  if (wave == kSmallNT / kWave - 1) {
+    const double total = wave_sum_d(lane < kSmallNT / kWave ? s_part[lane] : 0.0);
+    if (lane == 0) a.loss[0] = float(total);
   }
 }
 
@@ -357,12 +363,9 @@ static bool is_small(int64_t T, int32_t R, int32_t P) { return T <= kSmallT && R
 static unsigned blocks_of(int64_t n, int nt) { return unsigned((n + nt - 1) / nt); }
 
 // Everything behind the sums over the tokens.
-static void launch_pairs(const PairLoss& a, const PairWorkspace& w, RowRecord* rows, const int32_t* targets, int64_t T, float grad_scale,
-                         hipStream_t s) {
+static void launch_pairs(const PairLoss& a, const PairWorkspace& w, float* gradient, float grad_scale, hipStream_t s) {
   if (a.P > 0) hipLaunchKernelGGL(k_pair_terms, dim3(blocks_of(a.P, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part);
-  int64_t n = a.R > 1 ? a.R : 1;
-  if (rows && T > n) n = T;
-  hipLaunchKernelGGL(k_pair_finish, dim3(blocks_of(n, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part, rows, targets, T, grad_scale);
+  hipLaunchKernelGGL(k_pair_finish, dim3(blocks_of(a.R > 1 ? a.R : 1, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part, gradient, grad_scale);
 }
 static void launch_clear(const PairWorkspace& w, int32_t R, hipStream_t s) {
   const int64_t n = int64_t(R) * 2 * int64_t(sizeof(ExactSum)) / 16;
@@ -381,6 +384,7 @@ struct PairRows {
   int R;
   RowRecord* rows;
   ExactSum* ratio;      // NULL: the sums are formed later
+  int64_t keep_from;    // rows from here on are read by loads that leave them in the caches
   float* logprob_out;
   int32_t* err_flag;
 };
@@ -436,10 +440,40 @@ __device__ __forceinline__ double row_lse(SoftTotal st) {
   return st.s == st.s ? double(st.o) * 0.69314718055994531 + log_of(st.s) : __builtin_nan("");
 }
 
+// A thread's part of a row.  KEEP: by loads that leave it in the memory-side cache.
+template <int NT, int DT, bool VEC, bool KEEP> __device__ __forceinline__ RowSum row_sum(const RowView<DT, VEC>& row) {
+  constexpr int E = RowView<DT, VEC>::E, kAhead = 4;
+  const auto load = [&](int i) { return KEEP ? row.load_again(i) : row.load(i); };
+  const int tid = threadIdx.x, jr = row.ragged();
+  const float zr = jr >= 0 ? row.at(jr) : 0.f;
+  RowSum st{soft_identity(), 0.f};
+  int i = tid;
+  for (; i + (kAhead - 1) * NT < row.nvec; i += kAhead * NT) {
+    u32x4_t v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = load(i + u * NT);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      float z[E];
+      row.unpack(v[u], z);
+      row_update<E>(st, z);
+    }
+  }
+  for (; i < row.nvec; i += NT) {
+    float z[E];
+    row.unpack(load(i), z);
+    row_update<E>(st, z);
+  }
+  if (jr >= 0) {
+    float z[1] = {zr};
+    row_update<1>(st, z);
+  }
+  return st;
+}
+
 // A row's log-partition and its sampled token's log-prob: one workgroup reads it once.
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
-  constexpr int E = RowView<DT, VEC>::E, kAhead = 4;
   __shared__ SoftTotal lds[NT / kWave];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
@@ -453,30 +487,8 @@ __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
     return;
   }
   const RowView<DT, VEC> row(a.logits, t, a.ld, a.V);
-  const int jr = row.ragged();
-  const float zr = jr >= 0 ? row.at(jr) : 0.f, zy = row.at(y);
-  RowSum st{soft_identity(), 0.f};
-  int i = tid;
-  for (; i + (kAhead - 1) * NT < row.nvec; i += kAhead * NT) {
-    u32x4_t v[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = row.load(i + u * NT);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      float z[E];
-      row.unpack(v[u], z);
-      row_update<E>(st, z);
-    }
-  }
-  for (; i < row.nvec; i += NT) {
-    float z[E];
-    row.unpack(row.load(i), z);
-    row_update<E>(st, z);
-  }
-  if (jr >= 0) {
-    float z[1] = {zr};
-    row_update<1>(st, z);
-  }
+  const float zy = row.at(y);
+  const RowSum st = t < a.keep_from ? row_sum<NT, DT, VEC, false>(row) : row_sum<NT, DT, VEC, true>(row);
   const SoftTotal sum = row_total<NT>(st, lds);
   if (tid != 0) return;
   const double lse = row_lse(sum);
@@ -492,20 +504,26 @@ __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
 }
 
 // ---------------------------------------------------------------------------------- gradient rows
-template <int DT> __device__ __forceinline__ float grad_elt(const GradRecord& c, float z, int j) {
-  const float d = c.k * exp2_fast(fmaf(z, kLog2e, -c.offset));
-  return j == c.y ? d + c.g : d;
-}
+// dz_j = k exp2(z_j log2 e - offset) + g 1[j = y], k = -g / sum of the exponentials.
+struct RowGradient {
+  float g, k, offset;
+  int y;
+  template <int DT> __device__ __forceinline__ float at(float z, int j) const {
+    const float d = k * exp2_fast(fmaf(z, kLog2e, -offset));
+    return j == y ? d + g : d;
+  }
+};
 
 // (row, segment) per workgroup, a vector per thread, in the order of addresses from the end: what was read last is read first.
 template <int NT, int DT>
-__global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V, int64_t ld, int segs, const GradRecord* __restrict__ rows,
-                                                      void* dlogits) {
+__global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V, int64_t ld, int segs, const RowRecord* __restrict__ rows,
+                                                      const float* __restrict__ gradient, const int32_t* __restrict__ targets, void* dlogits) {
   constexpr int E = Storage<DT>::kPerVec;
   const unsigned block = gridDim.x - 1 - blockIdx.x;
   const int64_t t = block / segs;
   const int seg = block % segs;
-  const GradRecord c = rows[t];
+  const RowRecord row = rows[t];
+  if (row.rollout == AERO_ROW_UNTOUCHED) return;
   const RowGeom geom = row_geom<DT>(logits, t, ld, V);
   const char* zrow = row_ptr<DT>(logits, t, ld);
   char* drow = row_ptr<DT>(dlogits, t, ld);
@@ -514,14 +532,16 @@ __global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V,
   const int k = seg * NT + threadIdx.x;
   const bool in = k < geom.nvec;
   const int jr = seg == 0 ? ragged_elt<DT>(geom, V, threadIdx.x) : -1;
-  if (c.g == 0.f) {   // uniform: nothing to read
-    if (__float_as_uint(c.g) >> 31) return;
-    if (in) dv[k] = u32x4_t{0u, 0u, 0u, 0u};
+  const float g = row.rollout >= 0 ? gradient[row.rollout] : 0.f;
+  if (g == 0.f) {   // uniform: nothing to read
+    if (in) __builtin_nontemporal_store(u32x4_t{0u, 0u, 0u, 0u}, dv + k);
     if (jr >= 0) store_elt<DT>(drow, jr, 0.f);
     return;
   }
+  u32x4_t v = {0u, 0u, 0u, 0u};
+  if (in) v = zv[k];
+  const RowGradient c{g, -g * row.inv, row.offset, targets[t]};
   if (in) {
-    const u32x4_t v = zv[k];
     float z[E], d[E];
     unpack_vec<DT>(v, z);
 #pragma unroll
@@ -531,21 +551,24 @@ __global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V,
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] += e == (at & (E - 1)) ? c.g : 0.f;
     }
-    dv[k] = pack_vec<DT>(d);
+    __builtin_nontemporal_store(pack_vec<DT>(d), dv + k);
   }
-  if (jr >= 0) store_elt<DT>(drow, jr, grad_elt<DT>(c, load_elt<DT>(zrow, jr), jr));
+  if (jr >= 0) store_elt<DT>(drow, jr, c.at<DT>(load_elt<DT>(zrow, jr), jr));
 }
 
 // A row per workgroup, element by element: where logits and dlogits differ in their offset from 16 bytes, or a launch would not
 // hold the segments.
 template <int DT>
-__global__ __launch_bounds__(256) void k_pair_grad_row(const void* logits, int V, int64_t ld, const GradRecord* __restrict__ rows, void* dlogits) {
+__global__ __launch_bounds__(256) void k_pair_grad_row(const void* logits, int V, int64_t ld, const RowRecord* __restrict__ rows,
+                                                       const float* __restrict__ gradient, const int32_t* __restrict__ targets, void* dlogits) {
   const int64_t t = blockIdx.x;
-  const GradRecord c = rows[t];
-  if (c.g == 0.f && __float_as_uint(c.g) >> 31) return;
+  const RowRecord row = rows[t];
+  if (row.rollout == AERO_ROW_UNTOUCHED) return;
+  const float g = row.rollout >= 0 ? gradient[row.rollout] : 0.f;
+  const RowGradient c{g, -g * row.inv, row.offset, targets[t]};
   const char* zrow = row_ptr<DT>(logits, t, ld);
   char* drow = row_ptr<DT>(dlogits, t, ld);
-  for (int j = threadIdx.x; j < V; j += 256) store_elt<DT>(drow, j, c.g == 0.f ? 0.f : grad_elt<DT>(c, load_elt<DT>(zrow, j), j));
+  for (int j = threadIdx.x; j < V; j += 256) store_elt<DT>(drow, j, g == 0.f ? 0.f : c.at<DT>(load_elt<DT>(zrow, j), j));
 }
 
 template <int DT> static void launch_rows(const PairRows& a, hipStream_t s) {
@@ -562,32 +585,35 @@ template <int DT> static void launch_rows(const PairRows& a, hipStream_t s) {
   else launch(std::integral_constant<int, 512>{});
 }
 
-template <int DT> static void launch_grad(const PairRows& a, void* dlogits, hipStream_t s) {
-  const GradRecord* rows = reinterpret_cast<const GradRecord*>(a.rows);
+template <int DT> static void launch_grad(const PairRows& a, const float* gradient, void* dlogits, hipStream_t s) {
   const int64_t nvec = a.V / Storage<DT>::kPerVec + 1;
   const int nt = nvec <= 128 ? 64 : 256;
   const int64_t segs = (nvec + nt - 1) / nt;
   if (!rows_alike(a.logits, dlogits, Storage<DT>::kBytes) || !grid_fits(a.T * segs, nt)) {
-    hipLaunchKernelGGL(k_pair_grad_row<DT>, dim3(unsigned(a.T)), dim3(256), 0, s, a.logits, a.V, a.ld, rows, dlogits);
+    hipLaunchKernelGGL(k_pair_grad_row<DT>, dim3(unsigned(a.T)), dim3(256), 0, s, a.logits, a.V, a.ld, a.rows, gradient, a.targets, dlogits);
     return;
   }
-  const dim3 grid = dim3(unsigned(a.T * segs));
-  if (nt == 64) hipLaunchKernelGGL((k_pair_grad_seg<64, DT>), grid, dim3(64), 0, s, a.logits, a.V, a.ld, int(segs), rows, dlogits);
-  else hipLaunchKernelGGL((k_pair_grad_seg<256, DT>), grid, dim3(256), 0, s, a.logits, a.V, a.ld, int(segs), rows, dlogits);
+  const auto kernel = nt == 64 ? k_pair_grad_seg<64, DT> : k_pair_grad_seg<256, DT>;
+  hipLaunchKernelGGL(kernel, dim3(unsigned(a.T * segs)), dim3(nt), 0, s, a.logits, a.V, a.ld, int(segs), a.rows, gradient, a.targets, dlogits);
 }
+
+// The memory-side cache holds 256 MB: that much of the rows' end is still there when the gradient, which goes through the rows from their end, reads it.  Rows of
+// 300 MB 140 us (1000 x 151936 bf16) with nothing kept, 133 with this, 140 with all of them; 2.5 GB 1067 / 1060 / 1078.
+constexpr int64_t kKeptBytes = int64_t(256) << 20;
 
 template <int DT> static void run_rows(const PairRows& rows, const PairLoss& a, const PairWorkspace& w, float grad_scale, void* dlogits, hipStream_t s) {
   const bool small = is_small(rows.T, a.R, a.P);
   if (!small) launch_clear(w, a.R, s);
   PairRows r = rows;
   r.ratio = small ? nullptr : w.ratio;
+  r.keep_from = dlogits ? r.T - kKeptBytes / (int64_t(r.V) * Storage<DT>::kBytes) : r.T;
   if (r.T > 0) launch_rows<DT>(r, s);
   if (small) {
-    hipLaunchKernelGGL(k_pair_small<true>, dim3(1), dim3(kSmallNT), 0, s, Tokens{nullptr, nullptr, nullptr, r.T}, a, r.rows, r.targets, grad_scale);
+    hipLaunchKernelGGL(k_pair_small<true>, dim3(1), dim3(kSmallNT), 0, s, Tokens{nullptr, nullptr, nullptr, r.T}, a, r.rows, w.gradient, grad_scale);
   } else {
-    launch_pairs(a, w, dlogits ? r.rows : nullptr, r.targets, r.T, grad_scale, s);
+    launch_pairs(a, w, w.gradient, grad_scale, s);
   }
-  if (dlogits && r.T > 0) launch_grad<DT>(r, dlogits, s);
+  if (dlogits && r.T > 0) launch_grad<DT>(r, w.gradient, dlogits, s);
 }
 
 // ---------------------------------------------------------------------------------- the calls' checks
@@ -627,7 +653,7 @@ extern "C" aero_status aero_preference_loss(
   }
   launch_clear(w, R, s);
   if (T > 0) hipLaunchKernelGGL(k_pair_tokens, dim3(blocks_of(T, kTokenNT * kTokenRounds)), dim3(kTokenNT), 0, s, k, a, w.ratio);
-  launch_pairs(a, w, nullptr, nullptr, 0, 0.f, s);
+  launch_pairs(a, w, nullptr, 0.f, s);
   return launch_status();
 }
 
@@ -646,7 +672,7 @@ extern "C" aero_status aero_preference_loss_bwd(
   const PairWorkspace w = carve(workspace, T, R, P, nullptr);
   const PairLoss a{pair_chosen, pair_rejected, pair_weight, P, R, params->kind, params->average, params->beta, params->smoothing, params->margin,
                    loss, pair_margin, rollout_ratio, nullptr, err_flag};
-  const PairRows rows{logits, T, V, ld, targets, ref_logprob, token_rollout, R, w.rows, nullptr, logprob_out, err_flag};
+  const PairRows rows{logits, T, V, ld, targets, ref_logprob, token_rollout, R, w.rows, nullptr, 0, logprob_out, err_flag};
   hipStream_t s = as_stream(stream);
   switch (dtype) {
     case AERO_BF16: run_rows<kBF16>(rows, a, w, grad_scale, dlogits, s); break;
