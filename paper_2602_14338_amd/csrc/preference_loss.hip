@@ -184,24 +184,39 @@ __device__ __forceinline__ double pair_step(const PairLoss& a, int p, const Pair
 
 // ---------------------------------------------------------------------------------- tokens
 // Sums of tokens by rollout, a wave at a time over 64 tokens in a row: as long as they are one rollout's (a rollout's tokens usually stand together), lanes
-// add up by themselves and the wave at the end; otherwise rollout by rollout for up to four of them and lane by lane for the others.
+// add up by themselves and the wave at the end; otherwise rollout by rollout for up to four of them and lane by lane for the others.  What the wave has
+// added up waits in a lane of its own, so that many such sums go where they belong at once: each one by itself is as many instructions as all of them.
 struct TokenSums {
   ExactSum* sums;
-  int rollout;   // uniform; -1: nothing held
-  double held;
-  int count;
+  int rollout = -1;   // uniform; -1: nothing held
+  double held = 0.0;
+  int count = 0;
+  int waiting = 0;    // uniform
+  int lane_rollout = 0, lane_count = 0;
+  double lane_total = 0.0;
 
-  __device__ __forceinline__ void put(int r, double total, int n) {   // total and n: the same in every lane
-    if (threadIdx.x % kWave == 0) {
-      exact_add(&sums[r], total);
-      atomicAdd(&sums[r].count, n);
-    }
+  __device__ __forceinline__ explicit TokenSums(ExactSum* s) : sums(s) {}
+  __device__ __forceinline__ void to(int r, double d, int n) {
+    exact_add(&sums[r], d);
+    atomicAdd(&sums[r].count, n);
+  }
+  __device__ __forceinline__ void put(int r, double total, int n) {   // the same in every lane
+    const bool mine = int(threadIdx.x) % kWave == waiting;
+    lane_rollout = mine ? r : lane_rollout;
+    lane_total = mine ? total : lane_total;
+    lane_count = mine ? n : lane_count;
+    if (++waiting == kWave) end();
   }
   __device__ __forceinline__ void flush() {
-    if (rollout >= 0) put(rollout, wave_sum_d(held), count);
+    if (rollout < 0) return;
+    put(rollout, wave_sum_d(held), count);
     rollout = -1;
     held = 0.0;
     count = 0;
+  }
+  __device__ __forceinline__ void end() {
+    if (int(threadIdx.x) % kWave < waiting) to(lane_rollout, lane_total, lane_count);
+    waiting = 0;
   }
   __device__ __forceinline__ void add(int r, float d) {   // r < 0: no token
     uint64_t left = __ballot(r >= 0);
@@ -223,10 +238,7 @@ struct TokenSums {
       put(one, wave_sum_d(r == one ? double(d) : 0.0), __popcll(same));
       left &= ~same;
     }
-    if (left >> (threadIdx.x % kWave) & 1) {
-      exact_add(&sums[r], d);
-      atomicAdd(&sums[r].count, 1);
-    }
+    if (left >> (threadIdx.x % kWave) & 1) to(r, double(d), 1);
   }
 };
 
@@ -236,10 +248,10 @@ struct Tokens {
   const int32_t* rollout;
   int64_t T;
 };
-__device__ __forceinline__ void token_at(const Tokens& k, int64_t t, int R, int32_t* err_flag, int& r, float& d) {
+__device__ __forceinline__ void token_at(const Tokens& k, int64_t t, int64_t end, int R, int32_t* err_flag, int& r, float& d) {
   r = -1;
   d = 0.f;
-  if (t >= k.T) return;
+  if (t >= end) return;
   r = k.rollout[t];
   d = k.logprob[t] - (k.ref ? k.ref[t] : 0.f);   // asked for with the index; no use is made of it where that says so
   if (r >= R && err_flag) atomicOr(err_flag, AERO_DERR_BAD_ROLLOUT);
@@ -249,17 +261,28 @@ __device__ __forceinline__ void token_at(const Tokens& k, int64_t t, int R, int3
   }
 }
 
-constexpr int kTokenRounds = 8, kTokenNT = 256;
-__global__ __launch_bounds__(kTokenNT) void k_pair_tokens(Tokens k, PairLoss a, ExactSum* ratio) {
+// The tokens as rows of logits have left them.
+__device__ __forceinline__ void row_token(const RowRecord* rows, int64_t t, int64_t end, int& r, float& d) {
+  r = t < end ? max(rows[t].rollout, -1) : -1;
+  d = t < end ? rows[t].d : 0.f;
+}
+
+constexpr int kTokenRounds = 2, kTokenNT = 256;
+template <bool ROWS>
+__global__ __launch_bounds__(kTokenNT) void k_pair_tokens(Tokens k, PairLoss a, const RowRecord* __restrict__ rows, ExactSum* ratio) {
   const int64_t from = (int64_t(blockIdx.x) * kTokenNT + threadIdx.x / kWave * kWave) * kTokenRounds + threadIdx.x % kWave;
   int r[kTokenRounds];
   float d[kTokenRounds];
 #pragma unroll
-  for (int u = 0; u < kTokenRounds; ++u) token_at(k, from + u * kWave, a.R, a.err_flag, r[u], d[u]);
-  TokenSums sums{ratio, -1, 0.0, 0};
+  for (int u = 0; u < kTokenRounds; ++u) {
+    if constexpr (ROWS) row_token(rows, from + u * kWave, k.T, r[u], d[u]);
+    else token_at(k, from + u * kWave, k.T, a.R, a.err_flag, r[u], d[u]);
+  }
+  TokenSums sums(ratio);
 #pragma unroll
   for (int u = 0; u < kTokenRounds; ++u) sums.add(r[u], d[u]);
   sums.flush();
+  sums.end();
 }
 
 __global__ __launch_bounds__(256) void k_pair_clear(u32x4_t* p, int64_t n) {
@@ -294,12 +317,13 @@ __global__ __launch_bounds__(256) void k_pair_finish(PairLoss a, const ExactSum*
   if (threadIdx.x == 0) a.loss[0] = float(s_part[0] + s_part[1] + s_part[2] + s_part[3]);
 }
 
-// All of the above by one workgroup, the sums in LDS: for as many tokens, pairs and rollouts as take it less time than the launches.
+// The pairs by one workgroup, the rollouts' sums in LDS: for as few pairs and rollouts as take it less time than two launches; and the sums over the tokens as
+// well where those are few enough (kFromTokens, kFromRows; with kFromSums they are in memory).
+enum SumSource { kFromTokens, kFromRows, kFromSums };
 constexpr int kSmallNT = 1024, kSmallR = 256, kSmallP = 4096;
-constexpr int64_t kSmallT = 16384;
-template <bool ROWS>
-__global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, const RowRecord* __restrict__ rows, float* __restrict__ gradient,
-                                                         float grad_scale) {
+template <int SOURCE>
+__global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, const RowRecord* __restrict__ rows, const ExactSum* __restrict__ ratio,
+                                                         float* __restrict__ gradient, float grad_scale) {
   constexpr int kAhead = 8;
   __shared__ ExactSum s_ratio[kSmallR], s_slope[kSmallR];
   __shared__ double s_part[kSmallNT / kWave];
@@ -312,35 +336,34 @@ __global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, c
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int64_t t = from + (round + u) * kWave;
-      r[u] = -1;
-      d[u] = 0.f;
-      if (t >= end) continue;
-      if constexpr (ROWS) {
-        r[u] = max(rows[t].rollout, -1);
-        d[u] = rows[t].d;
-      } else {
-        token_at(k, t, a.R, a.err_flag, r[u], d[u]);
-      }
+      if constexpr (SOURCE == kFromRows) row_token(rows, t, end, r[u], d[u]);
+      else token_at(k, t, end, a.R, a.err_flag, r[u], d[u]);
     }
   };
-  load(0);
+  if constexpr (SOURCE != kFromSums) load(0);
   const Pair first_pair = pair_at(a, tid);   // on its way with the tokens
   {
     u32x4_t *p = reinterpret_cast<u32x4_t*>(s_ratio), *q = reinterpret_cast<u32x4_t*>(s_slope);
+    const u32x4_t* from = reinterpret_cast<const u32x4_t*>(ratio);
+    const u32x4_t zero = {0u, 0u, 0u, 0u};
     const int n = a.R * int(sizeof(ExactSum) / 16);
-    for (int i = tid; i < n; i += kSmallNT) p[i] = q[i] = u32x4_t{0u, 0u, 0u, 0u};
+    for (int i = tid; i < n; i += kSmallNT) {
+      p[i] = SOURCE == kFromSums ? from[i] : zero;
+      q[i] = zero;
+    }
   }
   __syncthreads();
-  {
-    TokenSums sums{s_ratio, -1, 0.0, 0};
+  if constexpr (SOURCE != kFromSums) {
+    TokenSums sums(s_ratio);
     for (int64_t round = 0; round < rounds; round += kAhead) {
       if (round > 0) load(round);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) sums.add(r[u], d[u]);
     }
     sums.flush();
+    sums.end();
+    __syncthreads();
   }
-  __syncthreads();
   double sum = 0.0;
   if (tid < a.P) sum = pair_step(a, tid, first_pair, s_ratio, s_slope);
   for (int p = tid + kSmallNT; p < a.P; p += kSmallNT) sum += pair_step(a, p, pair_at(a, p), s_ratio, s_slope);
@@ -351,7 +374,7 @@ __global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, c
     const float slope = slope_of(a, s_slope[i], s_ratio[i].count);
     if (a.rollout_ratio) a.rollout_ratio[i] = float(ratio_of(a, s_ratio[i]));
     if (a.drollout) a.drollout[i] = slope;
-    if constexpr (ROWS) gradient[i] = slope * grad_scale;
+    if (gradient) gradient[i] = slope * grad_scale;
   }
   if (wave == kSmallNT / kWave - 1) {
     const double total = wave_sum_d(lane < kSmallNT / kWave ? s_part[lane] : 0.0);
@@ -359,11 +382,16 @@ __global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, c
   }
 }
 
-static bool is_small(int64_t T, int32_t R, int32_t P) { return T <= kSmallT && R <= kSmallR && P <= kSmallP; }
+static bool is_small(int32_t R, int32_t P) { return R <= kSmallR && P <= kSmallP; }
 static unsigned blocks_of(int64_t n, int nt) { return unsigned((n + nt - 1) / nt); }
 
+static dim3 token_blocks(int64_t T) { return dim3(blocks_of(T, kTokenNT * kTokenRounds)); }
 // Everything behind the sums over the tokens.
 static void launch_pairs(const PairLoss& a, const PairWorkspace& w, float* gradient, float grad_scale, hipStream_t s) {
+  if (is_small(a.R, a.P)) {
+    hipLaunchKernelGGL(k_pair_small<kFromSums>, dim3(1), dim3(kSmallNT), 0, s, Tokens{}, a, nullptr, w.ratio, gradient, grad_scale);
+    return;
+  }
   if (a.P > 0) hipLaunchKernelGGL(k_pair_terms, dim3(blocks_of(a.P, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part);
   hipLaunchKernelGGL(k_pair_finish, dim3(blocks_of(a.R > 1 ? a.R : 1, 256)), dim3(256), 0, s, a, w.ratio, w.slope, w.part, gradient, grad_scale);
 }
@@ -383,7 +411,6 @@ struct PairRows {
   const int32_t* rollout;
   int R;
   RowRecord* rows;
-  ExactSum* ratio;      // NULL: the sums are formed later
   int64_t keep_from;    // rows from here on are read by loads that leave them in the caches
   float* logprob_out;
   int32_t* err_flag;
@@ -497,10 +524,6 @@ __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
   const float d = empty ? 0.f : float(a.ref ? lp - double(a.ref[t]) : lp);
   a.rows[t] = RowRecord{empty ? AERO_ROW_PADDING : r, d, sum.o, float(1.0 / sum.s)};
   if (a.logprob_out) a.logprob_out[t] = float(lp);
-  if (a.ratio && !empty) {
-    exact_add(&a.ratio[r], d);
-    atomicAdd(&a.ratio[r].count, 1);
-  }
 }
 
 // ---------------------------------------------------------------------------------- gradient rows
@@ -601,16 +624,22 @@ template <int DT> static void launch_grad(const PairRows& a, const float* gradie
 // 300 MB 140 us (1000 x 151936 bf16) with nothing kept, 133 with this, 140 with all of them; 2.5 GB 1067 / 1060 / 1078.
 constexpr int64_t kKeptBytes = int64_t(256) << 20;
 
+// Up to so many tokens one workgroup also adds them up, which saves a clearing launch and one for the sums.  One launch / three, us, of 16 and 256 rollouts: 512 tokens
+// 6.2 / 10.2, 6.9 / 11.1; 4096 7.3 / 10.2, 11.8 / 11.6; 8192 8.6 / 10.3, 14.3 / 11.3; 16384 10.7 / 10.5, 19.0 / 11.0; as rows of 512 logits 512 13.1 / 16.7, 14.0 / 17.8;
+// 4096 16.8 / 17.9, 21.1 / 20.3; 8192 21.6 / 21.1, 27.3 / 23.5.
+constexpr int64_t kOneRows = 4096, kOneTokens = 8192;
+
 template <int DT> static void run_rows(const PairRows& rows, const PairLoss& a, const PairWorkspace& w, float grad_scale, void* dlogits, hipStream_t s) {
-  const bool small = is_small(rows.T, a.R, a.P);
+  const bool small = rows.T <= kOneRows && is_small(a.R, a.P);
   if (!small) launch_clear(w, a.R, s);
   PairRows r = rows;
-  r.ratio = small ? nullptr : w.ratio;
   r.keep_from = dlogits ? r.T - kKeptBytes / (int64_t(r.V) * Storage<DT>::kBytes) : r.T;
   if (r.T > 0) launch_rows<DT>(r, s);
+  const Tokens k{nullptr, nullptr, nullptr, r.T};
   if (small) {
-    hipLaunchKernelGGL(k_pair_small<true>, dim3(1), dim3(kSmallNT), 0, s, Tokens{nullptr, nullptr, nullptr, r.T}, a, r.rows, w.gradient, grad_scale);
+    hipLaunchKernelGGL(k_pair_small<kFromRows>, dim3(1), dim3(kSmallNT), 0, s, k, a, r.rows, nullptr, w.gradient, grad_scale);
   } else {
+    if (r.T > 0) hipLaunchKernelGGL(k_pair_tokens<true>, token_blocks(r.T), dim3(kTokenNT), 0, s, k, a, r.rows, w.ratio);
     launch_pairs(a, w, w.gradient, grad_scale, s);
   }
   if (dlogits && r.T > 0) launch_grad<DT>(r, w.gradient, dlogits, s);
@@ -647,12 +676,12 @@ extern "C" aero_status aero_preference_loss(
                    loss, pair_margin, rollout_ratio, drollout, err_flag};
   const Tokens k{logprob, ref_logprob, token_rollout, T};
   hipStream_t s = as_stream(stream);
-  if (is_small(T, R, P)) {
-    hipLaunchKernelGGL(k_pair_small<false>, dim3(1), dim3(kSmallNT), 0, s, k, a, nullptr, nullptr, 0.f);
+  if (T <= kOneTokens && is_small(R, P)) {
+    hipLaunchKernelGGL(k_pair_small<kFromTokens>, dim3(1), dim3(kSmallNT), 0, s, k, a, nullptr, nullptr, nullptr, 0.f);
     return launch_status();
   }
   launch_clear(w, R, s);
-  if (T > 0) hipLaunchKernelGGL(k_pair_tokens, dim3(blocks_of(T, kTokenNT * kTokenRounds)), dim3(kTokenNT), 0, s, k, a, w.ratio);
+  if (T > 0) hipLaunchKernelGGL(k_pair_tokens<false>, token_blocks(T), dim3(kTokenNT), 0, s, k, a, nullptr, w.ratio);
   launch_pairs(a, w, nullptr, 0.f, s);
   return launch_status();
 }
@@ -672,7 +701,7 @@ extern "C" aero_status aero_preference_loss_bwd(
   const PairWorkspace w = carve(workspace, T, R, P, nullptr);
   const PairLoss a{pair_chosen, pair_rejected, pair_weight, P, R, params->kind, params->average, params->beta, params->smoothing, params->margin,
                    loss, pair_margin, rollout_ratio, nullptr, err_flag};
-  const PairRows rows{logits, T, V, ld, targets, ref_logprob, token_rollout, R, w.rows, nullptr, 0, logprob_out, err_flag};
+  const PairRows rows{logits, T, V, ld, targets, ref_logprob, token_rollout, R, w.rows, 0, logprob_out, err_flag};
   hipStream_t s = as_stream(stream);
   switch (dtype) {
     case AERO_BF16: run_rows<kBF16>(rows, a, w, grad_scale, dlogits, s); break;
