@@ -324,23 +324,23 @@ constexpr int kSmallNT = 1024, kSmallR = 256, kSmallP = 4096;
 template <int SOURCE>
 __global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, const RowRecord* __restrict__ rows, const ExactSum* __restrict__ ratio,
                                                          float* __restrict__ gradient, float grad_scale) {
-  constexpr int kAhead = 8;
+  constexpr int kAhead = 4;
   __shared__ ExactSum s_ratio[kSmallR], s_slope[kSmallR];
   __shared__ double s_part[kSmallNT / kWave];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   // each wave takes tokens that stand together, in as many rounds as it takes
   const int64_t rounds = (k.T + kSmallNT - 1) / kSmallNT, from = wave * rounds * kWave + lane, end = min(k.T, (wave + 1) * rounds * kWave);
-  int r[kAhead];
+  int r[kAhead];   // the next rounds' tokens, on their way
   float d[kAhead];
-  const auto load = [&](int64_t round) {
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int64_t t = from + (round + u) * kWave;
-      if constexpr (SOURCE == kFromRows) row_token(rows, t, end, r[u], d[u]);
-      else token_at(k, t, end, a.R, a.err_flag, r[u], d[u]);
-    }
+  const auto load = [&](int64_t round, int& r, float& d) {
+    const int64_t t = from + round * kWave;
+    if constexpr (SOURCE == kFromRows) row_token(rows, t, end, r, d);
+    else token_at(k, t, end, a.R, a.err_flag, r, d);
   };
-  if constexpr (SOURCE != kFromSums) load(0);
+  if constexpr (SOURCE != kFromSums) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) load(u, r[u], d[u]);
+  }
   const Pair first_pair = pair_at(a, tid);   // on its way with the tokens
   {
     u32x4_t *p = reinterpret_cast<u32x4_t*>(s_ratio), *q = reinterpret_cast<u32x4_t*>(s_slope);
@@ -355,10 +355,17 @@ __global__ __launch_bounds__(kSmallNT) void k_pair_small(Tokens k, PairLoss a, c
   __syncthreads();
   if constexpr (SOURCE != kFromSums) {
     TokenSums sums(s_ratio);
-    for (int64_t round = 0; round < rounds; round += kAhead) {
-      if (round > 0) load(round);
+#pragma clang loop unroll(disable)
+    for (int64_t round = 0; round < rounds; ++round) {
+      const int r_now = r[0];
+      const float d_now = d[0];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) sums.add(r[u], d[u]);
+      for (int u = 0; u + 1 < kAhead; ++u) {
+        r[u] = r[u + 1];
+        d[u] = d[u + 1];
+      }
+      load(round + kAhead, r[kAhead - 1], d[kAhead - 1]);
+      sums.add(r_now, d_now);
     }
     sums.flush();
     sums.end();
