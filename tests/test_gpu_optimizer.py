@@ -324,6 +324,22 @@ def test_norm(gh, grad, sizes):
         assert again.item() == norm.item()
 
 
+@pytest.mark.parametrize("sizes", [[70000, 333, 90000, 5000], [524288], [524289]])
+def test_norm_is_new_every_time(gh, sizes):
+    """Call after call on gradients that change in between, without a wait: each result is its own gradients'."""
+    import paper_2602_14338_amd as aero
+    from paper_2602_14338_amd import binding
+    flat = torch.randn(sum(sizes), device="cuda")
+    table = aero.TensorTable([dict(grad=x) for x in flat.split(sizes)])
+    ws = torch.empty(aero.aero_workspace_bytes(binding.OP_GRAD_NORM), dtype=torch.uint8, device="cuda")
+    got, want = torch.zeros(300, device="cuda"), torch.zeros(300, dtype=torch.float64, device="cuda")
+    for k in range(300):
+        flat.mul_(-0.97 if k % 3 else 1.1)
+        aero.aero_grad_norm(table, 1.0, 0.0, got[k:k + 1], None, ws)
+        want[k] = flat.double().square().sum().sqrt()
+    assert bool(((got.double() - want).abs() <= 2 * U * want).all())
+
+
 def test_norm_of_large_and_tiny_gradients(gh):
     import paper_2602_14338_amd as aero
     from paper_2602_14338_amd import binding
