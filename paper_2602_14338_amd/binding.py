@@ -455,6 +455,7 @@ class TensorTable:
         rows = (_TensorC * len(self.entries))()
         for k, e in enumerate(self.entries):
             self._fill(rows[k], e, f"entry {k}")
+        self._check_apart()
         size = int(_lib.aero_tensor_table_bytes(rows, len(self.entries)))
         self._host = torch.empty(size + 16, dtype=torch.uint8)
         self.image = (self._host.data_ptr() + 15) & ~15
@@ -463,6 +464,18 @@ class TensorTable:
         with torch.cuda.device(self.device):
             self.table = torch.empty(size, dtype=torch.uint8, device=self.device)
             self.table.copy_(self._host[at:at + size])
+
+    def _check_apart(self) -> None:
+        """What a step writes overlaps nothing else (the same tensor twice, say)."""
+        spans = sorted((e[name].data_ptr(), e[name].data_ptr() + _bytes(e[name]), name == "grad", f"entry {k}: {name}")
+                       for k, e in enumerate(self.entries) for name in self._NAMES if e.get(name) is not None and e[name].numel())
+        end = {False: (0, ""), True: (0, "")}   # of what is written, of gradients: the furthest so far
+        for first, last, reads, what in spans:
+            for kind in (False, True):
+                if first < end[kind][0] and not (reads and kind):
+                    raise AeroError(f"{what} overlaps {end[kind][1]}")
+            if last > end[reads][0]:
+                end[reads] = (last, what)
 
     def _fill(self, row: _TensorC, e: dict, where: str) -> None:
         unknown = set(e) - set(self._NAMES) - {"decay"}

@@ -438,6 +438,12 @@ def test_binding_refuses(gh):
             aero.TensorTable([dict(small, **more)])
     with pytest.raises(aero.AeroError):
         aero.TensorTable([])
+    flat = new(n=900)
+    for more in ([good, dict(good)], [dict(good, exp_avg_sq=good["exp_avg"])], [dict(good, param=good["grad"])],
+                 [dict(good, param=flat[:300]), dict(small, param=flat[299:599])], [dict(good, param=flat[10:310], grad=flat[:300])]):
+        with pytest.raises(aero.AeroError, match="overlaps"):
+            aero.TensorTable(more)
+    aero.TensorTable([dict(good, param=flat[:300]), dict(small, param=flat[300:600], grad=good["grad"]), dict(grad=good["grad"])])   # a gradient twice is read twice
     step, *_ = words()
     aero.aero_adamw_step(table, aero.AdamWParams(), step)
     for call in (lambda: aero.aero_adamw_step(table, aero.AdamWParams(eps=0.0), step), lambda: aero.aero_adamw_step(table, aero.AdamWParams(), step.long()),

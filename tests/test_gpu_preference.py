@@ -247,6 +247,35 @@ def test_terms_do_not_depend_on_order(gh, T, R, P):
         assert np.array_equal(x, y)
 
 
+def test_terms_of_the_largest_call(gh):
+    """As many tokens, rollouts and pairs as a call takes, against the same sums by the tensor library in 64 bits."""
+    import paper_2602_14338_amd as aero
+    from paper_2602_14338_amd import binding
+    T, R, P = (1 << 25) - 1, (1 << 22) - 1, (1 << 22) - 1
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rollout = torch.randint(-1, R, (T,), generator=g, device="cuda", dtype=torch.int32)
+    lp = -torch.rand(T, generator=g, device="cuda")
+    c, j = (torch.randint(0, R, (P,), generator=g, device="cuda", dtype=torch.int32) for _ in range(2))
+    loss, m, s, d = (torch.zeros(n, device="cuda") for n in (1, P, R, R))
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(aero.aero_workspace_bytes(binding.OP_PREFERENCE_LOSS, T=T, R=R, Q=P), dtype=torch.uint8, device="cuda")
+    how = how_of(smoothing=0.0, margin=0.0, average=1)
+    aero.aero_preference_loss(lp, T, None, rollout, R, c, j, None, P, params_of(how), loss, m, s, d, ws, err)
+    there = rollout >= 0
+    count = torch.zeros(R, dtype=torch.float64, device="cuda").index_add_(0, rollout[there].long(), torch.ones_like(lp[there]).double()).clamp(min=1)
+    ratio = torch.zeros(R, dtype=torch.float64, device="cuda").index_add_(0, rollout[there].long(), lp[there].double()) / count
+    x = how["beta"] * (ratio[c.long()] - ratio[j.long()])
+    share = -how["beta"] / P * torch.sigmoid(-x)
+    slope = torch.zeros(R, dtype=torch.float64, device="cuda").index_add_(0, c.long(), share).index_add_(0, j.long(), -share) / count
+    assert err.item() == 0
+    assert bool(((s.double() - ratio).abs() <= 4 * U * ratio.abs()).all())
+    assert bool(((m.double() - x).abs() <= 8 * U * how["beta"]).all())
+    # a share is rounded to 32 bits, and so is 1 / P; every one is 0.3 / P at most, and a rollout has 20 of them at most
+    assert bool(((d.double() - slope).abs() <= 20 * 4 * U * how["beta"] / P + 2 * U * slope.abs()).all())
+    want = torch.nn.functional.softplus(-x).mean()
+    assert abs(loss.item() - want.item()) <= 8 * U * want.item()
+
+
 # ------------------------------------------------------------------------------------------------ from logits
 def run_rows(z, T, V, ld, dtype, y, ref, rollout, R, chosen, rejected, weight, how, scale=1.0, inplace=False, want_dz=True, off=0):
     import paper_2602_14338_amd as aero
