@@ -410,8 +410,9 @@ aero_status aero_embedding_bwd(
  *   dlogits[t, j] = grad_scale drollout[token_rollout[t]] (1[j == targets[t]] - softmax(z[t])_j)
  * A rollout may be in any number of pairs.  Pairs with w_p == 0 or a negative index take no part, nor do those with an index >= R, which raise
  * AERO_DERR_BAD_ROLLOUT; their pair_margin is 0.
- * Log ratios, margins, losses and derivatives are formed in 64 bits from log-probs of 32 (of 64 in the call that takes logits); sums over the tokens and the pairs of
- * a rollout do not depend on their order: the same bits every time.
+ * Log ratios, margins, losses and derivatives are formed in 64 bits.  A token's difference and a pair's part of a derivative are rounded to 32 bits once; the
+ * same bits every time.  Pairs in another order change nothing but the loss's last bit, tokens in another order (or other tokens beside them) no more than 2^-47 of the
+ * sizes that are added up.
  * A token's logprob - ref_logprob that is infinite makes its rollout's s_r infinite, NaN (or infinities of both signs) NaN.  A
  * margin of +-inf has the loss's limit, and the derivative's; NaN makes the loss, the pair's margin and what derives from it NaN.
  *
@@ -431,7 +432,7 @@ typedef struct {
  * The loss from log-probs (those of aero_logprob_fwd or aero_lmhead_logprob_fused over all micro-batches of a step: a rollout's log ratio needs all
  * of its tokens).  The gradient of a micro-batch is then aero_grpo_loss_bwd's, or aero_lmhead_logprob_fused's, with adv[r] = -drollout[r],
  * weight[r] = 1 and old_logprob the log-probs themselves (a ratio of 1).
- * logprob f32[T] (not read where token_rollout is negative).  Outputs loss f32[1], pair_margin f32[P] (m_p) or NULL, rollout_ratio f32[R] (s_r) or
+ * logprob f32[T] (whatever it is where token_rollout is negative).  Outputs loss f32[1], pair_margin f32[P] (m_p) or NULL, rollout_ratio f32[R] (s_r) or
  * NULL, drollout f32[R] or NULL.
  * workspace: aero_workspace_bytes(AERO_OP_PREFERENCE_LOSS, T, 0, 0, R, P) (P in the place of Q).
  */

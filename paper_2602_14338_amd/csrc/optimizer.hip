@@ -1,11 +1,12 @@
 // What happens to gradients: their norm over many tensors, and Adam's step with decoupled weight decay on all of them at once, with moments
 // in 32 bits or in 8.
 //
-// A table describes the tensors.  Its elements are dealt out in chunks of 2048 of one tensor, 8 to a thread; the chunks of tensors of one class
-// (types of parameter, gradient and moments) stand together, and a class is one launch.
+// A table describes the tensors.  Its elements are dealt out in chunks of 2048 of one tensor; the chunks of tensors of one class (types of
+// parameter, gradient and moments) stand together, and a class is one launch.
 //
-// Both are bound by bytes: n of the gradient, and for a step what is read and written of weights and moments, 28 bytes an element for
-// 16-bit weights with a master and 32-bit moments, 10 for 16-bit weights with 8-bit moments.
+// Bound by bytes: n of the gradient for the norm (500 M bf16 154 us, 6.5 TB/s), for a step what is read and written of weights and moments (28 bytes an element for 16-bit weights with
+// a master and 32-bit moments: 300 M 1358 us, 6.2 TB/s).  With 8-bit moments (10 bytes an element) a step is bound by vector instructions, 97 an element where it rounds at random: 233 M
+// 550-600 us, of which the bytes are 370.  Small ones by one launch: 262 K elements 4.3 us, the norm of 150 K 4.0.
 #include <cmath>
 #include <cstring>
 
@@ -472,7 +473,7 @@ template <int N, class F> __device__ __forceinline__ void with_elements(const Pl
   else f(i, have_of<N>(p.e.n, i));
 }
 
-// A step's scalars: the two powers and quotients by two lanes at once.
+// A step's scalars: the two powers and quotients by two lanes at once (all of a wave's take part).
 __device__ __forceinline__ StepScalars step_scalars(const StepArgs& a) {
   const float factor = a.factor ? a.factor[0] : 1.f;
   const int step = a.step[0];
@@ -542,6 +543,7 @@ static StepKernel step_kernel(int cls, bool alone) {
 constexpr uint32_t kAloneUnits = 4096;
 
 // ---------------------------------------------------------------------------------- moments as numbers
+// Bound by bytes: 233 M moments in 8 bits as bf16 220 us (6.4 TB/s).
 template <bool SMALL, int DT>
 __global__ __launch_bounds__(kOptNT) void k_moments(void* table, int32_t count, uint32_t first, uint32_t first_unit, void* avg, void* sq) {
   constexpr int N = SMALL ? kCodeLane : kWideLane;

@@ -7,6 +7,10 @@
 // In between stand sums over tokens (by rollout) and over pairs (by rollout), in whatever order a batch brings them.  They are formed
 // exactly, in whole numbers, so that order does not matter: a 32-bit float is m 2^(p - 149) with a 24-bit m, and goes into two of nine
 // 64-bit limbs that stand for 2^(32 k - 149) (the low 32 bits of m 2^(p mod 32) and what is above), each below 2^32, so that 2^31 of them fit.
+//
+// Bound by the bytes of the rows, read twice and written once: 8192 x 151936 bf16, an eighth of them padding, 1058 us: 325 for the statistics (6.7 TB/s), 14 for the sums, 718 for
+// the gradient (6.5 TB/s).  Small batches by three launches in a row: 512 x 4096 fp32 14.2 us.  Log-probs alone by launches: 2^20 tokens of 4096 rollouts in 8192 pairs 17.8 us,
+// 4096 tokens 7.2.
 #include "row_scan.h"
 
 namespace aero {
@@ -267,6 +271,7 @@ __device__ __forceinline__ void row_token(const RowRecord* rows, int64_t t, int6
   d = t < end ? rows[t].d : 0.f;
 }
 
+// 128 tokens to a wave: 2^20 of them 5.4 us (12.6 MB); with 1024 to a wave 22, as the waves are too few to hide their loads, with 512 12.
 constexpr int kTokenRounds = 2, kTokenNT = 256;
 template <bool ROWS>
 __global__ __launch_bounds__(kTokenNT) void k_pair_tokens(Tokens k, PairLoss a, const RowRecord* __restrict__ rows, ExactSum* ratio) {
@@ -285,11 +290,13 @@ __global__ __launch_bounds__(kTokenNT) void k_pair_tokens(Tokens k, PairLoss a, 
   sums.end();
 }
 
+// The sums begin at 0 (a workspace holds anything).
 __global__ __launch_bounds__(256) void k_pair_clear(u32x4_t* p, int64_t n) {
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (i < n) p[i] = u32x4_t{0u, 0u, 0u, 0u};
 }
 
+// A thread for each pair: two log ratios, the pair's term and its share of two slopes.  Latency: 8192 pairs 6.8 us.
 __global__ __launch_bounds__(256) void k_pair_terms(PairLoss a, const ExactSum* __restrict__ ratio, ExactSum* slope, double* __restrict__ part) {
   const int p = blockIdx.x * 256 + threadIdx.x;
   const double term = wave_sum_d(p < a.P ? pair_step(a, p, pair_at(a, p), ratio, slope) : 0.0);
@@ -423,13 +430,14 @@ struct PairRows {
   int32_t* err_flag;
 };
 
-// A row's sum of exponentials, to 3e-8 where hundreds of tokens add up what is off.  Three errors go the same way in every row otherwise (1e-7 a token each, a
-// log ratio of 5 over 256 tokens to 5e-6 of itself):
-//   - beside a sampled token that has half of the row, a thread's other exponentials are mostly less than half a unit of its sum, which stays where it is:
-//     a vector's are added up first;
-//   - log2 e in 32 bits is off by a relative d = -1.3e-8, and the log-partition by d times the mean logit: the sum of e^z z sets it right;
-//   - an argument is rounded at its own size, and stored logits of 16 bits have few values, whose roundings do not even out: the offset
-//     follows the largest logit closely, so that the arguments that count are near 0.
+// A row's sum of exponentials.  Hundreds of tokens of a rollout add up what their log-probs are off, so what goes the same way in every row counts: summed as elsewhere in this
+// library a log-prob of 151936 bf16 logits is 3.9e-7 too high on the average, and a log ratio of 5 over 256 tokens 2.9e-5 of itself.  Three things set it right:
+//   - a vector's exponentials are added up before they meet the thread's sum: beside a sampled token that has half of the row, most of them are by themselves less than half a unit of
+//     that sum, which stays where it is (1.5e-7 left);
+//   - log2 e in 32 bits is off by a relative d = -1.3e-8, and the log-partition by d times the mean logit, which the sum of e^z z knows (3e-9 left);
+//   - an argument is rounded at its own size: the offset follows the largest logit closely, so that the arguments that count are near 0 (not the mean, but what a single log-prob is
+//     off: 1.0e-7 -> 0.7e-7, fp32 logits 1.2e-7 -> 0.4e-7).
+// Together 0-1 % of the call's time.
 struct RowSum {
   SoftSum st;
   float sz;   // the exponentials times their logits
@@ -505,7 +513,8 @@ template <int NT, int DT, bool VEC, bool KEEP> __device__ __forceinline__ RowSum
   return st;
 }
 
-// A row's log-partition and its sampled token's log-prob: one workgroup reads it once.
+// A row's log-partition and its sampled token's log-prob: one workgroup reads it once.  6.7 TB/s from some thousand rows of 151936 bf16 on, 5.3 for a thousand, which are all under
+// way at once and end together.  256 and 1024 threads instead of 512: 0-3 % longer; eight vectors ahead 0-1 %.
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
   __shared__ SoftTotal lds[NT / kWave];
@@ -544,7 +553,9 @@ struct RowGradient {
   }
 };
 
-// (row, segment) per workgroup, a vector per thread, in the order of addresses from the end: what was read last is read first.
+// (row, segment) per workgroup, a vector per thread, in the order of addresses from the end: what was read last is read first.  Stored past the caches, which
+// hold the rows then: 1000 rows of 151936 bf16 88 -> 80 us (7.2 TB/s, a part of it not from memory), 8192 rows 755 -> 718.  A vector asked for before it is known that its
+// rollout has a gradient takes 0.1-0.8 % less, but a satisfied hinge leaves most rows unread.
 template <int NT, int DT>
 __global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V, int64_t ld, int segs, const RowRecord* __restrict__ rows,
                                                       const float* __restrict__ gradient, const int32_t* __restrict__ targets, void* dlogits) {
