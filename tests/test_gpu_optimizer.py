@@ -383,12 +383,54 @@ def test_offsets_beyond_32_bits(gh):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
-def test_captured_replayed_and_on_another_stream(gh, bits):
+@pytest.mark.parametrize("more", [-1, 0, 1])
+def test_where_one_launch_ends(gh, bits, more):
+    """As many elements as one launch takes (1024 or 2048 to each of 4096 workgroups), one fewer, one more; and the norm's 1024 chunks of 2048."""
+    import paper_2602_14338_amd as aero
+    from paper_2602_14338_amd import binding
+    model = Model(13, [4096 * (1024 if bits == 32 else 2048) + more], "bf16", "bf16", 0, bits)
+    how = how_of(stochastic=True)
+    step, factor, _ = words(5, 1.5)
+    aero.aero_adamw_step(model.table, aero.AdamWParams(**how), step, factor)
+    torch.cuda.synchronize()
+    assert step.item() == 6
+    model.check(5, how, factor=1.5)
+    g = torch.randn(1024 * 2048 + more, device="cuda")
+    norm = torch.zeros(1, device="cuda")
+    ws = torch.empty(aero.aero_workspace_bytes(binding.OP_GRAD_NORM), dtype=torch.uint8, device="cuda")
+    aero.aero_grad_norm(aero.TensorTable([dict(grad=g)]), 1.0, 0.0, norm, None, ws)
+    want = g.double().square().sum().sqrt().item()
+    assert abs(norm.item() - want) <= 2 * U * want
+
+
+def test_a_step_that_does_not_take_place_in_many_launches(gh):
+    import paper_2602_14338_amd as aero
+    models = [Model([3, bits], [5000], "bf16", "f32", m, bits) for m in (0, 1) for bits in (8, 32)]
+    table = aero.TensorTable([e for m in models for e in m.entries])
+    before = [{k: x.clone() for k, x in m.flat.items()} for m in models]
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        step, factor, _ = words(9, bad)
+        aero.aero_adamw_step(table, aero.AdamWParams(**how_of()), step, factor)
+        torch.cuda.synchronize()
+        assert step.item() == 9
+        for m, held in zip(models, before):
+            for k, x in m.flat.items():
+                assert torch.equal(x, held[k]), k
+    step, factor, _ = words(9, 1.0)
+    aero.aero_adamw_step(table, aero.AdamWParams(**how_of()), step, factor)
+    torch.cuda.synchronize()
+    assert step.item() == 10
+    for k, m in enumerate(models):
+        m.check(9, how_of(), first_tensor=k)
+
+
+@pytest.mark.parametrize("bits,sizes", [(32, [5000, 33, 2048]), (8, [5000, 33, 2048]), (32, [4300000, 7]), (8, [8500000, 7])])
+def test_captured_replayed_and_on_another_stream(gh, bits, sizes):
     """Norm and step in a graph: every replay is one more step, with its own count and random bits."""
     import paper_2602_14338_amd as aero
     from paper_2602_14338_amd import binding
     how = how_of(stochastic=True)
-    a, b = (Model(14, [5000, 33, 2048], "bf16", "bf16", 0, bits) for _ in range(2))
+    a, b = (Model(14, sizes, "bf16", "bf16", 0, bits) for _ in range(2))
     ws = torch.empty(aero.aero_workspace_bytes(binding.OP_GRAD_NORM), dtype=torch.uint8, device="cuda")
     norm, factor, rate = (torch.ones(1, device="cuda") for _ in range(3))
     sa, sb = words()[0], words()[0]

@@ -164,7 +164,7 @@ def check_terms(seed, T, R, P, shape="packed", ref=True, weights=True, **kw):
 @pytest.mark.parametrize("average", [0, 1])
 @pytest.mark.parametrize("T,R,P,shape", [(1, 1, 1, "packed"), (1, 2, 1, "packed"), (63, 3, 2, "packed"), (65, 2, 5, "turns"), (1000, 16, 8, "packed"),
                                          (4097, 256, 300, "packed"), (5000, 257, 64, "packed"), (4096, 64, 4097, "turns"), (3000, 100, 50, "mixed"),
-                                         (16384, 7, 40, "packed"), (16385, 7, 40, "packed"), (20000, 3000, 2000, "mixed")])
+                                         (16384, 7, 40, "packed"), (16385, 7, 40, "packed"), (8192, 9, 4096, "packed"), (8193, 256, 4096, "turns"), (20000, 3000, 2000, "mixed")])
 def test_terms(gh, T, R, P, shape, kind, average):
     check_terms([T, R, P], T, R, P, shape, kind=kind, average=average)
 
@@ -346,6 +346,12 @@ def check_rows(seed, T, V, R, P, dtype, ld=None, off=0, off_d=None, shape="packe
     (20, 4097, 5, 5, 4100, 0), (300, 130, 300, 40, 130, 1), (7, 10007, 3, 2, 10007, 5), (4, 50257, 2, 2, 50257, 0), (3, 65537, 2, 1, 65600, 0), (3, 151936, 2, 2, 151936, 0)])
 def test_rows(gh, dtype, T, V, R, P, ld, off):
     check_rows([T, V], T, V, R, P, dtype, ld, off)
+
+
+@pytest.mark.parametrize("T,R,P", [(4096, 256, 40), (4097, 256, 40), (4096, 257, 40), (4100, 5, 4097)])
+def test_rows_where_the_forms_of_their_sums_meet(gh, T, R, P):
+    check_rows([T, R], T, 65, R, P, "f32", shape="packed")
+    check_rows([T, R, 1], T, 65, R, P, "bf16", ld=70, shape="turns")
 
 
 @pytest.mark.parametrize("kind", ["logistic", "hinge", "square"])
