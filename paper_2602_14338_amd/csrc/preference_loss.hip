@@ -97,7 +97,7 @@ static_assert(sizeof(RowRecord) == 16, "one scalar load");
 struct PairWorkspace {
   ExactSum *ratio, *slope;   // [R]
   double* part;              // [ceil(P / 64)] of the loss
-  float* gradient;           // [R] of a rollout's log-probs, times grad_scale
+  float* gradient;           // [R] of a rollout's log-probs, times grad_scale (T > 0)
   RowRecord* rows;           // [T]
 };
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256) void k_pair_terms(PairLoss a, const ExactSum* 
   if (threadIdx.x % kWave == 0 && p < a.P) part[p / kWave] = term;
 }
 
-// The rollouts' outputs (gradient: NULL without logits); the first workgroup adds up the loss.
+// The rollouts' outputs (gradient: NULL where no row asks for it); the first workgroup adds up the loss.
 __global__ __launch_bounds__(256) void k_pair_finish(PairLoss a, const ExactSum* __restrict__ ratio, const ExactSum* __restrict__ slope,
                                                      const double* __restrict__ part, float* __restrict__ gradient, float grad_scale) {
   const int r = blockIdx.x * 256 + threadIdx.x;
@@ -654,13 +654,14 @@ template <int DT> static void run_rows(const PairRows& rows, const PairLoss& a, 
   r.keep_from = dlogits ? r.T - kKeptBytes / (int64_t(r.V) * Storage<DT>::kBytes) : r.T;
   if (r.T > 0) launch_rows<DT>(r, s);
   const Tokens k{nullptr, nullptr, nullptr, r.T};
+  float* gradient = dlogits && r.T > 0 ? w.gradient : nullptr;   // read by the rows alone; without any the workspace has no room for it
   if (small) {
-    hipLaunchKernelGGL(k_pair_small<kFromRows>, dim3(1), dim3(kSmallNT), 0, s, k, a, r.rows, nullptr, w.gradient, grad_scale);
+    hipLaunchKernelGGL(k_pair_small<kFromRows>, dim3(1), dim3(kSmallNT), 0, s, k, a, r.rows, nullptr, gradient, grad_scale);
   } else {
     if (r.T > 0) hipLaunchKernelGGL(k_pair_tokens<true>, token_blocks(r.T), dim3(kTokenNT), 0, s, k, a, r.rows, w.ratio);
-    launch_pairs(a, w, w.gradient, grad_scale, s);
+    launch_pairs(a, w, gradient, grad_scale, s);
   }
-  if (dlogits && r.T > 0) launch_grad<DT>(r, w.gradient, dlogits, s);
+  if (gradient) launch_grad<DT>(r, gradient, dlogits, s);
 }
 
 // ---------------------------------------------------------------------------------- the calls' checks

@@ -469,6 +469,30 @@ def test_no_rows_no_rollouts_no_pairs(gh):
         near(loss, [want], 1e-6)
 
 
+@pytest.mark.parametrize("T,R,P", [(0, 256, 0), (0, 300, 0), (0, 256, 40), (0, 300, 40), (0, 4097, 5000), (3, 300, 40)])
+@pytest.mark.parametrize("want_dz", [True, False])
+def test_calls_stay_in_their_workspace(gh, T, R, P, want_dz):
+    """A workspace of exactly the size that is asked for, with or without rows: what stands behind it stays, and the outputs are those of rollouts without tokens."""
+    import paper_2602_14338_amd as aero
+    from paper_2602_14338_amd import binding
+    _, rollout, chosen, rejected, weight = batch(T + R, T, R, P)
+    V, behind = 50, 1 << 16
+    z = torch.zeros((T, V), dtype=torch.bfloat16, device="cuda")
+    loss, m, s = (torch.full((n,), 7.0, device="cuda") for n in (1, P, R))
+    size = aero.aero_workspace_bytes(binding.OP_PREFERENCE_LOSS_BWD, T=T, V=V, R=R, Q=P)
+    ws = torch.full((size + behind,), 0x5a, dtype=torch.uint8, device="cuda")
+    how = how_of()
+    aero.aero_preference_loss_bwd(z, T, V, V, on(np.zeros(T, np.int32)), None, on(rollout), R, on(chosen), on(rejected), on(weight), P, params_of(how), 1.0, loss,
+                                  m, s, torch.zeros(T, device="cuda"), torch.empty_like(z) if want_dz else None, ws[:size])
+    torch.cuda.synchronize()
+    assert (ws[size:] == 0x5a).all()
+    want = orc.preference(np.full(T, -np.log(V)), None, rollout, R, chosen, rejected, weight, **how)
+    e = T * (row(V, 0) + 4 * U)   # of a log ratio; margins are beta < 1/2 times two of them, the loss's slope is 1 at most
+    near(wide(s), want[2], e)
+    near(wide(m), want[1], e)
+    near(wide(loss), [want[0]], weight.sum() * e + 8 * U * abs(want[0]))
+
+
 def test_offsets_beyond_32_bits(gh):
     """More than 2^32 logits: the last rows' gradient is right."""
     import paper_2602_14338_amd as aero
