@@ -434,16 +434,26 @@ struct PairRows {
 // library a log-prob of 151936 bf16 logits is 3.9e-7 too high on the average, and a log ratio of 5 over 256 tokens 2.9e-5 of itself.  Three things set it right:
 //   - a vector's exponentials are added up before they meet the thread's sum: beside a sampled token that has half of the row, most of them are by themselves less than half a unit of
 //     that sum, which stays where it is (1.5e-7 left);
-//   - log2 e in 32 bits is off by a relative d = -1.3e-8, and the log-partition by d times the mean logit, which the sum of e^z z knows (3e-9 left);
+//   - log2 e in 32 bits, l, is off by a relative -1.3e-8, and the row's log-partition by that times the mean logit, which the exponentials times their arguments know (3e-9 left);
 //   - an argument is rounded at its own size: the offset follows the largest logit closely, so that the arguments that count are near 0 (not the mean, but what a single log-prob is
 //     off: 1.0e-7 -> 0.7e-7, fp32 logits 1.2e-7 -> 0.4e-7).
 // Together 0-1 % of the call's time.
+//
+// With arguments a_j = z_j l - o, S = sum of 2^a_j and m = (sum of 2^a_j a_j) / S:
+//   ln pi(y) = a_y ln 2 - ln S + c (a_y - m),  c = (log2 e - l) ln 2 / l,
+// to the first order in c times the spread of the logits that count.  All of it is near the offset: what holds for logits around 0 holds for those at 1e9.  (c times the logits
+// themselves is not small there, and has to stay out of S, by which the gradient divides exponentials that are formed with l.)
 struct RowSum {
   SoftSum st;
-  float sz;   // the exponentials times their logits
+  float sa;   // the exponentials times their arguments
+};
+struct RowTotal {
+  SoftTotal st;
+  double sa;
 };
 constexpr float kRowAbove = 2.f;
-constexpr double kLog2eOff = (1.4426950408889634074 - double(kLog2e)) * 0.69314718055994531;
+constexpr float kGone = -256.f;   // an argument whose exponential is 0
+constexpr double kLog2eOff = 9.2533473613469254e-9;   // c
 template <int N> __device__ __forceinline__ void row_update(RowSum& r, const float (&z)[N]) {
   const float vm = vec_max<N>(z);
   const bool grow = fmaf(vm, kLog2e, -r.st.o) > kRowAbove;
@@ -451,35 +461,45 @@ template <int N> __device__ __forceinline__ void row_update(RowSum& r, const flo
     asm volatile("" ::: "memory");   // stays a branch
     if (grow) {
       const float o = soft_offset(vm), f = exp2_fast(r.st.o - o);
+      r.sa = fmaf(r.st.o - o, r.st.s, r.sa) * f;
       r.st = SoftSum{o, r.st.s * f};
-      r.sz *= f;
     }
   }
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < N; ++k) {
-    const float e = exp2_fast(fmaf(z[k], kLog2e, -r.st.o));
+    const float a = fmaf(z[k], kLog2e, -r.st.o), e = exp2_fast(a);
     s += e;
-    r.sz = fmaf(e, fmaxf(z[k], kMasked), r.sz);   // 0 times a masked logit's -inf would be NaN
+    r.sa = fmaf(e, fmaxf(a, kGone), r.sa);   // 0 times a masked logit's -inf would be NaN
   }
   r.st.s += s;
 }
+template <bool WAVE> __device__ __forceinline__ RowTotal row_reduce(const RowTotal& r) {
+  const auto most = [](float x, float y) { return fmaxf(x, y); };
+  const auto all = [](double x) { return WAVE ? wave_sum_d(x) : row16_sum_d(x); };
+  const float o = WAVE ? wave_reduce(r.st.o, most) : row16_reduce(r.st.o, most);
+  const double f = double(exp2_fast(r.st.o - o));
+  return RowTotal{SoftTotal{o, all(r.st.s * f)}, all(fma(double(r.st.o - o), r.st.s, r.sa) * f)};
+}
 // Over the workgroup, with the sums of the threads added up in 64 bits.
-template <int NT> __device__ __forceinline__ SoftTotal row_total(const RowSum& r, SoftTotal* lds) {
-  const SoftTotal whole{r.st.o, double(r.st.s) + kLog2eOff * double(r.sz)};
-  SoftTotal a = soft_reduce<true>(whole);
+template <int NT> __device__ __forceinline__ RowTotal row_total(const RowSum& r, RowTotal* lds) {
+  RowTotal a = row_reduce<true>(RowTotal{soft_total(r.st), double(r.sa)});
   constexpr int kWaves = NT / kWave;
   if constexpr (kWaves > 1) {
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     if (lane == 0) lds[wave] = a;
     __syncthreads();
-    a = soft_reduce<false>(lane % 16 < kWaves ? lds[lane % 16] : soft_total(soft_identity()));
+    a = row_reduce<false>(lane % 16 < kWaves ? lds[lane % 16] : RowTotal{soft_total(soft_identity()), 0.0});
   }
   return a;
 }
-__device__ __forceinline__ double row_lse(SoftTotal st) {
-  if (st.s == 0.0) return -INFINITY;
-  return st.s == st.s ? double(st.o) * 0.69314718055994531 + log_of(st.s) : __builtin_nan("");
+// The log-prob of a logit; 0 in a row without an unmasked one, NaN in one with a NaN or too large one.
+__device__ __forceinline__ double row_logprob(const RowTotal& r, float z) {
+  if (r.st.s == 0.0) return 0.0;
+  if (r.st.s != r.st.s) return __builtin_nan("");
+  if (z <= kMasked) return -INFINITY;
+  const double a = fma(double(z), double(kLog2e), -double(r.st.o));   // to 2^-53 of itself
+  return fma(a, 0.69314718055994531, kLog2eOff * (a - r.sa / r.st.s)) - log_of(r.st.s);
 }
 
 // A thread's part of a row.  KEEP: by loads that leave it in the memory-side cache.
@@ -513,11 +533,11 @@ template <int NT, int DT, bool VEC, bool KEEP> __device__ __forceinline__ RowSum
   return st;
 }
 
-// A row's log-partition and its sampled token's log-prob: one workgroup reads it once.  6.7 TB/s from some thousand rows of 151936 bf16 on, 5.3 for a thousand, which are all under
+// A row's sum of exponentials and its sampled token's log-prob: one workgroup reads it once.  6.7 TB/s from some thousand rows of 151936 bf16 on, 5.3 for a thousand, which are all under
 // way at once and end together.  256 and 1024 threads instead of 512: 0-3 % longer; eight vectors ahead 0-1 %.
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
-  __shared__ SoftTotal lds[NT / kWave];
+  __shared__ RowTotal lds[NT / kWave];
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
   const int r = a.rollout[t], y = a.targets[t];
@@ -532,13 +552,12 @@ __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
   const RowView<DT, VEC> row(a.logits, t, a.ld, a.V);
   const float zy = row.at(y);
   const RowSum st = t < a.keep_from ? row_sum<NT, DT, VEC, false>(row) : row_sum<NT, DT, VEC, true>(row);
-  const SoftTotal sum = row_total<NT>(st, lds);
+  const RowTotal sum = row_total<NT>(st, lds);
   if (tid != 0) return;
-  const double lse = row_lse(sum);
-  const bool empty = sum.s == 0.0;
-  const double lp = empty ? 0.0 : zy <= kMasked ? (lse == lse ? -INFINITY : lse) : double(zy) - lse;
+  const bool empty = sum.st.s == 0.0;
+  const double lp = row_logprob(sum, zy);
   const float d = empty ? 0.f : float(a.ref ? lp - double(a.ref[t]) : lp);
-  a.rows[t] = RowRecord{empty ? AERO_ROW_PADDING : r, d, sum.o, float(1.0 / sum.s)};
+  a.rows[t] = RowRecord{empty ? AERO_ROW_PADDING : r, d, sum.st.o, float(1.0 / sum.st.s)};
   if (a.logprob_out) a.logprob_out[t] = float(lp);
 }
 

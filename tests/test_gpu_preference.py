@@ -293,7 +293,7 @@ def run_rows(z, T, V, ld, dtype, y, ref, rollout, R, chosen, rejected, weight, h
 
 
 def check_rows(seed, T, V, R, P, dtype, ld=None, off=0, off_d=None, shape="packed", ref=True, weights=True, inplace=False, change=None, err=0,
-               scale=None, sigma=3.0, **kw):
+               scale=None, sigma=3.0, distances=False, **kw):
     rng, rollout, chosen, rejected, weight = batch(seed, T, R, P, shape)
     values = rng.normal(0, sigma, size=(T, V)).astype(np.float32)
     y = rng.integers(0, V, T).astype(np.int32)
@@ -314,7 +314,16 @@ def check_rows(seed, T, V, R, P, dtype, ld=None, off=0, off_d=None, shape="packe
     np.add.at(count, rollout[part], 1)
     np.add.at(size, rollout[part], np.abs(d[part]))
     finite = np.abs(host[np.isfinite(host) & (np.abs(host) < 1.2e9)])
-    e = row(V, float(finite.max()) if finite.size else 0.0)
+    e, own, lost = row(V, float(finite.max()) if finite.size else 0.0), 0.0, 0.0
+    if distances:
+        # an argument is rounded near the offset, which is a whole number within 3 of the row's largest (or half a unit of 32 bits there)
+        half = 2.0 ** (np.frexp(1.4427 * np.abs(host).max())[1] - 25)
+        far = np.where(q > 0, host.max(axis=1, keepdims=True) - host, 0.0) * 1.4427 + 3 + half
+        # exponentials below 2^-126 are 0, in a sum that is at least its largest, 2^-(1 + half): at -1e9 (half a unit is 64) a logit 64 below the largest, e^-64 = 2^-92.3
+        # of the sum, has an argument down to -157
+        lost = 2.0 ** (-125 + half)
+        own = U * far
+        e = row(V, 0.0) + float((q * own).sum(axis=1).max())
     t_s, t_m, t_d, t_loss = bounds((w_loss, w_m, w_s, w_d), count, size, chosen, rejected, weight, how, e)
     loss, m, s, lp, dz, bits = run_rows(z, T, V, ld, dtype, y, rf, rollout, R, chosen, rejected, weight, how, scale, inplace,
                                         off=off if off_d is None else off_d)
@@ -328,7 +337,7 @@ def check_rows(seed, T, V, R, P, dtype, ld=None, off=0, off_d=None, shape="packe
     slope = np.where(part, w_d[np.clip(rollout, 0, max(R - 1, 0))] if R else 0.0, 0.0)
     t_slope = np.where(part, t_d[np.clip(rollout, 0, max(R - 1, 0))] if R else 0.0, 0.0)
     with np.errstate(all="ignore"):
-        tol = scale * (t_slope[:, None] * (hot + q) + np.abs(slope)[:, None] * (2 * e * q + 4 * U * (hot + q)))
+        tol = scale * (t_slope[:, None] * (hot + q) + np.abs(slope)[:, None] * ((2 * e + own) * q + lost + 4 * U * (hot + q)))
         tol = tol * (1 + HALF_ULP[dtype]) + HALF_ULP[dtype] * np.abs(w_dz) + HALF_LEAST[dtype]
     if dtype == "f8":
         w_dz = np.clip(w_dz, -448, 448)
@@ -433,6 +442,34 @@ def test_rows_of_large_logits(gh, size):
     def change(z, y, rollout):
         z += size
     check_rows(71, 20, 300, 4, 4, "f32", change=change)
+
+
+FAR = {"f32": [1e3, 1e5, 2.0 ** 23, 1e8, 1e9], "bf16": [1e3, 1e5, 1e8, 1e9], "f16": [1e3, 6e4]}
+
+
+@pytest.mark.parametrize("dtype,size", [(d, sign * x) for d, sizes in FAR.items() for x in sizes for sign in (1, -1)])
+def test_rows_far_from_0(gh, dtype, size):
+    """All of a row's logits far from 0, in steps of their type's unit there (or of an eighth); a log-prob is as exact as near 0, and the probabilities are those of
+    the distances from the largest logit.  Two rows are the same number throughout."""
+    digits = {"f32": 24, "bf16": 8, "f16": 11}[dtype]
+    unit = max(2.0 ** (np.frexp(size)[1] - digits), 0.125)
+
+    def change(z, y, rollout):
+        z[:] = size + unit * np.round(z / min(unit, 3.0))
+        z[[3, 7]] = size
+    check_rows(72, 24, 300, 4, 4, dtype, change=change, distances=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [-1e9, 1e9])
+@pytest.mark.parametrize("V", [300, 20000])
+def test_a_row_far_from_0_among_others(gh, dtype, size, V):
+    """A uniform row, whatever its number: log-prob -ln V, in a rollout of ordinary rows."""
+    def change(z, y, rollout):
+        rollout[:] = np.arange(len(rollout)) % 4
+        z[5] = size
+    dz = check_rows(73, 20, V, 4, 4, dtype, change=change, distances=True)
+    assert np.isfinite(dz).all() and (dz[5] != 0).all()
 
 
 def test_rollout_far_off_the_reference(gh):
