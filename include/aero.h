@@ -505,7 +505,7 @@ aero_status aero_grad_norm(
  *   p = p - rate (decay weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)),   rate = lr lr_factor,
  * then step[0] = t.  factor f32[1] or NULL (1), lr_factor f32[1] or NULL (1), step i32[1] (>= 0) are device words, so that a captured call
  * follows a schedule and counts its replays.  factor NaN or infinite: the step does not take place, step included.
- * Per element in 32 bits, every product and sum of m and v rounded by itself; 1 - beta^t in 64.
+ * Per element in 32 bits, every product and sum of m and v rounded by itself, the weight's change (decay and step) formed before it meets the weight; 1 - beta^t in 64.
  *
  * Moments in 8 bits: blocks of 256 elements of a tensor share a scale S,
  *   m = c |c| S, c = -127 .. 127, S = max|m| / 127^2;    v = c^4 S, c = 0 .. 255, S = max v / 255^4

@@ -383,7 +383,8 @@ template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
   }
   // The step, and its results to where they belong.
   __device__ __forceinline__ void step(const Tensor& e, const StepArgs& a, const StepScalars& s, uint64_t i, int have) const {
-    const float keep = float(1.0 - s.weight_decay * double(e.decay));
+    // By itself and not as 1 less it, which has steps of 2^-24 below 1: a rate of 1e-6 times a decay of 0.01 is nothing in them.  The whole change meets the weight in one sum.
+    const float fade = float(s.weight_decay * double(e.decay));
     float xg[N], xp[N], xm[N], xv[N], root[N];
     g.widen(xg);
     p.widen(xp);
@@ -404,7 +405,7 @@ template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
       }
       root[k] = __builtin_amdgcn_sqrtf(xv[k]);
       const float away = fmaf(root[k], s.by_second, a.eps);
-      xp[k] = fmaf(xp[k], keep, -(xm[k] * s.by_first) * __builtin_amdgcn_rcpf(away));
+      xp[k] -= fmaf(xp[k], fade, (xm[k] * s.by_first) * __builtin_amdgcn_rcpf(away));
     }
     uint32_t bits[N] = {};
     if ((SMALL || KIND == kParamBF16) && a.stochastic) {

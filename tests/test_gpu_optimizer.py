@@ -199,6 +199,37 @@ def test_no_momentum_and_no_rate(gh):
         model.check(0, how)
 
 
+@pytest.mark.parametrize("param,master,bits", [("f32", 0, 32), ("f32", 0, 8), ("bf16", 1, 32), ("f16", 1, 8)])
+@pytest.mark.parametrize("rate,weight_decay,decay,n", [(1e-6, 0.01, 1.0, 20000), (1e-6, 0.1, 1.0, 20000), (2e-6, 0.1, 1.0, 20000), (1e-6, 0.1, 0.5, 20000),
+                                                       (1e-6, 0.01, 1.0, 4500000)])
+def test_decay_at_small_rates(gh, param, master, bits, rate, weight_decay, decay, n):
+    """Weights of 0.55 to 0.95 over 200 steps of about `rate`, with decay and without, whose moments are the same: their means differ by what decays,
+    f = rate weight_decay decay of the weight a step, though that is less than a unit of the weight (2^-24).  Each of the steps on either side rounds by up to half
+    a unit, evenly, as the gradients are others every time: 5 standard deviations of the mean, sqrt(2 steps / 12 n) units.  (But for the first, which moves every weight by
+    the rate itself, whatever its gradient: 1e-6 are 16.78 units, 17 with or without a decay of 0.13 units, and so on every weight: half a unit on either side.)  The weights move by
+    4 x 200 rates at most (|m| / sqrt v <= 4 with these moments), their decay by that share of itself; f is rounded by 2^-24 of itself, as are the products."""
+    from paper_2602_14338_amd import optim
+    steps = 200 if n < 100000 else 60
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    start = (0.55 + 0.4 * torch.rand(n, generator=gen, device="cuda")).to(TORCH[param])
+    g = torch.zeros(n, device="cuda")
+    factor = torch.full((1,), 2.0 ** -10, device="cuda")
+    opts = [optim.AdamW([start.clone()], [g], lr=rate * 2.0 ** 10, betas=(0.9, 0.99), weight_decay=x, decay=[decay], bits=bits) for x in (weight_decay, 0.0)]
+    for _ in range(steps):
+        g.normal_(generator=gen)
+        for o in opts:
+            o.step(lr_factor=factor)
+    ends = [(o.table.entries[0]["master" if master else "param"]).double() for o in opts]
+    f = rate * weight_decay * decay
+    moved = float((ends[1] - start.double()).abs().max())
+    assert moved <= 4 * steps * rate
+    want = (1 - (1 - f) ** steps) * start.double().mean().item()
+    got = (ends[1] - ends[0]).mean().item()
+    tol = U + 5 * np.sqrt(steps / 6 / n) * U + want * (4 * steps * rate / 0.55 + 4 * U)
+    assert abs(got - want) <= tol, (got, want, tol)
+    assert tol < 0.15 * want
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_gradients_of_zero_and_tiny_ones(gh, bits):
     """All zeros, blocks of zeros beside others, numbers whose squares are below the smallest scale: no NaN, and what the checker says."""
