@@ -519,7 +519,7 @@ aero_status aero_grad_norm(
  * x = (x ^ x >> 15) 0xBB67AE85, x ^ x >> 16 (32 bits; fractions of sqrt 2 and sqrt 3):
  *   h = mix(mix(mix(seed_lo ^ mix(seed_hi ^ mix(t - 1))) + k) + i);   u = (low half of h + 1/2) / 2^16 for m, of the high half for v; the
  *   parameter's 16 bits are the high half of h 0x9E3779B1.
- * params is a host pointer, read before the call returns: 0 <= beta < 1, eps > 0 (as fp32 too), lr >= 0 and weight_decay finite (AERO_ERR_SHAPE).
+ * params is a host pointer, read before the call returns: 0 <= beta < 1, eps at least 2^-126 in fp32, lr >= 0 and weight_decay finite (AERO_ERR_SHAPE).
  */
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay;

@@ -385,7 +385,9 @@ template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
   __device__ __forceinline__ void step(const Tensor& e, const StepArgs& a, const StepScalars& s, uint64_t i, int have) const {
     // By itself and not as 1 less it, which has steps of 2^-24 below 1: a rate of 1e-6 times a decay of 0.01 is nothing in them.  The whole change meets the weight in one sum.
     const float fade = float(s.weight_decay * double(e.decay));
+    constexpr int kSubnormal = 0x90;   // of either sign
     float xg[N], xp[N], xm[N], xv[N], root[N];
+    bool low = false;
     g.widen(xg);
     p.widen(xp);
     if constexpr (SMALL) {
@@ -404,8 +406,20 @@ template <int KIND, int GRAD, bool SMALL, bool ALONE> struct Held {
         xv[k] = xv[k] * a.beta2 + (x * x) * a.beta2c;
       }
       root[k] = __builtin_amdgcn_sqrtf(xv[k]);
+      low |= __builtin_amdgcn_classf(xv[k], kSubnormal);
+    }
+    if (__builtin_amdgcn_ballot_w64(low) != 0) {   // the machine's root takes them as 0, which would leave m over eps alone
+      asm volatile("" ::: "memory");               // stays a branch
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (__builtin_amdgcn_classf(xv[k], kSubnormal)) root[k] = __builtin_amdgcn_sqrtf(xv[k] * 0x1p64f) * 0x1p-32f;
+    }
+    // eps is 2^-126 or more, so that the reciprocal is finite.  m goes over the root first: where both are tiny that is a number near 1, while m times the rate might lose
+    // its bits below 2^-126.
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
       const float away = fmaf(root[k], s.by_second, a.eps);
-      xp[k] -= fmaf(xp[k], fade, (xm[k] * s.by_first) * __builtin_amdgcn_rcpf(away));
+      xp[k] -= fmaf(xp[k], fade, (xm[k] * __builtin_amdgcn_rcpf(away)) * s.by_first);
     }
     uint32_t bits[N] = {};
     if ((SMALL || KIND == kParamBF16) && a.stochastic) {
@@ -746,7 +760,7 @@ extern "C" aero_status aero_adamw_step(const void* image, void* table, const aer
   const Table* t = table_of(image);
   if (!t) return AERO_ERR_SHAPE;
   if (!(p->beta1 >= 0.0 && p->beta1 < 1.0 && p->beta2 >= 0.0 && p->beta2 < 1.0)) return AERO_ERR_SHAPE;
-  if (!(float(p->eps) > 0.f) || !std::isfinite(float(p->eps)) || !(p->lr >= 0.0) || !std::isfinite(p->lr) || !std::isfinite(p->weight_decay))
+  if (!(float(p->eps) >= 0x1p-126f) || !std::isfinite(float(p->eps)) || !(p->lr >= 0.0) || !std::isfinite(p->lr) || !std::isfinite(p->weight_decay))
     return AERO_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(table) % 16 != 0) return AERO_ERR_ALIGN;
   hipStream_t s = as_stream(stream);

@@ -249,6 +249,33 @@ def test_gradients_of_zero_and_tiny_ones(gh, bits):
         model.check(t, how_of())
 
 
+@pytest.mark.parametrize("param,master", KINDS)
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-30, 1e-19, 1e-12])
+def test_smallest_eps(gh, param, master, bits, eps):
+    """Moments of 0 leave a weight to its decay alone, whatever eps is; second moments below 2^-126 (gradients of 3e-19 and less) count as what they are."""
+    import paper_2602_14338_amd as aero
+    sizes = [700, 256, 1500, 5000]
+    model = Model(19, sizes, param, "f32", master, bits)
+    rng = np.random.default_rng(20)
+    some = (rng.normal(0, 1, 5000) * 10.0 ** rng.uniform(-22, -15, 5000)).astype(np.float32)
+    model.g = [np.zeros(700, np.float32), np.full(256, 3e-19, np.float32), np.where(np.arange(1500) % 3 == 0, np.float32(-2e-20), np.float32(0)), some]
+    model.flat["grad"].copy_(model.b.put(model.g, torch.float32))
+    for k in ("exp_avg", "exp_avg_sq"):
+        for piece in model.b.pieces(model.flat[k]):
+            piece.zero_()
+    model.m = [np.zeros(s, np.float32) for s in sizes]
+    model.v = [np.zeros(s, np.float32) for s in sizes]
+    how = how_of(eps=eps)
+    step, *_ = words()
+    for t in range(2):
+        aero.aero_adamw_step(model.table, aero.AdamWParams(**how), step)
+        torch.cuda.synchronize()
+        # what the step is made on (squares below 2^-149 are 0 in 32 bits, and m over eps may be beyond fp16)
+        assert all(torch.isfinite(x.float()).all() for x in model.b.pieces(model.flat["master" if master else "param"]))
+        model.check(t, how)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 def test_bad_gradient_and_the_norm_in_front(gh, bits, bad):

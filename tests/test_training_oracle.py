@@ -261,3 +261,12 @@ def test_constants_match_the_header(tmp_path):
     subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
     got = [int(x) for x in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
     assert got == list(names.values())
+
+
+def test_an_eps_whose_reciprocal_is_infinite_is_refused():
+    b = library()
+    st, image, keep = image_of(b, entry(b))
+    assert st == 0
+    for eps in (1e-40, 2.0 ** -128, 2.0 ** -127, float(np.nextafter(np.float32(2.0 ** -126), np.float32(0)))):
+        params = C.byref(b.AdamWParams(eps=eps).to_c())
+        assert b._lib.aero_adamw_step(image, FAKE, params, FAKE, None, None, None) == 2, eps
