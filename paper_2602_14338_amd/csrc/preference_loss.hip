@@ -40,11 +40,20 @@ __device__ __forceinline__ void exact_add(ExactSum* s, float x) {
   if (low) atomicAdd(limb, (unsigned long long)((low ^ sign) - sign));
   if (high) atomicAdd(limb + 1, (unsigned long long)((high ^ sign) - sign));
 }
-// A 64-bit number to 48 bits.
+// A 64-bit number to 48 bits.  Beyond 32-bit floats, where the sum of a wave's finite tokens may be (log-probs of the type's lowest value, as masks write them), all 53 of
+// them: as a whole number of limb 7's units, 2^75, of which 512 tokens' sum is less than 2^62.
 __device__ __forceinline__ void exact_add(ExactSum* s, double x) {
   const float hi = float(x);
-  exact_add(s, hi);
-  if (fabsf(hi) < INFINITY) exact_add(s, float(x - double(hi)));
+  if (fabsf(hi) < INFINITY) {
+    exact_add(s, hi);
+    exact_add(s, float(x - double(hi)));
+  } else if (fabs(x) < INFINITY) {
+    const int64_t n = int64_t(x * 0x1p-75);
+    atomicAdd(s->limb + 7, (unsigned long long)(n & 0xffffffff));
+    atomicAdd(s->limb + 8, (unsigned long long)(n >> 32));   // rounded down: the low limb's part is never negative
+  } else {
+    exact_add(s, hi);
+  }
 }
 __device__ __forceinline__ double exact_value(const ExactSum& s) {
   if (s.flags) {

@@ -230,6 +230,41 @@ def test_log_probs_that_are_not_finite(gh, T, R, kind):
             near(d, want[3], 1e-5)
 
 
+@pytest.mark.parametrize("T,R", [(60, 6), (3000, 6), (20000, 300)])
+@pytest.mark.parametrize("packed", [True, False])
+def test_log_probs_of_the_lowest_value(gh, T, R, packed):
+    """Finite tokens whose sum is beyond 32 bits: log ratios are formed in 64, margins are finite where beta makes them so, and 0 between rollouts alike."""
+    rollout = np.sort(np.arange(T) % R).astype(np.int32) if packed else (np.arange(T) % R).astype(np.int32)
+    lp = np.full(T, -1.0, np.float32)
+    low = np.finfo(np.float32).min
+    of = [np.nonzero(rollout == r)[0] for r in range(6)]
+    lp[of[0][:3]] = lp[of[1][-3:]] = lp[of[2][:2]] = lp[of[4]] = low
+    lp[of[3][:2]], lp[of[5][[0, 1, 5]]] = -low, [low, low, -low]
+    chosen, rejected = np.array([0, 2, 1, 3, 4, 5], np.int32), np.array([1, 0, 2, 4, 5, 2], np.int32)
+    weight = np.array([0.5, 1.0, 2.0, 1.0, 0.25, 1.0], np.float32) / 1024
+    how = how_of(beta=2.0 ** -20, margin=0.0)
+    want = orc.preference(lp.astype(np.float64), None, rollout, R, chosen, rejected, weight, **how)
+    count, size = np.bincount(rollout, minlength=R), np.zeros(R)
+    np.add.at(size, rollout, np.abs(lp.astype(np.float64)))
+    t_ratio, t_m, t_slope, t_loss = bounds(want, count, size, chosen, rejected, weight, how, 0.0)
+    loss, m, s, d, err = run_terms(lp, None, rollout, R, chosen, rejected, weight, how)
+    with np.errstate(over="ignore"):
+        near(s, want[2].astype(np.float32), t_ratio)
+    near(m, want[1], t_m)
+    assert m[0] == 0.0
+    near(loss, [want[0]], t_loss)
+    # far from a margin of 0 the logistic form's slope is -1 or 0, less the smoothing
+    slope = np.zeros(R)
+    for p in range(1, 6):
+        k = how["beta"] * weight[p] * (how["smoothing"] - (1.0 if want[1][p] < 0 else 0.0))
+        slope[chosen[p]] += k
+        slope[rejected[p]] -= k
+    k = how["beta"] * weight[0] * (how["smoothing"] - 0.5)
+    slope[0] += k
+    slope[1] -= k
+    near(d, slope, 8 * U * how["beta"] * weight.sum())
+
+
 @pytest.mark.parametrize("T,R,P", [(4000, 50, 300), (30000, 500, 6000)])
 def test_terms_do_not_depend_on_order(gh, T, R, P):
     """Tokens and pairs in another order leave the same bits, in slopes whose terms differ by many magnitudes too."""
