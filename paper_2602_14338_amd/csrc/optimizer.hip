@@ -5,7 +5,7 @@
 // parameter, gradient and moments) stand together, and a class is one launch.
 //
 // Bound by bytes: n of the gradient for the norm (500 M bf16 154 us, 6.5 TB/s), for a step what is read and written of weights and moments (28 bytes an element for 16-bit weights with
-// a master and 32-bit moments: 300 M 1358 us, 6.2 TB/s).  With 8-bit moments (10 bytes an element) a step is bound by vector instructions, 97 an element where it rounds at random: 233 M
+// a master and 32-bit moments: 300 M 1351 us, 6.2 TB/s).  With 8-bit moments (10 bytes an element) a step is bound by vector instructions, 99 an element where it rounds at random: 233 M
 // 550-600 us, of which the bytes are 370.  Small ones by one launch: 262 K elements 4.3 us, the norm of 150 K 4.0.
 #include <cmath>
 #include <cstring>

@@ -8,9 +8,9 @@
 // exactly, in whole numbers, so that order does not matter: a 32-bit float is m 2^(p - 149) with a 24-bit m, and goes into two of nine
 // 64-bit limbs that stand for 2^(32 k - 149) (the low 32 bits of m 2^(p mod 32) and what is above), each below 2^32, so that 2^31 of them fit.
 //
-// Bound by the bytes of the rows, read twice and written once: 8192 x 151936 bf16, an eighth of them padding, 1058 us: 325 for the statistics (6.7 TB/s), 14 for the sums, 718 for
-// the gradient (6.5 TB/s).  Small batches by three launches in a row: 512 x 4096 fp32 14.2 us.  Log-probs alone by launches: 2^20 tokens of 4096 rollouts in 8192 pairs 17.8 us,
-// 4096 tokens 7.2.
+// Bound by the bytes of the rows, read twice and written once: 8192 x 151936 bf16, an eighth of them padding, 1060 us: 325 for the statistics (6.7 TB/s), 14 for the sums, 717 for
+// the gradient (6.5 TB/s).  Small batches by three launches in a row: 512 x 4096 fp32 14.3 us.  Log-probs alone by launches: 2^20 tokens of 4096 rollouts in 8192 pairs 18.2 us,
+// 4096 tokens 7.3.
 #include "row_scan.h"
 
 namespace aero {
@@ -542,7 +542,7 @@ template <int NT, int DT, bool VEC, bool KEEP> __device__ __forceinline__ RowSum
   return st;
 }
 
-// A row's sum of exponentials and its sampled token's log-prob: one workgroup reads it once.  6.7 TB/s from some thousand rows of 151936 bf16 on, 5.3 for a thousand, which are all under
+// A row's sum of exponentials and its sampled token's log-prob: one workgroup reads it once.  6.7 TB/s from some thousand rows of 151936 bf16 on, 5.2-5.7 for a thousand, which are all under
 // way at once and end together.  256 and 1024 threads instead of 512: 0-3 % longer; eight vectors ahead 0-1 %.
 template <int NT, int DT, bool VEC>
 __global__ __launch_bounds__(NT) void k_pair_rows(PairRows a) {
@@ -582,7 +582,7 @@ struct RowGradient {
 };
 
 // (row, segment) per workgroup, a vector per thread, in the order of addresses from the end: what was read last is read first.  Stored past the caches, which
-// hold the rows then: 1000 rows of 151936 bf16 88 -> 80 us (7.2 TB/s, a part of it not from memory), 8192 rows 755 -> 718.  A vector asked for before it is known that its
+// hold the rows then: 1000 rows of 151936 bf16 88 -> 80 us (7.2 TB/s, a part of it not from memory), 8192 rows 755 -> 717.  A vector asked for before it is known that its
 // rollout has a gradient takes 0.1-0.8 % less, but a satisfied hinge leaves most rows unread.
 template <int NT, int DT>
 __global__ __launch_bounds__(NT) void k_pair_grad_seg(const void* logits, int V, int64_t ld, int segs, const RowRecord* __restrict__ rows,
